@@ -187,7 +187,7 @@ def prepare(case, seed):
         out, den, _, _ = _plain_decay(case, x)
         x["out"] = out
         if case["norm"]:
-            x["den"] = den
+            x["den"] = den.contiguous()
     elif case["kind"] == "softmax_bwd":
         x["out"], x["lse"] = _plain_softmax(case, x)
     return {"case": case, "x": x}
