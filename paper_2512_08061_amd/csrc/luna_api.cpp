@@ -14,6 +14,7 @@
 #include <string>
 
 #include "luna_chunk.hpp"
+#include "luna_error.hpp"
 #include "luna_features.hpp"
 #include "luna_grad.hpp"
 #include "luna_kernels.hpp"
@@ -26,6 +27,25 @@ luna_status fail(luna_status s, const std::string& why) {
   g_last_error = why;
   return s;
 }
+
+}  // namespace
+
+namespace luna {
+
+luna_status set_error(luna_status s, const char* why) noexcept {
+  try {
+    g_last_error = why;
+  } catch (...) {  // (no memory for the text: the status stands alone)
+    g_last_error.clear();
+  }
+  return s;
+}
+
+void clear_error() noexcept { g_last_error.clear(); }
+
+}  // namespace luna
+
+namespace {
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 

@@ -1,0 +1,107 @@
+// luna_decay.hip -- around the chunked decay kernel (luna_decay.hpp): the discounted prefixes
+// of the pieces' states, the row weights of the backward pass, and which instantiation runs.
+#include "luna_seq.hpp"
+
+namespace luna {
+
+namespace {
+
+// Before: slot p of a sequence and head holds the state that its tokens add (all but the last
+// piece).  After: the state before piece p, S_p = f^piece S_{p-1} + X_{p-1}, from the caller's
+// state or zero.  One thread per element; loads of the next piece do not wait for the sums.
+__global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int64_t elems, int zwidth) {
+  const int head = blockIdx.y, b = blockIdx.z;
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= elems) return;
+  const SeqPiece sp = seq_of(a.s, b);
+  const int pieces = (int)(((int64_t)sp.len + a.piece - 1) / a.piece);
+  if (pieces == 0) return;
+  const int64_t slot = a.s.offsets ? sp.first / a.piece + b : b * ((a.s.rows + a.piece - 1) / a.piece);
+  const int64_t sf = decay_state_floats(a.dk, a.dv), step = a.H * sf;
+  float* x = a.states + (slot * a.H + head) * sf + e;
+  const float f = exp2f(decay_log2(a.log_decay[head]) * (float)a.piece);
+  const int64_t S_elems = (int64_t)a.dk * a.dv, at = (int64_t)b * a.H + head;
+  float run = 0.0f;
+  if (a.S) run = e < S_elems ? a.S[at * S_elems + e] : zwidth && a.z ? a.z[at * zwidth + e - S_elems] : 0.0f;
+  float next = pieces > 1 ? x[0] : 0.0f;
+  for (int p = 0; p < pieces; ++p) {
+    const float add = next;
+    if (p + 2 < pieces) next = x[(p + 1) * step];
+    x[p * step] = run;
+    run = fmaf(f, run, add);
+  }
+}
+
+// w_i = 1 / (den_i + eps), delta_i = -dO_i.out_i: a quarter wave per row.
+template <typename T>
+__global__ __launch_bounds__(256) void decay_weights_kernel(DecayWeightsArgs a, int tiles) {
+  const int head = blockIdx.y;
+  const SeqPiece sp = seq_piece(a.s, blockIdx.x, 64);
+  if (sp.seq < 0) return;
+  const bool packed = a.s.offsets != nullptr;
+  const int sub = threadIdx.x % 16;
+  for (int r = threadIdx.x / 16; r < 64; r += 16) {
+    const int i = sp.index * 64 + r;
+    if (i >= sp.len) break;
+    const T* g = reinterpret_cast<const T*>(seq_row(a.dO, sp, packed, head, i, sizeof(T)));
+    const T* o = reinterpret_cast<const T*>(seq_row(a.out, sp, packed, head, i, sizeof(T)));
+    float x = 0.0f;
+    for (int c = sub; c < a.d; c += 16) x = fmaf((float)g[c], (float)o[c], x);
+    x += __shfl_xor(x, 1);
+    x += __shfl_xor(x, 2);
+    x += __shfl_xor(x, 4);
+    x += __shfl_xor(x, 8);
+    if (sub == 0) {
+      const int64_t num = seq_num(a.s, sp, a.H, head, i);
+      a.w[num] = 1.0f / (a.den[num] + a.eps);
+      a.delta[num] = -x;
+    }
+  }
+}
+
+}  // namespace
+
+template <typename T, int MODE>
+hipError_t launch_decay_typed(const DecayArgs& a, bool out, hipStream_t s);
+extern template hipError_t launch_decay_typed<__bf16, kDecayPlain>(const DecayArgs&, bool, hipStream_t);
+extern template hipError_t launch_decay_typed<__bf16, kDecayNorm>(const DecayArgs&, bool, hipStream_t);
+extern template hipError_t launch_decay_typed<__bf16, kDecayAug>(const DecayArgs&, bool, hipStream_t);
+extern template hipError_t launch_decay_typed<float, kDecayPlain>(const DecayArgs&, bool, hipStream_t);
+extern template hipError_t launch_decay_typed<float, kDecayNorm>(const DecayArgs&, bool, hipStream_t);
+extern template hipError_t launch_decay_typed<float, kDecayAug>(const DecayArgs&, bool, hipStream_t);
+
+bool decay_supported(int dk, int dv) {
+  return (dk == 32 || dk == 64 || dk == 128 || dk == 256) && (dv == 32 || dv == 64 || dv == 128);
+}
+
+static hipError_t launch_decay(Dt dt, int mode, const DecayArgs& a, bool out, hipStream_t s) {
+  if (dt == Dt::BF16)
+    return mode == kDecayPlain ? launch_decay_typed<__bf16, kDecayPlain>(a, out, s)
+           : mode == kDecayNorm ? launch_decay_typed<__bf16, kDecayNorm>(a, out, s)
+                                : launch_decay_typed<__bf16, kDecayAug>(a, out, s);
+  return mode == kDecayPlain ? launch_decay_typed<float, kDecayPlain>(a, out, s)
+         : mode == kDecayNorm ? launch_decay_typed<float, kDecayNorm>(a, out, s)
+                              : launch_decay_typed<float, kDecayAug>(a, out, s);
+}
+hipError_t launch_decay_states(Dt dt, int mode, const DecayArgs& a, hipStream_t s) {
+  return launch_decay(dt, mode, a, false, s);
+}
+hipError_t launch_decay_out(Dt dt, int mode, const DecayArgs& a, hipStream_t s) { return launch_decay(dt, mode, a, true, s); }
+
+hipError_t launch_decay_scan(int mode, const DecayArgs& a, hipStream_t s) {
+  const int zwidth = mode == kDecayNorm ? a.dk : mode == kDecayAug ? a.dv : 0;
+  const int64_t elems = (int64_t)a.dk * a.dv + zwidth;
+  const dim3 grid((unsigned)((elems + 255) / 256), (unsigned)a.H, (unsigned)a.s.count);
+  hipLaunchKernelGGL(decay_scan_kernel, grid, dim3(256), 0, s, a, elems, zwidth);
+  return hipGetLastError();
+}
+
+hipError_t launch_decay_weights(Dt dt, const DecayWeightsArgs& a, hipStream_t s) {
+  const int64_t tiles = seq_slots(a.s, 64);
+  const dim3 grid((unsigned)tiles, (unsigned)a.H);
+  if (dt == Dt::BF16) hipLaunchKernelGGL(decay_weights_kernel<__bf16>, grid, dim3(256), 0, s, a, (int)tiles);
+  else hipLaunchKernelGGL(decay_weights_kernel<float>, grid, dim3(256), 0, s, a, (int)tiles);
+  return hipGetLastError();
+}
+
+}  // namespace luna

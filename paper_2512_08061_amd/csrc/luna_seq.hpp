@@ -1,0 +1,185 @@
+// luna_seq.hpp -- sequences of different lengths: what the host and the kernels of the
+// operators of luna_seq.h share (luna_decay*.hip, luna_softmax*.hip, luna_seq_api.cpp).
+//
+// Work over sequences is cut in pieces of equal length, numbered by slots that the host can
+// count without knowing the lengths.  Equal and padded sequences have ceil(rows / piece)
+// slots each.  Packed ones take slot floor(offsets[b] / piece) + b and the ones after it: a
+// sequence's ceil(len / piece) pieces always fit before the next one's first slot, and
+// floor(rows / piece) + count slots hold all of them.  The sequence of a slot is the last
+// whose first slot is not behind it.
+#pragma once
+
+#include "luna_device.hpp"
+#include "luna_kernels.hpp"
+
+namespace luna {
+
+struct SeqRows {  // luna_rows
+  char* data;
+  int64_t seq, head, row;
+};
+
+struct SeqSet {  // luna_seqs
+  int64_t count, rows;
+  const int32_t* offsets;
+  const int32_t* lens;
+};
+
+inline int64_t seq_slots(const SeqSet& s, int64_t piece) {
+  return s.offsets ? s.rows / piece + s.count : s.count * ((s.rows + piece - 1) / piece);
+}
+
+// One piece of one sequence.
+struct SeqPiece {
+  int seq;      // -1: the slot holds no piece
+  int index;    // piece of its sequence
+  int len;      // rows of the sequence
+  int64_t first;  // its first row in packed tensors, else 0
+};
+
+__device__ __forceinline__ int seq_clamp(int64_t x, int64_t lo, int64_t hi) {
+  return (int)(x < lo ? lo : x > hi ? hi : x);
+}
+
+__device__ __forceinline__ SeqPiece seq_of(const SeqSet& s, int b) {
+  SeqPiece p;
+  p.seq = b;
+  p.index = 0;
+  p.first = 0;
+  if (s.offsets) {
+    p.first = seq_clamp(s.offsets[b], 0, s.rows);
+    p.len = seq_clamp((int64_t)s.offsets[b + 1], p.first, s.rows) - (int)p.first;
+  } else {
+    p.len = s.lens ? seq_clamp(s.lens[b], 0, s.rows) : (int)s.rows;
+  }
+  return p;
+}
+
+// The piece of a slot (the whole wave calls this with one slot).
+__device__ __forceinline__ SeqPiece seq_piece(const SeqSet& s, int slot, int piece) {
+  SeqPiece p;
+  int first_slot;
+  if (s.offsets) {
+    int below = 0;  // sequences whose first slot is not behind this one
+    const int lane = threadIdx.x % kWave;
+    for (int b0 = 0; b0 < s.count; b0 += kWave) {
+      const int b = b0 + lane;
+      const bool in = b < s.count;
+      const int at = in ? seq_clamp(s.offsets[b], 0, s.rows) / piece + b : 0;
+      const uint64_t m = __ballot(in && at <= slot);
+      below += __popcll(m);
+      if (m != ~(uint64_t)0) break;
+    }
+    p.seq = __builtin_amdgcn_readfirstlane(below - 1);
+    if (p.seq < 0) return p;
+    p = seq_of(s, p.seq);
+    first_slot = (int)(p.first / piece) + p.seq;
+  } else {
+    const int each = (int)((s.rows + piece - 1) / piece);
+    p = seq_of(s, slot / each);
+    first_slot = p.seq * each;
+  }
+  p.index = __builtin_amdgcn_readfirstlane(slot - first_slot);
+  if (p.index < 0 || (int64_t)p.index * piece >= p.len) p.seq = -1;
+  return p;
+}
+
+// Address of row i of a sequence and head.
+__device__ __forceinline__ char* seq_row(const SeqRows& r, const SeqPiece& p, bool packed, int head, int64_t i, int esz) {
+  return r.data + (packed ? (p.first + i) * r.row + head * r.head : p.seq * r.seq + head * r.head + i * r.row) * esz;
+}
+// Index of row i among numbers per row.
+__device__ __forceinline__ int64_t seq_num(const SeqSet& s, const SeqPiece& p, int H, int head, int64_t i) {
+  return s.offsets ? head * s.rows + p.first + i : ((int64_t)p.seq * H + head) * s.rows + i;
+}
+
+// 2^x in one instruction (1 ulp; results below 2^-126 are 0).  Also where a result is not wanted: what
+// follows a matrix product and precedes the first reads of its result holds no branch, not
+// even around an exponential or a load.  (Where a short conditional block stood there, the
+// compiler left out the wait states on the path around it, and the reads came too early.)
+__device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Decay factor's exponent: log_decay within [-1e30, 0], so that multiples of it stay defined (0 times it
+// is 0), in base 2; NaN stays NaN.
+__device__ __forceinline__ float decay_log2(float g) {
+  g = g > 0.0f ? 0.0f : g < -1e30f ? -1e30f : g;
+  return g * 1.44269504088896340736f;
+}
+
+// ---------------------------------------------------------------------------
+// decay (luna_decay.hip, luna_decay_step.hip)
+// ---------------------------------------------------------------------------
+
+// How the sums are formed (luna_decay.hip): plain; with denominators; with one more key
+// component that is given per row.
+constexpr int kDecayPlain = 0, kDecayNorm = 1, kDecayAug = 2;
+
+struct DecayArgs {
+  SeqRows q, k, v, o;  // widths dk, dk, dv, dv
+  SeqSet s;
+  const float* log_decay;  // [H]
+  int H, dk, dv;
+  int piece, slots;        // tokens per piece (a multiple of 64)
+  int reverse;             // sums over later tokens instead of earlier ones
+  int exact_state;         // the state to fp32 accuracy (it is returned)
+  float* states;           // [slots][H][decay_state_floats]: state before each piece; null: one piece per sequence
+  float* S;                // [count][H][dk][dv] and z [count][H][dk], in and out, or null
+  float* z;
+  float* den;              // per row, out (kDecayNorm), or null
+  const float* kw;         // per row: weight of the row as a key, or null
+  const float* ka;         // per row: the key's further component (kDecayAug; null: 1)
+  const float* qa;         // per row: the query's (null: 1)
+  const float* ow;         // per row: factor of the output row, or null
+  float scale, eps;
+};
+__host__ __device__ inline int64_t decay_state_floats(int dk, int dv) {
+  return (int64_t)dk * dv + (dk > dv ? dk : dv);
+}
+bool decay_supported(int dk, int dv);
+// states of all pieces but each sequence's last, then (launch_decay_scan) their discounted prefixes
+hipError_t launch_decay_states(Dt dt, int mode, const DecayArgs& a, hipStream_t s);
+hipError_t launch_decay_scan(int mode, const DecayArgs& a, hipStream_t s);
+hipError_t launch_decay_out(Dt dt, int mode, const DecayArgs& a, hipStream_t s);
+
+// w = 1 / (den + eps) and wd = -dO.out per row
+struct DecayWeightsArgs {
+  SeqRows dO, out;
+  SeqSet s;
+  const float* den;
+  float* w;
+  float* delta;
+  int H, d;
+  float eps;
+};
+hipError_t launch_decay_weights(Dt dt, const DecayWeightsArgs& a, hipStream_t s);
+
+struct DecayStepArgs {
+  SeqRows q, k, v, o;
+  const float* log_decay;
+  int64_t count;
+  int m, H, D, d, normalize;
+  float scale, eps;
+  float* S;
+  float* z;
+};
+hipError_t launch_decay_step(Dt dt, const DecayStepArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------------------
+// softmax (luna_softmax*.hip)
+// ---------------------------------------------------------------------------
+
+struct SoftmaxArgs {
+  SeqRows q, k, v, o;
+  SeqSet qs, ks;
+  int H, Hk, d;
+  float scale;
+  float* lse;  // per query row, out (forward: may be null) or in (backward)
+  // backward
+  SeqRows dO, dq, dk, dv;
+  float* delta;  // per query row: dO.out, written by the query pass and read by the key pass
+};
+constexpr int kSoftmaxLeast = 64;  // the fewest rows of a tile: an upper bound for grids
+hipError_t launch_softmax_fwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
+hipError_t launch_softmax_bwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
+
+}  // namespace luna

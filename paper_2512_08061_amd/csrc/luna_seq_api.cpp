@@ -1,0 +1,422 @@
+// luna_seq_api.cpp -- host side of the C ABI declared in include/luna_seq.h: checks, the plan of
+// a call and its workspace, launches on the caller's stream.
+#include "luna_seq.h"
+
+#include <cmath>
+#include <cstdio>
+
+#include "luna_error.hpp"
+#include "luna_seq.hpp"
+
+namespace {
+
+using luna::set_error;
+
+constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxRow = (int64_t)1 << 20, kMaxGrid = ((int64_t)1 << 31) - 1;
+
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+luna::SeqRows rows_of(const luna_rows* r) {
+  return r ? luna::SeqRows{static_cast<char*>(r->data), r->seq, r->head, r->row} : luna::SeqRows{};
+}
+luna::SeqSet set_of(const luna_seqs* s) { return luna::SeqSet{s->count, s->rows, s->offsets, s->lens}; }
+
+luna_status check_seqs(const luna_seqs* s, const char* what) {
+  char why[128];
+  if (!s) {
+    snprintf(why, sizeof why, "%s is NULL", what);
+    return set_error(LUNA_ERR_INVALID_ARG, why);
+  }
+  if (s->count < 1 || s->rows < 0) {
+    snprintf(why, sizeof why, "%s: count must be >= 1 and rows >= 0", what);
+    return set_error(LUNA_ERR_INVALID_ARG, why);
+  }
+  if (s->offsets && s->lens) {
+    snprintf(why, sizeof why, "%s: offsets and lens exclude each other", what);
+    return set_error(LUNA_ERR_INVALID_ARG, why);
+  }
+  if (s->count > 65535 || s->rows > kMaxRows || (!s->offsets && s->count * s->rows > kMaxRows)) {
+    snprintf(why, sizeof why, "%s: more than 65535 sequences or 2^30 rows", what);
+    return set_error(LUNA_ERR_UNSUPPORTED, why);
+  }
+  return LUNA_OK;
+}
+
+// heads and sequences of an output must not share rows; those of an input may (stride 0)
+luna_status check_rows(const luna_rows* r, const char* what, luna_dtype dt, const luna_seqs& s, int64_t heads, int64_t width,
+                       bool output) {
+  char why[160];
+  const int64_t e = dt == LUNA_BF16 ? 8 : 4;  // elements of 16 bytes
+  const char* bad = nullptr;
+  if (!r || (!r->data && s.rows > 0)) bad = "is NULL";
+  else if (((uintptr_t)r->data & 15) != 0) bad = "must be 16-byte aligned";
+  else if (r->row < width) bad = "has rows closer than their width";
+  else if (r->head < 0 || r->seq < 0) bad = "has a negative stride";
+  else if (r->row % e || r->head % e || (!s.offsets && r->seq % e)) bad = "has strides that are no multiple of 16 bytes";
+  else if (output && ((heads > 1 && r->head < width) || (!s.offsets && s.count > 1 && r->seq < width))) bad = "has rows that overlap";
+  if (bad) {
+    snprintf(why, sizeof why, "%s %s", what, bad);
+    return set_error(LUNA_ERR_INVALID_ARG, why);
+  }
+  if (r->row > kMaxRow || r->head > ((int64_t)1 << 40) || r->seq > ((int64_t)1 << 40)) {
+    snprintf(why, sizeof why, "%s: strides above 2^20 elements (rows) or 2^40", what);
+    return set_error(LUNA_ERR_UNSUPPORTED, why);
+  }
+  return LUNA_OK;
+}
+
+luna_status check_ws(size_t need, const void* ws, size_t ws_bytes) {
+  if (need == 0) return LUNA_OK;
+  if (!ws || ((uintptr_t)ws & 255) != 0) return set_error(LUNA_ERR_INVALID_ARG, "workspace is NULL or not 256-byte aligned");
+  if (ws_bytes < need) {
+    char why[96];
+    snprintf(why, sizeof why, "workspace holds %zu bytes, %zu are needed", ws_bytes, need);
+    return set_error(LUNA_ERR_WORKSPACE, why);
+  }
+  return LUNA_OK;
+}
+
+luna_status hip_status(hipError_t e, const char* what) {
+  if (e == hipSuccess) return LUNA_OK;
+  char why[160];
+  snprintf(why, sizeof why, "%s: %s", what, hipGetErrorString(e));
+  return set_error(LUNA_ERR_HIP, why);
+}
+
+luna_status check_type(luna_dtype dt) {
+  return dt == LUNA_F32 || dt == LUNA_BF16 ? LUNA_OK : set_error(LUNA_ERR_INVALID_ARG, "dtype must be LUNA_F32 or LUNA_BF16");
+}
+
+// ---------------------------------------------------------------------------
+// decay
+// ---------------------------------------------------------------------------
+
+struct DecayPlan {
+  int piece = 0, slots = 0;
+  bool many = false;  // some sequence may have more than one piece
+  size_t states = 0, w = 0, delta = 0, total = 0;  // workspace offsets
+};
+
+// Tokens per piece.  A piece is a serial chain of chunks; pieces of one sequence cost a pass over their
+// keys and values for the states, and the states written, scanned and read.
+luna_status plan_decay(const luna_seqs& s, int64_t H, int64_t D, int64_t d, bool backward, bool normalize, DecayPlan* p) {
+  const int64_t per = s.rows, all = s.offsets ? s.rows : s.count * s.rows;
+  int64_t piece = ceil_div(ceil_div(all * H, 512), 64) * 64;
+  if (piece < 256) piece = 256;
+  const int64_t longest = ceil_div(per > 0 ? per : 1, 64) * 64;
+  if (piece > longest) piece = longest;
+  p->piece = (int)piece;
+  p->many = per > piece;
+  const luna::SeqSet set = set_of(&s);
+  const int64_t slots = luna::seq_slots(set, piece);
+  if (slots * H * 2 > kMaxGrid) return set_error(LUNA_ERR_UNSUPPORTED, "too many pieces of sequences and heads");
+  p->slots = (int)slots;
+  size_t off = 0;
+  auto take = [&](size_t& at, size_t bytes) {
+    at = off;
+    off = align256(off + bytes);
+  };
+  if (p->many) take(p->states, (size_t)slots * H * luna::decay_state_floats((int)D, (int)d) * 4);
+  if (backward && normalize) {
+    take(p->w, (size_t)all * H * 4);
+    take(p->delta, (size_t)all * H * 4);
+  }
+  p->total = off;
+  return LUNA_OK;
+}
+
+luna_status check_decay(luna_dtype dt, int64_t H, int64_t D, int64_t d, const float* log_decay, int32_t normalize, float scale,
+                        float eps) {
+  luna_status st = check_type(dt);
+  if (st != LUNA_OK) return st;
+  if (H < 1) return set_error(LUNA_ERR_INVALID_ARG, "H must be >= 1");
+  if (H > 65535) return set_error(LUNA_ERR_UNSUPPORTED, "H must be <= 65535");
+  if (D < 1 || d < 1) return set_error(LUNA_ERR_INVALID_ARG, "D and d must be >= 1");
+  if (D > 256 || d > 128 || !luna::decay_supported((int)D, (int)d))
+    return set_error(LUNA_ERR_UNSUPPORTED, "D must be 32, 64, 128 or 256 and d 32, 64 or 128");
+  if (!log_decay) return set_error(LUNA_ERR_INVALID_ARG, "log_decay is NULL");
+  if (normalize != 0 && normalize != 1) return set_error(LUNA_ERR_INVALID_ARG, "normalize must be 0 or 1");
+  if (!std::isfinite(scale)) return set_error(LUNA_ERR_INVALID_ARG, "scale must be finite");
+  if (!(std::isfinite(eps) && eps >= 0.0f)) return set_error(LUNA_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  return LUNA_OK;
+}
+
+luna_status check_state(const float* S, const float* z, int32_t normalize) {
+  if (((uintptr_t)S & 15) != 0) return set_error(LUNA_ERR_INVALID_ARG, "S must be 16-byte aligned");
+  if ((S != nullptr && normalize) != (z != nullptr))
+    return set_error(LUNA_ERR_INVALID_ARG, "z goes with S and normalize 1, and only with them");
+  return LUNA_OK;
+}
+
+// the states of all pieces, their prefixes, then the rows
+luna_status run_decay(luna::Dt dt, int mode, const DecayPlan& p, luna::DecayArgs& a, void* ws, hipStream_t s) {
+  a.piece = p.piece;
+  a.slots = p.slots;
+  a.states = nullptr;
+  luna_status st;
+  if (p.many) {
+    a.states = reinterpret_cast<float*>(static_cast<char*>(ws) + p.states);
+    if ((st = hip_status(luna::launch_decay_states(dt, mode, a, s), "decay state launch")) != LUNA_OK) return st;
+    if ((st = hip_status(luna::launch_decay_scan(mode, a, s), "decay scan launch")) != LUNA_OK) return st;
+  }
+  return hip_status(luna::launch_decay_out(dt, mode, a, s), "decay launch");
+}
+
+luna::Dt type_of(luna_dtype dt) { return dt == LUNA_BF16 ? luna::Dt::BF16 : luna::Dt::F32; }
+
+// ---------------------------------------------------------------------------
+// softmax
+// ---------------------------------------------------------------------------
+
+luna_status check_softmax(luna_dtype dt, const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d,
+                          float scale) {
+  luna_status st = check_type(dt);
+  if (st == LUNA_OK) st = check_seqs(seqs, "seqs");
+  if (st == LUNA_OK && keys) st = check_seqs(keys, "keys");
+  if (st != LUNA_OK) return st;
+  if (keys && keys->count != seqs->count) return set_error(LUNA_ERR_INVALID_ARG, "seqs and keys differ in count");
+  if (H < 1 || Hk < 1 || H % Hk) return set_error(LUNA_ERR_INVALID_ARG, "H must be a positive multiple of Hk");
+  if (H > 65535) return set_error(LUNA_ERR_UNSUPPORTED, "H must be <= 65535");
+  if (d != 32 && d != 64 && d != 128) return set_error(LUNA_ERR_UNSUPPORTED, "d must be 32, 64 or 128");
+  if (!std::isfinite(scale)) return set_error(LUNA_ERR_INVALID_ARG, "scale must be finite");
+  for (const luna_seqs* x : {seqs, keys ? keys : seqs})
+    if (luna::seq_slots(set_of(x), luna::kSoftmaxLeast) * H > kMaxGrid)
+      return set_error(LUNA_ERR_UNSUPPORTED, "too many tiles of sequences and heads");
+  return LUNA_OK;
+}
+
+luna::SoftmaxArgs softmax_args(const luna_rows* Q, const luna_rows* K, const luna_rows* V, const luna_rows* out,
+                               const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d, float scale) {
+  luna::SoftmaxArgs a{};
+  a.q = rows_of(Q);
+  a.k = rows_of(K);
+  a.v = rows_of(V);
+  a.o = rows_of(out);
+  a.qs = set_of(seqs);
+  a.ks = set_of(keys ? keys : seqs);
+  a.H = (int)H;
+  a.Hk = (int)Hk;
+  a.d = (int)d;
+  a.scale = scale;
+  return a;
+}
+
+int64_t all_rows(const luna_seqs& s) { return s.offsets ? s.rows : s.count * s.rows; }
+
+}  // namespace
+
+extern "C" {
+
+size_t luna_seq_workspace_bytes(int32_t op, luna_dtype dtype, const luna_seqs* seqs, const luna_seqs* keys, int64_t H,
+                                int64_t Hk, int64_t Dq, int64_t Dv) {
+  luna::clear_error();
+  if (op == LUNA_OP_DECAY_FWD || op == LUNA_OP_DECAY_BWD) {
+    const float one = 1.0f;
+    if (check_seqs(seqs, "seqs") != LUNA_OK || check_decay(dtype, H, Dq, Dv, &one, 1, 1.0f, 0.0f) != LUNA_OK) return 0;
+    DecayPlan p;
+    if (plan_decay(*seqs, H, Dq, Dv, op == LUNA_OP_DECAY_BWD, true, &p) != LUNA_OK) return 0;
+    return p.total;
+  }
+  if (op == LUNA_OP_SOFTMAX_FWD || op == LUNA_OP_SOFTMAX_BWD) {
+    if (check_softmax(dtype, seqs, keys, H, Hk, Dq, 1.0f) != LUNA_OK) return 0;
+    if (Dv != Dq) {
+      set_error(LUNA_ERR_INVALID_ARG, "Dq and Dv differ");
+      return 0;
+    }
+    return op == LUNA_OP_SOFTMAX_BWD ? align256((size_t)all_rows(*seqs) * H * 4) : 0;
+  }
+  set_error(LUNA_ERR_INVALID_ARG, "unknown operation");
+  return 0;
+}
+
+luna_status luna_decay_fwd(const luna_rows* Q, const luna_rows* K, const luna_rows* V, luna_dtype dtype,
+                           const luna_seqs* seqs, int64_t H, int64_t D, int64_t d, const float* log_decay,
+                           int32_t normalize, float scale, float eps, float* S, float* z, const luna_rows* out,
+                           float* den, void* ws, size_t ws_bytes, void* stream) {
+  luna::clear_error();
+  luna_status st;
+  if ((st = check_decay(dtype, H, D, d, log_decay, normalize, scale, eps)) != LUNA_OK) return st;
+  if ((st = check_seqs(seqs, "seqs")) != LUNA_OK) return st;
+  if ((st = check_state(S, z, normalize)) != LUNA_OK) return st;
+  if (den && !normalize) return set_error(LUNA_ERR_INVALID_ARG, "den goes with normalize 1");
+  if ((st = check_rows(Q, "Q", dtype, *seqs, H, D, false)) != LUNA_OK) return st;
+  if ((st = check_rows(K, "K", dtype, *seqs, H, D, false)) != LUNA_OK) return st;
+  if ((st = check_rows(V, "V", dtype, *seqs, H, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(out, "out", dtype, *seqs, H, d, true)) != LUNA_OK) return st;
+  DecayPlan p;
+  if ((st = plan_decay(*seqs, H, D, d, false, normalize, &p)) != LUNA_OK) return st;
+  if ((st = check_ws(p.total, ws, ws_bytes)) != LUNA_OK) return st;
+  if (seqs->rows == 0) return LUNA_OK;
+  luna::DecayArgs a{};
+  a.q = rows_of(Q);
+  a.k = rows_of(K);
+  a.v = rows_of(V);
+  a.o = rows_of(out);
+  a.s = set_of(seqs);
+  a.log_decay = log_decay;
+  a.H = (int)H;
+  a.dk = (int)D;
+  a.dv = (int)d;
+  a.S = S;
+  a.z = z;
+  a.exact_state = S != nullptr;
+  a.den = den;
+  a.scale = scale;
+  a.eps = eps;
+  return run_decay(type_of(dtype), normalize ? luna::kDecayNorm : luna::kDecayPlain, p, a, ws,
+                   reinterpret_cast<hipStream_t>(stream));
+}
+
+luna_status luna_decay_step(const luna_rows* Q, const luna_rows* K, const luna_rows* V, luna_dtype dtype, int64_t count,
+                            int64_t m, int64_t H, int64_t D, int64_t d, const float* log_decay, int32_t normalize,
+                            float scale, float eps, float* S, float* z, const luna_rows* out, void* stream) {
+  luna::clear_error();
+  luna_status st;
+  if ((st = check_decay(dtype, H, D, d, log_decay, normalize, scale, eps)) != LUNA_OK) return st;
+  const luna_seqs seqs{count, m, nullptr, nullptr};
+  if (m < 1) return set_error(LUNA_ERR_INVALID_ARG, "m must be >= 1");
+  if ((st = check_seqs(&seqs, "the tokens")) != LUNA_OK) return st;
+  if (!S) return set_error(LUNA_ERR_INVALID_ARG, "S is NULL");
+  if ((st = check_state(S, z, normalize)) != LUNA_OK) return st;
+  if ((st = check_rows(Q, "Q", dtype, seqs, H, D, false)) != LUNA_OK) return st;
+  if ((st = check_rows(K, "K", dtype, seqs, H, D, false)) != LUNA_OK) return st;
+  if ((st = check_rows(V, "V", dtype, seqs, H, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(out, "out", dtype, seqs, H, d, true)) != LUNA_OK) return st;
+  if (count * H * 4 > (int64_t)1 << 21) return set_error(LUNA_ERR_UNSUPPORTED, "count * H must be <= 2^19");
+  luna::DecayStepArgs a{};
+  a.q = rows_of(Q);
+  a.k = rows_of(K);
+  a.v = rows_of(V);
+  a.o = rows_of(out);
+  a.log_decay = log_decay;
+  a.count = count;
+  a.m = (int)m;
+  a.H = (int)H;
+  a.D = (int)D;
+  a.d = (int)d;
+  a.normalize = normalize;
+  a.scale = scale;
+  a.eps = eps;
+  a.S = S;
+  a.z = z;
+  return hip_status(luna::launch_decay_step(type_of(dtype), a, reinterpret_cast<hipStream_t>(stream)), "decay step launch");
+}
+
+luna_status luna_decay_bwd(const luna_rows* Q, const luna_rows* K, const luna_rows* V, const luna_rows* dO,
+                           luna_dtype dtype, const luna_seqs* seqs, int64_t H, int64_t D, int64_t d,
+                           const float* log_decay, int32_t normalize, float scale, float eps, const luna_rows* out,
+                           const float* den, const luna_rows* dQ, const luna_rows* dK, const luna_rows* dV, void* ws,
+                           size_t ws_bytes, void* stream) {
+  luna::clear_error();
+  luna_status st;
+  if ((st = check_decay(dtype, H, D, d, log_decay, normalize, scale, eps)) != LUNA_OK) return st;
+  if ((st = check_seqs(seqs, "seqs")) != LUNA_OK) return st;
+  if (normalize && !den) return set_error(LUNA_ERR_INVALID_ARG, "den is NULL");
+  if ((st = check_rows(Q, "Q", dtype, *seqs, H, D, false)) != LUNA_OK) return st;
+  if ((st = check_rows(K, "K", dtype, *seqs, H, D, false)) != LUNA_OK) return st;
+  if ((st = check_rows(V, "V", dtype, *seqs, H, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(dO, "dO", dtype, *seqs, H, d, false)) != LUNA_OK) return st;
+  if (normalize && (st = check_rows(out, "out", dtype, *seqs, H, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(dQ, "dQ", dtype, *seqs, H, D, true)) != LUNA_OK) return st;
+  if ((st = check_rows(dK, "dK", dtype, *seqs, H, D, true)) != LUNA_OK) return st;
+  if ((st = check_rows(dV, "dV", dtype, *seqs, H, d, true)) != LUNA_OK) return st;
+  DecayPlan p;
+  if ((st = plan_decay(*seqs, H, D, d, true, normalize, &p)) != LUNA_OK) return st;
+  if ((st = check_ws(p.total, ws, ws_bytes)) != LUNA_OK) return st;
+  if (seqs->rows == 0) return LUNA_OK;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const luna::Dt dt = type_of(dtype);
+  float* w = nullptr;
+  float* delta = nullptr;
+  if (normalize) {
+    w = reinterpret_cast<float*>(static_cast<char*>(ws) + p.w);
+    delta = reinterpret_cast<float*>(static_cast<char*>(ws) + p.delta);
+    luna::DecayWeightsArgs r{rows_of(dO), rows_of(out), set_of(seqs), den, w, delta, (int)H, (int)d, eps};
+    if ((st = hip_status(luna::launch_decay_weights(dt, r, s), "row weight launch")) != LUNA_OK) return st;
+  }
+  luna::DecayArgs a{};
+  a.s = set_of(seqs);
+  a.log_decay = log_decay;
+  a.H = (int)H;
+  a.scale = scale;
+  const int mode = normalize ? luna::kDecayAug : luna::kDecayPlain;
+  // dQ: dO against V, with K as values
+  a.q = rows_of(dO);
+  a.k = rows_of(V);
+  a.v = rows_of(K);
+  a.o = rows_of(dQ);
+  a.dk = (int)d;
+  a.dv = (int)D;
+  a.qa = delta;
+  a.ow = w;
+  if ((st = run_decay(dt, mode, p, a, ws, s)) != LUNA_OK) return st;
+  // dK: V against dO, with Q as values, over later tokens
+  a.q = rows_of(V);
+  a.k = rows_of(dO);
+  a.v = rows_of(Q);
+  a.o = rows_of(dK);
+  a.qa = nullptr;
+  a.ka = delta;
+  a.kw = w;
+  a.ow = nullptr;
+  a.reverse = 1;
+  if ((st = run_decay(dt, mode, p, a, ws, s)) != LUNA_OK) return st;
+  // dV: K against Q, with dO as values, over later tokens
+  a.q = rows_of(K);
+  a.k = rows_of(Q);
+  a.v = rows_of(dO);
+  a.o = rows_of(dV);
+  a.dk = (int)D;
+  a.dv = (int)d;
+  a.ka = nullptr;
+  return run_decay(dt, luna::kDecayPlain, p, a, ws, s);
+}
+
+luna_status luna_softmax_fwd(const luna_rows* Q, const luna_rows* K, const luna_rows* V, luna_dtype dtype,
+                             const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d,
+                             float scale, const luna_rows* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  luna::clear_error();
+  luna_status st;
+  if ((st = check_softmax(dtype, seqs, keys, H, Hk, d, scale)) != LUNA_OK) return st;
+  const luna_seqs& ks = keys ? *keys : *seqs;
+  if ((st = check_rows(Q, "Q", dtype, *seqs, H, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(K, "K", dtype, ks, Hk, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(V, "V", dtype, ks, Hk, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(out, "out", dtype, *seqs, H, d, true)) != LUNA_OK) return st;
+  if (seqs->rows == 0) return LUNA_OK;
+  luna::SoftmaxArgs a = softmax_args(Q, K, V, out, seqs, keys, H, Hk, d, scale);
+  a.lse = lse;
+  return hip_status(luna::launch_softmax_fwd(type_of(dtype), a, reinterpret_cast<hipStream_t>(stream)), "softmax launch");
+}
+
+luna_status luna_softmax_bwd(const luna_rows* Q, const luna_rows* K, const luna_rows* V, const luna_rows* out,
+                             const float* lse, const luna_rows* dO, luna_dtype dtype, const luna_seqs* seqs,
+                             const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d, float scale, const luna_rows* dQ,
+                             const luna_rows* dK, const luna_rows* dV, void* ws, size_t ws_bytes, void* stream) {
+  luna::clear_error();
+  luna_status st;
+  if ((st = check_softmax(dtype, seqs, keys, H, Hk, d, scale)) != LUNA_OK) return st;
+  const luna_seqs& ks = keys ? *keys : *seqs;
+  if (!lse) return set_error(LUNA_ERR_INVALID_ARG, "lse is NULL");
+  if ((st = check_rows(Q, "Q", dtype, *seqs, H, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(K, "K", dtype, ks, Hk, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(V, "V", dtype, ks, Hk, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(out, "out", dtype, *seqs, H, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(dO, "dO", dtype, *seqs, H, d, false)) != LUNA_OK) return st;
+  if ((st = check_rows(dQ, "dQ", dtype, *seqs, H, d, true)) != LUNA_OK) return st;
+  if ((st = check_rows(dK, "dK", dtype, ks, Hk, d, true)) != LUNA_OK) return st;
+  if ((st = check_rows(dV, "dV", dtype, ks, Hk, d, true)) != LUNA_OK) return st;
+  const size_t need = align256((size_t)all_rows(*seqs) * H * 4);
+  if ((st = check_ws(need, ws, ws_bytes)) != LUNA_OK) return st;
+  luna::SoftmaxArgs a = softmax_args(Q, K, V, out, seqs, keys, H, Hk, d, scale);
+  a.lse = const_cast<float*>(lse);
+  a.dO = rows_of(dO);
+  a.dq = rows_of(dQ);
+  a.dk = rows_of(dK);
+  a.dv = rows_of(dV);
+  a.delta = static_cast<float*>(ws);
+  return hip_status(luna::launch_softmax_bwd(type_of(dtype), a, reinterpret_cast<hipStream_t>(stream)), "softmax backward launch");
+}
+
+}  // extern "C"

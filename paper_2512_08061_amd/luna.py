@@ -16,6 +16,7 @@ import re
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libluna.so")
 HEADER = os.path.join(os.path.dirname(PKG), "include", "luna.h")
+SEQ_HEADER = os.path.join(os.path.dirname(PKG), "include", "luna_seq.h")
 
 LUNA_OK, LUNA_ERR_INVALID_ARG, LUNA_ERR_UNSUPPORTED, LUNA_ERR_WORKSPACE, LUNA_ERR_HIP = range(5)
 LUNA_F32, LUNA_BF16 = 0, 1
@@ -94,6 +95,20 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.luna_distill.argtypes = [vp, vp, i32, i64, i64, i64, i64, P, i32, ctypes.c_float, vp,
                                  ctypes.POINTER(PhiGradsC), vp, sz, vp]
     lib.luna_distill.restype = i32
+    # luna_seq.h: luna_rows and luna_seqs go as addresses
+    f32 = ctypes.c_float
+    lib.luna_seq_workspace_bytes.argtypes = [i32, i32, vp, vp, i64, i64, i64, i64]
+    lib.luna_seq_workspace_bytes.restype = sz
+    lib.luna_decay_fwd.argtypes = [vp, vp, vp, i32, vp, i64, i64, i64, vp, i32, f32, f32, vp, vp, vp, vp, vp, sz, vp]
+    lib.luna_decay_fwd.restype = i32
+    lib.luna_decay_step.argtypes = [vp, vp, vp, i32, i64, i64, i64, i64, i64, vp, i32, f32, f32, vp, vp, vp, vp]
+    lib.luna_decay_step.restype = i32
+    lib.luna_decay_bwd.argtypes = [vp, vp, vp, vp, i32, vp, i64, i64, i64, vp, i32, f32, f32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.luna_decay_bwd.restype = i32
+    lib.luna_softmax_fwd.argtypes = [vp, vp, vp, i32, vp, vp, i64, i64, i64, f32, vp, vp, vp, sz, vp]
+    lib.luna_softmax_fwd.restype = i32
+    lib.luna_softmax_bwd.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, vp, i64, i64, i64, f32, vp, vp, vp, vp, sz, vp]
+    lib.luna_softmax_bwd.restype = i32
     lib.luna_status_string.argtypes = [i32]
     lib.luna_status_string.restype = ctypes.c_char_p
     lib.luna_last_error.argtypes = []
@@ -555,3 +570,260 @@ class Plan:
         s = stream if stream is not None else _stream_ptr(self.Q.device)
         self._call(self.wsp, self.wsn, s)
         return self.out
+
+
+# ---------------------------------------------------------------------------
+# causal attention over sequences of different lengths (include/luna_seq.h)
+# ---------------------------------------------------------------------------
+
+OP_DECAY_FWD, OP_DECAY_BWD, OP_SOFTMAX_FWD, OP_SOFTMAX_BWD = range(4)
+
+
+class _Seqs:
+    """The sequences of a call (luna_seqs): of 4-dim tensors [B, H, n, width], with lens [B]
+    where fewer than n rows of each are used, or of 3-dim packed tensors [T, H, width] with offsets [B + 1]."""
+
+    def __init__(self, t, offsets, lens, what):
+        torch = _torch()
+        if t.dim() == 3:
+            if offsets is None or lens is not None:
+                raise LunaError(LUNA_ERR_INVALID_ARG, f"{what}: packed [T, H, width] tensors take offsets, and no lens")
+            self.count, self.rows = offsets.shape[0] - 1 if offsets.dim() == 1 else -1, t.shape[0]
+        elif t.dim() == 4:
+            if offsets is not None:
+                raise LunaError(LUNA_ERR_INVALID_ARG, f"{what}: offsets go with packed [T, H, width] tensors")
+            self.count, self.rows = t.shape[0], t.shape[2]
+        else:
+            raise LunaError(LUNA_ERR_INVALID_ARG, f"{what} must be [B, H, n, width] or packed [T, H, width]")
+        self.packed, self.device, self.dtype = t.dim() == 3, t.device, t.dtype
+        index = offsets if self.packed else lens
+        at = 0
+        if index is not None:
+            want = self.count + 1 if self.packed else self.count
+            if index.dtype != torch.int32 or index.device != t.device or not index.is_contiguous() or \
+                    index.dim() != 1 or index.shape[0] != want or self.count < 1:
+                raise LunaError(LUNA_ERR_INVALID_ARG, "offsets [B + 1] and lens [B] must be contiguous int32 tensors on "
+                                                      "the tensors' device")
+            at = index.data_ptr()
+        self.c = (ctypes.c_int64 * 4)(self.count, self.rows, at if self.packed else 0, 0 if self.packed else at)
+
+    def same(self, t) -> bool:
+        """Whether t lies in this form's sequences."""
+        return t.dim() == (3 if self.packed else 4) and t.shape[0] == (self.rows if self.packed else self.count) and \
+            (self.packed or t.shape[2] == self.rows)
+
+    def numbers(self, H):
+        """Shape of one number per row."""
+        return (H, self.rows) if self.packed else (self.count, H, self.rows)
+
+
+def _seq_rows(seqs, ts, heads, widths, names):
+    """luna_rows of each tensor, one behind the other, as an array of whole numbers."""
+    v = []
+    for t, H, w, name in zip(ts, heads, widths, names):
+        if t.dtype != seqs.dtype or t.device != seqs.device or not t.is_cuda:
+            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} must share the other tensors' dtype and GPU")
+        if not seqs.same(t) or t.shape[1] != H or t.shape[-1] != w:
+            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} has shape {tuple(t.shape)}: its sequences, {H} heads or width "
+                                                  f"{w} do not match")
+        st = t.stride()
+        if w > 1 and st[-1] != 1:
+            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name}'s rows must be contiguous")
+        if seqs.packed:  # (a stride of an extent of one is never used)
+            v += (t.data_ptr(), 0, st[1] if H > 1 else 0, st[0] if seqs.rows > 1 else w)
+        else:
+            v += (t.data_ptr(), st[0] if seqs.count > 1 else 0, st[1] if H > 1 else 0, st[2] if seqs.rows > 1 else w)
+    return (ctypes.c_int64 * len(v))(*v)
+
+
+def _f32_ptr(t, shape, device, name):
+    torch = _torch()
+    if tuple(t.shape) != tuple(shape) or t.dtype != torch.float32 or t.device != device or not t.is_contiguous():
+        raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} must be a contiguous fp32 {list(shape)} tensor on the tensors' device")
+    return t.data_ptr()
+
+
+class _on_device:
+    """The tensors' device as the current one during a call."""
+
+    def __init__(self, device):
+        torch = _torch()
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _new(t, lens):
+    """An output like t; with lens its unused rows are zeros."""
+    torch = _torch()
+    return torch.empty_like(t) if lens is None else torch.zeros_like(t)
+
+
+def _seq_workspace(op, seqs, keys, H, Hk, Dq, Dv, dt):
+    """(tensor to keep, address, bytes) of an operation's workspace."""
+    lib = load_library()
+    nb = int(lib.luna_seq_workspace_bytes(op, dt, ctypes.addressof(seqs.c), None if keys is None else ctypes.addressof(keys.c),
+                                          H, Hk, Dq, Dv))
+    return (None, None, 0) if nb == 0 else _workspace(nb, seqs.device)
+
+
+def _decay_state(S, z, count, H, D, d, normalize, device):
+    if S is None:
+        if z is not None:
+            raise LunaError(LUNA_ERR_INVALID_ARG, "z goes with S")
+        return None, None
+    sp = _f32_ptr(S, (count, H, D, d), device, "S")
+    if not normalize:
+        if z is not None:
+            raise LunaError(LUNA_ERR_INVALID_ARG, "z goes with normalize")
+        return sp, None
+    if z is None:
+        raise LunaError(LUNA_ERR_INVALID_ARG, "normalize needs z with S")
+    return sp, _f32_ptr(z, (count, H, D), device, "z")
+
+
+def decay_attn(Q, K, V, log_decay, S=None, z=None, normalize: bool = False, scale: float = 1.0, eps: float = 1e-6,
+               offsets=None, lens=None, out=None, den=None):
+    """Causal linear attention whose weights decay by exp(log_decay[h]) per token (luna_decay_fwd).
+
+    Q, K [B, H, n, D] and V [B, H, n, d] (lens [B]: the rows used of each sequence), or packed [T, H, D] and
+    [T, H, d] with offsets [B + 1] (int32 tensors on the device); any strides that keep rows contiguous and
+    16-byte aligned.  S [B, H, D, d] and, normalised, z [B, H, D] (fp32): the state before the first token,
+    overwritten by the state after the last.  Returns (out, den): out like V, and with normalize the
+    denominators [B, H, n] or [H, T] that decay_attn_bwd takes (else None).  Rows of no sequence are not
+    written: zeros in a new out for lens, undefined in one for offsets."""
+    torch = _torch()
+    lib = load_library()
+    seqs = _Seqs(Q, offsets, lens, "Q")
+    H, D, d = Q.shape[1], Q.shape[-1], V.shape[-1]
+    out = _new(V, lens) if out is None else out
+    rows = _seq_rows(seqs, (Q, K, V, out), (H, H, H, H), (D, D, d, d), ("Q", "K", "V", "out"))
+    gp = _f32_ptr(log_decay, (H,), seqs.device, "log_decay")
+    sp, zp = _decay_state(S, z, seqs.count, H, D, d, normalize, seqs.device)
+    dp = None
+    if normalize:
+        den = torch.empty(seqs.numbers(H), dtype=torch.float32, device=seqs.device) if den is None else den
+        dp = _f32_ptr(den, seqs.numbers(H), seqs.device, "den")
+    elif den is not None:
+        raise LunaError(LUNA_ERR_INVALID_ARG, "den goes with normalize")
+    dt, at = _dt(Q), ctypes.addressof(rows)
+    with _on_device(seqs.device):
+        ws, wsp, wsn = _seq_workspace(OP_DECAY_FWD, seqs, None, H, H, D, d, dt)
+        _check(lib.luna_decay_fwd(at, at + 32, at + 64, dt, ctypes.addressof(seqs.c), H, D, d, gp, int(normalize), scale, eps,
+                                  sp, zp, at + 96, dp, wsp, wsn, _stream_ptr(seqs.device)))
+    return out, den
+
+
+def decay_attn_step(Q, K, V, log_decay, S, z=None, normalize: bool = False, scale: float = 1.0, eps: float = 1e-6, out=None):
+    """The m next tokens of every sequence (luna_decay_step): Q, K [B, H, m, D], V [B, H, m, d] from the state
+    S [B, H, D, d] (and z [B, H, D], normalised), which is updated in place; returns out like V."""
+    lib = load_library()
+    if Q.dim() != 4:
+        raise LunaError(LUNA_ERR_INVALID_ARG, "Q must be [B, H, m, D]")
+    seqs = _Seqs(Q, None, None, "Q")
+    H, D, d = Q.shape[1], Q.shape[-1], V.shape[-1]
+    out = _new(V, None) if out is None else out
+    rows = _seq_rows(seqs, (Q, K, V, out), (H, H, H, H), (D, D, d, d), ("Q", "K", "V", "out"))
+    gp = _f32_ptr(log_decay, (H,), seqs.device, "log_decay")
+    sp, zp = _decay_state(S, z, seqs.count, H, D, d, normalize, seqs.device)
+    at = ctypes.addressof(rows)
+    with _on_device(seqs.device):
+        _check(lib.luna_decay_step(at, at + 32, at + 64, _dt(Q), seqs.count, seqs.rows, H, D, d, gp, int(normalize), scale, eps,
+                                   sp, zp, at + 96, _stream_ptr(seqs.device)))
+    return out
+
+
+def decay_attn_bwd(Q, K, V, dO, log_decay, out=None, den=None, normalize: bool = False, scale: float = 1.0,
+                   eps: float = 1e-6, offsets=None, lens=None, grads=None):
+    """Backward pass of decay_attn from an empty state (luna_decay_bwd): returns (dQ, dK, dV), into grads when
+    given.  With normalize, out and den are what the forward call returned."""
+    lib = load_library()
+    seqs = _Seqs(Q, offsets, lens, "Q")
+    H, D, d = Q.shape[1], Q.shape[-1], V.shape[-1]
+    dQ, dK, dV = tuple(_new(t, lens) for t in (Q, K, V)) if grads is None else grads
+    if normalize and (out is None or den is None):
+        raise LunaError(LUNA_ERR_INVALID_ARG, "normalize needs out and den of the forward call")
+    o = out if normalize else V  # (not read without normalize)
+    rows = _seq_rows(seqs, (Q, K, V, dO, o, dQ, dK, dV), (H,) * 8, (D, D, d, d, d, D, D, d),
+                     ("Q", "K", "V", "dO", "out", "dQ", "dK", "dV"))
+    gp = _f32_ptr(log_decay, (H,), seqs.device, "log_decay")
+    dp = _f32_ptr(den, seqs.numbers(H), seqs.device, "den") if normalize else None
+    dt, at = _dt(Q), ctypes.addressof(rows)
+    with _on_device(seqs.device):
+        ws, wsp, wsn = _seq_workspace(OP_DECAY_BWD, seqs, None, H, H, D, d, dt)
+        _check(lib.luna_decay_bwd(at, at + 32, at + 64, at + 96, dt, ctypes.addressof(seqs.c), H, D, d, gp, int(normalize),
+                                  scale, eps, at + 128 if normalize else None, dp, at + 160, at + 192, at + 224, wsp, wsn,
+                                  _stream_ptr(seqs.device)))
+    return dQ, dK, dV
+
+
+def _softmax_keys(Q, K, seqs, offsets, lens, k_offsets, k_lens):
+    """The key sequences, or None where they are the queries'."""
+    if k_offsets is None and k_lens is None and K.dim() == Q.dim() and seqs.same(K):
+        return None
+    keys = _Seqs(K, k_offsets, k_lens, "K")
+    if keys.count != seqs.count:
+        raise LunaError(LUNA_ERR_INVALID_ARG, f"{seqs.count} query sequences, {keys.count} key sequences")
+    return keys
+
+
+def softmax_attn(Q, K, V, scale: float | None = None, offsets=None, lens=None, k_offsets=None, k_lens=None, out=None,
+                 lse=None):
+    """Causal softmax attention (luna_softmax_fwd), scale 1 / sqrt(d) unless given.
+
+    Q [B, H, n, d], K and V [B, Hk, n, d] (H a multiple of Hk; lens [B]: the rows used), or packed [T, H, d]
+    and [T, Hk, d] with offsets [B + 1].  Keys of sequences of their own, whose last rows are the queries' tokens:
+    K and V [B, Hk, capacity, d] with k_lens [B] (a cache), or packed with k_offsets.  Returns (out, lse): out like
+    Q and the logarithm of each row's sum, [B, H, n] or [H, T], which softmax_attn_bwd takes.  A row
+    that sees no key has out 0 and lse -infinity.  Rows of no sequence are not written: zeros in a new out for
+    lens, undefined in one for offsets."""
+    torch = _torch()
+    lib = load_library()
+    seqs = _Seqs(Q, offsets, lens, "Q")
+    H, Hk, d = Q.shape[1], K.shape[1], Q.shape[-1]
+    keys = _softmax_keys(Q, K, seqs, offsets, lens, k_offsets, k_lens)
+    out = _new(Q, lens) if out is None else out
+    rows = _seq_rows(seqs, (Q, out), (H, H), (d, d), ("Q", "out"))
+    krows = _seq_rows(keys or seqs, (K, V), (Hk, Hk), (d, d), ("K", "V"))
+    if keys is not None and (keys.dtype != seqs.dtype or keys.device != seqs.device):
+        raise LunaError(LUNA_ERR_INVALID_ARG, "Q and K must share dtype and GPU")
+    lse = torch.empty(seqs.numbers(H), dtype=torch.float32, device=seqs.device) if lse is None else lse
+    lp = _f32_ptr(lse, seqs.numbers(H), seqs.device, "lse")
+    dt, at, ak = _dt(Q), ctypes.addressof(rows), ctypes.addressof(krows)
+    with _on_device(seqs.device):
+        ws, wsp, wsn = _seq_workspace(OP_SOFTMAX_FWD, seqs, keys, H, Hk, d, d, dt)
+        _check(lib.luna_softmax_fwd(at, ak, ak + 32, dt, ctypes.addressof(seqs.c),
+                                    None if keys is None else ctypes.addressof(keys.c), H, Hk, d,
+                                    d ** -0.5 if scale is None else scale, at + 32, lp, wsp, wsn, _stream_ptr(seqs.device)))
+    return out, lse
+
+
+def softmax_attn_bwd(Q, K, V, out, lse, dO, scale: float | None = None, offsets=None, lens=None, k_offsets=None,
+                     k_lens=None, grads=None):
+    """Backward pass of softmax_attn (luna_softmax_bwd) from its out and lse: returns (dQ, dK, dV), into grads when
+    given; dK and dV are summed over the query heads of each key head."""
+    lib = load_library()
+    seqs = _Seqs(Q, offsets, lens, "Q")
+    H, Hk, d = Q.shape[1], K.shape[1], Q.shape[-1]
+    keys = _softmax_keys(Q, K, seqs, offsets, lens, k_offsets, k_lens)
+    klens = lens if keys is None else k_lens
+    dQ, dK, dV = (_new(Q, lens), _new(K, klens), _new(V, klens)) if grads is None else grads
+    rows = _seq_rows(seqs, (Q, out, dO, dQ), (H,) * 4, (d,) * 4, ("Q", "out", "dO", "dQ"))
+    krows = _seq_rows(keys or seqs, (K, V, dK, dV), (Hk,) * 4, (d,) * 4, ("K", "V", "dK", "dV"))
+    if keys is not None and (keys.dtype != seqs.dtype or keys.device != seqs.device):
+        raise LunaError(LUNA_ERR_INVALID_ARG, "Q and K must share dtype and GPU")
+    lp = _f32_ptr(lse, seqs.numbers(H), seqs.device, "lse")
+    dt, at, ak = _dt(Q), ctypes.addressof(rows), ctypes.addressof(krows)
+    with _on_device(seqs.device):
+        ws, wsp, wsn = _seq_workspace(OP_SOFTMAX_BWD, seqs, keys, H, Hk, d, d, dt)
+        _check(lib.luna_softmax_bwd(at, ak, ak + 32, at + 32, lp, at + 64, dt, ctypes.addressof(seqs.c),
+                                    None if keys is None else ctypes.addressof(keys.c), H, Hk, d,
+                                    d ** -0.5 if scale is None else scale, at + 96, ak + 64, ak + 96, wsp, wsn,
+                                    _stream_ptr(seqs.device)))
+    return dQ, dK, dV

@@ -1,0 +1,234 @@
+"""Causal softmax attention over sequences (luna_softmax_fwd, _bwd) against plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+from gpu_util import say
+from paper_2512_08061_amd import luna
+from seq_util import (U32, assert_norm, assert_within, cut, cut_num, device, packed_offsets, rand, softmax_grads, softmax_ref,
+                      unit)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    luna.load_library()
+    yield
+    torch.cuda.synchronize()
+
+
+def i32(xs):
+    return torch.tensor(xs, dtype=torch.int32, device=device())
+
+
+def make(layout, lens, H, Hk, d, dtype, seed=0, extra=0, klens=None):
+    gen = torch.Generator(device=device()).manual_seed(seed)
+    klens = lens if klens is None else klens
+    if layout == "packed":
+        shape = lambda ls, h: (sum(ls) + extra, h, d)  # noqa: E731
+    else:
+        shape = lambda ls, h: (len(ls), h, max(ls) + extra, d)  # noqa: E731
+    return rand(shape(lens, H), dtype, gen), rand(shape(klens, Hk), dtype, gen), rand(shape(klens, Hk), dtype, gen), gen
+
+
+def check_forward(Q, K, V, out, lse, layout, lens, klens=None, scale=None, what=""):
+    """Probabilities and out are rounded once each (U of sum P |v|); scores carry d fp32 additions, which move a
+    probability by as much of itself (and lse by as much), the sums n."""
+    klens = lens if klens is None else klens
+    d, group = Q.shape[-1], Q.shape[1] // K.shape[1]
+    scale = d ** -0.5 if scale is None else scale
+    u = unit(out.dtype) if out.dtype == torch.bfloat16 else 0.0
+    for i, n in enumerate(lens):
+        q, k, v = cut(Q, layout, lens, i), cut(K, layout, klens, i), cut(V, layout, klens, i)
+        if n == 0:
+            continue
+        got, glse = cut(out, layout, lens, i), cut_num(lse, layout, lens, i)
+        ref, rlse, _, size, seen = softmax_ref(q, k, v, scale, group)
+        some = seen.any(-1)
+        assert (got[:, ~some] == 0).all() and (glse[:, ~some] == -math.inf).all(), f"{what}: rows that see nothing"
+        if not some.any():
+            continue
+        most = abs(scale) * (q.abs().amax(1) * k.repeat_interleave(group, 0).abs().amax(1)).sum(-1)  # of any score's terms
+        score = ((d + 8) * U32 * most)[:, None]
+        sums = (klens[i] + 16) * U32
+        bound = (u + 2 * score[..., None] + 2 * sums) * size + u * ref.abs() + 1e-30
+        assert_within(got[:, some], ref[:, some], bound[:, some], f"{what} out[{i}]")
+        assert_within(glse[:, some], rlse[:, some], (score + sums + 4 * U32 * rlse.abs())[:, some] + 1e-30, f"{what} lse[{i}]")
+
+
+CASES = [  # layout, lens, H, Hk, d, dtype
+    ("batch", [1, 1], 2, 1, 32, "bf16"), ("batch", [64], 4, 2, 64, "bf16"), ("batch", [65, 65], 3, 3, 128, "bf16"),
+    ("batch", [1000], 4, 1, 128, "bf16"), ("packed", [1, 63, 0, 64, 65, 127, 300], 4, 2, 128, "bf16"),
+    ("packed", [0, 513, 129, 0], 2, 2, 64, "bf16"), ("packed", [31, 33, 257], 8, 2, 32, "bf16"),
+    ("batch", [200], 2, 1, 128, "f32"), ("packed", [1, 31, 32, 0, 33, 100], 4, 2, 64, "f32"), ("batch", [70, 70], 2, 2, 32, "f32")]
+
+
+@pytest.mark.parametrize("layout,lens,H,Hk,d,dtype", CASES)
+def test_forward(layout, lens, H, Hk, d, dtype):
+    say(f"softmax forward {layout} {lens} H={H} Hk={Hk} d={d} {dtype}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    Q, K, V, _ = make(layout, lens, H, Hk, d, dt)
+    opt = {"offsets": packed_offsets(lens)} if layout == "packed" else {}
+    out, lse = luna.softmax_attn(Q, K, V, **opt)
+    check_forward(Q, K, V, out, lse, layout, lens)
+
+
+@pytest.mark.parametrize("lens,klens,H,Hk,d,dtype", [
+    ([1, 1, 1], [1, 777, 64], 8, 2, 128, "bf16"), ([1, 1], [4097, 130], 4, 4, 64, "bf16"), ([1], [300], 16, 1, 128, "bf16"),
+    ([17, 17], [17, 500], 4, 1, 64, "bf16"), ([5, 5, 5], [3, 0, 70], 2, 1, 32, "bf16"), ([200, 200], [450, 90], 4, 2, 128, "bf16"),
+    ([1, 1], [900, 33], 6, 2, 32, "f32"), ([9, 9], [4, 300], 2, 2, 128, "f32")])
+def test_over_a_cache(lens, klens, H, Hk, d, dtype):
+    """New tokens behind the keys of a cache, also more of them than keys; unused rows of the cache hold NaN."""
+    say(f"softmax over a cache {lens} {klens} H={H} Hk={Hk} d={d} {dtype}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    Q, K, V, _ = make("batch", lens, H, Hk, d, dt, klens=klens)
+    for t in (K, V):
+        for i, n in enumerate(klens):
+            t[i, :, n:] = float("nan")
+    out, lse = luna.softmax_attn(Q, K, V, k_lens=i32(klens))
+    check_forward(Q, K, V, out, lse, "batch", lens, klens)
+    q = torch.cat([Q[i].transpose(0, 1) for i in range(len(lens))])
+    k, v = (torch.cat([t[i, :, :n].transpose(0, 1) for i, n in enumerate(klens)]) for t in (K, V))
+    out, lse = luna.softmax_attn(q, k, v, offsets=packed_offsets(lens), k_offsets=packed_offsets(klens))
+    check_forward(q, k, v, out, lse, "packed", lens, klens)
+
+
+def test_padded_batch_keeps_other_rows():
+    lens, H, d = [70, 0, 129, 1], 2, 64
+    Q, K, V, gen = make("batch", lens, H, 1, d, torch.bfloat16, extra=9)
+    dO = rand(Q.shape, torch.bfloat16, gen)
+    for t in (Q, K, V, dO):
+        for i, n in enumerate(lens):
+            t[i, :, n:] = float("nan")
+    out, grads = torch.full_like(Q, 7.0), tuple(torch.full_like(t, 7.0) for t in (Q, K, V))
+    lse = torch.full(Q.shape[:3], 7.0, device=device())
+    luna.softmax_attn(Q, K, V, lens=i32(lens), out=out, lse=lse)
+    check_forward(Q, K, V, out, lse, "batch", lens)
+    luna.softmax_attn_bwd(Q, K, V, out, lse, dO, lens=i32(lens), grads=grads)
+    for t in (out, lse) + grads:
+        assert all((t[i, :, n:] == 7.0).all() for i, n in enumerate(lens))
+        assert all(torch.isfinite(t[i, :, :n].float()).all() for i, n in enumerate(lens))
+
+
+def test_strides():
+    """Slices of one projection [T, (H + 2 Hk) d], and a [B, n, H, d] batch."""
+    gen = torch.Generator(device=device()).manual_seed(3)
+    lens, H, Hk, d = [100, 31], 4, 2, 64
+    x = rand((131, (H + 2 * Hk) * d), torch.bfloat16, gen).view(131, H + 2 * Hk, d)
+    Q, K, V = x[:, :H], x[:, H:H + Hk], x[:, H + Hk:]
+    out, lse = luna.softmax_attn(Q, K, V, offsets=packed_offsets(lens))
+    check_forward(Q, K, V, out, lse, "packed", lens)
+    Q, K, V = (rand((2, 200, h, d), torch.bfloat16, gen).transpose(1, 2) for h in (H, Hk, Hk))
+    out, lse = luna.softmax_attn(Q, K, V)
+    check_forward(Q, K, V, out, lse, "batch", [200, 200])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_scores(dtype):
+    """Scores in the hundreds, either sign of the scale: the running maximum moves along the row."""
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    Q, K, V, _ = make("batch", [300], 2, 1, 64, dt)
+    for scale in (8.0, -8.0, 0.0):
+        out, lse = luna.softmax_attn(Q, K, V, scale=scale)
+        check_forward(Q, K, V, out, lse, "batch", [300], scale=scale)
+
+
+BWD = [("batch", [2], 2, 1, 32, "bf16"), ("batch", [130, 130], 4, 2, 128, "bf16"), ("packed", [1, 64, 0, 65, 300], 4, 1, 64, "bf16"),
+       ("packed", [511, 100], 2, 2, 128, "bf16"), ("batch", [100], 4, 2, 64, "f32"), ("packed", [33, 1, 150], 2, 1, 128, "f32"),
+       ("batch", [90], 3, 3, 32, "bf16")]
+
+
+def check_backward(Q, K, V, dO, grads, layout, lens, klens=None):
+    """bf16: P, dS, out in dO.out and the result are rounded once each; fp32 sums."""
+    klens = lens if klens is None else klens
+    d, group, dt = Q.shape[-1], Q.shape[1] // K.shape[1], Q.dtype
+    u = unit(dt) if dt == torch.bfloat16 else 0.0
+    for i, n in enumerate(lens):
+        q, g = cut(Q, layout, lens, i), cut(dO, layout, lens, i)
+        k, v = cut(K, layout, klens, i), cut(V, layout, klens, i)
+        refs, sizes = softmax_grads(q, k, v, g, d ** -0.5, group)
+        if n:
+            most = d ** -0.5 * (q.abs().amax((0, 1)) * k.abs().amax((0, 1))).sum().item() if k.shape[1] else 0.0
+        for got, ref, size, name, ls in zip(grads, refs, sizes, ("dQ", "dK", "dV"), (lens, klens, klens)):
+            x = cut(got, layout, ls, i)
+            if n == 0:
+                assert (x == 0).all()
+                continue
+            sums = (n * group + klens[i] + 2 * d + 32) * U32 + 4 * (d + 8) * U32 * most
+            assert_within(x, ref, (3 * u + sums) * size + u * ref.abs() + 1e-30, f"{name}[{i}]")
+
+
+@pytest.mark.parametrize("layout,lens,H,Hk,d,dtype", BWD)
+def test_backward(layout, lens, H, Hk, d, dtype):
+    say(f"softmax backward {layout} {lens} H={H} Hk={Hk} d={d} {dtype}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    Q, K, V, gen = make(layout, lens, H, Hk, d, dt)
+    dO = rand(Q.shape, dt, gen)
+    opt = {"offsets": packed_offsets(lens)} if layout == "packed" else {}
+    out, lse = luna.softmax_attn(Q, K, V, **opt)
+    grads = luna.softmax_attn_bwd(Q, K, V, out, lse, dO, **opt)
+    check_backward(Q, K, V, dO, grads, layout, lens)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_backward_behind_a_cache(dtype):
+    """More keys than queries, fewer, and none."""
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    lens, klens = [70, 70, 70], [300, 40, 0]
+    Q, K, V, gen = make("batch", lens, 4, 2, 64, dt, klens=klens)
+    dO = rand(Q.shape, dt, gen)
+    out, lse = luna.softmax_attn(Q, K, V, k_lens=i32(klens))
+    grads = luna.softmax_attn_bwd(Q, K, V, out, lse, dO, k_lens=i32(klens))
+    check_backward(Q, K, V, dO, grads, "batch", lens, klens)
+
+
+def test_backward_against_differences():
+    """fp32 gradients against central differences of the 64-bit form along random directions."""
+    Q, K, V, gen = make("batch", [50], 4, 2, 32, torch.float32)
+    dO = rand(Q.shape, torch.float32, gen)
+    out, lse = luna.softmax_attn(Q, K, V)
+    grads = luna.softmax_attn_bwd(Q, K, V, out, lse, dO)
+    x = [t[0].double() for t in (Q, K, V)]
+    for i, name in enumerate("QKV"):
+        u = torch.randn(x[i].shape, generator=gen, device=device(), dtype=torch.float64)
+        h = 1e-5
+        f = lambda s: (softmax_ref(*[t + s * h * u if j == i else t for j, t in enumerate(x)], 32 ** -0.5, 2)[0] *  # noqa: E731
+                       dO[0].double()).sum()
+        want = ((f(1) - f(-1)) / (2 * h)).item()
+        got = (grads[i][0].double() * u).sum().item()
+        size = (grads[i][0].double() * u).abs().sum().item()
+        assert abs(got - want) <= 1e-5 * size + 1e-6, (name, got, want)
+
+
+def test_same_bits_streams_and_graph():
+    lens = [300, 1, 700]
+    Q, K, V, gen = make("packed", lens, 4, 2, 128, torch.bfloat16)
+    dO, off, few = rand(Q.shape, torch.bfloat16, gen), packed_offsets(lens), i32([0, 1, 2, 4])
+
+    def call():
+        out, lse = luna.softmax_attn(Q, K, V, offsets=off)
+        new = luna.softmax_attn(Q[-4:], K, V, offsets=few, k_offsets=off)
+        return (out, lse) + new + luna.softmax_attn_bwd(Q, K, V, out, lse, dO, offsets=off)
+
+    want = call()
+    assert all(torch.equal(a, b) for a, b in zip(call(), want))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = call()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = call()
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert all(torch.equal(a, b) for a, b in zip(call(), want))
