@@ -176,10 +176,18 @@ struct SoftmaxArgs {
   float* lse;  // per query row, out (forward: may be null) or in (backward)
   // backward
   SeqRows dO, dq, dk, dv;
+  float* parts;  // few queries over long keys: [slots][Hk][rows][d + 2], see luna_softmax_split.hip
   float* delta;  // per query row: dO.out, written by the query pass and read by the key pass
 };
 constexpr int kSoftmaxLeast = 64;  // the fewest rows of a tile: an upper bound for grids
 hipError_t launch_softmax_fwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
+// Few queries over long keys: m tokens of equal or padded sequences, up to 64 rows per key head, whose keys
+// then share one read of the cache; cut in pieces of kSplitKeys keys.
+constexpr int kSplitKeys = 512, kSplitRows = 64;
+inline bool softmax_splits(const SeqSet& qs, const SeqSet& ks, int64_t H, int64_t Hk) {
+  return !qs.offsets && qs.rows * (H / Hk) <= kSplitRows && ks.rows > 128;
+}
+hipError_t launch_softmax_split(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 hipError_t launch_softmax_bwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 
 }  // namespace luna

@@ -202,6 +202,13 @@ luna::SoftmaxArgs softmax_args(const luna_rows* Q, const luna_rows* K, const lun
   return a;
 }
 
+// bytes of the split call's partial rows, or 0 where the call is not split
+size_t split_bytes(const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d) {
+  const luna::SeqSet qs = set_of(seqs), ks = set_of(keys ? keys : seqs);
+  if (!luna::softmax_splits(qs, ks, H, Hk)) return 0;
+  return align256((size_t)luna::seq_slots(ks, luna::kSplitKeys) * H * qs.rows * (d + 2) * 4);
+}
+
 int64_t all_rows(const luna_seqs& s) { return s.offsets ? s.rows : s.count * s.rows; }
 
 }  // namespace
@@ -224,7 +231,7 @@ size_t luna_seq_workspace_bytes(int32_t op, luna_dtype dtype, const luna_seqs* s
       set_error(LUNA_ERR_INVALID_ARG, "Dq and Dv differ");
       return 0;
     }
-    return op == LUNA_OP_SOFTMAX_BWD ? align256((size_t)all_rows(*seqs) * H * 4) : 0;
+    return op == LUNA_OP_SOFTMAX_BWD ? align256((size_t)all_rows(*seqs) * H * 4) : split_bytes(seqs, keys, H, Hk, Dq);
   }
   set_error(LUNA_ERR_INVALID_ARG, "unknown operation");
   return 0;
@@ -384,9 +391,15 @@ luna_status luna_softmax_fwd(const luna_rows* Q, const luna_rows* K, const luna_
   if ((st = check_rows(K, "K", dtype, ks, Hk, d, false)) != LUNA_OK) return st;
   if ((st = check_rows(V, "V", dtype, ks, Hk, d, false)) != LUNA_OK) return st;
   if ((st = check_rows(out, "out", dtype, *seqs, H, d, true)) != LUNA_OK) return st;
+  const size_t need = split_bytes(seqs, keys, H, Hk, d);
+  if ((st = check_ws(need, ws, ws_bytes)) != LUNA_OK) return st;
   if (seqs->rows == 0) return LUNA_OK;
   luna::SoftmaxArgs a = softmax_args(Q, K, V, out, seqs, keys, H, Hk, d, scale);
   a.lse = lse;
+  if (need) {
+    a.parts = static_cast<float*>(ws);
+    return hip_status(luna::launch_softmax_split(type_of(dtype), a, reinterpret_cast<hipStream_t>(stream)), "split softmax launch");
+  }
   return hip_status(luna::launch_softmax_fwd(type_of(dtype), a, reinterpret_cast<hipStream_t>(stream)), "softmax launch");
 }
 
