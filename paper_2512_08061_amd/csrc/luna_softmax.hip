@@ -117,6 +117,167 @@ __global__ __launch_bounds__(256) void softmax_fwd_kernel(SoftmaxArgs a) {
   if (a.lse && g == 0 && i < m) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (top + log2f(sum)) * kLn2;
 }
 
+// bf16 with d = 64 and 128: 32 x 32 x 16 products, a wave with 32 queries of a workgroup's 128, keys in blocks of 64.
+// Lane (h, c) of a 32-key block of S^T holds keys 8 (i / 4) + 4 h + i % 4 of query c; eight of the sixteen
+// are the k-slots of its half for the product with V.  The next block is on its way to registers while one is worked on.
+// The output is rescaled only when some row's maximum has grown by more than 2^8 since its last rescaling (a sum of
+// at most 2^8 times larger terms keeps its relative accuracy), which most blocks skip.
+template <int DH>
+struct SoftmaxLds32 {
+  static constexpr int KB = 64, P = DH + 16;
+  __bf16 k[2][KB][P], v[2][KB][P];
+};
+
+template <int DH>
+__global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
+  using Lds = SoftmaxLds32<DH>;
+  constexpr int KB = Lds::KB, P = Lds::P, KS = DH / 16, CT = DH / 32, NL = KB * DH / 8 / 256, esz = 2;
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  Lds& l = *reinterpret_cast<Lds*>(raw);
+  const int lane = threadIdx.x % kWave, wave = wave_id(), h = lane / 32, c = lane % 32;
+  const int head = head_of(blockIdx.x % a.H, a.H), slot = gridDim.x / a.H - 1 - blockIdx.x / a.H;
+  const SeqPiece sq = seq_piece(a.qs, slot, 128);
+  if (sq.seq < 0) return;
+  const SeqPiece sk = seq_of(a.ks, sq.seq);
+  const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
+  const int q0 = sq.index * 128, m = min(128, sq.len - q0);
+  const int shift = sk.len - sq.len;
+  const int kend = min(sk.len, max(0, q0 + m + shift));
+  const int i = 32 * wave + c, last = q0 + i + shift;
+  const int wfirst = q0 + 32 * wave + shift, wlast = min(wfirst + 31, kend - 1);  // the wave's rows see all keys up to / none behind
+  const int hk = head / (a.H / a.Hk);
+
+  bf16x8 qf[KS];
+  {
+    const Buf b = buffer(seq_row(a.q, sq, pq, head, q0, esz), (int)(((m - 1) * a.q.row + DH) * esz));
+#pragma unroll
+    for (int t = 0; t < KS; ++t)
+      qf[t] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(
+                                             b, i < m ? (i * (int)a.q.row + 16 * t + 8 * h) * esz : kPastEnd, 0, 0));
+  }
+  const float scale = a.scale * kLog2e;
+  f32x16 o[CT];
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
+  float base = -__builtin_inff(), sum = 0.0f;
+
+  i32x4 kr[NL], vr[NL];
+  const auto load = [&](int k0) {
+    const int kn = min(KB, kend - k0);
+    const Buf bk = buffer(seq_row(a.k, sk, pk, hk, k0, esz), kn > 0 ? (int)(((kn - 1) * a.k.row + DH) * esz) : 0);
+    const Buf bv = buffer(seq_row(a.v, sk, pk, hk, k0, esz), kn > 0 ? (int)(((kn - 1) * a.v.row + DH) * esz) : 0);
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int idx = threadIdx.x + 256 * j, r = idx / (DH / 8), col = idx % (DH / 8) * 8;
+      kr[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(bk, r < kn ? (r * (int)a.k.row + col) * esz : kPastEnd, 0, 0));
+      vr[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(bv, r < kn ? (r * (int)a.v.row + col) * esz : kPastEnd, 0, 0));
+    }
+  };
+  const auto store = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < NL; ++j) {
+      const int idx = threadIdx.x + 256 * j, r = idx / (DH / 8), col = idx % (DH / 8) * 8;
+      *reinterpret_cast<i32x4*>(&l.k[buf][r][col]) = kr[j];
+      *reinterpret_cast<i32x4*>(&l.v[buf][r][col]) = vr[j];
+    }
+  };
+  load(0);
+  int buf = 0;
+  for (int k0 = 0; k0 < kend; k0 += KB, buf ^= 1) {
+    store(buf);
+    load(k0 + KB);
+    __syncthreads();
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int kb = k0 + 32 * half;
+      if (kb > wlast) break;
+      f32x16 s;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+#pragma unroll
+      for (int t = 0; t < KS; ++t) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(&l.k[buf][32 * half + c][16 * t + 8 * h]);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[t], s, 0, 0, 0);
+      }
+      float most = -__builtin_inff();
+      if (kb + 31 <= wfirst) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[e] *= scale;
+          most = fmaxf(most, s[e]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int key = kb + 8 * (e / 4) + 4 * h + e % 4;
+          const float x = s[e] * scale;
+          s[e] = key <= last && key < kend ? x : -__builtin_inff();
+          most = fmaxf(most, s[e]);
+        }
+      }
+      {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+        most = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+      }
+      const bool grow = most > base + 8.0f;  // (base -inf: any key seen; NaN: no)
+      if (__any(grow)) {
+        const float to = grow ? most : base;
+        const float f = exp2_raw(base - (to == -__builtin_inff() ? 0.0f : to));
+        base = to;
+        sum *= f;
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[t][e] *= f;
+      }
+      const float b = base == -__builtin_inff() ? 0.0f : base;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[e] = exp2_raw(s[e] - b);
+        sum += s[e];
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        Frag<__bf16> pf;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) pf.set2(e, s[8 * ks + e], s[8 * ks + e + 1]);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          Frag<__bf16> vf;
+          const int row = 32 * half + 16 * ks + 4 * h, col = 32 * t + 16 * ((lane / 16) % 2);
+          load_tr4(vf, 0, &l.v[buf][0][0], P, row, col, lane);
+          load_tr4(vf, 4, &l.v[buf][0][0], P, row + 8, col, lane);
+          o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf.v, o[t], 0, 0, 0);
+        }
+      }
+    }
+  }
+  {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    sum = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;  // (NaN stays)
+  const Buf b = buffer(seq_row(a.o, sq, pq, head, q0, esz), (int)(((m - 1) * a.o.row + DH) * esz));
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      buf_store4<__bf16>(b, i < m ? (i * (int)a.o.row + 32 * t + 2 * e + 4 * h) * esz : kPastEnd, o[t][e] * inv, o[t][e + 1] * inv,
+                         o[t][e + 2] * inv, o[t][e + 3] * inv);
+  if (a.lse && h == 0 && i < m) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (base + log2f(sum)) * kLn2;
+}
+
+template <int DH>
+hipError_t launch_fwd32(const SoftmaxArgs& a, hipStream_t s) {
+  constexpr int bytes = (int)sizeof(SoftmaxLds32<DH>);
+  const hipError_t e = allow_lds<softmax_fwd32_kernel<DH>>(bytes);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((softmax_fwd32_kernel<DH>), dim3((unsigned)(seq_slots(a.qs, 128) * a.H)), dim3(256), bytes, s, a);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_fwd(const SoftmaxArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(seq_slots(a.qs, kSoftmaxTile) * a.H));
@@ -129,7 +290,8 @@ hipError_t launch_fwd(const SoftmaxArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_softmax_fwd(Dt dt, const SoftmaxArgs& a, hipStream_t s) {
-  return dt == Dt::BF16 ? launch_fwd<__bf16>(a, s) : launch_fwd<float>(a, s);
+  if (dt == Dt::F32) return launch_fwd<float>(a, s);
+  return a.d == 32 ? launch_fwd<__bf16>(a, s) : a.d == 64 ? launch_fwd32<64>(a, s) : launch_fwd32<128>(a, s);
 }
 
 }  // namespace luna

@@ -43,6 +43,12 @@ __device__ __forceinline__ float groups_max(float x) {
   return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+// Head of a workgroup of H consecutive ones: consecutive workgroups go to the eight dies in turn, so that heads
+// i, i + 8, ... meet on one; it gets neighbours, which share key heads.
+__device__ __forceinline__ int head_of(int i, int H) { return H % 8 == 0 ? i % 8 * (H / 8) + i / 8 : i; }
+
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kSoftmaxTile = 64;  // query rows (key rows) of a workgroup
 
