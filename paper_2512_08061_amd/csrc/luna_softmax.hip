@@ -124,16 +124,14 @@ __global__ __launch_bounds__(256) void softmax_fwd_kernel(SoftmaxArgs a) {
 // at most 2^8 times larger terms keeps its relative accuracy), which most blocks skip.
 template <int DH>
 struct SoftmaxLds32 {
-  static constexpr int KB = 64, P = DH + 16;
-  __bf16 k[2][KB][P], v[2][KB][P];
+  Tile<DH> k[2], v[2];
 };
 
 template <int DH>
 __global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
-  using Lds = SoftmaxLds32<DH>;
-  constexpr int KB = Lds::KB, P = Lds::P, KS = DH / 16, CT = DH / 32, NL = KB * DH / 8 / 256, esz = 2;
+  constexpr int KB = 64, KS = DH / 16, CT = DH / 32, esz = 2;
   extern __shared__ __attribute__((aligned(16))) char raw[];
-  Lds& l = *reinterpret_cast<Lds*>(raw);
+  SoftmaxLds32<DH>& l = *reinterpret_cast<SoftmaxLds32<DH>*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id(), h = lane / 32, c = lane % 32;
   const int head = head_of(blockIdx.x % a.H, a.H), slot = gridDim.x / a.H - 1 - blockIdx.x / a.H;
   const SeqPiece sq = seq_piece(a.qs, slot, 128);
@@ -147,15 +145,19 @@ __global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
   const int wfirst = q0 + 32 * wave + shift, wlast = min(wfirst + 31, kend - 1);  // the wave's rows see all keys up to / none behind
   const int hk = head / (a.H / a.Hk);
 
+  // scores are taken with |scale|, the sign going to q (0 as a tiny scale, so that masked scores stay -infinity)
   bf16x8 qf[KS];
   {
     const Buf b = buffer(seq_row(a.q, sq, pq, head, q0, esz), (int)(((m - 1) * a.q.row + DH) * esz));
+    const int flip = a.scale < 0.0f ? (int)0x80008000 : 0;
 #pragma unroll
-    for (int t = 0; t < KS; ++t)
-      qf[t] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(
-                                             b, i < m ? (i * (int)a.q.row + 16 * t + 8 * h) * esz : kPastEnd, 0, 0));
+    for (int t = 0; t < KS; ++t) {
+      i32x4 x = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                              b, i < m ? (i * (int)a.q.row + 16 * t + 8 * h) * esz : kPastEnd, 0, 0));
+      qf[t] = __builtin_bit_cast(bf16x8, x ^ flip);
+    }
   }
-  const float scale = a.scale * kLog2e;
+  const float scale = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f);
   f32x16 o[CT];
 #pragma unroll
   for (int t = 0; t < CT; ++t)
@@ -163,63 +165,56 @@ __global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
     for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
   float base = -__builtin_inff(), sum = 0.0f;
 
-  i32x4 kr[NL], vr[NL];
+  TileRegs<DH> kr, vr;
   const auto load = [&](int k0) {
-    const int kn = min(KB, kend - k0);
-    const Buf bk = buffer(seq_row(a.k, sk, pk, hk, k0, esz), kn > 0 ? (int)(((kn - 1) * a.k.row + DH) * esz) : 0);
-    const Buf bv = buffer(seq_row(a.v, sk, pk, hk, k0, esz), kn > 0 ? (int)(((kn - 1) * a.v.row + DH) * esz) : 0);
-#pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const int idx = threadIdx.x + 256 * j, r = idx / (DH / 8), col = idx % (DH / 8) * 8;
-      kr[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(bk, r < kn ? (r * (int)a.k.row + col) * esz : kPastEnd, 0, 0));
-      vr[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(bv, r < kn ? (r * (int)a.v.row + col) * esz : kPastEnd, 0, 0));
-    }
-  };
-  const auto store = [&](int buf) {
-#pragma unroll
-    for (int j = 0; j < NL; ++j) {
-      const int idx = threadIdx.x + 256 * j, r = idx / (DH / 8), col = idx % (DH / 8) * 8;
-      *reinterpret_cast<i32x4*>(&l.k[buf][r][col]) = kr[j];
-      *reinterpret_cast<i32x4*>(&l.v[buf][r][col]) = vr[j];
-    }
+    Tile<DH>::load(kr, seq_row(a.k, sk, pk, hk, k0, esz), a.k.row, min(KB, kend - k0));
+    Tile<DH>::load(vr, seq_row(a.v, sk, pk, hk, k0, esz), a.v.row, min(KB, kend - k0));
   };
   load(0);
+  l.k[0].store(kr);
+  l.v[0].store(vr);
   int buf = 0;
   for (int k0 = 0; k0 < kend; k0 += KB, buf ^= 1) {
-    store(buf);
+    __syncthreads();  // this block is whole, and the one before no longer read
     load(k0 + KB);
-    __syncthreads();
+    if (k0 <= wlast) {
+      f32x16 s[2];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int kb = k0 + 32 * half;
-      if (kb > wlast) break;
-      f32x16 s;
+      for (int half = 0; half < 2; ++half)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+        for (int e = 0; e < 16; ++e) s[half][e] = 0.0f;
 #pragma unroll
-      for (int t = 0; t < KS; ++t) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(&l.k[buf][32 * half + c][16 * t + 8 * h]);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[t], s, 0, 0, 0);
-      }
-      float most = -__builtin_inff();
-      if (kb + 31 <= wfirst) {
+      for (int t = 0; t < KS; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          s[e] *= scale;
-          most = fmaxf(most, s[e]);
+        for (int half = 0; half < 2; ++half)
+          s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(l.k[buf].row8(32 * half + c, 2 * t + h), qf[t], s[half], 0, 0, 0);
+      // V operands of 16 keys, read one step before their products (by itself the compiler reads each right before
+      // its use and waits out the LDS 16 times a block)
+      Frag<__bf16> vf[2][CT];
+      const auto read_v = [&](int ks) {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          const int row = 16 * ks + 4 * h, col = 32 * t + 16 * ((lane / 16) % 2);
+          l.v[buf].tr4(vf[ks % 2][t], 0, row, col, lane);
+          l.v[buf].tr4(vf[ks % 2][t], 4, row + 8, col, lane);
         }
-      } else {
+      };
+      read_v(0);
+      if (k0 + KB - 1 > wfirst || k0 + KB > kend) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = kb + 8 * (e / 4) + 4 * h + e % 4;
-          const float x = s[e] * scale;
-          s[e] = key <= last && key < kend ? x : -__builtin_inff();
-          most = fmaxf(most, s[e]);
-        }
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int key = k0 + 32 * half + 8 * (e / 4) + 4 * h + e % 4;
+            s[half][e] = key <= last && key < kend ? s[half][e] : -__builtin_inff();
+          }
       }
+      float most = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+      for (int e = 1; e < 16; ++e) most = fmaxf(fmaxf(most, s[0][e]), s[1][e]);
       {
         const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
-        most = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+        most = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])) * scale;
       }
       const bool grow = most > base + 8.0f;  // (base -inf: any key seen; NaN: no)
       if (__any(grow)) {
@@ -234,25 +229,25 @@ __global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
       }
       const float b = base == -__builtin_inff() ? 0.0f : base;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[e] = exp2_raw(s[e] - b);
-        sum += s[e];
-      }
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
+      for (int ks = 0; ks < 4; ++ks) {
         Frag<__bf16> pf;
+        float part = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) pf.set2(e, s[8 * ks + e], s[8 * ks + e + 1]);
-#pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          Frag<__bf16> vf;
-          const int row = 32 * half + 16 * ks + 4 * h, col = 32 * t + 16 * ((lane / 16) % 2);
-          load_tr4(vf, 0, &l.v[buf][0][0], P, row, col, lane);
-          load_tr4(vf, 4, &l.v[buf][0][0], P, row + 8, col, lane);
-          o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf.v, o[t], 0, 0, 0);
+        for (int e = 0; e < 8; e += 2) {
+          const float x = exp2_raw(fmaf(s[ks / 2][8 * (ks % 2) + e], scale, -b));
+          const float y = exp2_raw(fmaf(s[ks / 2][8 * (ks % 2) + e + 1], scale, -b));
+          part += x + y;
+          pf.set2(e, x, y);
         }
+        sum += part;
+        if (ks < 3) read_v(ks + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks % 2][t].v, pf.v, o[t], 0, 0, 0);
       }
     }
+    l.k[buf ^ 1].store(kr);
+    l.v[buf ^ 1].store(vr);
   }
   {
     const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);

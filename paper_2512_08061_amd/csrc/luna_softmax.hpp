@@ -49,6 +49,55 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 // i, i + 8, ... meet on one; it gets neighbours, which share key heads.
 __device__ __forceinline__ int head_of(int i, int H) { return H % 8 == 0 ? i % 8 * (H / 8) + i / 8 : i; }
 
+// A tile of 64 bf16 rows in LDS.  The 16-byte pieces of a row are swapped among each other by the row's number, so
+// that eight rows' pieces of one column, and the two pieces by four rows of a transposing read, lie in different banks.
+// Rows come through registers: a thread's pieces are asked for a tile ahead and stored when the tile is free.  (Loads
+// that go to LDS directly save those registers and stores, but the compiler waits for all of them before
+// any transposing read.)
+template <int DH>
+struct TileRegs {
+  i32x4 x[64 * DH / 8 / 256];
+};
+template <int DH>
+struct Tile {
+  static constexpr int PIECES = DH / 8;
+  __bf16 x[64 * DH];
+
+  static __device__ __forceinline__ int swap(int row) {
+    return DH == 128 ? (row % 4) * 2 + (row / 4) % 2 : ((row / 2) % 4) * 2;
+  }
+  // `n` rows from `base`, the others as zeros
+  static __device__ __forceinline__ void load(TileRegs<DH>& t, const char* base, int64_t row, int n) {
+    const Buf b = buffer(base, n > 0 ? (int)(((n - 1) * row + DH) * 2) : 0);
+#pragma unroll
+    for (int j = 0; j < 64 * PIECES / 256; ++j) {
+      const int at = threadIdx.x + 256 * j, r = at / PIECES, piece = at % PIECES;
+      t.x[j] = __builtin_bit_cast(
+          i32x4, __builtin_amdgcn_raw_buffer_load_b128(b, r < n ? (r * (int)row + piece * 8) * 2 : kPastEnd, 0, 0));
+    }
+  }
+  __device__ __forceinline__ void store(const TileRegs<DH>& t) {
+#pragma unroll
+    for (int j = 0; j < 64 * PIECES / 256; ++j) {
+      const int at = threadIdx.x + 256 * j, r = at / PIECES, piece = at % PIECES;
+      *reinterpret_cast<i32x4*>(&x[r * DH + ((piece ^ swap(r)) * 8)]) = t.x[j];
+    }
+  }
+  // elements 8 piece .. 8 piece + 7 of a row
+  __device__ __forceinline__ bf16x8 row8(int row, int piece) const {
+    return *reinterpret_cast<const bf16x8*>(&x[row * DH + ((piece ^ swap(row)) * 8)]);
+  }
+  // transposed: rows k0 .. k0 + 3 of column c0 + lane % 16 into slots e0 .. e0 + 3 (see load_tr4)
+  __device__ __forceinline__ void tr4(Frag<__bf16>& f, int e0, int k0, int c0, int lane) const {
+    const int i = lane % 16, row = k0 + i / 4, col = c0 + 4 * (i % 4);
+    typedef __attribute__((ext_vector_type(4))) short i16x4;
+    const __bf16* src = &x[row * DH + (((col / 8) ^ swap(row)) * 8) + col % 8];
+    const i16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) i16x4*)(__attribute__((address_space(3))) void*)(src));
+    const bf16x4 b = __builtin_bit_cast(bf16x4, v);
+    f.v[e0 + 0] = b[0]; f.v[e0 + 1] = b[1]; f.v[e0 + 2] = b[2]; f.v[e0 + 3] = b[3];
+  }
+};
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kSoftmaxTile = 64;  // query rows (key rows) of a workgroup
 
