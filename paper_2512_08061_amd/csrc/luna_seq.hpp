@@ -176,7 +176,8 @@ struct SoftmaxArgs {
   float* lse;  // per query row, out (forward: may be null) or in (backward)
   // backward
   SeqRows dO, dq, dk, dv;
-  float* parts;  // few queries over long keys: [slots][Hk][rows][d + 2], see luna_softmax_split.hip
+  float* parts;  // few queries over long keys: [slots][Hk][rows][d + 2], see luna_softmax_split.hip;
+                 // backward: [H] numbers per key row of 2 d floats, see softmax_head_parts
   float* delta;  // per query row: dO.out, written by the query pass and read by the key pass
 };
 constexpr int kSoftmaxLeast = 64;  // the fewest rows of a tile: an upper bound for grids
@@ -188,6 +189,11 @@ inline bool softmax_splits(const SeqSet& qs, const SeqSet& ks, int64_t H, int64_
   return !qs.offsets && qs.rows * (H / Hk) <= kSplitRows && ks.rows > 128;
 }
 hipError_t launch_softmax_split(Dt dt, const SoftmaxArgs& a, hipStream_t s);
+// Whether dK and dV are formed per query head, in fp32 parts that are added up: where key tiles and heads alone
+// would not fill the compute units a few times over (their work is very unequal: early keys are seen by more queries).
+inline bool softmax_head_parts(Dt dt, const SeqSet& ks, int64_t H, int64_t Hk, int64_t d) {
+  return dt == Dt::BF16 && d >= 64 && H > Hk && seq_slots(ks, 128) * Hk < 1024;
+}
 hipError_t launch_softmax_bwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 
 }  // namespace luna

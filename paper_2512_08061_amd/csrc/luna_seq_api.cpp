@@ -202,6 +202,16 @@ luna::SoftmaxArgs softmax_args(const luna_rows* Q, const luna_rows* K, const lun
   return a;
 }
 
+int64_t all_rows(const luna_seqs& s) { return s.offsets ? s.rows : s.count * s.rows; }
+
+// bytes of the backward pass's dO.out per query row, and of the key rows' parts behind them
+size_t delta_bytes(const luna_seqs* seqs, int64_t H) { return align256((size_t)all_rows(*seqs) * H * 4); }
+size_t head_part_bytes(luna_dtype dt, const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d) {
+  const luna_seqs* ks = keys ? keys : seqs;
+  if (!luna::softmax_head_parts(type_of(dt), set_of(ks), H, Hk, d)) return 0;
+  return align256((size_t)all_rows(*ks) * H * 2 * d * 4);
+}
+
 // bytes of the split call's partial rows, or 0 where the call is not split
 size_t split_bytes(const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d) {
   const luna::SeqSet qs = set_of(seqs), ks = set_of(keys ? keys : seqs);
@@ -209,7 +219,6 @@ size_t split_bytes(const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int6
   return align256((size_t)luna::seq_slots(ks, luna::kSplitKeys) * H * qs.rows * (d + 2) * 4);
 }
 
-int64_t all_rows(const luna_seqs& s) { return s.offsets ? s.rows : s.count * s.rows; }
 
 }  // namespace
 
@@ -231,7 +240,8 @@ size_t luna_seq_workspace_bytes(int32_t op, luna_dtype dtype, const luna_seqs* s
       set_error(LUNA_ERR_INVALID_ARG, "Dq and Dv differ");
       return 0;
     }
-    return op == LUNA_OP_SOFTMAX_BWD ? align256((size_t)all_rows(*seqs) * H * 4) : split_bytes(seqs, keys, H, Hk, Dq);
+    return op == LUNA_OP_SOFTMAX_BWD ? delta_bytes(seqs, H) + head_part_bytes(dtype, seqs, keys, H, Hk, Dq)
+                                     : split_bytes(seqs, keys, H, Hk, Dq);
   }
   set_error(LUNA_ERR_INVALID_ARG, "unknown operation");
   return 0;
@@ -420,8 +430,8 @@ luna_status luna_softmax_bwd(const luna_rows* Q, const luna_rows* K, const luna_
   if ((st = check_rows(dQ, "dQ", dtype, *seqs, H, d, true)) != LUNA_OK) return st;
   if ((st = check_rows(dK, "dK", dtype, ks, Hk, d, true)) != LUNA_OK) return st;
   if ((st = check_rows(dV, "dV", dtype, ks, Hk, d, true)) != LUNA_OK) return st;
-  const size_t need = align256((size_t)all_rows(*seqs) * H * 4);
-  if ((st = check_ws(need, ws, ws_bytes)) != LUNA_OK) return st;
+  const size_t deltas = delta_bytes(seqs, H), parts = head_part_bytes(dtype, seqs, keys, H, Hk, d);
+  if ((st = check_ws(deltas + parts, ws, ws_bytes)) != LUNA_OK) return st;
   luna::SoftmaxArgs a = softmax_args(Q, K, V, out, seqs, keys, H, Hk, d, scale);
   a.lse = const_cast<float*>(lse);
   a.dO = rows_of(dO);
@@ -429,6 +439,7 @@ luna_status luna_softmax_bwd(const luna_rows* Q, const luna_rows* K, const luna_
   a.dk = rows_of(dK);
   a.dv = rows_of(dV);
   a.delta = static_cast<float*>(ws);
+  if (parts) a.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + deltas);
   return hip_status(luna::launch_softmax_bwd(type_of(dtype), a, reinterpret_cast<hipStream_t>(stream)), "softmax backward launch");
 }
 

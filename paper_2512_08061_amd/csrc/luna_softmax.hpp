@@ -54,9 +54,9 @@ __device__ __forceinline__ int head_of(int i, int H) { return H % 8 == 0 ? i % 8
 // Rows come through registers: a thread's pieces are asked for a tile ahead and stored when the tile is free.  (Loads
 // that go to LDS directly save those registers and stores, but the compiler waits for all of them before
 // any transposing read.)
-template <int DH>
+template <int DH, int THREADS = 256>
 struct TileRegs {
-  i32x4 x[64 * DH / 8 / 256];
+  i32x4 x[64 * DH / 8 / THREADS];
 };
 template <int DH>
 struct Tile {
@@ -67,19 +67,21 @@ struct Tile {
     return DH == 128 ? (row % 4) * 2 + (row / 4) % 2 : ((row / 2) % 4) * 2;
   }
   // `n` rows from `base`, the others as zeros
-  static __device__ __forceinline__ void load(TileRegs<DH>& t, const char* base, int64_t row, int n) {
+  template <int THREADS>
+  static __device__ __forceinline__ void load(TileRegs<DH, THREADS>& t, const char* base, int64_t row, int n) {
     const Buf b = buffer(base, n > 0 ? (int)(((n - 1) * row + DH) * 2) : 0);
 #pragma unroll
-    for (int j = 0; j < 64 * PIECES / 256; ++j) {
-      const int at = threadIdx.x + 256 * j, r = at / PIECES, piece = at % PIECES;
+    for (int j = 0; j < 64 * PIECES / THREADS; ++j) {
+      const int at = threadIdx.x + THREADS * j, r = at / PIECES, piece = at % PIECES;
       t.x[j] = __builtin_bit_cast(
           i32x4, __builtin_amdgcn_raw_buffer_load_b128(b, r < n ? (r * (int)row + piece * 8) * 2 : kPastEnd, 0, 0));
     }
   }
-  __device__ __forceinline__ void store(const TileRegs<DH>& t) {
+  template <int THREADS>
+  __device__ __forceinline__ void store(const TileRegs<DH, THREADS>& t) {
 #pragma unroll
-    for (int j = 0; j < 64 * PIECES / 256; ++j) {
-      const int at = threadIdx.x + 256 * j, r = at / PIECES, piece = at % PIECES;
+    for (int j = 0; j < 64 * PIECES / THREADS; ++j) {
+      const int at = threadIdx.x + THREADS * j, r = at / PIECES, piece = at % PIECES;
       *reinterpret_cast<i32x4*>(&x[r * DH + ((piece ^ swap(r)) * 8)]) = t.x[j];
     }
   }
@@ -98,6 +100,18 @@ struct Tile {
     f.v[e0 + 0] = b[0]; f.v[e0 + 1] = b[1]; f.v[e0 + 2] = b[2]; f.v[e0 + 3] = b[3];
   }
 };
+// x over the two halves of a wave
+__device__ __forceinline__ float halves_sum(float x) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+  return z;
+}
+
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kSoftmaxTile = 64;  // query rows (key rows) of a workgroup
 

@@ -199,6 +199,319 @@ __global__ __launch_bounds__(256) void softmax_dkdv_kernel(SoftmaxArgs a) {
   }
 }
 
+// bf16 with d = 64 and 128: 32 x 32 x 16 products (lane (h, c) of a result holds rows 8 (i / 4) + 4 h + i % 4 of column
+// c), 32 rows of a workgroup's 128 to a wave.
+template <int DH>
+struct SoftmaxBwdLds32 {
+  Tile<DH> x[2], y[2];
+};
+
+// this lane's row as B operands
+template <int DH>
+__device__ __forceinline__ void row_operands(bf16x8 (&f)[DH / 16], const char* base, int64_t row, int m, int r, int h) {
+  const Buf b = buffer(base, m > 0 ? (int)(((m - 1) * row + DH) * 2) : 0);
+#pragma unroll
+  for (int t = 0; t < DH / 16; ++t)
+    f[t] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(
+                                          b, r < m ? (r * (int)row + 16 * t + 8 * h) * 2 : kPastEnd, 0, 0));
+}
+
+template <int DH>
+__device__ __forceinline__ void store_rows(char* base, int64_t row, int m, int r, int h, const f32x16 (&x)[DH / 32], float f) {
+  const Buf b = buffer(base, (int)(((m - 1) * row + DH) * 2));
+#pragma unroll
+  for (int t = 0; t < DH / 32; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      buf_store4<__bf16>(b, r < m ? (r * (int)row + 32 * t + 2 * e + 4 * h) * 2 : kPastEnd, x[t][e] * f, x[t][e + 1] * f,
+                         x[t][e + 2] * f, x[t][e + 3] * f);
+}
+
+template <int DH>
+__global__ __launch_bounds__(256, 2) void softmax_dq32_kernel(SoftmaxArgs a) {
+  constexpr int KB = 64, KS = DH / 16, CT = DH / 32, esz = 2;
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  SoftmaxBwdLds32<DH>& l = *reinterpret_cast<SoftmaxBwdLds32<DH>*>(raw);
+  const int lane = threadIdx.x % kWave, wave = wave_id(), h = lane / 32, c = lane % 32;
+  const int head = head_of(blockIdx.x % a.H, a.H), slot = gridDim.x / a.H - 1 - blockIdx.x / a.H;
+  const SeqPiece sq = seq_piece(a.qs, slot, 128);
+  if (sq.seq < 0) return;
+  const SeqPiece sk = seq_of(a.ks, sq.seq);
+  const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
+  const int q0 = sq.index * 128, m = min(128, sq.len - q0);
+  const int shift = sk.len - sq.len;
+  const int kend = min(sk.len, max(0, q0 + m + shift));
+  const int i = 32 * wave + c, last = q0 + i + shift;
+  const int wfirst = q0 + 32 * wave + shift, wlast = min(wfirst + 31, kend - 1);
+  const int hk = head / (a.H / a.Hk);
+  const int64_t num = seq_num(a.qs, sq, a.H, head, q0 + i);
+
+  bf16x8 qf[KS], gf[KS];
+  row_operands<DH>(qf, seq_row(a.q, sq, pq, head, q0, esz), a.q.row, m, i, h);
+  row_operands<DH>(gf, seq_row(a.dO, sq, pq, head, q0, esz), a.dO.row, m, i, h);
+  float delta = 0.0f;
+  {
+    bf16x8 of[KS];
+    row_operands<DH>(of, seq_row(a.o, sq, pq, head, q0, esz), a.o.row, m, i, h);
+#pragma unroll
+    for (int t = 0; t < KS; ++t)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf((float)gf[t][e], (float)of[t][e], delta);
+  }
+  delta = halves_sum(delta);
+  if (h == 0 && i < m) a.delta[num] = delta;
+  if (a.scale < 0.0f)  // (the sign of the scale goes to q, as in the forward pass)
+#pragma unroll
+    for (int t = 0; t < KS; ++t) qf[t] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(i32x4, qf[t]) ^ (int)0x80008000);
+  const float scale = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f);
+  float lse = i < m ? a.lse[num] * kLog2e : 0.0f;
+  if (lse == -__builtin_inff()) lse = __builtin_inff();  // (a row that sees nothing: exp2(-infinity - infinity) below)
+  f32x16 dq[CT];
+#pragma unroll
+  for (int t = 0; t < CT; ++t) dq[t] = zero16();
+
+  TileRegs<DH> kr, vr;
+  const auto load = [&](int k0) {
+    Tile<DH>::load(kr, seq_row(a.k, sk, pk, hk, k0, esz), a.k.row, min(KB, kend - k0));
+    Tile<DH>::load(vr, seq_row(a.v, sk, pk, hk, k0, esz), a.v.row, min(KB, kend - k0));
+  };
+  load(0);
+  l.x[0].store(kr);
+  l.y[0].store(vr);
+  int buf = 0;
+  for (int k0 = 0; k0 < kend; k0 += KB, buf ^= 1) {
+    __syncthreads();  // this block is whole, and the one before no longer read
+    load(k0 + KB);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int kb = k0 + 32 * half;
+      if (kb > wlast) break;
+      f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+      for (int t = 0; t < KS; ++t) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(l.x[buf].row8(32 * half + c, 2 * t + h), qf[t], s, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(l.y[buf].row8(32 * half + c, 2 * t + h), gf[t], dp, 0, 0, 0);
+      }
+      // K^T operands of 16 keys, read a step before their products
+      Frag<__bf16> kf[2][CT];
+      const auto read_k = [&](int ks) {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          const int row = 32 * half + 16 * ks + 4 * h, col = 32 * t + 16 * ((lane / 16) % 2);
+          l.x[buf].tr4(kf[ks][t], 0, row, col, lane);
+          l.x[buf].tr4(kf[ks][t], 4, row + 8, col, lane);
+        }
+      };
+      read_k(0);
+      if (kb + 31 > wfirst) {  // some row does not see some key
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int key = kb + 8 * (e / 4) + 4 * h + e % 4;
+          s[e] = key <= last && key < kend ? s[e] : -__builtin_inff();
+        }
+      }
+      Frag<__bf16> ds[2];
+#pragma unroll
+      for (int e = 0; e < 16; e += 2)
+        ds[e / 8].set2(e % 8, exp2_raw(fmaf(s[e], scale, -lse)) * (dp[e] - delta),
+                       exp2_raw(fmaf(s[e + 1], scale, -lse)) * (dp[e + 1] - delta));
+      read_k(1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int t = 0; t < CT; ++t) dq[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks][t].v, ds[ks].v, dq[t], 0, 0, 0);
+    }
+    l.x[buf ^ 1].store(kr);
+    l.y[buf ^ 1].store(vr);
+  }
+  store_rows<DH>(seq_row(a.dq, sq, pq, head, q0, esz), a.dq.row, m, i, h, dq, a.scale);
+}
+
+// Two waves share 32 keys: one forms S, P and dV, the other, a step of 64 queries behind it, dP, dS and dK from the same
+// P, which comes through LDS (rounded to bf16, lane for lane as both need it).  Either does the same two products (its
+// rows against a tile, a transposed tile against its result) with half of the operands and gradients, so that two
+// waves fit a SIMD; one wave with all of them took 490 registers, moved half of them about and reached 20% of the matrix
+// cores' time.  With parts a workgroup takes one query head and leaves fp32 rows there, which softmax_sum_kernel adds up.
+template <int DH>
+struct SoftmaxKeyLds {
+  Tile<DH> x[3], y[3];
+  bf16x8 p[2][4][4][kWave];  // per step parity, key tile and 16 queries
+  float lse[3][64], delta[3][64];
+};
+
+template <int DH>
+__global__ __launch_bounds__(512, 2) void softmax_dkdv32_kernel(SoftmaxArgs a) {
+  constexpr int KB = 64, KS = DH / 16, CT = DH / 32, esz = 2;
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  SoftmaxKeyLds<DH>& l = *reinterpret_cast<SoftmaxKeyLds<DH>*>(raw);
+  const int lane = threadIdx.x % kWave, wave = wave_id() % 4, h = lane / 32, c = lane % 32;
+  const bool second = wave_id() >= 4;  // dP, dS, dK
+  const int group = a.H / a.Hk, heads = a.parts ? a.H : a.Hk;
+  const int unit = head_of(blockIdx.x % heads, heads), slot = blockIdx.x / heads;  // (earlier tiles are seen by more queries)
+  const int hk = a.parts ? unit / group : unit, head0 = a.parts ? unit : unit * group, each = a.parts ? 1 : group;
+  const SeqPiece sk = seq_piece(a.ks, slot, 128);
+  if (sk.seq < 0) return;
+  const SeqPiece sq = seq_of(a.qs, sk.seq);
+  const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
+  const int k0 = sk.index * 128, m = min(128, sk.len - k0);
+  const int shift = sk.len - sq.len;
+  const int i = 32 * wave + c, key = k0 + i;
+  const int wfirst = k0 + 32 * wave, wlast = wfirst + 31;  // the wave's keys
+  const int qbegin = max(0, k0 - shift) / KB * KB;  // the first query that sees the tile's first key
+  const int blocks = qbegin < sq.len ? (sq.len - qbegin + KB - 1) / KB : 0, steps = each * blocks;
+
+  bf16x8 rf[KS];  // K rows (with the scale's sign, as in the forward pass) or V rows
+  row_operands<DH>(rf, seq_row(second ? a.v : a.k, sk, pk, hk, k0, esz), second ? a.v.row : a.k.row, m, i, h);
+  if (!second && a.scale < 0.0f)
+#pragma unroll
+    for (int t = 0; t < KS; ++t) rf[t] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(i32x4, rf[t]) ^ (int)0x80008000);
+  const float scale = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f);
+  f32x16 acc[CT];
+#pragma unroll
+  for (int t = 0; t < CT; ++t) acc[t] = zero16();
+
+  TileRegs<DH, 512> xr, yr;
+  float lse = 0.0f, delta = 0.0f;  // of query threadIdx.x of the step
+  const auto load = [&](int step) {
+    const int head = head0 + step / blocks, q0 = qbegin + step % blocks * KB, qn = min(KB, sq.len - q0);
+    Tile<DH>::load(xr, seq_row(a.q, sq, pq, head, q0, esz), a.q.row, qn);
+    Tile<DH>::load(yr, seq_row(a.dO, sq, pq, head, q0, esz), a.dO.row, qn);
+    const int64_t num = seq_num(a.qs, sq, a.H, head, q0 + min((int)threadIdx.x % KB, qn - 1));
+    lse = a.lse[num];
+    delta = a.delta[num];
+  };
+  const auto store = [&](int buf) {
+    l.x[buf].store(xr);
+    l.y[buf].store(yr);
+    if (threadIdx.x < KB) {  // (a row that sees nothing: exp2(-infinity - infinity) below)
+      l.lse[buf][threadIdx.x] = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+      l.delta[buf][threadIdx.x] = delta;
+    }
+  };
+  if (steps > 0) {
+    load(0);
+    store(0);
+  }
+  for (int step = 0; step <= steps && steps > 0; ++step) {
+    __syncthreads();  // the tiles of this step and P of the one before are whole
+    load(min(step + 1, steps - 1));
+    const int at = second ? step - 1 : step;  // this wave's step
+    const int q0 = qbegin + at % blocks * KB, qn = min(KB, sq.len - q0), buf = at % 3;
+    if (at >= 0 && at < steps && q0 + KB - 1 + shift >= wfirst) {  // (uniform) some query sees a key of the wave
+      const Tile<DH>& rows = second ? l.y[buf] : l.x[buf];
+      const Tile<DH>& cols = second ? l.x[buf] : l.y[buf];
+      f32x16 s[2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) s[half] = zero16();
+#pragma unroll
+      for (int t = 0; t < KS; ++t)
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rows.row8(32 * half + c, 2 * t + h), rf[t], s[half], 0, 0, 0);
+      // transposed operands of 16 queries, read a step before their products
+      Frag<__bf16> f[2][CT], pf[4];
+      const auto read = [&](int ks) {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          const int row = 16 * ks + 4 * h, col = 32 * t + 16 * ((lane / 16) % 2);
+          cols.tr4(f[ks % 2][t], 0, row, col, lane);
+          cols.tr4(f[ks % 2][t], 4, row + 8, col, lane);
+        }
+      };
+      read(0);
+      if (!second) {
+        if (q0 + shift < wlast || qn < KB || m < 128) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int r = 32 * half + 8 * (e / 4) + 4 * h + e % 4;
+              s[half][e] = key <= q0 + r + shift && r < qn && i < m ? s[half][e] : -__builtin_inff();
+            }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const f32x4 ls = *reinterpret_cast<const f32x4*>(&l.lse[buf][32 * half + 2 * e + 4 * h]);
+#pragma unroll
+            for (int j = 0; j < 4; j += 2)
+              pf[2 * half + e / 8].set2(e % 8 + j, exp2_raw(fmaf(s[half][e + j], scale, -ls[j])),
+                                        exp2_raw(fmaf(s[half][e + j + 1], scale, -ls[j + 1])));
+          }
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) l.p[at % 2][wave][ks][lane] = pf[ks].v;
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          const bf16x8 p = l.p[at % 2][wave][ks][lane];
+          const f32x4 d0 = *reinterpret_cast<const f32x4*>(&l.delta[buf][16 * ks + 4 * h]);
+          const f32x4 d1 = *reinterpret_cast<const f32x4*>(&l.delta[buf][16 * ks + 8 + 4 * h]);
+#pragma unroll
+          for (int e = 0; e < 8; e += 2)
+            pf[ks].set2(e, (float)p[e] * (s[ks / 2][8 * (ks % 2) + e] - (e < 4 ? d0[e] : d1[e - 4])),
+                        (float)p[e + 1] * (s[ks / 2][8 * (ks % 2) + e + 1] - (e < 4 ? d0[e + 1] : d1[e - 3])));
+        }
+      }
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        if (ks < 3) read(ks + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[ks % 2][t].v, pf[ks].v, acc[t], 0, 0, 0);
+      }
+    }
+    if (step + 1 < steps) store((step + 1) % 3);
+  }
+  if (a.parts) {
+    if (i >= m) return;
+    float* part = a.parts + seq_num(a.ks, sk, a.H, unit, k0 + i) * (2 * DH) + (second ? 0 : DH);
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) store4(part + 32 * t + 2 * e + 4 * h, acc[t][e], acc[t][e + 1], acc[t][e + 2], acc[t][e + 3]);
+    return;
+  }
+  if (second) store_rows<DH>(seq_row(a.dk, sk, pk, hk, k0, esz), a.dk.row, m, i, h, acc, a.scale);
+  else store_rows<DH>(seq_row(a.dv, sk, pk, hk, k0, esz), a.dv.row, m, i, h, acc, 1.0f);
+}
+
+// dK and dV of a key head from its query heads' rows in a.parts, in order of the heads.
+template <int DH>
+__global__ __launch_bounds__(256) void softmax_sum_kernel(SoftmaxArgs a) {
+  constexpr int PER = DH / 4;  // threads per row of each gradient
+  const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
+  const SeqPiece sk = seq_piece(a.ks, slot, 128);
+  if (sk.seq < 0) return;
+  const bool pk = a.ks.offsets != nullptr;
+  const int k0 = sk.index * 128, m = min(128, sk.len - k0), group = a.H / a.Hk;
+  for (int idx = threadIdx.x; idx < m * 2 * PER; idx += 256) {
+    const int r = idx / (2 * PER), at = idx % (2 * PER), which = at / PER, col = at % PER * 4;
+    f32x4 sum = zero4();
+    for (int g = 0; g < group; ++g)
+      sum += *reinterpret_cast<const f32x4*>(a.parts + seq_num(a.ks, sk, a.H, hk * group + g, k0 + r) * (2 * DH) + which * DH + col);
+    const float f = which ? 1.0f : a.scale;
+    __bf16* to = reinterpret_cast<__bf16*>(seq_row(which ? a.dv : a.dk, sk, pk, hk, k0 + r, 2)) + col;
+    store4(to, sum[0] * f, sum[1] * f, sum[2] * f, sum[3] * f);
+  }
+}
+
+template <int DH>
+hipError_t launch_width32(const SoftmaxArgs& a, hipStream_t s) {
+  constexpr int bytes = (int)sizeof(SoftmaxBwdLds32<DH>), key_bytes = (int)sizeof(SoftmaxKeyLds<DH>);
+  hipError_t e = allow_lds<softmax_dq32_kernel<DH>>(bytes);
+  if (e == hipSuccess) e = allow_lds<softmax_dkdv32_kernel<DH>>(key_bytes);
+  if (e != hipSuccess) return e;
+  const int64_t qt = seq_slots(a.qs, 128), kt = seq_slots(a.ks, 128);
+  if (qt > 0) hipLaunchKernelGGL((softmax_dq32_kernel<DH>), dim3((unsigned)(qt * a.H)), dim3(256), bytes, s, a);
+  if ((e = hipGetLastError()) != hipSuccess || kt == 0) return e;
+  hipLaunchKernelGGL((softmax_dkdv32_kernel<DH>), dim3((unsigned)(kt * (a.parts ? a.H : a.Hk))), dim3(512), key_bytes, s, a);
+  if ((e = hipGetLastError()) != hipSuccess || !a.parts) return e;
+  hipLaunchKernelGGL((softmax_sum_kernel<DH>), dim3((unsigned)(kt * a.Hk)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
 template <typename T, int DH>
 hipError_t launch_width(const SoftmaxArgs& a, hipStream_t s) {
   constexpr int bytes = (int)sizeof(SoftmaxBwdLds<T, DH>);
@@ -222,7 +535,8 @@ hipError_t launch_bwd(const SoftmaxArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_softmax_bwd(Dt dt, const SoftmaxArgs& a, hipStream_t s) {
-  return dt == Dt::BF16 ? launch_bwd<__bf16>(a, s) : launch_bwd<float>(a, s);
+  if (dt == Dt::F32) return launch_bwd<float>(a, s);
+  return a.d == 32 ? launch_width<__bf16, 32>(a, s) : a.d == 64 ? launch_width32<64>(a, s) : launch_width32<128>(a, s);
 }
 
 }  // namespace luna
