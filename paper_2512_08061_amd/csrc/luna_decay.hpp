@@ -11,18 +11,20 @@
 //   dK  (reverse)  q = V,  k = dO, v = Q,  a = 1, b_j = -dO_j.out_j, w_j = 1 / (den_j + eps)
 //   dV  (reverse)  q = K,  k = Q,  v = dO, w_j as before
 //
-// A workgroup of four waves takes one piece of one sequence and head (and up to 128 columns
-// of v) in chunks of C tokens, with the discounted state S of the tokens before the chunk
-// in registers: wave w holds its columns of S (all features), as accumulator tiles.  Per chunk
+// A workgroup takes one piece of one sequence and head (and up to 128 columns of v) in chunks of C
+// tokens, with the discounted state S of the tokens before the chunk in registers: a wave for 16
+// columns of S (all features), as accumulator tiles.  Per chunk
 //
-//   P = mask(Q K^T)                    each wave 16 queries' rows, rounded to T, through LDS
+//   P = mask(Q K^T)                    16 x 16 blocks shared out among the waves, rounded to T, through LDS
 //   out^T = f^(i+1) S^T Q^T + V^T P^T  each wave its columns: S's accumulator tiles are the A
 //                                      operand as they are (features 4g + j of two tiles are
 //                                      the 8 k-slots of a lane group; Q is read in that order)
 //   S = f^C S + K^T (f^(C-1-j) w_j V)  the V operand of P's product, scaled
 //
-// With S returned (exact_state) the scaled V is split in three bf16 parts, so that S has fp32
-// accuracy; else it is rounded to bf16 (2^-9 of each term, as S itself is as an operand).
+// The next chunk's rows are on their way to registers while a chunk is worked on.  A wave holds few registers (16
+// columns), so that up to four share a SIMD: a chunk is a chain of dependent steps with three barriers, whose waits
+// other waves and workgroups fill.  The scaled V is split in bf16 parts, two (2^-17 of each term), or three with S
+// returned (exact_state), so that S then has fp32 accuracy.
 // Denominators are sums of P before its rounding plus q.z with z in fp32 (LDS), so they have
 // fp32 accuracy.
 #pragma once
@@ -41,25 +43,36 @@ struct DecayLds {
   static constexpr int C = kDecayChunk<T>, PAD = 16 / (int)sizeof(T);
   static constexpr int PK = DK + PAD, PV = DVW + PAD, PA = C + PAD;
   T q[C][PK], k[C][PK], v[C][PV], p[C][PA];
-  float pw[C + 4];                         // f^0 .. f^C
-  float dec[C], kw[C], ka[C], qa[C], den[C];  // f^(m-1-j) w_j, w_j, b_j, a_i, denominators
+  float pw[C + 4];                               // f^0 .. f^C
+  float dec[C], kw[C], ka[C], qa[C], ow[C];      // f^(m-1-j) w_j, w_j, b_j, a_i, c_i
+  float den[2][C];                               // two waves' shares of the denominators
   float z[DK];
 };
 
-// `m` rows of width w (at most W) into LDS rows of pitch P; rows past m and columns past w as zeros.
-template <typename T, int C, int W, int P>
-__device__ __forceinline__ void decay_load_rows(T* dst, const char* base, int64_t row, int m, int w, bool reverse) {
-  constexpr int E = 16 / (int)sizeof(T), PER = W / E;
-  static_assert(C * PER % 256 == 0, "whole pieces per thread");
-  const Buf b = buffer(base, m > 0 ? (int)(((m - 1) * row + w) * (int)sizeof(T)) : 0);
+// Rows of one tensor on their way from memory to LDS: C rows of width w (at most W), rows past m and columns past w as
+// zeros.
+template <typename T, int C, int W, int P, int THREADS>
+struct DecayRows {
+  static constexpr int E = 16 / (int)sizeof(T), PER = W / E, N = (C * PER + THREADS - 1) / THREADS;
+  i32x4 x[N];
+  __device__ __forceinline__ void load(const char* base, int64_t row, int m, int w, bool reverse) {
+    const Buf b = buffer(base, m > 0 ? (int)(((m - 1) * row + w) * (int)sizeof(T)) : 0);
 #pragma unroll
-  for (int i = 0; i < C * PER / 256; ++i) {
-    const int idx = threadIdx.x + 256 * i, r = idx / PER, c = (idx % PER) * E;
-    const int at = (reverse ? m - 1 - r : r) * (int)row + c;
-    const auto x = __builtin_amdgcn_raw_buffer_load_b128(b, r < m && c < w ? at * (int)sizeof(T) : kPastEnd, 0, 0);
-    *reinterpret_cast<i32x4*>(&dst[r * P + c]) = __builtin_bit_cast(i32x4, x);
+    for (int i = 0; i < N; ++i) {
+      const int idx = threadIdx.x + THREADS * i, r = idx / PER, c = (idx % PER) * E;
+      const int at = (reverse ? m - 1 - r : r) * (int)row + c;
+      x[i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                           b, r < m && c < w ? at * (int)sizeof(T) : kPastEnd, 0, 0));
+    }
   }
-}
+  __device__ __forceinline__ void store(T* dst) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int idx = threadIdx.x + THREADS * i, r = idx / PER, c = (idx % PER) * E;
+      if (N * THREADS == C * PER || r < C) *reinterpret_cast<i32x4*>(&dst[r * P + c]) = x[i];
+    }
+  }
+};
 
 // x summed over the four lane groups
 __device__ __forceinline__ float sum_groups(float x) {
@@ -69,7 +82,7 @@ __device__ __forceinline__ float sum_groups(float x) {
   return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
-// The scaled values of a fragment as one operand, and their split in parts.
+// The scaled values of a fragment as one operand (fp32) or in parts (bf16: two, or three where exact).
 template <typename T>
 struct DecayScaled;
 template <>
@@ -84,30 +97,25 @@ struct DecayScaled<float> {
 template <>
 struct DecayScaled<__bf16> {
   Split3 x;
-  __device__ __forceinline__ void set(const Frag<__bf16>& v, const float (&w)[8], bool exact) {
+  __device__ __forceinline__ void set(const Frag<__bf16>& v, const float (&w)[8], bool) {
     float y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = v.get(e) * w[e];
-    if (exact) {
-      split3(x, y);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) x.p[0].set2(e, y[e], y[e + 1]);
-    }
+    split3(x, y);
   }
   __device__ __forceinline__ void mma_into(f32x4& c, const Frag<__bf16>& a, bool exact) const {
-    if (exact) {
-      mma(c, a, x.p[2]);
-      mma(c, a, x.p[1]);
-    }
+    if (exact) mma(c, a, x.p[2]);
+    mma(c, a, x.p[1]);
     mma(c, a, x.p[0]);
   }
 };
 
-template <typename T, int DK, int DVW, int MODE, bool OUT>
-__global__ __launch_bounds__(256) void decay_kernel(DecayArgs a) {
+template <typename T, int DK, int DVW, int MODE, bool OUT, bool EXACT>
+__global__ __launch_bounds__(4 * DVW, 2) void decay_kernel(DecayArgs a) {
   using Lds = DecayLds<T, DK, DVW>;
-  constexpr int C = Lds::C, FT = DK / 16, CT = DVW / 64, KT = C / 16, KS = C / 32;
+  constexpr int C = Lds::C, FT = DK / 16, KT = C / 16, KS = C / 32, NW = DVW / 16, THREADS = 64 * NW;
+  constexpr int SHARE = NW >= 2 * KT ? 2 : 1;  // waves per 16 queries of P
+  constexpr int esz = (int)sizeof(T);
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
 
@@ -121,16 +129,33 @@ __global__ __launch_bounds__(256) void decay_kernel(DecayArgs a) {
   const int begin = sp.index * a.piece, end = min(sp.len, begin + a.piece);
   if (!OUT && end == sp.len) return;  // (nothing starts from the state after the last piece)
   const int col0 = slice * DVW, cols = min(DVW, a.dv - col0);
-  const int wcol = 16 * CT * wave;  // this wave's first column of the slice
-  const bool exact = a.exact_state;
+  const int wcol = 16 * wave;  // this wave's first column of the slice
 
   const float g2 = decay_log2(a.log_decay[head]);
-  for (int i = tid; i <= C; i += 256) l.pw[i] = exp2f(g2 * (float)i);
+  for (int i = tid; i <= C; i += THREADS) l.pw[i] = exp2_raw(g2 * (float)i);
+
+  // a chunk's rows, and thread tid's numbers of row tid, a chunk ahead
+  DecayRows<T, C, DK, Lds::PK, THREADS> qr, kr;
+  DecayRows<T, C, DVW, Lds::PV, THREADS> vr;
+  float kw = 1.0f, ka = 1.0f, qa = 1.0f, ow = 1.0f;
+  const auto load = [&](int t0) {
+    const int m = min(C, end - t0);
+    const int64_t lo = rev ? sp.len - t0 - m : t0;  // the chunk's first row in memory
+    if (OUT) qr.load(seq_row(a.q, sp, packed, head, lo, esz), a.q.row, m, a.dk, rev);
+    kr.load(seq_row(a.k, sp, packed, head, lo, esz), a.k.row, m, a.dk, rev);
+    vr.load(seq_row(a.v, sp, packed, head, lo, esz) + col0 * esz, a.v.row, m, cols, rev);
+    const int r = min(tid, m - 1);
+    const int64_t num = seq_num(a.s, sp, a.H, head, lo + (rev ? m - 1 - r : r));
+    if (a.kw) kw = a.kw[num];
+    if (MODE == kDecayAug && a.ka) ka = a.ka[num];
+    if (MODE == kDecayAug && OUT && a.qa) qa = a.qa[num];
+    if (OUT && a.ow) ow = a.ow[num];
+  };
+  load(begin);
 
   // the state before the piece
   const int64_t sf = decay_state_floats(a.dk, a.dv);
   float* st = a.states ? a.states + ((int64_t)slot * a.H + head) * sf : nullptr;
-  f32x4 S[FT][CT], za[CT];  // za: row 0 is the further key component's row of S (kDecayAug)
   const float* S0 = nullptr;
   const float* z0 = nullptr;
   if (OUT) {
@@ -142,132 +167,122 @@ __global__ __launch_bounds__(256) void decay_kernel(DecayArgs a) {
       z0 = MODE == kDecayNorm ? a.z + at * a.dk : nullptr;
     }
   }
+  const int mycol = wcol + c;
+  f32x4 S[FT], za = zero4();  // za: row 0 is the further key component's row of S (kDecayAug)
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const int col = wcol + 16 * ct + c;
+  for (int ft = 0; ft < FT; ++ft) S[ft] = zero4();
+  if (S0 && mycol < cols) {
 #pragma unroll
     for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int f = 16 * ft + 4 * g + j;
-        S[ft][ct][j] = S0 && f < a.dk && col < cols ? S0[(int64_t)f * a.dv + col0 + col] : 0.0f;
+        if (f < a.dk) S[ft][j] = S0[(int64_t)f * a.dv + col0 + mycol];
       }
-    za[ct] = zero4();
-    if (MODE == kDecayAug && S0 && g == 0 && col < cols) za[ct][0] = z0[col0 + col];
+    if (MODE == kDecayAug && g == 0) za[0] = z0[col0 + mycol];
   }
   if (MODE == kDecayNorm)
-    for (int f = tid; f < DK; f += 256) l.z[f] = S0 && f < a.dk ? z0[f] : 0.0f;
+    for (int f = tid; f < DK; f += THREADS) l.z[f] = S0 && f < a.dk ? z0[f] : 0.0f;
 
   for (int t0 = begin; t0 < end; t0 += C) {
     const int m = min(C, end - t0);
-    const int64_t lo = rev ? sp.len - t0 - m : t0;  // the chunk's first row in memory
-    constexpr int esz = (int)sizeof(T);
-    __syncthreads();  // the chunk before is no longer read
-    if (OUT) decay_load_rows<T, C, DK, Lds::PK>(&l.q[0][0], seq_row(a.q, sp, packed, head, lo, esz), a.q.row, m, a.dk, rev);
-    decay_load_rows<T, C, DK, Lds::PK>(&l.k[0][0], seq_row(a.k, sp, packed, head, lo, esz), a.k.row, m, a.dk, rev);
-    decay_load_rows<T, C, DVW, Lds::PV>(&l.v[0][0], seq_row(a.v, sp, packed, head, lo, esz) + col0 * esz, a.v.row, m, cols, rev);
+    __syncthreads();  // the chunk before is no longer read (at first: f^i are written)
+    if (OUT) qr.store(&l.q[0][0]);
+    kr.store(&l.k[0][0]);
+    vr.store(&l.v[0][0]);
     if (tid < C) {
       const bool in = tid < m;
-      const int64_t num = seq_num(a.s, sp, a.H, head, lo + (rev ? m - 1 - tid : tid));
-      const float w = !in ? 0.0f : a.kw ? a.kw[num] : 1.0f;
-      l.kw[tid] = w;
-      l.dec[tid] = in ? w * exp2f(g2 * (float)(m - 1 - tid)) : 0.0f;
+      l.kw[tid] = in ? kw : 0.0f;
+      l.dec[tid] = in ? kw * l.pw[max(m - 1 - tid, 0)] : 0.0f;
       if (MODE == kDecayAug) {
-        l.ka[tid] = !in ? 0.0f : a.ka ? a.ka[num] : 1.0f;
-        l.qa[tid] = !in ? 0.0f : a.qa ? a.qa[num] : 1.0f;
+        l.ka[tid] = in ? ka : 0.0f;
+        if (OUT) l.qa[tid] = in ? qa : 0.0f;
       }
+      if (OUT) l.ow[tid] = ow;
     }
+    if (t0 + C < end) load(t0 + C);
     __syncthreads();
 
-    f32x4 o[KT][CT];
+    f32x4 o[KT];
     if (OUT) {
-      // P: wave w forms the rows of query tile w, over the keys before them
-      if (wave < KT) {
-        const int qt = wave, i = 16 * qt + c;
+      // P: SHARE waves form the rows of a query tile, over the keys before them
+      if (wave < SHARE * KT) {
+        const int qt = wave / SHARE, share = wave % SHARE, i = 16 * qt + c;
         Frag<T> qf[DK / 32];
 #pragma unroll
         for (int t = 0; t < DK / 32; ++t) load8(qf[t], &l.q[i][32 * t + 8 * g]);
         float den = 0.0f;
-        if (MODE == kDecayNorm) {
+        if (MODE == kDecayNorm && share == 0) {
 #pragma unroll
           for (int t = 0; t < DK / 32; ++t)
 #pragma unroll
             for (int e = 0; e < 8; ++e) den = fmaf(qf[t].get(e), l.z[32 * t + 8 * g + e], den);
           den *= l.pw[i + 1];
         }
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
+        const float qai = MODE == kDecayAug ? l.qa[i] : 0.0f;
+        for (int kt = share; kt < KT && kt <= qt + 1; kt += SHARE) {  // (a block behind the diagonal as zeros)
           f32x4 acc = zero4();
-          if (kt <= qt) {
+          const f32x4 w = *reinterpret_cast<const f32x4*>(&l.kw[16 * kt + 4 * g]);
+          const f32x4 b = MODE == kDecayAug ? *reinterpret_cast<const f32x4*>(&l.ka[16 * kt + 4 * g]) : zero4();
+          float f[4];
 #pragma unroll
-            for (int t = 0; t < DK / 32; ++t) {
-              Frag<T> kf;
-              load8(kf, &l.k[16 * kt + c][32 * t + 8 * g]);
-              mma(acc, kf, qf[t]);
-            }
+          for (int j = 0; j < 4; ++j) f[j] = l.pw[max(i - (16 * kt + 4 * g + j), 0)] * w[j];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int key = 16 * kt + 4 * g + j;
-              float x = acc[j];
-              if (MODE == kDecayAug) x = fmaf(l.qa[i], l.ka[key], x);
-              x *= l.pw[max(i - key, 0)] * l.kw[key];
-              acc[j] = key <= i ? x : 0.0f;
-              if (MODE == kDecayNorm) den += acc[j];
-            }
+          for (int t = 0; t < DK / 32; ++t) {
+            Frag<T> kf;
+            load8(kf, &l.k[16 * kt + c][32 * t + 8 * g]);
+            mma(acc, kf, qf[t]);
           }
-          if (kt <= qt + 1) store4(&l.p[i][16 * kt + 4 * g], acc[0], acc[1], acc[2], acc[3]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float x = (MODE == kDecayAug ? fmaf(qai, b[j], acc[j]) : acc[j]) * f[j];
+            acc[j] = 16 * kt + 4 * g + j <= i ? x : 0.0f;
+            if (MODE == kDecayNorm) den += acc[j];
+          }
+          store4(&l.p[i][16 * kt + 4 * g], acc[0], acc[1], acc[2], acc[3]);
         }
         if (MODE == kDecayNorm) {
           den = sum_groups(den);
-          if (g == 0) l.den[i] = den;
+          if (g == 0) l.den[share][i] = den;
         }
       }
       // f^(i+1) S^T Q^T
 #pragma unroll
-      for (int qt = 0; qt < KT; ++qt)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) o[qt][ct] = zero4();
+      for (int qt = 0; qt < KT; ++qt) o[qt] = zero4();
 #pragma unroll
       for (int t = 0; t < FT / 2; ++t) {
-        Frag<T> sf_[CT];
+        Frag<T> sf_;
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            sf_[ct].set2(e, S[2 * t][ct][e], S[2 * t][ct][e + 1]);
-            sf_[ct].set2(4 + e, S[2 * t + 1][ct][e], S[2 * t + 1][ct][e + 1]);
-          }
+        for (int e = 0; e < 4; e += 2) {
+          sf_.set2(e, S[2 * t][e], S[2 * t][e + 1]);
+          sf_.set2(4 + e, S[2 * t + 1][e], S[2 * t + 1][e + 1]);
+        }
 #pragma unroll
         for (int qt = 0; qt < KT; ++qt) {
           Frag<T> qf;
           load4(qf, 0, &l.q[16 * qt + c][32 * t + 4 * g]);
           load4(qf, 4, &l.q[16 * qt + c][32 * t + 16 + 4 * g]);
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) mma(o[qt][ct], sf_[ct], qf);
+          mma(o[qt], sf_, qf);
         }
       }
       if (MODE == kDecayAug) {
+        Frag<T> zf;
+        zf.zero();
+        zf.set(0, g == 0 ? za[0] : 0.0f);
 #pragma unroll
         for (int qt = 0; qt < KT; ++qt) {
+          const float x = l.qa[16 * qt + c];
           Frag<T> qf;
           qf.zero();
-          qf.set(0, g == 0 ? l.qa[16 * qt + c] : 0.0f);
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) {
-            Frag<T> zf;
-            zf.zero();
-            zf.set(0, g == 0 ? za[ct][0] : 0.0f);
-            mma(o[qt][ct], zf, qf);
-          }
+          qf.set(0, g == 0 ? x : 0.0f);
+          mma(o[qt], zf, qf);
         }
       }
 #pragma unroll
       for (int qt = 0; qt < KT; ++qt) {
         const float f = l.pw[16 * qt + c + 1];
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[qt][ct][j] *= f;
+        for (int j = 0; j < 4; ++j) o[qt][j] *= f;
       }
       __syncthreads();  // P is whole; z has been read
     }
@@ -276,38 +291,32 @@ __global__ __launch_bounds__(256) void decay_kernel(DecayArgs a) {
     {
       const float f = l.pw[m];
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
+      for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
-        for (int ft = 0; ft < FT; ++ft)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) S[ft][ct][j] *= f;
-        za[ct][0] *= f;
-      }
+        for (int j = 0; j < 4; ++j) S[ft][j] *= f;
+      za[0] *= f;
     }
-    f32x4 zacc[(FT + 3) / 4];
+    constexpr int ZT = (FT + NW - 1) / NW;  // tiles of z per wave
+    f32x4 zacc[ZT];
     if (MODE == kDecayNorm)
 #pragma unroll
-      for (int i = 0; i < (FT + 3) / 4; ++i) zacc[i] = zero4();
+      for (int i = 0; i < ZT; ++i) zacc[i] = zero4();
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       float dec[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) dec[e] = l.dec[32 * ks + 8 * g + e];
-      Frag<T> vf[CT];
-      DecayScaled<T> vs[CT];
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        load_tr4(vf[ct], 0, &l.v[0][0], Lds::PV, 32 * ks + 8 * g, wcol + 16 * ct, lane);
-        load_tr4(vf[ct], 4, &l.v[0][0], Lds::PV, 32 * ks + 8 * g + 4, wcol + 16 * ct, lane);
-        vs[ct].set(vf[ct], dec, exact);
-      }
+      Frag<T> vf;
+      load_tr4(vf, 0, &l.v[0][0], Lds::PV, 32 * ks + 8 * g, wcol, lane);
+      load_tr4(vf, 4, &l.v[0][0], Lds::PV, 32 * ks + 8 * g + 4, wcol, lane);
+      DecayScaled<T> vs;
+      vs.set(vf, dec, EXACT);
       if (OUT) {
 #pragma unroll
         for (int qt = 2 * ks; qt < KT; ++qt) {
           Frag<T> pf;
           load8(pf, &l.p[16 * qt + c][32 * ks + 8 * g]);
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) mma(o[qt][ct], vf[ct], pf);
+          mma(o[qt], vf, pf);
         }
       }
       DecayScaled<T> one;  // columns 0 .. 2: the parts of the discounts
@@ -328,52 +337,52 @@ __global__ __launch_bounds__(256) void decay_kernel(DecayArgs a) {
         Frag<T> kf;
         load_tr4(kf, 0, &l.k[0][0], Lds::PK, 32 * ks + 8 * g, 16 * ft, lane);
         load_tr4(kf, 4, &l.k[0][0], Lds::PK, 32 * ks + 8 * g + 4, 16 * ft, lane);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) vs[ct].mma_into(S[ft][ct], kf, exact);
-        if (MODE == kDecayNorm)
-          if (ft % 4 == wave) one.mma_into(zacc[ft / 4], kf, false);
+        vs.mma_into(S[ft], kf, EXACT);
+        if (MODE == kDecayNorm && ft % NW == wave) {
+          if constexpr (sizeof(T) == 2) mma(zacc[ft / NW], kf, one.x.p[0]);
+          else mma(zacc[ft / NW], kf, one.x);
+        }
       }
       if (MODE == kDecayAug) {
         Frag<T> kf;
         kf.zero();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) kf.set(e, c == 0 ? l.ka[32 * ks + 8 * g + e] : 0.0f);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) vs[ct].mma_into(za[ct], kf, exact);
+        for (int e = 0; e < 8; ++e) {
+          const float x = l.ka[32 * ks + 8 * g + e];
+          kf.set(e, c == 0 ? x : 0.0f);
+        }
+        vs.mma_into(za, kf, EXACT);
       }
     }
     if (MODE == kDecayNorm) {
 #pragma unroll
-      for (int i = 0; i < (FT + 3) / 4; ++i) {
+      for (int i = 0; i < ZT; ++i) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {  // the three parts' columns, in every quad of lanes
           float x = zacc[i][j];
           x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xB1, 0xf, 0xf, true));
           x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4E, 0xf, 0xf, true));
-          const int f = 16 * (4 * i + wave) + 4 * g + j;
+          const int f = 16 * (NW * i + wave) + 4 * g + j;
           if (c == 0 && f < DK) l.z[f] = fmaf(l.pw[m], l.z[f], x);
         }
       }
     }
 
     if (OUT) {
+      const int64_t lo = rev ? sp.len - t0 - m : t0;
       const Buf b = buffer(seq_row(a.o, sp, packed, head, lo, esz) + col0 * esz, (int)(((m - 1) * a.o.row + cols) * esz));
 #pragma unroll
       for (int qt = 0; qt < KT; ++qt) {
         const int i = 16 * qt + c, r = rev ? m - 1 - i : i;
-        float f = a.scale;
+        float f = a.scale * l.ow[i];
         if (MODE == kDecayNorm) {
-          const float den = a.scale * l.den[i];
+          const float den = a.scale * (SHARE == 2 ? l.den[0][i] + l.den[1][i] : l.den[0][i]);
           f = a.scale / (den + a.eps);
           if (a.den && wave == 0 && g == 0 && slice == 0 && i < m) a.den[seq_num(a.s, sp, a.H, head, lo + r)] = den;
         }
-        if (a.ow && i < m) f *= a.ow[seq_num(a.s, sp, a.H, head, lo + r)];
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          const int col = wcol + 16 * ct + 4 * g;
-          buf_store4<T>(b, i < m && col < cols ? (r * (int)a.o.row + col) * esz : kPastEnd, f * o[qt][ct][0],
-                        f * o[qt][ct][1], f * o[qt][ct][2], f * o[qt][ct][3]);
-        }
+        const int col = wcol + 4 * g;
+        buf_store4<T>(b, i < m && col < cols ? (r * (int)a.o.row + col) * esz : kPastEnd, f * o[qt][0], f * o[qt][1],
+                      f * o[qt][2], f * o[qt][3]);
       }
     }
   }
@@ -390,41 +399,45 @@ __global__ __launch_bounds__(256) void decay_kernel(DecayArgs a) {
     z1 = MODE == kDecayNorm ? a.z + at * a.dk : nullptr;
   }
   if (!S1) return;
+  if (mycol < cols) {
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const int col = wcol + 16 * ct + c;
-    if (col < cols) {
+    for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
-      for (int ft = 0; ft < FT; ++ft)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int f = 16 * ft + 4 * g + j;
-          if (f < a.dk) S1[(int64_t)f * a.dv + col0 + col] = S[ft][ct][j];
-        }
-      if (MODE == kDecayAug && g == 0) z1[col0 + col] = za[ct][0];
-    }
+      for (int j = 0; j < 4; ++j) {
+        const int f = 16 * ft + 4 * g + j;
+        if (f < a.dk) S1[(int64_t)f * a.dv + col0 + mycol] = S[ft][j];
+      }
+    if (MODE == kDecayAug && g == 0) z1[col0 + mycol] = za[0];
   }
   if (MODE == kDecayNorm && slice == 0) {
     __syncthreads();
-    for (int f = tid; f < a.dk; f += 256) z1[f] = l.z[f];
+    for (int f = tid; f < a.dk; f += THREADS) z1[f] = l.z[f];
   }
 }
 
-template <typename T, int DK, int DVW, int MODE, bool OUT>
+template <typename T, int DK, int DVW, int MODE, bool OUT, bool EXACT>
 hipError_t launch_decay_one(const DecayArgs& a, hipStream_t s) {
   constexpr int bytes = (int)sizeof(DecayLds<T, DK, DVW>);
   static_assert(bytes <= 160 * 1024, "one workgroup's LDS");
-  const hipError_t e = allow_lds<decay_kernel<T, DK, DVW, MODE, OUT>>(bytes);
+  const hipError_t e = allow_lds<decay_kernel<T, DK, DVW, MODE, OUT, EXACT>>(bytes);
   if (e != hipSuccess) return e;
   const int slices = (a.dv + DVW - 1) / DVW;
-  hipLaunchKernelGGL((decay_kernel<T, DK, DVW, MODE, OUT>), dim3((unsigned)((int64_t)a.slots * a.H * slices)), dim3(256),
-                     bytes, s, a);
+  hipLaunchKernelGGL((decay_kernel<T, DK, DVW, MODE, OUT, EXACT>), dim3((unsigned)((int64_t)a.slots * a.H * slices)),
+                     dim3(4 * DVW), bytes, s, a);
   return hipGetLastError();
+}
+
+// (fp32 has one form; gradients return no state)
+template <typename T, int DK, int DVW, int MODE, bool OUT>
+hipError_t launch_decay_exact(const DecayArgs& a, hipStream_t s) {
+  if constexpr (sizeof(T) == 2 && MODE != kDecayAug)
+    if (a.exact_state) return launch_decay_one<T, DK, DVW, MODE, OUT, true>(a, s);
+  return launch_decay_one<T, DK, DVW, MODE, OUT, false>(a, s);
 }
 
 template <typename T, int DK, int MODE, bool OUT>
 hipError_t launch_decay_width(const DecayArgs& a, hipStream_t s) {
-  return a.dv <= 64 ? launch_decay_one<T, DK, 64, MODE, OUT>(a, s) : launch_decay_one<T, DK, 128, MODE, OUT>(a, s);
+  return a.dv <= 64 ? launch_decay_exact<T, DK, 64, MODE, OUT>(a, s) : launch_decay_exact<T, DK, 128, MODE, OUT>(a, s);
 }
 
 template <typename T, int MODE, bool OUT>
