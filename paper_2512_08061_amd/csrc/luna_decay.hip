@@ -8,27 +8,32 @@ namespace {
 
 // Before: slot p of a sequence and head holds the state that its tokens add (all but the last
 // piece).  After: the state before piece p, S_p = f^piece S_{p-1} + X_{p-1}, from the caller's
-// state or zero.  One thread per element; loads of the next piece do not wait for the sums.
-__global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int64_t elems, int zwidth) {
+// state or zero.  Four elements per thread; loads of the next piece do not wait for the sums.
+__global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int64_t elems) {
   const int head = blockIdx.y, b = blockIdx.z;
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t e = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
   if (e >= elems) return;
   const SeqPiece sp = seq_of(a.s, b);
   const int pieces = (int)(((int64_t)sp.len + a.piece - 1) / a.piece);
-  if (pieces == 0) return;
+  if (pieces < 2) return;
   const int64_t slot = a.s.offsets ? sp.first / a.piece + b : b * ((a.s.rows + a.piece - 1) / a.piece);
-  const int64_t sf = decay_state_floats(a.dk, a.dv), step = a.H * sf;
-  float* x = a.states + (slot * a.H + head) * sf + e;
-  const float f = exp2f(decay_log2(a.log_decay[head]) * (float)a.piece);
-  const int64_t S_elems = (int64_t)a.dk * a.dv, at = (int64_t)b * a.H + head;
-  float run = 0.0f;
-  if (a.S) run = e < S_elems ? a.S[at * S_elems + e] : zwidth && a.z ? a.z[at * zwidth + e - S_elems] : 0.0f;
-  float next = pieces > 1 ? x[0] : 0.0f;
+  const int64_t step = a.H * decay_state_floats(a.dk, a.dv);
+  float* x = a.states + slot * step + head * decay_state_floats(a.dk, a.dv) + e;
+  const auto at = [&](int p) { return reinterpret_cast<f32x4*>(x + p * step); };
+  const float f = exp2_raw(decay_log2(a.log_decay[head]) * (float)a.piece);
+  f32x4 run = zero4(), next = *at(0);
+  if (a.S) {
+    const int64_t zat = (int64_t)a.dk * a.dv, user = (int64_t)b * a.H + head;
+    if (e < zat) run = *reinterpret_cast<const f32x4*>(a.S + user * zat + e);
+    else if (a.z && e - zat < a.dk)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) run[j] = a.z[user * a.dk + e - zat + j];
+  }
   for (int p = 0; p < pieces; ++p) {
-    const float add = next;
-    if (p + 2 < pieces) next = x[(p + 1) * step];
-    x[p * step] = run;
-    run = fmaf(f, run, add);
+    const f32x4 add = next;
+    if (p + 2 < pieces) next = *at(p + 1);
+    *at(p) = run;
+    run = f * run + add;
   }
 }
 
@@ -88,11 +93,10 @@ hipError_t launch_decay_states(Dt dt, int mode, const DecayArgs& a, hipStream_t 
 }
 hipError_t launch_decay_out(Dt dt, int mode, const DecayArgs& a, hipStream_t s) { return launch_decay(dt, mode, a, true, s); }
 
-hipError_t launch_decay_scan(int mode, const DecayArgs& a, hipStream_t s) {
-  const int zwidth = mode == kDecayNorm ? a.dk : mode == kDecayAug ? a.dv : 0;
-  const int64_t elems = (int64_t)a.dk * a.dv + zwidth;
-  const dim3 grid((unsigned)((elems + 255) / 256), (unsigned)a.H, (unsigned)a.s.count);
-  hipLaunchKernelGGL(decay_scan_kernel, grid, dim3(256), 0, s, a, elems, zwidth);
+hipError_t launch_decay_scan(const DecayArgs& a, hipStream_t s) {
+  const int64_t elems = decay_state_floats(a.dk, a.dv);  // (a multiple of 4; unused ones of z too)
+  const dim3 grid((unsigned)((elems / 4 + 255) / 256), (unsigned)a.H, (unsigned)a.s.count);
+  hipLaunchKernelGGL(decay_scan_kernel, grid, dim3(256), 0, s, a, elems);
   return hipGetLastError();
 }
 

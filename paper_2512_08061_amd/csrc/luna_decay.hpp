@@ -11,6 +11,8 @@
 //   dK  (reverse)  q = V,  k = dO, v = Q,  a = 1, b_j = -dO_j.out_j, w_j = 1 / (den_j + eps)
 //   dV  (reverse)  q = K,  k = Q,  v = dO, w_j as before
 //
+// The states of dK are those of dV transposed (with z of weights b_j as their further row), so one state pass serves both.
+//
 // A workgroup takes one piece of one sequence and head (and up to 128 columns of v) in chunks of C
 // tokens, with the discounted state S of the tokens before the chunk in registers: a wave for 16
 // columns of S (all features), as accumulator tiles.  Per chunk
@@ -110,8 +112,13 @@ struct DecayScaled<__bf16> {
   }
 };
 
+// Waves per SIMD: two workgroups of a compute unit where the registers suffice (128 features without denominators: 546 ->
+// 487 us of the long batch's row pass; the others would spill).
+template <typename T, int DK, int MODE, bool EXACT>
+constexpr int kDecayWaves = DK <= 64 || (DK == 128 && MODE == kDecayPlain && !EXACT) ? 4 : 2;
+
 template <typename T, int DK, int DVW, int MODE, bool OUT, bool EXACT>
-__global__ __launch_bounds__(4 * DVW, 2) void decay_kernel(DecayArgs a) {
+__global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, MODE, EXACT>)) void decay_kernel(DecayArgs a) {
   using Lds = DecayLds<T, DK, DVW>;
   constexpr int C = Lds::C, FT = DK / 16, KT = C / 16, KS = C / 32, NW = DVW / 16, THREADS = 64 * NW;
   constexpr int SHARE = NW >= 2 * KT ? 2 : 1;  // waves per 16 queries of P
@@ -147,43 +154,63 @@ __global__ __launch_bounds__(4 * DVW, 2) void decay_kernel(DecayArgs a) {
     const int r = min(tid, m - 1);
     const int64_t num = seq_num(a.s, sp, a.H, head, lo + (rev ? m - 1 - r : r));
     if (a.kw) kw = a.kw[num];
-    if (MODE == kDecayAug && a.ka) ka = a.ka[num];
+    if ((MODE == kDecayAug || (MODE == kDecayNorm && !OUT)) && a.ka) ka = a.ka[num];
     if (MODE == kDecayAug && OUT && a.qa) qa = a.qa[num];
     if (OUT && a.ow) ow = a.ow[num];
   };
   load(begin);
 
   // the state before the piece
-  const int64_t sf = decay_state_floats(a.dk, a.dv);
+  const int64_t sf = decay_state_floats(a.dk, a.dv), sheads = (int64_t)a.H * sf;
   float* st = a.states ? a.states + ((int64_t)slot * a.H + head) * sf : nullptr;
-  const float* S0 = nullptr;
-  const float* z0 = nullptr;
-  if (OUT) {
-    const int64_t at = (int64_t)sp.seq * a.H + head;
-    if (a.states) {
-      if (begin > 0 || a.S) S0 = st, z0 = st + (int64_t)a.dk * a.dv;
-    } else if (a.S) {
-      S0 = a.S + at * a.dk * a.dv;
-      z0 = MODE == kDecayNorm ? a.z + at * a.dk : nullptr;
-    }
-  }
+  const int64_t user = (int64_t)sp.seq * a.H + head;
   const int mycol = wcol + c;
   f32x4 S[FT], za = zero4();  // za: row 0 is the further key component's row of S (kDecayAug)
 #pragma unroll
   for (int ft = 0; ft < FT; ++ft) S[ft] = zero4();
-  if (S0 && mycol < cols) {
-#pragma unroll
-    for (int ft = 0; ft < FT; ++ft)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int f = 16 * ft + 4 * g + j;
-        if (f < a.dk) S[ft][j] = S0[(int64_t)f * a.dv + col0 + mycol];
-      }
-    if (MODE == kDecayAug && g == 0) za[0] = z0[col0 + mycol];
+  if (MODE == kDecayNorm) {
+    for (int f = tid; f < DK; f += THREADS) l.z[f] = 0.0f;
   }
-  if (MODE == kDecayNorm)
-    for (int f = tid; f < DK; f += THREADS) l.z[f] = S0 && f < a.dk ? z0[f] : 0.0f;
-
+  const int64_t zat = (int64_t)a.dk * a.dv;
+  {
+    const float* x = nullptr;
+    const float* xz = nullptr;
+    if (OUT && a.states && (begin > 0 || end < sp.len)) {
+      if (begin > 0 || a.S) x = st, xz = st + zat;
+    } else if (OUT && a.S) {
+      x = a.S + user * zat;
+      if (MODE == kDecayNorm) xz = a.z + user * a.dk;
+    }
+    if (x) {
+      const int64_t row = a.transposed ? 1 : a.dv, col = (int64_t)(col0 + mycol) * (a.transposed ? a.dk : 1);
+      if (mycol < cols) {
+#pragma unroll
+        for (int ft = 0; ft < FT; ++ft)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int k = 16 * ft + 4 * g + j;
+            if (k < a.dk) S[ft][j] = x[k * row + col];
+          }
+        if (MODE == kDecayAug && g == 0) za[0] = xz[col0 + mycol];
+      }
+      if (MODE == kDecayNorm)
+        for (int k = tid; k < a.dk; k += THREADS) l.z[k] = xz[k];
+    }
+  }
+  const auto write_state = [&](float* S1, float* z1) {
+    if (mycol < cols) {
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int k = 16 * ft + 4 * g + j;
+          if (k < a.dk) S1[(int64_t)k * a.dv + col0 + mycol] = S[ft][j];
+        }
+      if (MODE == kDecayAug && g == 0) z1[col0 + mycol] = za[0];
+    }
+    if (MODE == kDecayNorm && slice == 0)
+      for (int k = tid; k < a.dk; k += THREADS) z1[k] = l.z[k];
+  };
   for (int t0 = begin; t0 < end; t0 += C) {
     const int m = min(C, end - t0);
     __syncthreads();  // the chunk before is no longer read (at first: f^i are written)
@@ -198,6 +225,7 @@ __global__ __launch_bounds__(4 * DVW, 2) void decay_kernel(DecayArgs a) {
         l.ka[tid] = in ? ka : 0.0f;
         if (OUT) l.qa[tid] = in ? qa : 0.0f;
       }
+      if (MODE == kDecayNorm && !OUT) l.ka[tid] = ka;
       if (OUT) l.ow[tid] = ow;
     }
     if (t0 + C < end) load(t0 + C);
@@ -319,8 +347,12 @@ __global__ __launch_bounds__(4 * DVW, 2) void decay_kernel(DecayArgs a) {
           mma(o[qt], vf, pf);
         }
       }
-      DecayScaled<T> one;  // columns 0 .. 2: the parts of the discounts
+      DecayScaled<T> one;  // columns 0 .. 2: the parts of the discounts (times b_j)
       if (MODE == kDecayNorm) {
+        if (!OUT) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dec[e] *= l.ka[32 * ks + 8 * g + e];
+        }
         if constexpr (sizeof(T) == 2) {
           Split3 parts;
           split3(parts, dec);
@@ -387,32 +419,10 @@ __global__ __launch_bounds__(4 * DVW, 2) void decay_kernel(DecayArgs a) {
     }
   }
 
-  // the state after the piece: to the next piece's prefix (state pass), or after the sequence's last token
-  float* S1 = nullptr;
-  float* z1 = nullptr;
-  if (!OUT) {
-    S1 = st;
-    z1 = st + (int64_t)a.dk * a.dv;
-  } else if (a.S && end == sp.len) {
-    const int64_t at = (int64_t)sp.seq * a.H + head;
-    S1 = a.S + at * a.dk * a.dv;
-    z1 = MODE == kDecayNorm ? a.z + at * a.dk : nullptr;
-  }
-  if (!S1) return;
-  if (mycol < cols) {
-#pragma unroll
-    for (int ft = 0; ft < FT; ++ft)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int f = 16 * ft + 4 * g + j;
-        if (f < a.dk) S1[(int64_t)f * a.dv + col0 + mycol] = S[ft][j];
-      }
-    if (MODE == kDecayAug && g == 0) z1[col0 + mycol] = za[0];
-  }
-  if (MODE == kDecayNorm && slice == 0) {
-    __syncthreads();
-    for (int f = tid; f < a.dk; f += THREADS) z1[f] = l.z[f];
-  }
+  // the state after the piece (state pass), or after the sequence's last token
+  if (MODE == kDecayNorm) __syncthreads();  // z is whole
+  if (!OUT) write_state(st, st + zat);
+  else if (a.S && end == sp.len) write_state(a.S + user * a.dk * a.dv, MODE == kDecayNorm ? a.z + user * a.dk : nullptr);
 }
 
 template <typename T, int DK, int DVW, int MODE, bool OUT, bool EXACT>

@@ -123,6 +123,7 @@ struct DecayArgs {
   int reverse;             // sums over later tokens instead of earlier ones
   int exact_state;         // the state to fp32 accuracy (it is returned)
   float* states;           // [slots][H][decay_state_floats]: state before each piece; null: one piece per sequence
+  int transposed;          // states: of k and v exchanged
   float* S;                // [count][H][dk][dv] and z [count][H][dk], in and out, or null
   float* z;
   float* den;              // per row, out (kDecayNorm), or null
@@ -136,9 +137,11 @@ __host__ __device__ inline int64_t decay_state_floats(int dk, int dv) {
   return (int64_t)dk * dv + (dk > dv ? dk : dv);
 }
 bool decay_supported(int dk, int dv);
-// states of all pieces but each sequence's last, then (launch_decay_scan) their discounted prefixes
+// What every piece but its sequence's last adds to the state, then the states before the pieces in their place.  (A row
+// pass that adds up the pieces before its own by itself, without the second launch, waits for them one after the
+// other: LUNA backward 256 -> 455 us.)
 hipError_t launch_decay_states(Dt dt, int mode, const DecayArgs& a, hipStream_t s);
-hipError_t launch_decay_scan(int mode, const DecayArgs& a, hipStream_t s);
+hipError_t launch_decay_scan(const DecayArgs& a, hipStream_t s);
 hipError_t launch_decay_out(Dt dt, int mode, const DecayArgs& a, hipStream_t s);
 
 // w = 1 / (den + eps) and wd = -dO.out per row

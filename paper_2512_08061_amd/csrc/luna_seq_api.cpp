@@ -2,6 +2,7 @@
 // a call and its workspace, launches on the caller's stream.
 #include "luna_seq.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 
@@ -98,18 +99,35 @@ struct DecayPlan {
   size_t states = 0, w = 0, delta = 0, total = 0;  // workspace offsets
 };
 
-// Tokens per piece.  A piece is a serial chain of chunks; pieces of one sequence cost a pass over their
-// keys and values for the states, and the states written, scanned and read.
-luna_status plan_decay(const luna_seqs& s, int64_t H, int64_t D, int64_t d, bool backward, bool normalize, DecayPlan* p) {
+// Tokens per piece.  A piece is a serial chain of chunks, so cutting sequences fills the device; but pieces cost a pass
+// over the keys and values of all but each sequence's last one, and their states written, scanned and read.  Estimated
+// from: a 64-token chunk about 4 us with 128 features and d = 128 in bf16, three times as much in fp32, one workgroup
+// a compute unit (two with 64 features), and a sixth more while no second one fills its waits; 4.5 TB/s.  Measured, us a call by piece: 8 x 16
+// heads of 16384 tokens, D = d = 128, one 932, 8192 759, 4096 700, 2048 730; backward of 2 x 16 heads of 2048 tokens
+// with 256 features 256 228, 384 258, 512 236; fp32 backward of 4096 tokens in 12 heads, 64 features, 64 120, 128 107,
+// 256 123.
+luna_status plan_decay(luna_dtype dt, const luna_seqs& s, int64_t H, int64_t D, int64_t d, bool backward, bool normalize,
+                       DecayPlan* p) {
   const int64_t per = s.rows, all = s.offsets ? s.rows : s.count * s.rows;
-  int64_t piece = ceil_div(ceil_div(all * H, 512), 64) * 64;
-  if (piece < 256) piece = 256;
   const int64_t longest = ceil_div(per > 0 ? per : 1, 64) * 64;
-  if (piece > longest) piece = longest;
-  p->piece = (int)piece;
-  p->many = per > piece;
   const luna::SeqSet set = set_of(&s);
-  const int64_t slots = luna::seq_slots(set, piece);
+  const double chunk = (1.5 + 1.5e-4 * (double)(D * d)) * (dt == LUNA_BF16 ? 1.0 : 3.0);
+  const double state = (double)luna::decay_state_floats((int)D, (int)d) * 4;
+  const int64_t room = D <= 64 ? 512 : 256;
+  double best = 0.0;
+  for (int64_t piece = longest; piece >= 64; piece = piece > 64 && piece < 128 ? 64 : piece / 128 * 64) {
+    // sequences of the same length, or packed ones, with half a piece left over at the end of each
+    const int64_t pieces = s.offsets ? ceil_div(all, piece) + s.count / 2 : s.count * ceil_div(per, piece);
+    const double groups = (double)(pieces * H);
+    const double one = (double)ceil_div(pieces * H, room) * (double)ceil_div(piece, 64) * chunk * (groups < 2 * room ? 1.17 : 1.0);
+    const double cost = piece == longest ? one : 1.4 * one + 8.0 + 4.0 * groups * state / 4.5e6;
+    if (p->piece == 0 || cost < best) {
+      best = cost;
+      p->piece = (int)piece;
+    }
+  }
+  p->many = per > p->piece;
+  const int64_t slots = luna::seq_slots(set, p->piece);
   if (slots * H * 2 > kMaxGrid) return set_error(LUNA_ERR_UNSUPPORTED, "too many pieces of sequences and heads");
   p->slots = (int)slots;
   size_t off = 0;
@@ -149,17 +167,18 @@ luna_status check_state(const float* S, const float* z, int32_t normalize) {
   return LUNA_OK;
 }
 
-// the states of all pieces, their prefixes, then the rows
-luna_status run_decay(luna::Dt dt, int mode, const DecayPlan& p, luna::DecayArgs& a, void* ws, hipStream_t s) {
+void set_plan(const DecayPlan& p, luna::DecayArgs& a, void* ws) {
   a.piece = p.piece;
   a.slots = p.slots;
-  a.states = nullptr;
-  luna_status st;
-  if (p.many) {
-    a.states = reinterpret_cast<float*>(static_cast<char*>(ws) + p.states);
-    if ((st = hip_status(luna::launch_decay_states(dt, mode, a, s), "decay state launch")) != LUNA_OK) return st;
-    if ((st = hip_status(luna::launch_decay_scan(mode, a, s), "decay scan launch")) != LUNA_OK) return st;
-  }
+  a.states = p.many ? reinterpret_cast<float*>(static_cast<char*>(ws) + p.states) : nullptr;
+}
+luna_status run_decay_states(luna::Dt dt, int mode, const luna::DecayArgs& a, hipStream_t s) {
+  if (!a.states) return LUNA_OK;
+  const luna_status st = hip_status(luna::launch_decay_states(dt, mode, a, s), "decay state launch");
+  if (st != LUNA_OK) return st;
+  return hip_status(luna::launch_decay_scan(a, s), "decay scan launch");
+}
+luna_status run_decay_rows(luna::Dt dt, int mode, const luna::DecayArgs& a, hipStream_t s) {
   return hip_status(luna::launch_decay_out(dt, mode, a, s), "decay launch");
 }
 
@@ -231,7 +250,7 @@ size_t luna_seq_workspace_bytes(int32_t op, luna_dtype dtype, const luna_seqs* s
     const float one = 1.0f;
     if (check_seqs(seqs, "seqs") != LUNA_OK || check_decay(dtype, H, Dq, Dv, &one, 1, 1.0f, 0.0f) != LUNA_OK) return 0;
     DecayPlan p;
-    if (plan_decay(*seqs, H, Dq, Dv, op == LUNA_OP_DECAY_BWD, true, &p) != LUNA_OK) return 0;
+    if (plan_decay(dtype, *seqs, H, Dq, Dv, op == LUNA_OP_DECAY_BWD, true, &p) != LUNA_OK) return 0;
     return p.total;
   }
   if (op == LUNA_OP_SOFTMAX_FWD || op == LUNA_OP_SOFTMAX_BWD) {
@@ -262,7 +281,7 @@ luna_status luna_decay_fwd(const luna_rows* Q, const luna_rows* K, const luna_ro
   if ((st = check_rows(V, "V", dtype, *seqs, H, d, false)) != LUNA_OK) return st;
   if ((st = check_rows(out, "out", dtype, *seqs, H, d, true)) != LUNA_OK) return st;
   DecayPlan p;
-  if ((st = plan_decay(*seqs, H, D, d, false, normalize, &p)) != LUNA_OK) return st;
+  if ((st = plan_decay(dtype, *seqs, H, D, d, false, normalize, &p)) != LUNA_OK) return st;
   if ((st = check_ws(p.total, ws, ws_bytes)) != LUNA_OK) return st;
   if (seqs->rows == 0) return LUNA_OK;
   luna::DecayArgs a{};
@@ -281,8 +300,11 @@ luna_status luna_decay_fwd(const luna_rows* Q, const luna_rows* K, const luna_ro
   a.den = den;
   a.scale = scale;
   a.eps = eps;
-  return run_decay(type_of(dtype), normalize ? luna::kDecayNorm : luna::kDecayPlain, p, a, ws,
-                   reinterpret_cast<hipStream_t>(stream));
+  const int mode = normalize ? luna::kDecayNorm : luna::kDecayPlain;
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  set_plan(p, a, ws);
+  if ((st = run_decay_states(type_of(dtype), mode, a, hs)) != LUNA_OK) return st;
+  return run_decay_rows(type_of(dtype), mode, a, hs);
 }
 
 luna_status luna_decay_step(const luna_rows* Q, const luna_rows* K, const luna_rows* V, luna_dtype dtype, int64_t count,
@@ -339,7 +361,7 @@ luna_status luna_decay_bwd(const luna_rows* Q, const luna_rows* K, const luna_ro
   if ((st = check_rows(dK, "dK", dtype, *seqs, H, D, true)) != LUNA_OK) return st;
   if ((st = check_rows(dV, "dV", dtype, *seqs, H, d, true)) != LUNA_OK) return st;
   DecayPlan p;
-  if ((st = plan_decay(*seqs, H, D, d, true, normalize, &p)) != LUNA_OK) return st;
+  if ((st = plan_decay(dtype, *seqs, H, D, d, true, normalize, &p)) != LUNA_OK) return st;
   if ((st = check_ws(p.total, ws, ws_bytes)) != LUNA_OK) return st;
   if (seqs->rows == 0) return LUNA_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -357,6 +379,7 @@ luna_status luna_decay_bwd(const luna_rows* Q, const luna_rows* K, const luna_ro
   a.log_decay = log_decay;
   a.H = (int)H;
   a.scale = scale;
+  set_plan(p, a, ws);
   const int mode = normalize ? luna::kDecayAug : luna::kDecayPlain;
   // dQ: dO against V, with K as values
   a.q = rows_of(dO);
@@ -367,27 +390,31 @@ luna_status luna_decay_bwd(const luna_rows* Q, const luna_rows* K, const luna_ro
   a.dv = (int)D;
   a.qa = delta;
   a.ow = w;
-  if ((st = run_decay(dt, mode, p, a, ws, s)) != LUNA_OK) return st;
-  // dK: V against dO, with Q as values, over later tokens
-  a.q = rows_of(V);
-  a.k = rows_of(dO);
-  a.v = rows_of(Q);
-  a.o = rows_of(dK);
-  a.qa = nullptr;
-  a.ka = delta;
-  a.kw = w;
-  a.ow = nullptr;
+  if ((st = run_decay_states(dt, mode, a, s)) != LUNA_OK) return st;
+  if ((st = run_decay_rows(dt, mode, a, s)) != LUNA_OK) return st;
+  // over later tokens: dV, K against Q with dO as values (whose states, and z of weights delta, are dK's, too)
   a.reverse = 1;
-  if ((st = run_decay(dt, mode, p, a, ws, s)) != LUNA_OK) return st;
-  // dV: K against Q, with dO as values, over later tokens
   a.q = rows_of(K);
   a.k = rows_of(Q);
   a.v = rows_of(dO);
   a.o = rows_of(dV);
   a.dk = (int)D;
   a.dv = (int)d;
-  a.ka = nullptr;
-  return run_decay(dt, luna::kDecayPlain, p, a, ws, s);
+  a.qa = nullptr;
+  a.ka = delta;
+  a.kw = w;
+  a.ow = nullptr;
+  if ((st = run_decay_states(dt, normalize ? luna::kDecayNorm : luna::kDecayPlain, a, s)) != LUNA_OK) return st;
+  if ((st = run_decay_rows(dt, luna::kDecayPlain, a, s)) != LUNA_OK) return st;
+  // dK: V against dO, with Q as values
+  a.q = rows_of(V);
+  a.k = rows_of(dO);
+  a.v = rows_of(Q);
+  a.o = rows_of(dK);
+  a.dk = (int)d;
+  a.dv = (int)D;
+  a.transposed = 1;
+  return run_decay_rows(dt, mode, a, s);
 }
 
 luna_status luna_softmax_fwd(const luna_rows* Q, const luna_rows* K, const luna_rows* V, luna_dtype dtype,
