@@ -579,12 +579,30 @@ class Plan:
 OP_DECAY_FWD, OP_DECAY_BWD, OP_SOFTMAX_FWD, OP_SOFTMAX_BWD = range(4)
 
 
+# What a call of a few microseconds needs from torch, looked up once.
+_seq_torch = None
+
+
+def _seq_init():
+    global _seq_torch
+    import types
+
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    stream = (lambda device: raw(device.index)) if raw is not None else _stream_ptr
+    _seq_torch = types.SimpleNamespace(
+        f32=torch.float32, i32=torch.int32, bf16=torch.bfloat16, empty=torch.empty, empty_like=torch.empty_like,
+        zeros_like=torch.zeros_like, device=torch.cuda.device, current=torch.cuda.current_device, stream=stream,
+        lib=load_library())
+    return _seq_torch
+
+
 class _Seqs:
     """The sequences of a call (luna_seqs): of 4-dim tensors [B, H, n, width], with lens [B]
     where fewer than n rows of each are used, or of 3-dim packed tensors [T, H, width] with offsets [B + 1]."""
 
     def __init__(self, t, offsets, lens, what):
-        torch = _torch()
+        T = _seq_torch or _seq_init()
         if t.dim() == 3:
             if offsets is None or lens is not None:
                 raise LunaError(LUNA_ERR_INVALID_ARG, f"{what}: packed [T, H, width] tensors take offsets, and no lens")
@@ -600,7 +618,7 @@ class _Seqs:
         at = 0
         if index is not None:
             want = self.count + 1 if self.packed else self.count
-            if index.dtype != torch.int32 or index.device != t.device or not index.is_contiguous() or \
+            if index.dtype != T.i32 or index.device != t.device or not index.is_contiguous() or \
                     index.dim() != 1 or index.shape[0] != want or self.count < 1:
                 raise LunaError(LUNA_ERR_INVALID_ARG, "offsets [B + 1] and lens [B] must be contiguous int32 tensors on "
                                                       "the tensors' device")
@@ -620,55 +638,53 @@ class _Seqs:
 def _seq_rows(seqs, ts, heads, widths, names):
     """luna_rows of each tensor, one behind the other, as an array of whole numbers."""
     v = []
+    dtype, device, packed, count, rows = seqs.dtype, seqs.device, seqs.packed, seqs.count, seqs.rows
     for t, H, w, name in zip(ts, heads, widths, names):
-        if t.dtype != seqs.dtype or t.device != seqs.device or not t.is_cuda:
+        if t.dtype != dtype or t.device != device or not t.is_cuda:
             raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} must share the other tensors' dtype and GPU")
-        if not seqs.same(t) or t.shape[1] != H or t.shape[-1] != w:
-            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} has shape {tuple(t.shape)}: its sequences, {H} heads or width "
+        shape, st = t.shape, t.stride()
+        if shape != ((rows, H, w) if packed else (count, H, rows, w)):
+            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} has shape {tuple(shape)}: its sequences, {H} heads or width "
                                                   f"{w} do not match")
-        st = t.stride()
         if w > 1 and st[-1] != 1:
             raise LunaError(LUNA_ERR_INVALID_ARG, f"{name}'s rows must be contiguous")
-        if seqs.packed:  # (a stride of an extent of one is never used)
-            v += (t.data_ptr(), 0, st[1] if H > 1 else 0, st[0] if seqs.rows > 1 else w)
+        if packed:  # (a stride of an extent of one is never used)
+            v += (t.data_ptr(), 0, st[1] if H > 1 else 0, st[0] if rows > 1 else w)
         else:
-            v += (t.data_ptr(), st[0] if seqs.count > 1 else 0, st[1] if H > 1 else 0, st[2] if seqs.rows > 1 else w)
+            v += (t.data_ptr(), st[0] if count > 1 else 0, st[1] if H > 1 else 0, st[2] if rows > 1 else w)
     return (ctypes.c_int64 * len(v))(*v)
 
 
 def _f32_ptr(t, shape, device, name):
-    torch = _torch()
-    if tuple(t.shape) != tuple(shape) or t.dtype != torch.float32 or t.device != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype != _seq_torch.f32 or t.device != device or not t.is_contiguous():
         raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} must be a contiguous fp32 {list(shape)} tensor on the tensors' device")
     return t.data_ptr()
 
 
-class _on_device:
-    """The tensors' device as the current one during a call."""
-
-    def __init__(self, device):
-        torch = _torch()
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
+class _NoGuard:
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
+        pass
 
     def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        pass
+
+
+_no_guard = _NoGuard()
+
+
+def _on_device(device):
+    """The tensors' device as the current one during a call."""
+    return _no_guard if device.index == _seq_torch.current() else _seq_torch.device(device)
 
 
 def _new(t, lens):
     """An output like t; with lens its unused rows are zeros."""
-    torch = _torch()
-    return torch.empty_like(t) if lens is None else torch.zeros_like(t)
+    return _seq_torch.empty_like(t) if lens is None else _seq_torch.zeros_like(t)
 
 
 def _seq_workspace(op, seqs, keys, H, Hk, Dq, Dv, dt):
     """(tensor to keep, address, bytes) of an operation's workspace."""
-    lib = load_library()
-    nb = int(lib.luna_seq_workspace_bytes(op, dt, ctypes.addressof(seqs.c), None if keys is None else ctypes.addressof(keys.c),
+    nb = int(_seq_torch.lib.luna_seq_workspace_bytes(op, dt, ctypes.addressof(seqs.c), None if keys is None else ctypes.addressof(keys.c),
                                           H, Hk, Dq, Dv))
     return (None, None, 0) if nb == 0 else _workspace(nb, seqs.device)
 
@@ -698,8 +714,7 @@ def decay_attn(Q, K, V, log_decay, S=None, z=None, normalize: bool = False, scal
     overwritten by the state after the last.  Returns (out, den): out like V, and with normalize the
     denominators [B, H, n] or [H, T] that decay_attn_bwd takes (else None).  Rows of no sequence are not
     written: zeros in a new out for lens, undefined in one for offsets."""
-    torch = _torch()
-    lib = load_library()
+    lib = (_seq_torch or _seq_init()).lib
     seqs = _Seqs(Q, offsets, lens, "Q")
     H, D, d = Q.shape[1], Q.shape[-1], V.shape[-1]
     out = _new(V, lens) if out is None else out
@@ -708,7 +723,7 @@ def decay_attn(Q, K, V, log_decay, S=None, z=None, normalize: bool = False, scal
     sp, zp = _decay_state(S, z, seqs.count, H, D, d, normalize, seqs.device)
     dp = None
     if normalize:
-        den = torch.empty(seqs.numbers(H), dtype=torch.float32, device=seqs.device) if den is None else den
+        den = _seq_torch.empty(seqs.numbers(H), dtype=_seq_torch.f32, device=seqs.device) if den is None else den
         dp = _f32_ptr(den, seqs.numbers(H), seqs.device, "den")
     elif den is not None:
         raise LunaError(LUNA_ERR_INVALID_ARG, "den goes with normalize")
@@ -716,14 +731,14 @@ def decay_attn(Q, K, V, log_decay, S=None, z=None, normalize: bool = False, scal
     with _on_device(seqs.device):
         ws, wsp, wsn = _seq_workspace(OP_DECAY_FWD, seqs, None, H, H, D, d, dt)
         _check(lib.luna_decay_fwd(at, at + 32, at + 64, dt, ctypes.addressof(seqs.c), H, D, d, gp, int(normalize), scale, eps,
-                                  sp, zp, at + 96, dp, wsp, wsn, _stream_ptr(seqs.device)))
+                                  sp, zp, at + 96, dp, wsp, wsn, _seq_torch.stream(seqs.device)))
     return out, den
 
 
 def decay_attn_step(Q, K, V, log_decay, S, z=None, normalize: bool = False, scale: float = 1.0, eps: float = 1e-6, out=None):
     """The m next tokens of every sequence (luna_decay_step): Q, K [B, H, m, D], V [B, H, m, d] from the state
     S [B, H, D, d] (and z [B, H, D], normalised), which is updated in place; returns out like V."""
-    lib = load_library()
+    lib = (_seq_torch or _seq_init()).lib
     if Q.dim() != 4:
         raise LunaError(LUNA_ERR_INVALID_ARG, "Q must be [B, H, m, D]")
     seqs = _Seqs(Q, None, None, "Q")
@@ -735,7 +750,7 @@ def decay_attn_step(Q, K, V, log_decay, S, z=None, normalize: bool = False, scal
     at = ctypes.addressof(rows)
     with _on_device(seqs.device):
         _check(lib.luna_decay_step(at, at + 32, at + 64, _dt(Q), seqs.count, seqs.rows, H, D, d, gp, int(normalize), scale, eps,
-                                   sp, zp, at + 96, _stream_ptr(seqs.device)))
+                                   sp, zp, at + 96, _seq_torch.stream(seqs.device)))
     return out
 
 
@@ -743,7 +758,7 @@ def decay_attn_bwd(Q, K, V, dO, log_decay, out=None, den=None, normalize: bool =
                    eps: float = 1e-6, offsets=None, lens=None, grads=None):
     """Backward pass of decay_attn from an empty state (luna_decay_bwd): returns (dQ, dK, dV), into grads when
     given.  With normalize, out and den are what the forward call returned."""
-    lib = load_library()
+    lib = (_seq_torch or _seq_init()).lib
     seqs = _Seqs(Q, offsets, lens, "Q")
     H, D, d = Q.shape[1], Q.shape[-1], V.shape[-1]
     dQ, dK, dV = tuple(_new(t, lens) for t in (Q, K, V)) if grads is None else grads
@@ -759,7 +774,7 @@ def decay_attn_bwd(Q, K, V, dO, log_decay, out=None, den=None, normalize: bool =
         ws, wsp, wsn = _seq_workspace(OP_DECAY_BWD, seqs, None, H, H, D, d, dt)
         _check(lib.luna_decay_bwd(at, at + 32, at + 64, at + 96, dt, ctypes.addressof(seqs.c), H, D, d, gp, int(normalize),
                                   scale, eps, at + 128 if normalize else None, dp, at + 160, at + 192, at + 224, wsp, wsn,
-                                  _stream_ptr(seqs.device)))
+                                  _seq_torch.stream(seqs.device)))
     return dQ, dK, dV
 
 
@@ -783,8 +798,7 @@ def softmax_attn(Q, K, V, scale: float | None = None, offsets=None, lens=None, k
     Q and the logarithm of each row's sum, [B, H, n] or [H, T], which softmax_attn_bwd takes.  A row
     that sees no key has out 0 and lse -infinity.  Rows of no sequence are not written: zeros in a new out for
     lens, undefined in one for offsets."""
-    torch = _torch()
-    lib = load_library()
+    lib = (_seq_torch or _seq_init()).lib
     seqs = _Seqs(Q, offsets, lens, "Q")
     H, Hk, d = Q.shape[1], K.shape[1], Q.shape[-1]
     keys = _softmax_keys(Q, K, seqs, offsets, lens, k_offsets, k_lens)
@@ -793,14 +807,14 @@ def softmax_attn(Q, K, V, scale: float | None = None, offsets=None, lens=None, k
     krows = _seq_rows(keys or seqs, (K, V), (Hk, Hk), (d, d), ("K", "V"))
     if keys is not None and (keys.dtype != seqs.dtype or keys.device != seqs.device):
         raise LunaError(LUNA_ERR_INVALID_ARG, "Q and K must share dtype and GPU")
-    lse = torch.empty(seqs.numbers(H), dtype=torch.float32, device=seqs.device) if lse is None else lse
+    lse = _seq_torch.empty(seqs.numbers(H), dtype=_seq_torch.f32, device=seqs.device) if lse is None else lse
     lp = _f32_ptr(lse, seqs.numbers(H), seqs.device, "lse")
     dt, at, ak = _dt(Q), ctypes.addressof(rows), ctypes.addressof(krows)
     with _on_device(seqs.device):
         ws, wsp, wsn = _seq_workspace(OP_SOFTMAX_FWD, seqs, keys, H, Hk, d, d, dt)
         _check(lib.luna_softmax_fwd(at, ak, ak + 32, dt, ctypes.addressof(seqs.c),
                                     None if keys is None else ctypes.addressof(keys.c), H, Hk, d,
-                                    d ** -0.5 if scale is None else scale, at + 32, lp, wsp, wsn, _stream_ptr(seqs.device)))
+                                    d ** -0.5 if scale is None else scale, at + 32, lp, wsp, wsn, _seq_torch.stream(seqs.device)))
     return out, lse
 
 
@@ -808,7 +822,7 @@ def softmax_attn_bwd(Q, K, V, out, lse, dO, scale: float | None = None, offsets=
                      k_lens=None, grads=None):
     """Backward pass of softmax_attn (luna_softmax_bwd) from its out and lse: returns (dQ, dK, dV), into grads when
     given; dK and dV are summed over the query heads of each key head."""
-    lib = load_library()
+    lib = (_seq_torch or _seq_init()).lib
     seqs = _Seqs(Q, offsets, lens, "Q")
     H, Hk, d = Q.shape[1], K.shape[1], Q.shape[-1]
     keys = _softmax_keys(Q, K, seqs, offsets, lens, k_offsets, k_lens)
@@ -825,5 +839,5 @@ def softmax_attn_bwd(Q, K, V, out, lse, dO, scale: float | None = None, offsets=
         _check(lib.luna_softmax_bwd(at, ak, ak + 32, at + 32, lp, at + 64, dt, ctypes.addressof(seqs.c),
                                     None if keys is None else ctypes.addressof(keys.c), H, Hk, d,
                                     d ** -0.5 if scale is None else scale, at + 96, ak + 64, ak + 96, wsp, wsn,
-                                    _stream_ptr(seqs.device)))
+                                    _seq_torch.stream(seqs.device)))
     return dQ, dK, dV
