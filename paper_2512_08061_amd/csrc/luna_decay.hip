@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int64_t el
 
 // w_i = 1 / (den_i + eps), delta_i = -dO_i.out_i: a quarter wave per row.
 template <typename T>
-__global__ __launch_bounds__(256) void decay_weights_kernel(DecayWeightsArgs a, int tiles) {
+__global__ __launch_bounds__(256) void decay_weights_kernel(DecayWeightsArgs a) {
   const int head = blockIdx.y;
   const SeqPiece sp = seq_piece(a.s, blockIdx.x, 64);
   if (sp.seq < 0) return;
@@ -101,10 +101,9 @@ hipError_t launch_decay_scan(const DecayArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_decay_weights(Dt dt, const DecayWeightsArgs& a, hipStream_t s) {
-  const int64_t tiles = seq_slots(a.s, 64);
-  const dim3 grid((unsigned)tiles, (unsigned)a.H);
-  if (dt == Dt::BF16) hipLaunchKernelGGL(decay_weights_kernel<__bf16>, grid, dim3(256), 0, s, a, (int)tiles);
-  else hipLaunchKernelGGL(decay_weights_kernel<float>, grid, dim3(256), 0, s, a, (int)tiles);
+  const dim3 grid((unsigned)seq_slots(a.s, 64), (unsigned)a.H);
+  if (dt == Dt::BF16) hipLaunchKernelGGL(decay_weights_kernel<__bf16>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(decay_weights_kernel<float>, grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

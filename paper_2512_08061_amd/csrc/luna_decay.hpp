@@ -452,9 +452,9 @@ hipError_t launch_decay_width(const DecayArgs& a, hipStream_t s) {
 
 template <typename T, int MODE, bool OUT>
 hipError_t launch_decay_mode(const DecayArgs& a, hipStream_t s) {
-  return a.dk <= 64    ? launch_decay_width<T, 64, MODE, OUT>(a, s)
-         : a.dk <= 128 ? launch_decay_width<T, 128, MODE, OUT>(a, s)
-                       : launch_decay_width<T, 256, MODE, OUT>(a, s);
+  if constexpr (MODE != kDecayAug)  // (whose keys are V or dO)
+    if (a.dk > 128) return launch_decay_width<T, 256, MODE, OUT>(a, s);
+  return a.dk <= 64 ? launch_decay_width<T, 64, MODE, OUT>(a, s) : launch_decay_width<T, 128, MODE, OUT>(a, s);
 }
 
 // one translation unit per element type and mode (luna_decay_*.hip)

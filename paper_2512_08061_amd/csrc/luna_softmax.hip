@@ -122,17 +122,20 @@ __global__ __launch_bounds__(256) void softmax_fwd_kernel(SoftmaxArgs a) {
 // are the k-slots of its half for the product with V.  The next block is on its way to registers while one is worked on.
 // The output is rescaled only when some row's maximum has grown by more than 2^8 since its last rescaling (a sum of
 // at most 2^8 times larger terms keeps its relative accuracy), which most blocks skip.
-template <int DH>
+// With GROUPS = 2 two groups of four waves take the key blocks in turn, each with its own maxima, sums and rows, which are
+// joined at the end: the last tile of a sequence is a chain half as long.
+template <int DH, int GROUPS>
 struct SoftmaxLds32 {
-  Tile<DH> k[2], v[2];
+  Tile<DH> k[GROUPS][2], v[GROUPS][2];  // per group of waves, twice
 };
 
-template <int DH>
-__global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
+template <int DH, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
   constexpr int KB = 64, KS = DH / 16, CT = DH / 32, esz = 2;
   extern __shared__ __attribute__((aligned(16))) char raw[];
-  SoftmaxLds32<DH>& l = *reinterpret_cast<SoftmaxLds32<DH>*>(raw);
-  const int lane = threadIdx.x % kWave, wave = wave_id(), h = lane / 32, c = lane % 32;
+  SoftmaxLds32<DH, GROUPS>& l = *reinterpret_cast<SoftmaxLds32<DH, GROUPS>*>(raw);
+  const int lane = threadIdx.x % kWave, wave = wave_id() % 4, h = lane / 32, c = lane % 32;
+  const int group = GROUPS == 1 ? 0 : wave_id() / 4, tid = threadIdx.x % 256;
   const int head = head_of(blockIdx.x % a.H, a.H), slot = gridDim.x / a.H - 1 - blockIdx.x / a.H;
   const SeqPiece sq = seq_piece(a.qs, slot, 128);
   if (sq.seq < 0) return;
@@ -167,16 +170,16 @@ __global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
 
   TileRegs<DH> kr, vr;
   const auto load = [&](int k0) {
-    Tile<DH>::load(kr, seq_row(a.k, sk, pk, hk, k0, esz), a.k.row, min(KB, kend - k0));
-    Tile<DH>::load(vr, seq_row(a.v, sk, pk, hk, k0, esz), a.v.row, min(KB, kend - k0));
+    Tile<DH>::load(kr, tid, seq_row(a.k, sk, pk, hk, k0, esz), a.k.row, min(KB, kend - k0));
+    Tile<DH>::load(vr, tid, seq_row(a.v, sk, pk, hk, k0, esz), a.v.row, min(KB, kend - k0));
   };
-  load(0);
-  l.k[0].store(kr);
-  l.v[0].store(vr);
+  load(KB * group);
+  l.k[group][0].store(kr, tid);
+  l.v[group][0].store(vr, tid);
   int buf = 0;
-  for (int k0 = 0; k0 < kend; k0 += KB, buf ^= 1) {
+  for (int k0 = KB * group; k0 - KB * group < kend; k0 += GROUPS * KB, buf ^= 1) {
     __syncthreads();  // this block is whole, and the one before no longer read
-    load(k0 + KB);
+    load(k0 + GROUPS * KB);
     if (k0 <= wlast) {
       f32x16 s[2];
 #pragma unroll
@@ -187,7 +190,7 @@ __global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
       for (int t = 0; t < KS; ++t)
 #pragma unroll
         for (int half = 0; half < 2; ++half)
-          s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(l.k[buf].row8(32 * half + c, 2 * t + h), qf[t], s[half], 0, 0, 0);
+          s[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(l.k[group][buf].row8(32 * half + c, 2 * t + h), qf[t], s[half], 0, 0, 0);
       // V operands of 16 keys, read one step before their products (by itself the compiler reads each right before
       // its use and waits out the LDS 16 times a block)
       Frag<__bf16> vf[2][CT];
@@ -195,8 +198,8 @@ __global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
           const int row = 16 * ks + 4 * h, col = 32 * t + 16 * ((lane / 16) % 2);
-          l.v[buf].tr4(vf[ks % 2][t], 0, row, col, lane);
-          l.v[buf].tr4(vf[ks % 2][t], 4, row + 8, col, lane);
+          l.v[group][buf].tr4(vf[ks % 2][t], 0, row, col, lane);
+          l.v[group][buf].tr4(vf[ks % 2][t], 4, row + 8, col, lane);
         }
       };
       read_v(0);
@@ -246,12 +249,37 @@ __global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
         for (int t = 0; t < CT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ks % 2][t].v, pf.v, o[t], 0, 0, 0);
       }
     }
-    l.k[buf ^ 1].store(kr);
-    l.v[buf ^ 1].store(vr);
+    l.k[group][buf ^ 1].store(kr, tid);
+    l.v[group][buf ^ 1].store(vr, tid);
   }
-  {
-    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
-    sum = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  sum = halves_sum(sum);
+  if constexpr (GROUPS == 2) {  // the second group's rows join the first's
+    constexpr int ROWS = 4 * kWave * CT * 16;
+    static_assert(sizeof(l) >= (ROWS + 256) * sizeof(float), "a group's rows fit the tiles");
+    float* part = reinterpret_cast<float*>(raw);
+    f32x4* rows = reinterpret_cast<f32x4*>(raw);
+    __syncthreads();
+    if (group == 1) {
+#pragma unroll
+      for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          rows[((t * 4 + e) * 4 + wave) * kWave + lane] = f32x4{o[t][4 * e], o[t][4 * e + 1], o[t][4 * e + 2], o[t][4 * e + 3]};
+      if (h == 0) {
+        part[ROWS + i] = base;
+        part[ROWS + 128 + i] = sum;
+      }
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const float other = part[ROWS + i], most = fmaxf(base, other), to = most == -__builtin_inff() ? 0.0f : most;
+    const float f = exp2_raw(base - to), g = exp2_raw(other - to);
+    base = most;
+    sum = sum * f + part[ROWS + 128 + i] * g;
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[t][e] = fmaf(o[t][e], f, g * rows[((t * 4 + e / 4) * 4 + wave) * kWave + lane][e % 4]);
   }
   const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;  // (NaN stays)
   const Buf b = buffer(seq_row(a.o, sq, pq, head, q0, esz), (int)(((m - 1) * a.o.row + DH) * esz));
@@ -264,29 +292,36 @@ __global__ __launch_bounds__(256, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
   if (a.lse && h == 0 && i < m) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (base + log2f(sum)) * kLn2;
 }
 
-template <int DH>
-hipError_t launch_fwd32(const SoftmaxArgs& a, hipStream_t s) {
-  constexpr int bytes = (int)sizeof(SoftmaxLds32<DH>);
-  const hipError_t e = allow_lds<softmax_fwd32_kernel<DH>>(bytes);
+template <int DH, int GROUPS>
+hipError_t launch_groups(const SoftmaxArgs& a, hipStream_t s) {
+  constexpr int bytes = (int)sizeof(SoftmaxLds32<DH, GROUPS>);
+  const hipError_t e = allow_lds<softmax_fwd32_kernel<DH, GROUPS>>(bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((softmax_fwd32_kernel<DH>), dim3((unsigned)(seq_slots(a.qs, 128) * a.H)), dim3(256), bytes, s, a);
+  const dim3 grid((unsigned)(seq_slots(a.qs, 128) * a.H));
+  hipLaunchKernelGGL((softmax_fwd32_kernel<DH, GROUPS>), grid, dim3(256 * GROUPS), bytes, s, a);
   return hipGetLastError();
 }
 
-template <typename T>
+// Two groups where the longest chain counts: up to two workgroups a compute unit (of which one with two groups, or
+// two with one, run at once).  d = 128, one group and two: 16 heads of 1999 tokens 46.6 and 41.9 us, 32 heads 57.2 and
+// 55.1, 16 heads of 4000 tokens 98 and 88, but 8 x 512 tokens 25.0 and 33.2, 12 heads of 8000 tokens 228 and 247.
+template <int DH>
+hipError_t launch_fwd32(const SoftmaxArgs& a, hipStream_t s) {
+  return seq_slots(a.qs, 128) * a.H <= 512 ? launch_groups<DH, 2>(a, s) : launch_groups<DH, 1>(a, s);
+}
+
+template <typename T, int DH>
 hipError_t launch_fwd(const SoftmaxArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(seq_slots(a.qs, kSoftmaxTile) * a.H));
-  if (a.d == 32) hipLaunchKernelGGL((softmax_fwd_kernel<T, 32>), grid, dim3(256), 0, s, a);
-  else if (a.d == 64) hipLaunchKernelGGL((softmax_fwd_kernel<T, 64>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((softmax_fwd_kernel<T, 128>), grid, dim3(256), 0, s, a);
+  hipLaunchKernelGGL((softmax_fwd_kernel<T, DH>), dim3((unsigned)(seq_slots(a.qs, kSoftmaxTile) * a.H)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_softmax_fwd(Dt dt, const SoftmaxArgs& a, hipStream_t s) {
-  if (dt == Dt::F32) return launch_fwd<float>(a, s);
-  return a.d == 32 ? launch_fwd<__bf16>(a, s) : a.d == 64 ? launch_fwd32<64>(a, s) : launch_fwd32<128>(a, s);
+  if (dt == Dt::F32)
+    return a.d == 32 ? launch_fwd<float, 32>(a, s) : a.d == 64 ? launch_fwd<float, 64>(a, s) : launch_fwd<float, 128>(a, s);
+  return a.d == 32 ? launch_fwd<__bf16, 32>(a, s) : a.d == 64 ? launch_fwd32<64>(a, s) : launch_fwd32<128>(a, s);
 }
 
 }  // namespace luna

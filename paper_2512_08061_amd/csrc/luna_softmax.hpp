@@ -66,22 +66,22 @@ struct Tile {
   static __device__ __forceinline__ int swap(int row) {
     return DH == 128 ? (row % 4) * 2 + (row / 4) % 2 : ((row / 2) % 4) * 2;
   }
-  // `n` rows from `base`, the others as zeros
+  // `n` rows from `base`, the others as zeros, by THREADS threads of which this is tid
   template <int THREADS>
-  static __device__ __forceinline__ void load(TileRegs<DH, THREADS>& t, const char* base, int64_t row, int n) {
+  static __device__ __forceinline__ void load(TileRegs<DH, THREADS>& t, int tid, const char* base, int64_t row, int n) {
     const Buf b = buffer(base, n > 0 ? (int)(((n - 1) * row + DH) * 2) : 0);
 #pragma unroll
     for (int j = 0; j < 64 * PIECES / THREADS; ++j) {
-      const int at = threadIdx.x + THREADS * j, r = at / PIECES, piece = at % PIECES;
+      const int at = tid + THREADS * j, r = at / PIECES, piece = at % PIECES;
       t.x[j] = __builtin_bit_cast(
           i32x4, __builtin_amdgcn_raw_buffer_load_b128(b, r < n ? (r * (int)row + piece * 8) * 2 : kPastEnd, 0, 0));
     }
   }
   template <int THREADS>
-  __device__ __forceinline__ void store(const TileRegs<DH, THREADS>& t) {
+  __device__ __forceinline__ void store(const TileRegs<DH, THREADS>& t, int tid) {
 #pragma unroll
     for (int j = 0; j < 64 * PIECES / THREADS; ++j) {
-      const int at = threadIdx.x + THREADS * j, r = at / PIECES, piece = at % PIECES;
+      const int at = tid + THREADS * j, r = at / PIECES, piece = at % PIECES;
       *reinterpret_cast<i32x4*>(&x[r * DH + ((piece ^ swap(r)) * 8)]) = t.x[j];
     }
   }

@@ -272,12 +272,12 @@ __global__ __launch_bounds__(256, 2) void softmax_dq32_kernel(SoftmaxArgs a) {
 
   TileRegs<DH> kr, vr;
   const auto load = [&](int k0) {
-    Tile<DH>::load(kr, seq_row(a.k, sk, pk, hk, k0, esz), a.k.row, min(KB, kend - k0));
-    Tile<DH>::load(vr, seq_row(a.v, sk, pk, hk, k0, esz), a.v.row, min(KB, kend - k0));
+    Tile<DH>::load(kr, threadIdx.x, seq_row(a.k, sk, pk, hk, k0, esz), a.k.row, min(KB, kend - k0));
+    Tile<DH>::load(vr, threadIdx.x, seq_row(a.v, sk, pk, hk, k0, esz), a.v.row, min(KB, kend - k0));
   };
   load(0);
-  l.x[0].store(kr);
-  l.y[0].store(vr);
+  l.x[0].store(kr, threadIdx.x);
+  l.y[0].store(vr, threadIdx.x);
   int buf = 0;
   for (int k0 = 0; k0 < kend; k0 += KB, buf ^= 1) {
     __syncthreads();  // this block is whole, and the one before no longer read
@@ -322,8 +322,8 @@ __global__ __launch_bounds__(256, 2) void softmax_dq32_kernel(SoftmaxArgs a) {
 #pragma unroll
         for (int t = 0; t < CT; ++t) dq[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks][t].v, ds[ks].v, dq[t], 0, 0, 0);
     }
-    l.x[buf ^ 1].store(kr);
-    l.y[buf ^ 1].store(vr);
+    l.x[buf ^ 1].store(kr, threadIdx.x);
+    l.y[buf ^ 1].store(vr, threadIdx.x);
   }
   store_rows<DH>(seq_row(a.dq, sq, pq, head, q0, esz), a.dq.row, m, i, h, dq, a.scale);
 }
@@ -375,15 +375,15 @@ __global__ __launch_bounds__(512, 2) void softmax_dkdv32_kernel(SoftmaxArgs a) {
   float lse = 0.0f, delta = 0.0f;  // of query threadIdx.x of the step
   const auto load = [&](int step) {
     const int head = head0 + step / blocks, q0 = qbegin + step % blocks * KB, qn = min(KB, sq.len - q0);
-    Tile<DH>::load(xr, seq_row(a.q, sq, pq, head, q0, esz), a.q.row, qn);
-    Tile<DH>::load(yr, seq_row(a.dO, sq, pq, head, q0, esz), a.dO.row, qn);
+    Tile<DH>::load(xr, threadIdx.x, seq_row(a.q, sq, pq, head, q0, esz), a.q.row, qn);
+    Tile<DH>::load(yr, threadIdx.x, seq_row(a.dO, sq, pq, head, q0, esz), a.dO.row, qn);
     const int64_t num = seq_num(a.qs, sq, a.H, head, q0 + min((int)threadIdx.x % KB, qn - 1));
     lse = a.lse[num];
     delta = a.delta[num];
   };
   const auto store = [&](int buf) {
-    l.x[buf].store(xr);
-    l.y[buf].store(yr);
+    l.x[buf].store(xr, threadIdx.x);
+    l.y[buf].store(yr, threadIdx.x);
     if (threadIdx.x < KB) {  // (a row that sees nothing: exp2(-infinity - infinity) below)
       l.lse[buf][threadIdx.x] = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
       l.delta[buf][threadIdx.x] = delta;

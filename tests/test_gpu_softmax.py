@@ -76,6 +76,15 @@ def test_forward(layout, lens, H, Hk, d, dtype):
     check_forward(Q, K, V, out, lse, layout, lens)
 
 
+@pytest.mark.parametrize("H,Hk,d", [(8, 2, 128), (12, 12, 64)])
+def test_forward_many_tiles(H, Hk, d):
+    say(f"softmax forward, many tiles H={H} Hk={Hk} d={d}")
+    lens = [130] * 30 + [700, 0, 1, 64, 65, 511] + [129] * 6
+    Q, K, V, _ = make("packed", lens, H, Hk, d, torch.bfloat16, seed=3)
+    out, lse = luna.softmax_attn(Q, K, V, offsets=packed_offsets(lens))
+    check_forward(Q, K, V, out, lse, "packed", lens)
+
+
 @pytest.mark.parametrize("lens,klens,H,Hk,d,dtype", [
     ([1, 1, 1], [1, 777, 64], 8, 2, 128, "bf16"), ([1, 1], [4097, 130], 4, 4, 64, "bf16"), ([1], [300], 16, 1, 128, "bf16"),
     ([17, 17], [17, 500], 4, 1, 64, "bf16"), ([5, 5, 5], [3, 0, 70], 2, 1, 32, "bf16"), ([200, 200], [450, 90], 4, 2, 128, "bf16"),
