@@ -84,6 +84,33 @@ __device__ __forceinline__ SeqPiece seq_piece(const SeqSet& s, int slot, int pie
   return p;
 }
 
+// The same with the longest work first, where a piece's work grows with its distance from the end of its
+// sequence (late: from the start): all pieces at the largest distance, then those at the next, so that no long one
+// begins when the others end.  Up to 64 sequences, one a lane; more fill the device one after the other.
+__device__ __forceinline__ SeqPiece seq_piece_by_work(const SeqSet& s, int slot, int slots, int piece, bool late) {
+  if (s.count > kWave) return seq_piece(s, late ? slots - 1 - slot : slot, piece);
+  SeqPiece p;
+  p.seq = -1;
+  const int lane = threadIdx.x % kWave, count = (int)s.count;
+  const int mine = lane < count ? (int)(((int64_t)seq_of(s, lane).len + piece - 1) / piece) : 0;  // pieces
+  // the largest distance with more than `slot` pieces at it or beyond, from 64 guesses at a time
+  int far = 0, step = 1;
+  while (s.rows / piece >= (int64_t)step * kWave) step *= kWave;
+  for (; step > 0; step /= kWave) {
+    int beyond = 0;
+    for (int b = 0; b < count; ++b) beyond += max(0, __builtin_amdgcn_readlane(mine, b) - (far + step * lane));
+    const int most = __popcll(__ballot(beyond > slot));
+    if (most == 0) return p;
+    far += step * (most - 1);
+  }
+  for (int b = 0; b < count; ++b) slot -= max(0, __builtin_amdgcn_readlane(mine, b) - far - 1);
+  const uint64_t have = __ballot(mine > far);
+  const bool hit = mine > far && __popcll(have & (((uint64_t)1 << lane) - 1)) == slot;
+  p = seq_of(s, __builtin_ctzll(__ballot(hit)));
+  p.index = late ? far : __builtin_amdgcn_readlane(mine, p.seq) - 1 - far;
+  return p;
+}
+
 // Address of row i of a sequence and head.
 __device__ __forceinline__ char* seq_row(const SeqRows& r, const SeqPiece& p, bool packed, int head, int64_t i, int esz) {
   return r.data + (packed ? (p.first + i) * r.row + head * r.head : p.seq * r.seq + head * r.head + i * r.row) * esz;

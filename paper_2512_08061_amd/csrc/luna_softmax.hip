@@ -28,8 +28,8 @@ __global__ __launch_bounds__(256) void softmax_fwd_kernel(SoftmaxArgs a) {
   __shared__ __attribute__((aligned(16))) char raw[sizeof(Lds)];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
-  const int head = blockIdx.x % a.H, slot = gridDim.x / a.H - 1 - blockIdx.x / a.H;  // (later tiles have more keys)
-  const SeqPiece sq = seq_piece(a.qs, slot, kSoftmaxTile);
+  const int head = blockIdx.x % a.H;
+  const SeqPiece sq = seq_piece_by_work(a.qs, blockIdx.x / a.H, gridDim.x / a.H, kSoftmaxTile, true);
   if (sq.seq < 0) return;
   const SeqPiece sk = seq_of(a.ks, sq.seq);
   const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
@@ -136,8 +136,8 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxA
   SoftmaxLds32<DH, GROUPS>& l = *reinterpret_cast<SoftmaxLds32<DH, GROUPS>*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id() % 4, h = lane / 32, c = lane % 32;
   const int group = GROUPS == 1 ? 0 : wave_id() / 4, tid = threadIdx.x % 256;
-  const int head = head_of(blockIdx.x % a.H, a.H), slot = gridDim.x / a.H - 1 - blockIdx.x / a.H;
-  const SeqPiece sq = seq_piece(a.qs, slot, 128);
+  const int head = head_of(blockIdx.x % a.H, a.H);
+  const SeqPiece sq = seq_piece_by_work(a.qs, blockIdx.x / a.H, gridDim.x / a.H, 128, true);
   if (sq.seq < 0) return;
   const SeqPiece sk = seq_of(a.ks, sq.seq);
   const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;

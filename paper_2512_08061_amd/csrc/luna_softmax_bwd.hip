@@ -30,8 +30,8 @@ __global__ __launch_bounds__(256) void softmax_dq_kernel(SoftmaxArgs a) {
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
-  const int head = blockIdx.x % a.H, slot = gridDim.x / a.H - 1 - blockIdx.x / a.H;
-  const SeqPiece sq = seq_piece(a.qs, slot, kSoftmaxTile);
+  const int head = blockIdx.x % a.H;
+  const SeqPiece sq = seq_piece_by_work(a.qs, blockIdx.x / a.H, gridDim.x / a.H, kSoftmaxTile, true);
   if (sq.seq < 0) return;
   const SeqPiece sk = seq_of(a.ks, sq.seq);
   const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
@@ -113,8 +113,8 @@ __global__ __launch_bounds__(256) void softmax_dkdv_kernel(SoftmaxArgs a) {
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
-  const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;  // (earlier tiles are seen by more queries)
-  const SeqPiece sk = seq_piece(a.ks, slot, kSoftmaxTile);
+  const int hk = blockIdx.x % a.Hk;
+  const SeqPiece sk = seq_piece_by_work(a.ks, blockIdx.x / a.Hk, gridDim.x / a.Hk, kSoftmaxTile, false);
   if (sk.seq < 0) return;
   const SeqPiece sq = seq_of(a.qs, sk.seq);
   const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
@@ -233,8 +233,8 @@ __global__ __launch_bounds__(256, 2) void softmax_dq32_kernel(SoftmaxArgs a) {
   extern __shared__ __attribute__((aligned(16))) char raw[];
   SoftmaxBwdLds32<DH>& l = *reinterpret_cast<SoftmaxBwdLds32<DH>*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id(), h = lane / 32, c = lane % 32;
-  const int head = head_of(blockIdx.x % a.H, a.H), slot = gridDim.x / a.H - 1 - blockIdx.x / a.H;
-  const SeqPiece sq = seq_piece(a.qs, slot, 128);
+  const int head = head_of(blockIdx.x % a.H, a.H);
+  const SeqPiece sq = seq_piece_by_work(a.qs, blockIdx.x / a.H, gridDim.x / a.H, 128, true);
   if (sq.seq < 0) return;
   const SeqPiece sk = seq_of(a.ks, sq.seq);
   const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
@@ -348,9 +348,9 @@ __global__ __launch_bounds__(512, 2) void softmax_dkdv32_kernel(SoftmaxArgs a) {
   const int lane = threadIdx.x % kWave, wave = wave_id() % 4, h = lane / 32, c = lane % 32;
   const bool second = wave_id() >= 4;  // dP, dS, dK
   const int group = a.H / a.Hk, heads = a.parts ? a.H : a.Hk;
-  const int unit = head_of(blockIdx.x % heads, heads), slot = blockIdx.x / heads;  // (earlier tiles are seen by more queries)
+  const int unit = head_of(blockIdx.x % heads, heads);
   const int hk = a.parts ? unit / group : unit, head0 = a.parts ? unit : unit * group, each = a.parts ? 1 : group;
-  const SeqPiece sk = seq_piece(a.ks, slot, 128);
+  const SeqPiece sk = seq_piece_by_work(a.ks, blockIdx.x / heads, gridDim.x / heads, 128, false);
   if (sk.seq < 0) return;
   const SeqPiece sq = seq_of(a.qs, sk.seq);
   const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
