@@ -29,7 +29,7 @@ extern "C" {
  *   (offsets[b] + i) * row + h * head (packed sequences; seq is not read).
  * data is 16-byte aligned and every stride a multiple of 16 bytes; row is at least the
  * width and at most 2^20 elements.  head or seq may be 0 for inputs whose heads or
- * sequences share their rows.
+ * sequences share their rows.  An output overlaps no other tensor of the call.
  */
 typedef struct luna_rows {
   void* data;
@@ -48,6 +48,9 @@ typedef struct luna_rows {
  * and lens to [0, rows], so other contents give undefined results, but no access outside the
  * tensors.  1 <= count <= 65535, 0 <= rows <= 2^30
  * (2^30 rows in all where every sequence has its own).
+ * The masks of the operators weigh what they hide with zero: a NaN or an infinity in a row of a sequence
+ * may reach any row of the same sequence and (key) head, those before it too.  It reaches no
+ * other sequence or head, and what lies in rows of no sequence reaches nothing.
  */
 typedef struct luna_seqs {
   int64_t count, rows;

@@ -13,7 +13,8 @@ namespace {
 
 using luna::set_error;
 
-constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxRow = (int64_t)1 << 20, kMaxGrid = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxRow = (int64_t)1 << 20;
+constexpr int64_t kMaxGrid = ((int64_t)1 << 32) / 512 - 1;  // workgroups: a launch has fewer than 2^32 threads
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -202,6 +203,8 @@ luna_status check_softmax(luna_dtype dt, const luna_seqs* seqs, const luna_seqs*
   for (const luna_seqs* x : {seqs, keys ? keys : seqs})
     if (luna::seq_slots(set_of(x), luna::kSoftmaxLeast) * H > kMaxGrid)
       return set_error(LUNA_ERR_UNSUPPORTED, "too many tiles of sequences and heads");
+  if (luna::softmax_splits(set_of(seqs), set_of(keys ? keys : seqs), H, Hk) && seqs->count * H * seqs->rows > kMaxGrid)
+    return set_error(LUNA_ERR_UNSUPPORTED, "too many query rows");
   return LUNA_OK;
 }
 
