@@ -45,13 +45,20 @@ __global__ __launch_bounds__(256) void decay_weights_kernel(DecayWeightsArgs a) 
   if (sp.seq < 0) return;
   const bool packed = a.s.offsets != nullptr;
   const int sub = threadIdx.x % 16;
+  constexpr int E = 16 / (int)sizeof(T);
   for (int r = threadIdx.x / 16; r < 64; r += 16) {
     const int i = sp.index * 64 + r;
     if (i >= sp.len) break;
-    const T* g = reinterpret_cast<const T*>(seq_row(a.dO, sp, packed, head, i, sizeof(T)));
-    const T* o = reinterpret_cast<const T*>(seq_row(a.out, sp, packed, head, i, sizeof(T)));
+    const char* g = seq_row(a.dO, sp, packed, head, i, sizeof(T));
+    const char* o = seq_row(a.out, sp, packed, head, i, sizeof(T));
     float x = 0.0f;
-    for (int c = sub; c < a.d; c += 16) x = fmaf((float)g[c], (float)o[c], x);
+    for (int c = sub * E; c < a.d; c += 16 * E) {
+      const i32x4 gv = *reinterpret_cast<const i32x4*>(g + c * sizeof(T)), ov = *reinterpret_cast<const i32x4*>(o + c * sizeof(T));
+      const T* gt = reinterpret_cast<const T*>(&gv);
+      const T* ot = reinterpret_cast<const T*>(&ov);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x = fmaf((float)gt[e], (float)ot[e], x);
+    }
     x += __shfl_xor(x, 1);
     x += __shfl_xor(x, 2);
     x += __shfl_xor(x, 4);
