@@ -329,14 +329,19 @@ __global__ __launch_bounds__(256, 2) void softmax_dq32_kernel(SoftmaxArgs a) {
 }
 
 // Two waves share 32 keys: one forms S, P and dV, the other, a step of 64 queries behind it, dP, dS and dK from the same
-// P, which comes through LDS (rounded to bf16, lane for lane as both need it).  Either does the same two products (its
-// rows against a tile, a transposed tile against its result) with half of the operands and gradients, so that two
+// P, which comes through LDS, lane for lane as both need it: times 2^15 in fp16 (2^-12 of P, down to 2^-29; in bf16 it
+// would be a third rounding to 2^-9 of dK's terms: error 0.0030 instead of 0.0025, 1% less time).  P keeps
+// that factor until the gradients are stored.  Either wave does the same two products (its rows against a tile, a
+// transposed tile against its result) with half of the operands and gradients, so that two
 // waves fit a SIMD; one wave with all of them took 490 registers, moved half of them about and reached 20% of the matrix
 // cores' time.  With parts a workgroup takes one query head and leaves fp32 rows there, which softmax_sum_kernel adds up.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+constexpr int kKeyShift = 15;  // P times 2^15 in the key pass
+
 template <int DH>
 struct SoftmaxKeyLds {
   Tile<DH> x[3], y[3];
-  bf16x8 p[2][4][4][kWave];  // per step parity, key tile and 16 queries
+  f16x8 p[2][4][4][kWave];  // per step parity, key tile and 16 queries
   float lse[3][64], delta[3][64];
 };
 
@@ -385,7 +390,7 @@ __global__ __launch_bounds__(512, 2) void softmax_dkdv32_kernel(SoftmaxArgs a) {
     l.x[buf].store(xr, threadIdx.x);
     l.y[buf].store(yr, threadIdx.x);
     if (threadIdx.x < KB) {  // (a row that sees nothing: exp2(-infinity - infinity) below)
-      l.lse[buf][threadIdx.x] = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+      l.lse[buf][threadIdx.x] = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e - kKeyShift;
       l.delta[buf][threadIdx.x] = delta;
     }
   };
@@ -421,6 +426,7 @@ __global__ __launch_bounds__(512, 2) void softmax_dkdv32_kernel(SoftmaxArgs a) {
       };
       read(0);
       if (!second) {
+        f16x8 ph[4];
         if (q0 + shift < wlast || qn < KB || m < 128) {
 #pragma unroll
           for (int half = 0; half < 2; ++half)
@@ -436,16 +442,20 @@ __global__ __launch_bounds__(512, 2) void softmax_dkdv32_kernel(SoftmaxArgs a) {
           for (int e = 0; e < 16; e += 4) {
             const f32x4 ls = *reinterpret_cast<const f32x4*>(&l.lse[buf][32 * half + 2 * e + 4 * h]);
 #pragma unroll
-            for (int j = 0; j < 4; j += 2)
-              pf[2 * half + e / 8].set2(e % 8 + j, exp2_raw(fmaf(s[half][e + j], scale, -ls[j])),
-                                        exp2_raw(fmaf(s[half][e + j + 1], scale, -ls[j + 1])));
+            for (int j = 0; j < 4; j += 2) {
+              const float x = exp2_raw(fmaf(s[half][e + j], scale, -ls[j]));
+              const float y = exp2_raw(fmaf(s[half][e + j + 1], scale, -ls[j + 1]));
+              pf[2 * half + e / 8].set2(e % 8 + j, x, y);
+              ph[2 * half + e / 8][e % 8 + j] = (_Float16)x;
+              ph[2 * half + e / 8][e % 8 + j + 1] = (_Float16)y;
+            }
           }
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) l.p[at % 2][wave][ks][lane] = pf[ks].v;
+        for (int ks = 0; ks < 4; ++ks) l.p[at % 2][wave][ks][lane] = ph[ks];
       } else {
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
-          const bf16x8 p = l.p[at % 2][wave][ks][lane];
+          const f16x8 p = l.p[at % 2][wave][ks][lane];
           const f32x4 d0 = *reinterpret_cast<const f32x4*>(&l.delta[buf][16 * ks + 4 * h]);
           const f32x4 d1 = *reinterpret_cast<const f32x4*>(&l.delta[buf][16 * ks + 8 + 4 * h]);
 #pragma unroll
@@ -473,8 +483,9 @@ __global__ __launch_bounds__(512, 2) void softmax_dkdv32_kernel(SoftmaxArgs a) {
       for (int e = 0; e < 16; e += 4) store4(part + 32 * t + 2 * e + 4 * h, acc[t][e], acc[t][e + 1], acc[t][e + 2], acc[t][e + 3]);
     return;
   }
-  if (second) store_rows<DH>(seq_row(a.dk, sk, pk, hk, k0, esz), a.dk.row, m, i, h, acc, a.scale);
-  else store_rows<DH>(seq_row(a.dv, sk, pk, hk, k0, esz), a.dv.row, m, i, h, acc, 1.0f);
+  constexpr float unit_p = 1.0f / (1 << kKeyShift);
+  if (second) store_rows<DH>(seq_row(a.dk, sk, pk, hk, k0, esz), a.dk.row, m, i, h, acc, a.scale * unit_p);
+  else store_rows<DH>(seq_row(a.dv, sk, pk, hk, k0, esz), a.dv.row, m, i, h, acc, unit_p);
 }
 
 // dK and dV of a key head from its query heads' rows in a.parts, in order of the heads.
@@ -491,7 +502,7 @@ __global__ __launch_bounds__(256) void softmax_sum_kernel(SoftmaxArgs a) {
     f32x4 sum = zero4();
     for (int g = 0; g < group; ++g)
       sum += *reinterpret_cast<const f32x4*>(a.parts + seq_num(a.ks, sk, a.H, hk * group + g, k0 + r) * (2 * DH) + which * DH + col);
-    const float f = which ? 1.0f : a.scale;
+    const float f = (which ? 1.0f : a.scale) / (1 << kKeyShift);
     __bf16* to = reinterpret_cast<__bf16*>(seq_row(which ? a.dv : a.dk, sk, pk, hk, k0 + r, 2)) + col;
     store4(to, sum[0] * f, sum[1] * f, sum[2] * f, sum[3] * f);
   }
