@@ -39,12 +39,18 @@ namespace luna {
 template <typename T>
 constexpr int kDecayChunk = sizeof(T) == 2 ? 64 : 32;
 
+// Parts of P in the product with V: in bf16 with denominators two, P and what its rounding left (out's error on packed LUNA
+// prompts 0.0023 -> 0.0017 of its norm, 384 -> 389 us).  One elsewhere: two workgroups a compute unit would not have
+// the registers (128 features: 704 -> 787 us).
+template <typename T, int MODE, bool OUT>
+constexpr int kDecayParts = sizeof(T) == 2 && MODE == kDecayNorm && OUT ? 2 : 1;
+
 // LDS of a workgroup: the chunk's q, k, v and P rows (padded by 16 bytes), then fp32 tables.
-template <typename T, int DK, int DVW>
+template <typename T, int DK, int DVW, int PP>
 struct DecayLds {
   static constexpr int C = kDecayChunk<T>, PAD = 16 / (int)sizeof(T);
   static constexpr int PK = DK + PAD, PV = DVW + PAD, PA = C + PAD;
-  T q[C][PK], k[C][PK], v[C][PV], p[C][PA];
+  T q[C][PK], k[C][PK], v[C][PV], p[PP][C][PA];
   float pw[C + 4];                               // f^0 .. f^C
   float dec[C], kw[C], ka[C], qa[C], ow[C];      // f^(m-1-j) w_j, w_j, b_j, a_i, c_i
   float den[2][C];                               // two waves' shares of the denominators
@@ -119,7 +125,8 @@ constexpr int kDecayWaves = DK <= 64 || (DK == 128 && MODE == kDecayPlain && !EX
 
 template <typename T, int DK, int DVW, int MODE, bool OUT, bool EXACT>
 __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, MODE, EXACT>)) void decay_kernel(DecayArgs a) {
-  using Lds = DecayLds<T, DK, DVW>;
+  constexpr int PP = kDecayParts<T, MODE, OUT>;
+  using Lds = DecayLds<T, DK, DVW, PP>;
   constexpr int C = Lds::C, FT = DK / 16, KT = C / 16, KS = C / 32, NW = DVW / 16, THREADS = 64 * NW;
   constexpr int SHARE = NW >= 2 * KT ? 2 : 1;  // waves per 16 queries of P
   constexpr int esz = (int)sizeof(T);
@@ -267,7 +274,10 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, MODE, EXACT>)) void de
             acc[j] = 16 * kt + 4 * g + j <= i ? x : 0.0f;
             if (MODE == kDecayNorm) den += acc[j];
           }
-          store4(&l.p[i][16 * kt + 4 * g], acc[0], acc[1], acc[2], acc[3]);
+          store4(&l.p[0][i][16 * kt + 4 * g], acc[0], acc[1], acc[2], acc[3]);
+          if constexpr (PP == 2)
+            store4(&l.p[1][i][16 * kt + 4 * g], acc[0] - (float)(T)acc[0], acc[1] - (float)(T)acc[1],
+                   acc[2] - (float)(T)acc[2], acc[3] - (float)(T)acc[3]);
         }
         if (MODE == kDecayNorm) {
           den = sum_groups(den);
@@ -342,9 +352,12 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, MODE, EXACT>)) void de
       if (OUT) {
 #pragma unroll
         for (int qt = 2 * ks; qt < KT; ++qt) {
-          Frag<T> pf;
-          load8(pf, &l.p[16 * qt + c][32 * ks + 8 * g]);
-          mma(o[qt], vf, pf);
+#pragma unroll
+          for (int part = PP - 1; part >= 0; --part) {
+            Frag<T> pf;
+            load8(pf, &l.p[part][16 * qt + c][32 * ks + 8 * g]);
+            mma(o[qt], vf, pf);
+          }
         }
       }
       DecayScaled<T> one;  // columns 0 .. 2: the parts of the discounts (times b_j)
@@ -427,7 +440,7 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, MODE, EXACT>)) void de
 
 template <typename T, int DK, int DVW, int MODE, bool OUT, bool EXACT>
 hipError_t launch_decay_one(const DecayArgs& a, hipStream_t s) {
-  constexpr int bytes = (int)sizeof(DecayLds<T, DK, DVW>);
+  constexpr int bytes = (int)sizeof(DecayLds<T, DK, DVW, kDecayParts<T, MODE, OUT>>);
   static_assert(bytes <= 160 * 1024, "one workgroup's LDS");
   const hipError_t e = allow_lds<decay_kernel<T, DK, DVW, MODE, OUT, EXACT>>(bytes);
   if (e != hipSuccess) return e;
