@@ -119,12 +119,13 @@ struct DecayScaled<__bf16> {
 };
 
 // Waves per SIMD: two workgroups of a compute unit where the registers suffice (128 features without denominators: 546 ->
-// 487 us of the long batch's row pass; the others would spill).
-template <typename T, int DK, int MODE, bool EXACT>
-constexpr int kDecayWaves = DK <= 64 || (DK == 128 && MODE == kDecayPlain && !EXACT) ? 4 : 2;
+// 487 us of the long batch's row pass).  The others would spill (128 features and 64 columns, whose half as many waves carry
+// twice the rows in flight: 254 -> 517 us for 8 x 16 heads of 8192 tokens).
+template <typename T, int DK, int DVW, int MODE, bool EXACT>
+constexpr int kDecayWaves = DK <= 64 || (DK == 128 && DVW == 128 && MODE == kDecayPlain && !EXACT) ? 4 : 2;
 
 template <typename T, int DK, int DVW, int MODE, bool OUT, bool EXACT>
-__global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, MODE, EXACT>)) void decay_kernel(DecayArgs a) {
+__global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) void decay_kernel(DecayArgs a) {
   constexpr int PP = kDecayParts<T, MODE, OUT>;
   using Lds = DecayLds<T, DK, DVW, PP>;
   constexpr int C = Lds::C, FT = DK / 16, KT = C / 16, KS = C / 32, NW = DVW / 16, THREADS = 64 * NW;
