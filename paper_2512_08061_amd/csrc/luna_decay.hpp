@@ -48,6 +48,7 @@ constexpr int kDecayParts = sizeof(T) == 2 && MODE == kDecayNorm && OUT ? 2 : 1;
 // LDS of a workgroup: the chunk's q, k, v and P rows (padded by 16 bytes), then fp32 tables.
 template <typename T, int DK, int DVW, int PP>
 struct DecayLds {
+  static constexpr int FS = DK > 128 && DVW <= 64 ? 2 : 1;  // waves that share the features of 16 columns
   static constexpr int C = kDecayChunk<T>, PAD = 16 / (int)sizeof(T);
   static constexpr int PK = DK + PAD, PV = DVW + PAD, PA = C + PAD;
   T q[C][PK], k[C][PK], v[C][PV], p[PP][C][PA];
@@ -55,6 +56,8 @@ struct DecayLds {
   float dec[C], kw[C], ka[C], qa[C], ow[C];      // f^(m-1-j) w_j, w_j, b_j, a_i, c_i
   float den[2][C];                               // two waves' shares of the denominators
   float z[DK];
+  f32x4 o[FS > 1 ? DVW / 16 : 1][FS][C / 32][kWave];  // half of out's tiles, from one such wave to the other
+  T one[4][C];  // the parts of f^(m-1-j) w_j, times b_j in state passes, and zeros
 };
 
 // Rows of one tensor on their way from memory to LDS: C rows of width w (at most W), rows past m and columns past w as
@@ -118,6 +121,9 @@ struct DecayScaled<__bf16> {
   }
 };
 
+template <int DK, int DVW>
+constexpr int kDecayThreads = 4 * DVW * (DK > 128 && DVW <= 64 ? 2 : 1);
+
 // Waves per SIMD: two workgroups of a compute unit where the registers suffice (128 features without denominators: 546 ->
 // 487 us of the long batch's row pass).  The others would spill (128 features and 64 columns, whose half as many waves carry
 // twice the rows in flight: 254 -> 517 us for 8 x 16 heads of 8192 tokens).
@@ -125,11 +131,13 @@ template <typename T, int DK, int DVW, int MODE, bool EXACT>
 constexpr int kDecayWaves = DK <= 64 || (DK == 128 && DVW == 128 && MODE == kDecayPlain && !EXACT) ? 4 : 2;
 
 template <typename T, int DK, int DVW, int MODE, bool OUT, bool EXACT>
-__global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) void decay_kernel(DecayArgs a) {
+__global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, MODE, EXACT>)) void decay_kernel(DecayArgs a) {
   constexpr int PP = kDecayParts<T, MODE, OUT>;
   using Lds = DecayLds<T, DK, DVW, PP>;
-  constexpr int C = Lds::C, FT = DK / 16, KT = C / 16, KS = C / 32, NW = DVW / 16, THREADS = 64 * NW;
-  constexpr int SHARE = NW >= 2 * KT ? 2 : 1;  // waves per 16 queries of P
+  constexpr int C = Lds::C, FS = Lds::FS, FT = DK / 16 / FS, KT = C / 16, KS = C / 32, NW = DVW / 16;
+  constexpr int THREADS = kDecayThreads<DK, DVW>, SHARE = FS * NW >= 2 * KT ? 2 : 1;  // SHARE: waves per 16 queries of P
+  constexpr int UNROLL = DK > 128 ? 1 : 8;  // (registers)
+  static_assert(FS == 1 || MODE != kDecayAug, "za is one wave's");
   constexpr int esz = (int)sizeof(T);
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
@@ -144,7 +152,8 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) vo
   const int begin = sp.index * a.piece, end = min(sp.len, begin + a.piece);
   if (!OUT && end == sp.len) return;  // (nothing starts from the state after the last piece)
   const int col0 = slice * DVW, cols = min(DVW, a.dv - col0);
-  const int wcol = 16 * wave;  // this wave's first column of the slice
+  const int cw = wave % NW, half = FS == 1 ? 0 : wave / NW;
+  const int wcol = 16 * cw, wfeat = half * (DK / FS);  // this wave's first column of the slice and first feature
 
   const float g2 = decay_log2(a.log_decay[head]);
   for (int i = tid; i <= C; i += THREADS) l.pw[i] = exp2_raw(g2 * (float)i);
@@ -196,7 +205,7 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) vo
         for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int k = 16 * ft + 4 * g + j;
+            const int k = wfeat + 16 * ft + 4 * g + j;
             if (k < a.dk) S[ft][j] = x[k * row + col];
           }
         if (MODE == kDecayAug && g == 0) za[0] = xz[col0 + mycol];
@@ -211,7 +220,7 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) vo
       for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int k = 16 * ft + 4 * g + j;
+          const int k = wfeat + 16 * ft + 4 * g + j;
           if (k < a.dk) S1[(int64_t)k * a.dv + col0 + mycol] = S[ft][j];
         }
       if (MODE == kDecayAug && g == 0) z1[col0 + mycol] = za[0];
@@ -233,7 +242,14 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) vo
         l.ka[tid] = in ? ka : 0.0f;
         if (OUT) l.qa[tid] = in ? qa : 0.0f;
       }
-      if (MODE == kDecayNorm && !OUT) l.ka[tid] = ka;
+      if (MODE == kDecayNorm) {  // the discounts of z (times b_j), bf16: in three parts
+        const float x = l.dec[tid] * (OUT ? 1.0f : ka);
+        const T part0 = (T)x, part1 = (T)(x - (float)part0);
+        l.one[0][tid] = part0;
+        l.one[1][tid] = part1;
+        l.one[2][tid] = (T)(x - (float)part0 - (float)part1);
+        l.one[3][tid] = (T)0.0f;
+      }
       if (OUT) l.ow[tid] = ow;
     }
     if (t0 + C < end) load(t0 + C);
@@ -244,17 +260,21 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) vo
       // P: SHARE waves form the rows of a query tile, over the keys before them
       if (wave < SHARE * KT) {
         const int qt = wave / SHARE, share = wave % SHARE, i = 16 * qt + c;
+        float den = 0.0f;
+        if (MODE == kDecayNorm) {
+#pragma unroll UNROLL
+          for (int t = 0; t < DK / 32; t += SHARE) {
+            const int f = 32 * (t + share) + 8 * g;
+            Frag<T> x;
+            load8(x, &l.q[i][f]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) den = fmaf(x.get(e), l.z[f + e], den);
+          }
+          den *= l.pw[i + 1];
+        }
         Frag<T> qf[DK / 32];
 #pragma unroll
         for (int t = 0; t < DK / 32; ++t) load8(qf[t], &l.q[i][32 * t + 8 * g]);
-        float den = 0.0f;
-        if (MODE == kDecayNorm && share == 0) {
-#pragma unroll
-          for (int t = 0; t < DK / 32; ++t)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) den = fmaf(qf[t].get(e), l.z[32 * t + 8 * g + e], den);
-          den *= l.pw[i + 1];
-        }
         const float qai = MODE == kDecayAug ? l.qa[i] : 0.0f;
         for (int kt = share; kt < KT && kt <= qt + 1; kt += SHARE) {  // (a block behind the diagonal as zeros)
           f32x4 acc = zero4();
@@ -299,8 +319,8 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) vo
 #pragma unroll
         for (int qt = 0; qt < KT; ++qt) {
           Frag<T> qf;
-          load4(qf, 0, &l.q[16 * qt + c][32 * t + 4 * g]);
-          load4(qf, 4, &l.q[16 * qt + c][32 * t + 16 + 4 * g]);
+          load4(qf, 0, &l.q[16 * qt + c][wfeat + 32 * t + 4 * g]);
+          load4(qf, 4, &l.q[16 * qt + c][wfeat + 32 * t + 16 + 4 * g]);
           mma(o[qt], sf_, qf);
         }
       }
@@ -350,7 +370,7 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) vo
       load_tr4(vf, 4, &l.v[0][0], Lds::PV, 32 * ks + 8 * g + 4, wcol, lane);
       DecayScaled<T> vs;
       vs.set(vf, dec, EXACT);
-      if (OUT) {
+      if (OUT && ks % FS == half) {
 #pragma unroll
         for (int qt = 2 * ks; qt < KT; ++qt) {
 #pragma unroll
@@ -361,32 +381,16 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) vo
           }
         }
       }
-      DecayScaled<T> one;  // columns 0 .. 2: the parts of the discounts (times b_j)
-      if (MODE == kDecayNorm) {
-        if (!OUT) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) dec[e] *= l.ka[32 * ks + 8 * g + e];
-        }
-        if constexpr (sizeof(T) == 2) {
-          Split3 parts;
-          split3(parts, dec);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            one.x.p[0].v[e] = c == 0 ? parts.p[0].v[e] : c == 1 ? parts.p[1].v[e] : c == 2 ? parts.p[2].v[e] : (__bf16)0.0f;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) one.x.v[e] = c == 0 ? dec[e] : 0.0f;
-        }
-      }
+      Frag<T> one;  // columns 0 .. 2: the parts
+      if (MODE == kDecayNorm) load8(one, &l.one[min(c, 3)][32 * ks + 8 * g]);
 #pragma unroll
       for (int ft = 0; ft < FT; ++ft) {
         Frag<T> kf;
-        load_tr4(kf, 0, &l.k[0][0], Lds::PK, 32 * ks + 8 * g, 16 * ft, lane);
-        load_tr4(kf, 4, &l.k[0][0], Lds::PK, 32 * ks + 8 * g + 4, 16 * ft, lane);
+        load_tr4(kf, 0, &l.k[0][0], Lds::PK, 32 * ks + 8 * g, wfeat + 16 * ft, lane);
+        load_tr4(kf, 4, &l.k[0][0], Lds::PK, 32 * ks + 8 * g + 4, wfeat + 16 * ft, lane);
         vs.mma_into(S[ft], kf, EXACT);
-        if (MODE == kDecayNorm && ft % NW == wave) {
-          if constexpr (sizeof(T) == 2) mma(zacc[ft / NW], kf, one.x.p[0]);
-          else mma(zacc[ft / NW], kf, one.x);
+        if (MODE == kDecayNorm && ft % NW == cw) {
+          mma(zacc[ft / NW], kf, one);
         }
       }
       if (MODE == kDecayAug) {
@@ -408,8 +412,8 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) vo
           float x = zacc[i][j];
           x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xB1, 0xf, 0xf, true));
           x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4E, 0xf, 0xf, true));
-          const int f = 16 * (NW * i + wave) + 4 * g + j;
-          if (c == 0 && f < DK) l.z[f] = fmaf(l.pw[m], l.z[f], x);
+          const int f = 16 * (NW * i + cw) + 4 * g + j;
+          if (c == 0 && f < DK / FS) l.z[wfeat + f] = fmaf(l.pw[m], l.z[wfeat + f], x);
         }
       }
     }
@@ -417,18 +421,29 @@ __global__ __launch_bounds__(4 * DVW, (kDecayWaves<T, DK, DVW, MODE, EXACT>)) vo
     if (OUT) {
       const int64_t lo = rev ? sp.len - t0 - m : t0;
       const Buf b = buffer(seq_row(a.o, sp, packed, head, lo, esz) + col0 * esz, (int)(((m - 1) * a.o.row + cols) * esz));
+      constexpr int QT = KT / FS;  // query tiles that this wave writes
+      f32x4 x[QT];
 #pragma unroll
-      for (int qt = 0; qt < KT; ++qt) {
-        const int i = 16 * qt + c, r = rev ? m - 1 - i : i;
+      for (int t = 0; t < QT; ++t) x[t] = half ? o[KT - QT + t] : o[t];
+      if constexpr (FS == 2) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) l.o[cw][half][t][lane] = half ? o[t] : o[KT - QT + t];
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < QT; ++t) x[t] += l.o[cw][1 - half][t][lane];
+      }
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const int i = 16 * (QT * half + t) + c, r = rev ? m - 1 - i : i;
         float f = a.scale * l.ow[i];
         if (MODE == kDecayNorm) {
           const float den = a.scale * (SHARE == 2 ? l.den[0][i] + l.den[1][i] : l.den[0][i]);
           f = a.scale / (den + a.eps);
-          if (a.den && wave == 0 && g == 0 && slice == 0 && i < m) a.den[seq_num(a.s, sp, a.H, head, lo + r)] = den;
+          if (a.den && cw == 0 && g == 0 && slice == 0 && i < m) a.den[seq_num(a.s, sp, a.H, head, lo + r)] = den;
         }
         const int col = wcol + 4 * g;
-        buf_store4<T>(b, i < m && col < cols ? (r * (int)a.o.row + col) * esz : kPastEnd, f * o[qt][0], f * o[qt][1],
-                      f * o[qt][2], f * o[qt][3]);
+        buf_store4<T>(b, i < m && col < cols ? (r * (int)a.o.row + col) * esz : kPastEnd, f * x[t][0], f * x[t][1],
+                      f * x[t][2], f * x[t][3]);
       }
     }
   }
@@ -447,7 +462,7 @@ hipError_t launch_decay_one(const DecayArgs& a, hipStream_t s) {
   if (e != hipSuccess) return e;
   const int slices = (a.dv + DVW - 1) / DVW;
   hipLaunchKernelGGL((decay_kernel<T, DK, DVW, MODE, OUT, EXACT>), dim3((unsigned)((int64_t)a.slots * a.H * slices)),
-                     dim3(4 * DVW), bytes, s, a);
+                     dim3(kDecayThreads<DK, DVW>), bytes, s, a);
   return hipGetLastError();
 }
 
