@@ -194,14 +194,28 @@ __global__ __launch_bounds__(DH) void softmax_join_kernel(SoftmaxArgs a) {
   const int64_t slot = a.ks.offsets ? sk.first / kSplitKeys + b : b * ((a.ks.rows + kSplitKeys - 1) / kSplitKeys);
   const int64_t step = (int64_t)a.Hk * rows * (DH + 2);
   const float* part = a.parts + ((slot * a.Hk + hk) * rows + r) * (DH + 2);
+  // the pieces' maxima and factors a thread each; then their rows, whose loads do not wait for one another
+  __shared__ float w[DH], part_sum[DH];
   float most = -__builtin_inff();
-  for (int p = 0; p < pieces; ++p) most = fmaxf(most, part[p * step + DH + 1]);
+  for (int p = x; p < pieces; p += DH) most = fmaxf(most, part[p * step + DH + 1]);
+  w[x] = most;
+  __syncthreads();
+  for (int i = 0; i < min(pieces, DH); ++i) most = fmaxf(most, w[i]);
   const float base = most == -__builtin_inff() ? 0.0f : most;
   float y = 0.0f, sum = 0.0f;
-  for (int p = 0; p < pieces; ++p) {
-    const float f = exp2_raw(part[p * step + DH + 1] - base);
-    y = fmaf(f, part[p * step + x], y);
-    sum = fmaf(f, part[p * step + DH], sum);
+  for (int p0 = 0; p0 < pieces; p0 += DH) {
+    const int n = min(DH, pieces - p0);
+    __syncthreads();  // the weights before are no longer read
+    if (x < n) {
+      w[x] = exp2_raw(part[(p0 + x) * step + DH + 1] - base);
+      part_sum[x] = w[x] * part[(p0 + x) * step + DH];
+    }
+    __syncthreads();
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+      y = fmaf(w[i], part[(p0 + i) * step + x], y);
+      sum += part_sum[i];
+    }
   }
   const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
   reinterpret_cast<T*>(seq_row(a.o, sq, false, head, t, (int)sizeof(T)))[x] = (T)(y * inv);

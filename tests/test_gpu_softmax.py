@@ -105,6 +105,13 @@ def test_over_a_cache(lens, klens, H, Hk, d, dtype):
     check_forward(q, k, v, out, lse, "packed", lens, klens)
 
 
+def test_over_a_long_cache():
+    """More pieces of keys than the join has threads in a workgroup."""
+    Q, K, V, _ = make("batch", [1, 1], 4, 1, 32, torch.bfloat16, klens=[20000, 3])
+    out, lse = luna.softmax_attn(Q, K, V, k_lens=i32([20000, 3]))
+    check_forward(Q, K, V, out, lse, "batch", [1, 1], [20000, 3])
+
+
 def test_padded_batch_keeps_other_rows():
     lens, H, d = [70, 0, 129, 1], 2, 64
     Q, K, V, gen = make("batch", lens, H, 1, d, torch.bfloat16, extra=9)
