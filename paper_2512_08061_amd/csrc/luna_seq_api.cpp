@@ -103,10 +103,11 @@ struct DecayPlan {
 // Tokens per piece.  A piece is a serial chain of chunks, so cutting sequences fills the device; but pieces cost a pass
 // over the keys and values of all but each sequence's last one, and their states written, scanned and read.  Estimated
 // from: a 64-token chunk about 4 us with 128 features and d = 128 in bf16, three times as much in fp32, one workgroup
-// a compute unit (two with 64 features), and a sixth more while no second one fills its waits; 4.5 TB/s.  Measured, us a call by piece: 8 x 16
-// heads of 16384 tokens, D = d = 128, one 932, 8192 759, 4096 700, 2048 730; backward of 2 x 16 heads of 2048 tokens
-// with 256 features 256 228, 384 258, 512 236; fp32 backward of 4096 tokens in 12 heads, 64 features, 64 120, 128 107,
-// 256 123.
+// a compute unit (two with 64 features), and a sixth more while no second one fills its waits; 4.5 TB/s.  Measured, us a
+// call by piece: 8 x 16 heads of 16384 tokens, D = d = 128, one 1070, 4096 683, 2048 726, 1024 783; backward of 2 x 16
+// heads of 2048 tokens with 256 features 128 289, 256 214, 384 244, 512 222; fp32 backward of 4096 tokens in 12 heads, 64
+// features, 64 114, 128 101, 256 118.  How lengths fall into pieces is on the device and not known here (packed
+// prompts with 256 features: 384 us by the estimate's 1024, 353 by 576).
 luna_status plan_decay(luna_dtype dt, const luna_seqs& s, int64_t H, int64_t D, int64_t d, bool backward, bool normalize,
                        DecayPlan* p) {
   const int64_t per = s.rows, all = s.offsets ? s.rows : s.count * s.rows;
