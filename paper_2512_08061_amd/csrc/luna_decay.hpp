@@ -28,7 +28,13 @@
 // other waves and workgroups fill.  The scaled V is split in bf16 parts, two (2^-17 of each term), or three with S
 // returned (exact_state), so that S then has fp32 accuracy.
 // Denominators are sums of P before its rounding plus q.z with z in fp32 (LDS), so they have
-// fp32 accuracy.
+// fp32 accuracy.  With 256 features and up to 64 columns two waves share the features of 16 columns (four waves alone
+// leave a SIMD one each: 249 -> 157 us for 4 x 16 heads of 4096 tokens); with 128 columns that was no faster (384 -> 390).
+//
+// Measured: 8 x 16 heads of 16384 tokens, D = d = 128: 675 us, of which state pass 190, scan 11, row pass 480 (1.3 GB at
+// 2.7 TB/s; LDS active 68% of the time).  Six packed prompts, 16 heads, 256 features, with denominators: 346 us (80, 24,
+// 250); matrix cores 14% busy, bound by the chain of a chunk, one workgroup a compute unit, and the count of
+// pieces over the compute units.
 #pragma once
 
 #include "luna_seq.hpp"
