@@ -110,12 +110,25 @@ __global__ __launch_bounds__(256) void softmax_fwd_kernel(SoftmaxArgs a) {
   }
   sum = groups_sum(sum);
   const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;  // (NaN stays)
+  bool bad = false;
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      o[t][j] *= inv;
+      bad |= not_finite(o[t][j]);
+    }
+  uint64_t rows = __ballot(bad && i < m);
+  rows = (rows | rows >> 32) & 0xffffffff;
+  rows = (rows | rows >> 16) & 0xffff;
+  const bool good = i < m && !(rows >> c & 1);
   const Buf b = buffer(seq_row(a.o, sq, pq, head, q0, esz), (int)(((m - 1) * a.o.row + DH) * esz));
 #pragma unroll
   for (int t = 0; t < CT; ++t)
-    buf_store4<T>(b, i < m ? (i * (int)a.o.row + 16 * t + 4 * g) * esz : kPastEnd, o[t][0] * inv, o[t][1] * inv,
-                  o[t][2] * inv, o[t][3] * inv);
-  if (a.lse && g == 0 && i < m) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (top + log2f(sum)) * kLn2;
+    buf_store4<T>(b, good ? (i * (int)a.o.row + 16 * t + 4 * g) * esz : kPastEnd, o[t][0], o[t][1], o[t][2],
+                  o[t][3]);
+  if (a.lse && g == 0 && good) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (top + log2f(sum)) * kLn2;
+  for (; rows; rows &= rows - 1) softmax_row<T, DH, kWave>(a, sq, sk, head, q0 + 16 * wave + __builtin_ctzll(rows));
 }
 
 // bf16 with d = 64 and 128: 32 x 32 x 16 products, a wave with 32 queries of a workgroup's 128, keys in blocks of 64.
@@ -285,14 +298,26 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxA
       for (int e = 0; e < 16; ++e) o[t][e] = fmaf(o[t][e], f, g * rows[((t * 4 + e / 4) * 4 + wave) * kWave + lane][e % 4]);
   }
   const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;  // (NaN stays)
+  bool bad = false;
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      o[t][e] *= inv;
+      bad |= not_finite(o[t][e]);
+    }
+  uint64_t rows = __ballot(bad && i < m);
+  rows = (rows | rows >> 32) & 0xffffffff;
+  const bool good = i < m && !(rows >> c & 1);
   const Buf b = buffer(seq_row(a.o, sq, pq, head, q0, esz), (int)(((m - 1) * a.o.row + DH) * esz));
 #pragma unroll
   for (int t = 0; t < CT; ++t)
 #pragma unroll
     for (int e = 0; e < 16; e += 4)
-      buf_store4<__bf16>(b, i < m ? (i * (int)a.o.row + 32 * t + 2 * e + 4 * h) * esz : kPastEnd, o[t][e] * inv, o[t][e + 1] * inv,
-                         o[t][e + 2] * inv, o[t][e + 3] * inv);
-  if (a.lse && h == 0 && i < m) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (base + log2f(sum)) * kLn2;
+      buf_store4<__bf16>(b, good ? (i * (int)a.o.row + 32 * t + 2 * e + 4 * h) * esz : kPastEnd, o[t][e], o[t][e + 1], o[t][e + 2],
+                         o[t][e + 3]);
+  if (a.lse && h == 0 && good) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (base + log2f(sum)) * kLn2;
+  for (; rows; rows &= rows - 1) softmax_row<__bf16, DH, kWave>(a, sq, sk, head, q0 + 32 * wave + __builtin_ctzll(rows));
 }
 
 template <int DH, int GROUPS>

@@ -119,4 +119,61 @@ constexpr int kSoftmaxTile = 64;  // query rows (key rows) of a workgroup
 template <typename T>
 constexpr int kSoftmaxStep = sizeof(T) == 2 ? 64 : 32;
 
+// One query row by itself, key by key in fp32, by LANES lanes of a wave.  For rows whose result is not finite: in a tile's
+// product with V a hidden key weighs 0, and 0 times an infinity or a NaN of its values is NaN.  So a row has what
+// the keys that it sees give it, whatever lies behind them, and tiles of finite values pay one test of their results.
+template <typename T, int DH, int LANES>
+__device__ __forceinline__ void softmax_row(const SoftmaxArgs& a, const SeqPiece& sq, const SeqPiece& sk, int head, int i) {
+  constexpr int PER = (DH + LANES - 1) / LANES, esz = (int)sizeof(T);
+  const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
+  const int lane = threadIdx.x % LANES, hk = head / (a.H / a.Hk), last = min(sk.len - 1, i + sk.len - sq.len);
+  const T* q = reinterpret_cast<const T*>(seq_row(a.q, sq, pq, head, i, esz));
+  float top = -__builtin_inff(), sum = 0.0f, acc[PER];
+#pragma unroll
+  for (int c = 0; c < PER; ++c) acc[c] = 0.0f;
+#pragma unroll 1
+  for (int k0 = 0; k0 <= last; k0 += LANES) {
+    const int n = min(LANES, last - k0 + 1);
+    const T* k = reinterpret_cast<const T*>(seq_row(a.k, sk, pk, hk, k0 + min(lane, n - 1), esz));
+    float s = 0.0f;
+#pragma unroll 4
+    for (int c = 0; c < DH; c += 8) {
+      Frag<T> qf, kf;
+      load8(qf, q + c);
+      load8(kf, k + c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf(qf.get(e), kf.get(e), s);
+    }
+    s = lane < n ? s * (a.scale * kLog2e) : -__builtin_inff();
+    float most = fmaxf(top, s);
+#pragma unroll
+    for (int x = LANES / 2; x > 0; x /= 2) most = fmaxf(most, __shfl_xor(most, x));
+    const float base = most == -__builtin_inff() ? 0.0f : most, f = exp2_raw(top - base), p = exp2_raw(s - base);
+    top = most;
+    sum = fmaf(sum, f, p);
+#pragma unroll
+    for (int c = 0; c < PER; ++c) acc[c] *= f;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) {
+      const T* v = reinterpret_cast<const T*>(seq_row(a.v, sk, pk, hk, k0 + j, esz));
+      const float pj = __shfl(p, j);
+#pragma unroll
+      for (int c = 0; c < PER; ++c) acc[c] = fmaf(pj, (float)v[min(lane + LANES * c, DH - 1)], acc[c]);
+    }
+    bool lost = isnan(sum);
+#pragma unroll
+    for (int c = 0; c < PER; ++c) lost &= isnan(acc[c]);
+    if (__all(lost)) break;  // nothing but NaN is left of the row
+  }
+#pragma unroll
+  for (int x = LANES / 2; x > 0; x /= 2) sum += __shfl_xor(sum, x);
+  const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
+  T* o = reinterpret_cast<T*>(seq_row(a.o, sq, pq, head, i, esz));
+#pragma unroll
+  for (int c = 0; c < PER; ++c)
+    if (lane + LANES * c < DH) o[lane + LANES * c] = (T)(acc[c] * inv);
+  if (a.lse && lane == 0) a.lse[seq_num(a.qs, sq, a.H, head, i)] = (top + log2f(sum)) * kLn2;
+}
+__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) < __builtin_inff()); }
+
 }  // namespace luna

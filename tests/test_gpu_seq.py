@@ -160,3 +160,41 @@ def test_what_is_not_finite_stays_in_its_sequence(dtype, bad):
     assert torch.equal(gS[1, :2], wS[1, :2])
     assert torch.equal(glast[first:first + 2], wlast[first:first + 2])
     assert torch.equal(glast[first + 3:first + 7], wlast[first + 3:first + 7])
+
+
+@pytest.mark.parametrize("H,Hk,d,dtype,lens,m", [(4, 2, 128, "bf16", [300, 1, 129], 0), (8, 8, 64, "bf16", [130] * 40 + [450], 0),
+                                                 (2, 1, 32, "bf16", [200], 0), (2, 1, 64, "f32", [150, 70], 0),
+                                                 (4, 2, 128, "bf16", [700, 20, 90], 9), (2, 2, 32, "f32", [600, 5, 33], 5)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_later_tokens_do_not_reach_earlier_rows(H, Hk, d, dtype, lens, m, bad):
+    """Keys and values that are not finite from one token on: the rows before it are what they are without them (up to
+    the rounding that either way of forming a row has), those that see NaN are NaN."""
+    say(f"later tokens: H={H} d={d} {dtype} {lens} m={m} {bad}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator(device=device()).manual_seed(7)
+    n = max(lens)
+    qlens = [min(m, x) for x in lens] if m else lens
+    K, V = (rand((len(lens), Hk, n, d), dt, gen) for _ in range(2))
+    Q = rand((len(lens), H, m or n, d), dt, gen)
+    opt = {"lens": torch.tensor(qlens, dtype=torch.int32, device=device())}
+    if m:
+        opt["k_lens"] = torch.tensor(lens, dtype=torch.int32, device=device())
+    want, wl = luna.softmax_attn(Q, K, V, **opt)
+    K2, V2 = K.clone(), V.clone()
+    first = [max(x - (m // 2 + 1 if m else x // 3), 0) for x in lens]
+    for i, a in enumerate(first):
+        V2[i, :, a:, ::3] = bad
+        K2[i, :, a + 1:] = math.nan
+    out, lse = luna.softmax_attn(Q, K2, V2, **opt)
+    u = unit(dt) if dt == torch.bfloat16 else 0.0
+    for i, a in enumerate(first):
+        rows = max(qlens[i] - (lens[i] - a), 0)  # that see none of it
+        q, k, v = Q[i, :, :rows].double(), K[i, :, :a].double(), V[i, :, :a].double()
+        ref, rlse, _, size, _ = softmax_ref(q, k, v, d ** -0.5, H // Hk)
+        most = d ** -0.5 * (q.abs().amax((0, 1)) * k.abs().amax((0, 1))).sum().item() if rows and a else 0.0
+        score, sums = (d + 8) * U32 * most, (lens[i] + 16) * U32
+        assert_within(out[i, :, :rows], ref, (u + 2 * score + 2 * sums) * size + u * ref.abs() + 1e-30, f"out[{i}]")
+        assert_within(lse[i, :, :rows], rlse, score + sums + 4 * U32 * rlse.abs() + 1e-30, f"lse[{i}]")
+        assert torch.isnan(out[i, :, rows + 1:qlens[i]].float()).all(), "rows that see a NaN key"
+        if rows < qlens[i]:  # sees the first bad values, through finite keys
+            assert not torch.isfinite(out[i, :, rows, ::3].float()).any()
