@@ -48,9 +48,11 @@ typedef struct luna_rows {
  * and lens to [0, rows], so other contents give undefined results, but no access outside the
  * tensors.  1 <= count <= 65535, 0 <= rows <= 2^30
  * (2^30 rows in all where every sequence has its own).
- * The masks of the operators weigh what they hide with zero: a NaN or an infinity in a row of a sequence
- * may reach any row of the same sequence and (key) head, those before it too.  It reaches no
- * other sequence or head, and what lies in rows of no sequence reaches nothing.
+ * NaN and infinities.  In the forward calls what is not finite in a row's query, or in the keys and
+ * values of tokens that the row sees, reaches that row alone: nothing comes from later tokens, other sequences or
+ * other (key) heads, or from rows of no sequence.  In luna_decay_fwd a value that is not finite makes its column
+ * NaN from its token on (in out, and in the state).  Gradients are defined for finite inputs: one that is not may reach every
+ * gradient row of its own sequence and (key) head, and no other.
  */
 typedef struct luna_seqs {
   int64_t count, rows;
@@ -94,8 +96,8 @@ size_t luna_seq_workspace_bytes(int32_t op, luna_dtype dtype, const luna_seqs* s
  * den (normalize 1, may be NULL): denominators per row, without eps, which the backward
  * pass takes.
  * Precision: LUNA_F32 computes in fp32.  LUNA_BF16 takes products of the bf16 operands with fp32
- * accumulation; the weights of a chunk of 64 tokens and the state are rounded to bf16 as
- * operands of the products that form out, whose sums are fp32.  The state that the call
+ * accumulation; the weights of a chunk of 64 tokens (in two parts with normalize 1) and the state are
+ * rounded to bf16 as operands of the products that form out, whose sums are fp32.  The state that the call
  * returns and den have fp32 accuracy for both types.
  */
 luna_status luna_decay_fwd(const luna_rows* Q, const luna_rows* K, const luna_rows* V, luna_dtype dtype,

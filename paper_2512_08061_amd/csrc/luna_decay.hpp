@@ -27,6 +27,8 @@
 // columns), so that up to four share a SIMD: a chunk is a chain of dependent steps with three barriers, whose waits
 // other waves and workgroups fill.  The scaled V is split in bf16 parts, two (2^-17 of each term), or three with S
 // returned (exact_state), so that S then has fp32 accuracy.
+// A hidden token weighs 0 in the product with V, and 0 times an infinity or NaN of its value would reach the rows before
+// it: in the forward pass such values enter as zeros, and from their token on the column is NaN (3% of the time).
 // Denominators are sums of P before its rounding plus q.z with z in fp32 (LDS), so they have
 // fp32 accuracy.  With 256 features and up to 64 columns two waves share the features of 16 columns (four waves alone
 // leave a SIMD one each: 249 -> 157 us for 4 x 16 heads of 4096 tokens); with 128 columns that was no faster (384 -> 390).
@@ -62,6 +64,7 @@ struct DecayLds {
   float dec[C], kw[C], ka[C], qa[C], ow[C];      // f^(m-1-j) w_j, w_j, b_j, a_i, c_i
   float den[2][C];                               // two waves' shares of the denominators
   float z[DK];
+  int since[DVW];  // per column: the first token with a value that is not finite
   f32x4 o[FS > 1 ? DVW / 16 : 1][FS][C / 32][kWave];  // half of out's tiles, from one such wave to the other
   T one[4][C];  // the parts of f^(m-1-j) w_j, times b_j in state passes, and zeros
 };
@@ -87,6 +90,30 @@ struct DecayRows {
     for (int i = 0; i < N; ++i) {
       const int idx = threadIdx.x + THREADS * i, r = idx / PER, c = (idx % PER) * E;
       if (N * THREADS == C * PER || r < C) *reinterpret_cast<i32x4*>(&dst[r * P + c]) = x[i];
+    }
+  }
+  // Infinities and NaN as zeros; since[column]: the first token, t0 + row, that had one.
+  __device__ __forceinline__ void clean(int* since, int t0) {
+    constexpr uint32_t ALL = sizeof(T) == 2 ? 0x7fff7fff : 0x7fffffff, ONE = sizeof(T) == 2 ? 0x00800080 : 0x00800000;
+    constexpr uint32_t TOP = sizeof(T) == 2 ? 0x80008000 : 0x80000000;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any |= ((uint32_t)x[i][e] & ALL) + ONE;  // (an exponent of ones carries into the sign's place)
+    if (!(any & TOP)) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int idx = threadIdx.x + THREADS * i, r = idx / PER, c = (idx % PER) * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int word = e * (int)sizeof(T) / 4, shift = sizeof(T) == 2 ? 16 * (e % 2) : 0;
+        const uint32_t part = sizeof(T) == 2 ? 0xffffu << shift : 0xffffffffu;
+        if ((((uint32_t)x[i][word] & ALL) + ONE) & TOP & part) {
+          x[i][word] &= (int)~part;
+          atomicMin(&since[c + e], t0 + r);
+        }
+      }
     }
   }
 };
@@ -163,6 +190,8 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
 
   const float g2 = decay_log2(a.log_decay[head]);
   for (int i = tid; i <= C; i += THREADS) l.pw[i] = exp2_raw(g2 * (float)i);
+  constexpr int kNever = 1 << 30;  // (behind any token)
+  for (int i = tid; i < DVW; i += THREADS) l.since[i] = kNever;
 
   // a chunk's rows, and thread tid's numbers of row tid, a chunk ahead
   DecayRows<T, C, DK, Lds::PK, THREADS> qr, kr;
@@ -222,14 +251,15 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
   }
   const auto write_state = [&](float* S1, float* z1) {
     if (mycol < cols) {
+      const bool lost = l.since[mycol] != kNever;
 #pragma unroll
       for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int k = wfeat + 16 * ft + 4 * g + j;
-          if (k < a.dk) S1[(int64_t)k * a.dv + col0 + mycol] = S[ft][j];
+          if (k < a.dk) S1[(int64_t)k * a.dv + col0 + mycol] = lost ? __builtin_nanf("") : S[ft][j];
         }
-      if (MODE == kDecayAug && g == 0) z1[col0 + mycol] = za[0];
+      if (MODE == kDecayAug && g == 0) z1[col0 + mycol] = lost ? __builtin_nanf("") : za[0];
     }
     if (MODE == kDecayNorm && slice == 0)
       for (int k = tid; k < a.dk; k += THREADS) z1[k] = l.z[k];
@@ -239,6 +269,7 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
     __syncthreads();  // the chunk before is no longer read (at first: f^i are written)
     if (OUT) qr.store(&l.q[0][0]);
     kr.store(&l.k[0][0]);
+    if (MODE != kDecayAug && a.guard) vr.clean(l.since, t0);
     vr.store(&l.v[0][0]);
     if (tid < C) {
       const bool in = tid < m;
@@ -395,8 +426,15 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
         load_tr4(kf, 0, &l.k[0][0], Lds::PK, 32 * ks + 8 * g, wfeat + 16 * ft, lane);
         load_tr4(kf, 4, &l.k[0][0], Lds::PK, 32 * ks + 8 * g + 4, wfeat + 16 * ft, lane);
         vs.mma_into(S[ft], kf, EXACT);
-        if (MODE == kDecayNorm && ft % NW == cw) {
-          mma(zacc[ft / NW], kf, one);
+      }
+      if (MODE == kDecayNorm) {  // (read again, so that no wave's products stand behind a branch)
+#pragma unroll
+        for (int i = 0; i < ZT; ++i) {
+          const int f = wfeat + 16 * min(NW * i + cw, FT - 1);
+          Frag<T> kf;
+          load_tr4(kf, 0, &l.k[0][0], Lds::PK, 32 * ks + 8 * g, f, lane);
+          load_tr4(kf, 4, &l.k[0][0], Lds::PK, 32 * ks + 8 * g + 4, f, lane);
+          mma(zacc[i], kf, one);
         }
       }
       if (MODE == kDecayAug) {
@@ -428,6 +466,7 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
       const int64_t lo = rev ? sp.len - t0 - m : t0;
       const Buf b = buffer(seq_row(a.o, sp, packed, head, lo, esz) + col0 * esz, (int)(((m - 1) * a.o.row + cols) * esz));
       constexpr int QT = KT / FS;  // query tiles that this wave writes
+      const i32x4 since = *reinterpret_cast<const i32x4*>(&l.since[wcol + 4 * g]);
       f32x4 x[QT];
 #pragma unroll
       for (int t = 0; t < QT; ++t) x[t] = half ? o[KT - QT + t] : o[t];
@@ -448,8 +487,9 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
           if (a.den && cw == 0 && g == 0 && slice == 0 && i < m) a.den[seq_num(a.s, sp, a.H, head, lo + r)] = den;
         }
         const int col = wcol + 4 * g;
-        buf_store4<T>(b, i < m && col < cols ? (r * (int)a.o.row + col) * esz : kPastEnd, f * x[t][0], f * x[t][1],
-                      f * x[t][2], f * x[t][3]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[t][e] = MODE != kDecayAug && t0 + i >= since[e] ? __builtin_nanf("") : f * x[t][e];
+        buf_store4<T>(b, i < m && col < cols ? (r * (int)a.o.row + col) * esz : kPastEnd, x[t][0], x[t][1], x[t][2], x[t][3]);
       }
     }
   }

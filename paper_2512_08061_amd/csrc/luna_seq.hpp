@@ -151,6 +151,7 @@ struct DecayArgs {
   int exact_state;         // the state to fp32 accuracy (it is returned)
   float* states;           // [slots][H][decay_state_floats]: state before each piece; null: one piece per sequence
   int transposed;          // states: of k and v exchanged
+  int guard;               // values that are not finite reach no earlier token
   float* S;                // [count][H][dk][dv] and z [count][H][dk], in and out, or null
   float* z;
   float* den;              // per row, out (kDecayNorm), or null

@@ -301,6 +301,7 @@ luna_status luna_decay_fwd(const luna_rows* Q, const luna_rows* K, const luna_ro
   a.S = S;
   a.z = z;
   a.exact_state = S != nullptr;
+  a.guard = 1;
   a.den = den;
   a.scale = scale;
   a.eps = eps;

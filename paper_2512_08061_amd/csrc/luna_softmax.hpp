@@ -153,13 +153,15 @@ __device__ __forceinline__ void softmax_row(const SoftmaxArgs& a, const SeqPiece
     sum = fmaf(sum, f, p);
 #pragma unroll
     for (int c = 0; c < PER; ++c) acc[c] *= f;
-#pragma unroll 8
-    for (int j = 0; j < n; ++j) {
-      const T* v = reinterpret_cast<const T*>(seq_row(a.v, sk, pk, hk, k0 + j, esz));
-      const float pj = __shfl(p, j);
+#pragma unroll 1
+    for (int j0 = 0; j0 < n; j0 += 8)
 #pragma unroll
-      for (int c = 0; c < PER; ++c) acc[c] = fmaf(pj, (float)v[min(lane + LANES * c, DH - 1)], acc[c]);
-    }
+      for (int j = 0; j < 8; ++j) {  // (behind the last key: the last one again, times 0)
+        const T* v = reinterpret_cast<const T*>(seq_row(a.v, sk, pk, hk, k0 + min(j0 + j, n - 1), esz));
+        const float pj = __shfl(p, j0 + j);
+#pragma unroll
+        for (int c = 0; c < PER; ++c) acc[c] = fmaf(pj, (float)v[min(lane + LANES * c, DH - 1)], acc[c]);
+      }
     bool lost = isnan(sum);
 #pragma unroll
     for (int c = 0; c < PER; ++c) lost &= isnan(acc[c]);

@@ -198,3 +198,45 @@ def test_later_tokens_do_not_reach_earlier_rows(H, Hk, d, dtype, lens, m, bad):
         assert torch.isnan(out[i, :, rows + 1:qlens[i]].float()).all(), "rows that see a NaN key"
         if rows < qlens[i]:  # sees the first bad values, through finite keys
             assert not torch.isfinite(out[i, :, rows, ::3].float()).any()
+
+
+@pytest.mark.parametrize("H,D,d,dtype,norm,lens", [(2, 128, 128, "bf16", False, [300, 65]), (2, 256, 128, "bf16", True, [200, 700]),
+                                                   (3, 256, 64, "bf16", True, [130]), (2, 64, 32, "bf16", False, [90]),
+                                                   (2, 64, 64, "f32", True, [100, 33]), (1, 256, 64, "f32", False, [75])])
+@pytest.mark.parametrize("bad", [math.nan, -math.inf])
+def test_later_tokens_do_not_reach_earlier_rows_of_linear_attention(H, D, d, dtype, norm, lens, bad):
+    """Values that are not finite from one token on (in some columns), later a key: rows before, and columns without, are as
+    without them; the others are NaN, and so is the state."""
+    say(f"later tokens, decay: H={H} D={D} d={d} {dtype} {norm} {lens} {bad}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator(device=device()).manual_seed(8)
+    B, n, g = len(lens), max(lens), decays(H)
+    Q, K = (rand((B, H, n, D), dt, gen, True) for _ in range(2))
+    V = rand((B, H, n, d), dt, gen)
+    opt = {"lens": torch.tensor(lens, dtype=torch.int32, device=device()), "normalize": norm, "eps": EPS}
+
+    def call(k, v):
+        S = torch.zeros((B, H, D, d), device=device())
+        z = torch.zeros((B, H, D), device=device()) if norm else None
+        return luna.decay_attn(Q, k, v, g, S=S, z=z, **opt) + (S, z)
+
+    want, wden, wS, wz = call(K, V)
+    V2, K2 = V.clone(), K.clone()
+    first, key = [x // 3 for x in lens], [x - 3 for x in lens]
+    for i in range(B):
+        V2[i, :, first[i]:, 1::4] = bad
+    out, den, S, z = call(K, V2)
+    for i in range(B):
+        a, m = first[i], lens[i]
+        assert torch.equal(out[i, :, :a], want[i, :, :a]), "rows before"
+        for c in (0, 2, 3):
+            assert torch.equal(out[i, :, a:m, c::4], want[i, :, a:m, c::4]), "columns without"
+        assert torch.isnan(out[i, :, a:m, 1::4].float()).all()
+        assert torch.isnan(S[i, :, :, 1::4]).all() and torch.equal(S[i, :, :, ::4], wS[i, :, :, ::4])
+        if norm:
+            assert torch.equal(den[i, :, :m], wden[i, :, :m]) and torch.equal(z, wz)
+        K2[i, :, key[i], 5] = math.nan
+    out, _, S, _ = call(K2, V)
+    for i in range(B):
+        assert torch.equal(out[i, :, :key[i]], want[i, :, :key[i]]), "rows before the key"
+        assert torch.isnan(out[i, :, key[i]:lens[i]].float()).all() and torch.isnan(S[i, :, 5]).all()
