@@ -33,9 +33,9 @@
 // fp32 accuracy.  With 256 features and up to 64 columns two waves share the features of 16 columns (four waves alone
 // leave a SIMD one each: 249 -> 157 us for 4 x 16 heads of 4096 tokens); with 128 columns that was no faster (384 -> 390).
 //
-// Measured: 8 x 16 heads of 16384 tokens, D = d = 128: 675 us, of which state pass 190, scan 11, row pass 480 (1.3 GB at
-// 2.7 TB/s; LDS active 68% of the time).  Six packed prompts, 16 heads, 256 features, with denominators: 346 us (80, 24,
-// 250); matrix cores 14% busy, bound by the chain of a chunk, one workgroup a compute unit, and the count of
+// Measured: 8 x 16 heads of 16384 tokens, D = d = 128: 706 us, of which state pass 190, scan 11, row pass 500 (1.3 GB at
+// 2.6 TB/s; LDS active 68% of the time).  Six packed prompts, 16 heads, 256 features, with denominators: 342 us (78, 23,
+// 244); matrix cores 14% busy, bound by the chain of a chunk, one workgroup a compute unit, and the count of
 // pieces over the compute units.
 #pragma once
 
@@ -48,7 +48,7 @@ template <typename T>
 constexpr int kDecayChunk = sizeof(T) == 2 ? 64 : 32;
 
 // Parts of P in the product with V: in bf16 with denominators two, P and what its rounding left (out's error on packed LUNA
-// prompts 0.0023 -> 0.0017 of its norm, 384 -> 389 us).  One elsewhere: two workgroups a compute unit would not have
+// prompts 0.0023 -> 0.0017 of its norm, 385 -> 391 us).  One elsewhere: two workgroups a compute unit would not have
 // the registers (128 features: 704 -> 787 us).
 template <typename T, int MODE, bool OUT>
 constexpr int kDecayParts = sizeof(T) == 2 && MODE == kDecayNorm && OUT ? 2 : 1;
