@@ -240,3 +240,55 @@ def test_later_tokens_do_not_reach_earlier_rows_of_linear_attention(H, D, d, dty
     for i in range(B):
         assert torch.equal(out[i, :, :key[i]], want[i, :, :key[i]]), "rows before the key"
         assert torch.isnan(out[i, :, key[i]:lens[i]].float()).all() and torch.isnan(S[i, :, 5]).all()
+
+
+def test_more_sequences_than_lanes():
+    """Packed sequences beyond 64, empty ones among them, in every pass."""
+    lens = [(7 * i) % 5 if i % 3 else (13 * i) % 140 for i in range(150)]
+    H, Hk, d = 4, 2, 64
+    gen = torch.Generator(device=device()).manual_seed(11)
+    T, off, g = sum(lens), packed_offsets(lens), decays(H)
+    Q, dO, K1, V1 = (rand((T, H, d), torch.bfloat16, gen) for _ in range(4))
+    K2, V2 = (rand((T, Hk, d), torch.bfloat16, gen) for _ in range(2))
+    out, lse = luna.softmax_attn(Q, K2, V2, offsets=off)
+    check_softmax(Q, K2, V2, out, lse, "packed", lens)
+    check_backward(Q, K2, V2, dO, luna.softmax_attn_bwd(Q, K2, V2, out, lse, dO, offsets=off), "packed", lens)
+    S = torch.zeros((len(lens), H, d, d), device=device())
+    a, _ = luna.decay_attn(Q, K1, V1, g, S=S, offsets=off)
+    check_decay(Q, K1, V1, g, a, None, "packed", lens, False, 1.0, S=S)
+    u, grads = unit(torch.bfloat16), luna.decay_attn_bwd(Q, K1, V1, dO, g, offsets=off)
+    for i, n in enumerate(lens):
+        refs, sizes = decay_grads(*(cut(t, "packed", lens, i) for t in (Q, K1, V1, dO)), g)
+        for got, ref, size, name in zip(grads, refs, sizes, ("dQ", "dK", "dV")):
+            bound = (5 * u + (2 * n + 2 * d + 32) * U32) * size + u * ref.abs() + 1e-30
+            assert_within(cut(got, "packed", lens, i), ref, bound, f"{name}[{i}]")
+
+
+def test_offsets_beyond_32_bits():
+    """Rows 2^20 elements apart and sequences more than 2^31, so that addresses pass 2^32 bytes within and between sequences."""
+    H, d, n, row, seq = 2, 64, 2100, 1 << 20, 2101 << 20
+    gen = torch.Generator(device=device()).manual_seed(12)
+    store = torch.empty(2 * seq + 1024, dtype=torch.bfloat16, device=device())
+    far = lambda at: store.as_strided((2, H, n, d), (seq, d, row, 1), at)  # noqa: E731
+    Q, K, V, dO = (rand((2, H, n, d), torch.bfloat16, gen) for _ in range(4))
+    Kf, Vf, out = far(0), far(H * d), far(2 * H * d)
+    Kf.copy_(K)
+    Vf.copy_(V)
+    g = decays(H)
+    say("offsets beyond 32 bits: store filled")
+    luna.decay_attn(Q, Kf, Vf, g, out=out)
+    want, _ = luna.decay_attn(Q, K, V, g)
+    assert torch.equal(out, want)
+    want, wl = luna.softmax_attn(Q, K, V)
+    _, lse = luna.softmax_attn(Q, Kf, Vf, out=out)
+    assert torch.equal(out, want) and torch.equal(lse, wl)
+    lens = torch.tensor([n, n - 3], dtype=torch.int32, device=device())
+    for m in (1, 5):
+        a, _ = luna.softmax_attn(Q[:, :, :m], Kf, Vf, k_lens=lens)
+        b, _ = luna.softmax_attn(Q[:, :, :m], K, V, k_lens=lens)
+        assert torch.equal(a, b)
+    grads = [far(i * H * d) for i in range(3, 6)]
+    luna.softmax_attn_bwd(Q, Kf, Vf, want, wl, dO, grads=grads)
+    assert all(torch.equal(a, b) for a, b in zip(grads, luna.softmax_attn_bwd(Q, K, V, want, wl, dO)))
+    luna.decay_attn_bwd(Q, Kf, Vf, dO, g, grads=grads)
+    assert all(torch.equal(a, b) for a, b in zip(grads, luna.decay_attn_bwd(Q, K, V, dO, g)))
