@@ -121,13 +121,14 @@ __global__ __launch_bounds__(256) void softmax_fwd_kernel(SoftmaxArgs a) {
   uint64_t rows = __ballot(bad && i < m);
   rows = (rows | rows >> 32) & 0xffffffff;
   rows = (rows | rows >> 16) & 0xffff;
+  if (rows && !softmax_odd_values<T, DH, kWave>(a, sk, hk, q0 + 16 * wave + shift + 1, kend)) rows = 0;
   const bool good = i < m && !(rows >> c & 1);
   const Buf b = buffer(seq_row(a.o, sq, pq, head, q0, esz), (int)(((m - 1) * a.o.row + DH) * esz));
 #pragma unroll
   for (int t = 0; t < CT; ++t)
     buf_store4<T>(b, good ? (i * (int)a.o.row + 16 * t + 4 * g) * esz : kPastEnd, o[t][0], o[t][1], o[t][2],
                   o[t][3]);
-  if (a.lse && g == 0 && good) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (top + log2f(sum)) * kLn2;
+  if (a.lse && g == 0 && i < m) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (top + log2f(sum)) * kLn2;
   for (; rows; rows &= rows - 1) softmax_row<T, DH, kWave>(a, sq, sk, head, q0 + 16 * wave + __builtin_ctzll(rows));
 }
 
@@ -308,6 +309,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxA
     }
   uint64_t rows = __ballot(bad && i < m);
   rows = (rows | rows >> 32) & 0xffffffff;
+  if (rows && !softmax_odd_values<__bf16, DH, kWave>(a, sk, hk, wfirst + 1, kend)) rows = 0;
   const bool good = i < m && !(rows >> c & 1);
   const Buf b = buffer(seq_row(a.o, sq, pq, head, q0, esz), (int)(((m - 1) * a.o.row + DH) * esz));
 #pragma unroll
@@ -316,7 +318,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxA
     for (int e = 0; e < 16; e += 4)
       buf_store4<__bf16>(b, good ? (i * (int)a.o.row + 32 * t + 2 * e + 4 * h) * esz : kPastEnd, o[t][e], o[t][e + 1], o[t][e + 2],
                          o[t][e + 3]);
-  if (a.lse && h == 0 && good) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (base + log2f(sum)) * kLn2;
+  if (a.lse && h == 0 && i < m) a.lse[seq_num(a.qs, sq, a.H, head, q0 + i)] = (base + log2f(sum)) * kLn2;
   for (; rows; rows &= rows - 1) softmax_row<__bf16, DH, kWave>(a, sq, sk, head, q0 + 32 * wave + __builtin_ctzll(rows));
 }
 

@@ -119,9 +119,32 @@ constexpr int kSoftmaxTile = 64;  // query rows (key rows) of a workgroup
 template <typename T>
 constexpr int kSoftmaxStep = sizeof(T) == 2 ? 64 : 32;
 
-// One query row by itself, key by key in fp32, by LANES lanes of a wave.  For rows whose result is not finite: in a tile's
-// product with V a hidden key weighs 0, and 0 times an infinity or a NaN of its values is NaN.  So a row has what
-// the keys that it sees give it, whatever lies behind them, and tiles of finite values pay one test of their results.
+__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) < __builtin_inff()); }
+
+// In a tile's product with V a hidden key weighs 0, and 0 times an infinity or a NaN of its values is NaN.  So where a
+// row's result is not finite and values of keys that are hidden from it (or rows beside it) are not either, softmax_row
+// forms it again from the keys that it sees.  Tiles of finite values pay one test of their results, and rows that see what
+// is not finite, far from the tile where it lies, one more.  (The log-sum is right as it is: scores are masked one by one.)
+
+// Whether the values of keys first .. end - 1 hold any that is not finite (for all lanes).
+template <typename T, int DH, int LANES>
+__device__ __forceinline__ bool softmax_odd_values(const SoftmaxArgs& a, const SeqPiece& sk, int hk, int first, int end) {
+  bool odd = false;
+#pragma unroll 1
+  for (int key = max(first, 0) + (int)threadIdx.x % LANES; key < end; key += LANES) {
+    const T* v = reinterpret_cast<const T*>(seq_row(a.v, sk, a.ks.offsets != nullptr, hk, key, (int)sizeof(T)));
+#pragma unroll 4
+    for (int c = 0; c < DH; c += 8) {
+      Frag<T> f;
+      load8(f, v + c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) odd |= not_finite(f.get(e));
+    }
+  }
+  return __any(odd);
+}
+
+// One query row by itself, key by key in fp32, by LANES lanes of a wave.
 template <typename T, int DH, int LANES>
 __device__ __forceinline__ void softmax_row(const SoftmaxArgs& a, const SeqPiece& sq, const SeqPiece& sk, int head, int i) {
   constexpr int PER = (DH + LANES - 1) / LANES, esz = (int)sizeof(T);
@@ -162,7 +185,7 @@ __device__ __forceinline__ void softmax_row(const SoftmaxArgs& a, const SeqPiece
 #pragma unroll
         for (int c = 0; c < PER; ++c) acc[c] = fmaf(pj, (float)v[min(lane + LANES * c, DH - 1)], acc[c]);
       }
-    bool lost = isnan(sum);
+    bool lost = true;
 #pragma unroll
     for (int c = 0; c < PER; ++c) lost &= isnan(acc[c]);
     if (__all(lost)) break;  // nothing but NaN is left of the row
@@ -174,8 +197,6 @@ __device__ __forceinline__ void softmax_row(const SoftmaxArgs& a, const SeqPiece
 #pragma unroll
   for (int c = 0; c < PER; ++c)
     if (lane + LANES * c < DH) o[lane + LANES * c] = (T)(acc[c] * inv);
-  if (a.lse && lane == 0) a.lse[seq_num(a.qs, sq, a.H, head, i)] = (top + log2f(sum)) * kLn2;
 }
-__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) < __builtin_inff()); }
 
 }  // namespace luna

@@ -219,12 +219,15 @@ __global__ __launch_bounds__(DH) void softmax_join_kernel(SoftmaxArgs a) {
     }
   }
   const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
-  if (__syncthreads_or(not_finite(y * inv))) {
-    if (x < kWave) softmax_row<T, DH, (DH < kWave ? DH : kWave)>(a, sq, sk, head, t);
-    return;
+  if (a.lse && x == 0) a.lse[seq_num(a.qs, sq, a.H, head, t)] = (most + log2f(sum)) * kLn2;
+  if (__syncthreads_or(not_finite(y * inv))) {  // (uniform)
+    constexpr int LANES = DH < kWave ? DH : kWave;
+    if (softmax_odd_values<T, DH, LANES>(a, sk, hk, t + sk.len - sq.len + 1, sk.len)) {
+      if (x < kWave) softmax_row<T, DH, LANES>(a, sq, sk, head, t);
+      return;
+    }
   }
   reinterpret_cast<T*>(seq_row(a.o, sq, false, head, t, (int)sizeof(T)))[x] = (T)(y * inv);
-  if (a.lse && x == 0) a.lse[seq_num(a.qs, sq, a.H, head, t)] = (most + log2f(sum)) * kLn2;
 }
 
 template <typename T, int DH, int RT>
