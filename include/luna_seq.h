@@ -146,7 +146,9 @@ luna_status luna_softmax_fwd(const luna_rows* Q, const luna_rows* K, const luna_
 /*
  * Gradients of luna_softmax_fwd: from its out and lse and dO = dL/dout writes dQ (H heads)
  * and dK, dV (Hk heads, summed over the query heads of each).  Sums are taken in a fixed
- * order: the same call gives the same bits.
+ * order: the same call gives the same bits.  Scores and lse are fp32, so a P_ij carries about
+ * 2^-22 |score| of itself; it is never taken as more than 1.  (Scores from 2^31 on are outside
+ * of what either call is made for.)
  */
 luna_status luna_softmax_bwd(const luna_rows* Q, const luna_rows* K, const luna_rows* V, const luna_rows* out,
                              const float* lse, const luna_rows* dO, luna_dtype dtype, const luna_seqs* seqs,

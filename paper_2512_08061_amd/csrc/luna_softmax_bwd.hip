@@ -16,6 +16,14 @@ namespace luna {
 
 namespace {
 
+// A weight 2^x times 2^SHIFT, at most 2^SHIFT (NaN stays NaN).  lse carries a few roundings to 2^-24 of itself, which for
+// scores of millions is no longer a small number: without the limit rows of scores about 10^7 had weights above 2,
+// infinite in fp16, and larger ones any factor too much.
+template <int SHIFT = 0>
+__device__ __forceinline__ float weight(float x) {
+  return exp2_raw(__builtin_elementwise_minimum(x, (float)SHIFT));
+}
+
 template <typename T, int DH>
 struct SoftmaxBwdLds {
   static constexpr int KB = kSoftmaxStep<T>, P = DH + 16 / (int)sizeof(T);
@@ -84,7 +92,7 @@ __global__ __launch_bounds__(256) void softmax_dq_kernel(SoftmaxArgs a) {
         for (int j = 0; j < 4; ++j) {
           const int key = k0 + 16 * kt + 4 * g + j;
           const bool seen = key <= last && key < kend;
-          const float e = exp2_raw(fmaf(s[j], scale, -lse)) * (dp[j] - delta);
+          const float e = weight(fmaf(s[j], scale, -lse)) * (dp[j] - delta);
           s[j] = seen ? e : 0.0f;
         }
         ds.set2(4 * h, s[0], s[1]);
@@ -166,7 +174,7 @@ __global__ __launch_bounds__(256) void softmax_dkdv_kernel(SoftmaxArgs a) {
           for (int j = 0; j < 4; ++j) {
             const int r = 16 * qt + 4 * g + j, query = q0 + r;
             const bool seen = key <= query + shift && r < qn && i < m;
-            const float e = exp2_raw(fmaf(s[j], scale, -lse[j]));
+            const float e = weight(fmaf(s[j], scale, -lse[j]));
             p[j] = seen ? e : 0.0f;
             s[j] = seen ? e * (dp[j] - delta[j]) : 0.0f;
           }
@@ -313,8 +321,8 @@ __global__ __launch_bounds__(256, 2) void softmax_dq32_kernel(SoftmaxArgs a) {
       Frag<__bf16> ds[2];
 #pragma unroll
       for (int e = 0; e < 16; e += 2)
-        ds[e / 8].set2(e % 8, exp2_raw(fmaf(s[e], scale, -lse)) * (dp[e] - delta),
-                       exp2_raw(fmaf(s[e + 1], scale, -lse)) * (dp[e + 1] - delta));
+        ds[e / 8].set2(e % 8, weight(fmaf(s[e], scale, -lse)) * (dp[e] - delta),
+                       weight(fmaf(s[e + 1], scale, -lse)) * (dp[e + 1] - delta));
       read_k(1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -444,8 +452,8 @@ __global__ __launch_bounds__(512, 2) void softmax_dkdv32_kernel(SoftmaxArgs a) {
             const f32x4 ls = *reinterpret_cast<const f32x4*>(&l.lse[buf][32 * half + 2 * e + 4 * h]);
 #pragma unroll
             for (int j = 0; j < 4; j += 2) {
-              const float x = exp2_raw(fmaf(s[half][e + j], scale, -ls[j]));
-              const float y = exp2_raw(fmaf(s[half][e + j + 1], scale, -ls[j + 1]));
+              const float x = weight<kKeyShift>(fmaf(s[half][e + j], scale, -ls[j]));
+              const float y = weight<kKeyShift>(fmaf(s[half][e + j + 1], scale, -ls[j + 1]));
               pf[2 * half + e / 8].set2(e % 8 + j, x, y);
               ph[2 * half + e / 8][e % 8 + j] = (_Float16)x;
               ph[2 * half + e / 8][e % 8 + j + 1] = (_Float16)y;
