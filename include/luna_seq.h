@@ -47,7 +47,9 @@ typedef struct luna_rows {
  * the last offset) are neither read nor written.  The kernels clamp what they read from offsets
  * and lens to [0, rows], so other contents give undefined results, but no access outside the
  * tensors.  1 <= count <= 65535, 0 <= rows <= 2^30
- * (2^30 rows in all where every sequence has its own).
+ * (2^30 rows in all where every sequence has its own), 1 <= H <= 65535, and no launch of a call may have
+ * 2^32 threads or more: one has 256 to 512 per sequence, head and 64 tokens or more (luna_softmax_fwd of few queries over
+ * long keys: 256 per 512 keys of a key head, and d per query row), and a call beyond that is refused (LUNA_ERR_UNSUPPORTED).
  * NaN and infinities.  In the forward calls what is not finite in a row's query, or in the keys and
  * values of tokens that the row sees, reaches that row alone: nothing comes from later tokens, other sequences or
  * other (key) heads, or from rows of no sequence.  In luna_decay_fwd a value that is not finite makes its column
@@ -108,8 +110,8 @@ luna_status luna_decay_fwd(const luna_rows* Q, const luna_rows* K, const luna_ro
 /*
  * The same for the m next tokens of every sequence, token by token in fp32 from the state
  * (S, z), which is read and updated in place: the recurrent form for decoding.  Q, K, V, out
- * hold `count` sequences of m rows (packed and padded forms are not taken).  It needs no
- * workspace.
+ * hold `count` sequences of m rows (packed and padded forms are not taken); count * H <= 2^19.
+ * It needs no workspace.
  */
 luna_status luna_decay_step(const luna_rows* Q, const luna_rows* K, const luna_rows* V, luna_dtype dtype, int64_t count,
                             int64_t m, int64_t H, int64_t D, int64_t d, const float* log_decay, int32_t normalize,

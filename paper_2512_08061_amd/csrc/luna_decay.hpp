@@ -155,7 +155,7 @@ struct DecayScaled<__bf16> {
 };
 
 template <int DK, int DVW>
-constexpr int kDecayThreads = 4 * DVW * (DK > 128 && DVW <= 64 ? 2 : 1);
+constexpr int kDecayThreads = decay_threads(DK, DVW);
 
 // Waves per SIMD: two workgroups of a compute unit where the registers suffice (128 features without denominators: 546 ->
 // 487 us of the long batch's row pass).  The others would spill (128 features and 64 columns, whose half as many waves carry
@@ -506,8 +506,7 @@ hipError_t launch_decay_one(const DecayArgs& a, hipStream_t s) {
   static_assert(bytes <= 160 * 1024, "one workgroup's LDS");
   const hipError_t e = allow_lds<decay_kernel<T, DK, DVW, MODE, OUT, EXACT>>(bytes);
   if (e != hipSuccess) return e;
-  const int slices = (a.dv + DVW - 1) / DVW;
-  hipLaunchKernelGGL((decay_kernel<T, DK, DVW, MODE, OUT, EXACT>), dim3((unsigned)((int64_t)a.slots * a.H * slices)),
+  hipLaunchKernelGGL((decay_kernel<T, DK, DVW, MODE, OUT, EXACT>), dim3((unsigned)decay_groups(a.slots, a.H, a.dv)),
                      dim3(kDecayThreads<DK, DVW>), bytes, s, a);
   return hipGetLastError();
 }
@@ -522,7 +521,7 @@ hipError_t launch_decay_exact(const DecayArgs& a, hipStream_t s) {
 
 template <typename T, int DK, int MODE, bool OUT>
 hipError_t launch_decay_width(const DecayArgs& a, hipStream_t s) {
-  return a.dv <= 64 ? launch_decay_exact<T, DK, 64, MODE, OUT>(a, s) : launch_decay_exact<T, DK, 128, MODE, OUT>(a, s);
+  return decay_columns(a.dv) == 64 ? launch_decay_exact<T, DK, 64, MODE, OUT>(a, s) : launch_decay_exact<T, DK, 128, MODE, OUT>(a, s);
 }
 
 template <typename T, int MODE, bool OUT>

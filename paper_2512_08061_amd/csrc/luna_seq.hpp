@@ -165,6 +165,11 @@ __host__ __device__ inline int64_t decay_state_floats(int dk, int dv) {
   return (int64_t)dk * dv + (dk > dv ? dk : dv);
 }
 bool decay_supported(int dk, int dv);
+// Columns of v of a workgroup, and its threads (16 columns a wave; two waves where more than 128 features meet few columns).
+constexpr int decay_columns(int dv) { return dv <= 64 ? 64 : 128; }
+constexpr int decay_threads(int dk, int dv) { return 4 * decay_columns(dv) * (dk > 128 && dv <= 64 ? 2 : 1); }
+// Workgroups of a pass.
+inline int64_t decay_groups(int64_t slots, int64_t H, int dv) { return slots * H * ((dv + decay_columns(dv) - 1) / decay_columns(dv)); }
 // What every piece but its sequence's last adds to the state, then the states before the pieces in their place.  (A row
 // pass that adds up the pieces before its own by itself, without the second launch, waits for them one after the
 // other: LUNA backward 256 -> 455 us.)
@@ -211,7 +216,9 @@ struct SoftmaxArgs {
                  // backward: [H] numbers per key row of 2 d floats, see softmax_head_parts
   float* delta;  // per query row: dO.out, written by the query pass and read by the key pass
 };
-constexpr int kSoftmaxLeast = 64;  // the fewest rows of a tile: an upper bound for grids
+// Query rows of a workgroup of the forward call and of the backward pass over queries, and key rows of one of the pass over
+// keys: four waves of 32 or 16.
+constexpr int softmax_tile(Dt dt, int64_t d) { return dt == Dt::BF16 && d >= 64 ? 128 : 64; }
 hipError_t launch_softmax_fwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 // Few queries over long keys: m tokens of equal or padded sequences, up to 64 rows per key head, whose keys
 // then share one read of the cache; cut in pieces of kSplitKeys keys.

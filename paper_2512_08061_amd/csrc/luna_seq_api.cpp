@@ -14,10 +14,11 @@ namespace {
 using luna::set_error;
 
 constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxRow = (int64_t)1 << 20;
-constexpr int64_t kMaxGrid = ((int64_t)1 << 32) / 512 - 1;  // workgroups: a launch has fewer than 2^32 threads
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// A launch has fewer than 2^32 threads.
+bool launchable(int64_t groups, int threads) { return groups < ((int64_t)1 << 32) / threads; }
 
 luna::SeqRows rows_of(const luna_rows* r) {
   return r ? luna::SeqRows{static_cast<char*>(r->data), r->seq, r->head, r->row} : luna::SeqRows{};
@@ -86,6 +87,7 @@ luna_status hip_status(hipError_t e, const char* what) {
   return set_error(LUNA_ERR_HIP, why);
 }
 
+luna::Dt type_of(luna_dtype dt) { return dt == LUNA_BF16 ? luna::Dt::BF16 : luna::Dt::F32; }
 luna_status check_type(luna_dtype dt) {
   return dt == LUNA_F32 || dt == LUNA_BF16 ? LUNA_OK : set_error(LUNA_ERR_INVALID_ARG, "dtype must be LUNA_F32 or LUNA_BF16");
 }
@@ -130,7 +132,10 @@ luna_status plan_decay(luna_dtype dt, const luna_seqs& s, int64_t H, int64_t D, 
   }
   p->many = per > p->piece;
   const int64_t slots = luna::seq_slots(set, p->piece);
-  if (slots * H * 2 > kMaxGrid) return set_error(LUNA_ERR_UNSUPPORTED, "too many pieces of sequences and heads");
+  const int dk = (int)D, dv = (int)d;  // (the other way round: dQ and dK)
+  if (!launchable(luna::decay_groups(slots, H, dv), luna::decay_threads(dk, dv)) ||
+      (backward && !launchable(luna::decay_groups(slots, H, dk), luna::decay_threads(dv, dk))))
+    return set_error(LUNA_ERR_UNSUPPORTED, "too many pieces of sequences and heads");
   p->slots = (int)slots;
   size_t off = 0;
   auto take = [&](size_t& at, size_t bytes) {
@@ -184,14 +189,12 @@ luna_status run_decay_rows(luna::Dt dt, int mode, const luna::DecayArgs& a, hipS
   return hip_status(luna::launch_decay_out(dt, mode, a, s), "decay launch");
 }
 
-luna::Dt type_of(luna_dtype dt) { return dt == LUNA_BF16 ? luna::Dt::BF16 : luna::Dt::F32; }
-
 // ---------------------------------------------------------------------------
 // softmax
 // ---------------------------------------------------------------------------
 
 luna_status check_softmax(luna_dtype dt, const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d,
-                          float scale) {
+                          float scale, bool backward) {
   luna_status st = check_type(dt);
   if (st == LUNA_OK) st = check_seqs(seqs, "seqs");
   if (st == LUNA_OK && keys) st = check_seqs(keys, "keys");
@@ -201,12 +204,20 @@ luna_status check_softmax(luna_dtype dt, const luna_seqs* seqs, const luna_seqs*
   if (H > 65535) return set_error(LUNA_ERR_UNSUPPORTED, "H must be <= 65535");
   if (d != 32 && d != 64 && d != 128) return set_error(LUNA_ERR_UNSUPPORTED, "d must be 32, 64 or 128");
   if (!std::isfinite(scale)) return set_error(LUNA_ERR_INVALID_ARG, "scale must be finite");
-  for (const luna_seqs* x : {seqs, keys ? keys : seqs})
-    if (luna::seq_slots(set_of(x), luna::kSoftmaxLeast) * H > kMaxGrid)
-      return set_error(LUNA_ERR_UNSUPPORTED, "too many tiles of sequences and heads");
-  if (luna::softmax_splits(set_of(seqs), set_of(keys ? keys : seqs), H, Hk) && seqs->count * H * seqs->rows > kMaxGrid)
-    return set_error(LUNA_ERR_UNSUPPORTED, "too many query rows");
-  return LUNA_OK;
+  const luna::SeqSet qs = set_of(seqs), ks = set_of(keys ? keys : seqs);
+  const luna::Dt t = type_of(dt);
+  const int tile = luna::softmax_tile(t, d);
+  const int64_t qtiles = luna::seq_slots(qs, tile), ktiles = luna::seq_slots(ks, tile);
+  bool fits;
+  if (backward) {
+    fits = launchable(qtiles * H, 256) &&
+           launchable(ktiles * (luna::softmax_head_parts(t, ks, H, Hk, d) ? H : Hk), tile == 128 ? 512 : 256);
+  } else if (luna::softmax_splits(qs, ks, H, Hk)) {
+    fits = launchable(luna::seq_slots(ks, luna::kSplitKeys) * Hk, 256) && launchable(qs.count * H * qs.rows, (int)d);
+  } else {
+    fits = launchable(qtiles * H, 256);
+  }
+  return fits ? LUNA_OK : set_error(LUNA_ERR_UNSUPPORTED, "too many tiles of sequences and heads");
 }
 
 luna::SoftmaxArgs softmax_args(const luna_rows* Q, const luna_rows* K, const luna_rows* V, const luna_rows* out,
@@ -258,7 +269,7 @@ size_t luna_seq_workspace_bytes(int32_t op, luna_dtype dtype, const luna_seqs* s
     return p.total;
   }
   if (op == LUNA_OP_SOFTMAX_FWD || op == LUNA_OP_SOFTMAX_BWD) {
-    if (check_softmax(dtype, seqs, keys, H, Hk, Dq, 1.0f) != LUNA_OK) return 0;
+    if (check_softmax(dtype, seqs, keys, H, Hk, Dq, 1.0f, op == LUNA_OP_SOFTMAX_BWD) != LUNA_OK) return 0;
     if (Dv != Dq) {
       set_error(LUNA_ERR_INVALID_ARG, "Dq and Dv differ");
       return 0;
@@ -427,7 +438,7 @@ luna_status luna_softmax_fwd(const luna_rows* Q, const luna_rows* K, const luna_
                              float scale, const luna_rows* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
   luna::clear_error();
   luna_status st;
-  if ((st = check_softmax(dtype, seqs, keys, H, Hk, d, scale)) != LUNA_OK) return st;
+  if ((st = check_softmax(dtype, seqs, keys, H, Hk, d, scale, false)) != LUNA_OK) return st;
   const luna_seqs& ks = keys ? *keys : *seqs;
   if ((st = check_rows(Q, "Q", dtype, *seqs, H, d, false)) != LUNA_OK) return st;
   if ((st = check_rows(K, "K", dtype, ks, Hk, d, false)) != LUNA_OK) return st;
@@ -451,7 +462,7 @@ luna_status luna_softmax_bwd(const luna_rows* Q, const luna_rows* K, const luna_
                              const luna_rows* dK, const luna_rows* dV, void* ws, size_t ws_bytes, void* stream) {
   luna::clear_error();
   luna_status st;
-  if ((st = check_softmax(dtype, seqs, keys, H, Hk, d, scale)) != LUNA_OK) return st;
+  if ((st = check_softmax(dtype, seqs, keys, H, Hk, d, scale, true)) != LUNA_OK) return st;
   const luna_seqs& ks = keys ? *keys : *seqs;
   if (!lse) return set_error(LUNA_ERR_INVALID_ARG, "lse is NULL");
   if ((st = check_rows(Q, "Q", dtype, *seqs, H, d, false)) != LUNA_OK) return st;

@@ -113,7 +113,10 @@ __device__ __forceinline__ f32x16 zero16() {
 }
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr int kSoftmaxTile = 64;  // query rows (key rows) of a workgroup
+// query rows (key rows) of a workgroup: 16 x 16 products, and 32 x 32 ones (bf16 with d = 64 and 128)
+constexpr int kSoftmaxTile = softmax_tile(Dt::F32, 128), kSoftmaxTile32 = softmax_tile(Dt::BF16, 128);
+static_assert(kSoftmaxTile == 64 && softmax_tile(Dt::BF16, 32) == 64 && softmax_tile(Dt::BF16, 64) == kSoftmaxTile32, "tiles");
+static_assert(kSoftmaxTile32 == 128, "four waves of 32 rows");
 
 // keys per step of the tile kernels: the staged rows of two tensors fit 64 KiB and a bit
 template <typename T>
