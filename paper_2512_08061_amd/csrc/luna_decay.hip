@@ -6,19 +6,25 @@ namespace luna {
 
 namespace {
 
-// Before: slot p of a sequence and head holds the state that its tokens add (all but the last
-// piece).  After: the state before piece p, S_p = f^piece S_{p-1} + X_{p-1}, from the caller's
-// state or zero.  Four elements per thread; loads of the next piece do not wait for the sums.
+// Before: state p of a sequence and head is what piece p adds (all but the last piece).  After: the state before piece p,
+// S_p = f^piece S_{p-1} + X_{p-1}, from the caller's state or zero.  Four elements per thread; loads of the next piece do
+// not wait for the sums.  A workgroup per sequence, or, where the sequences are more than the states, per state: the
+// sequence whose first one it is, which is the last whose first state is not behind it, if that is longer than a piece.
 __global__ __launch_bounds__(256) void decay_scan_kernel(DecayArgs a, int64_t elems) {
-  const int head = blockIdx.y, b = blockIdx.z;
+  const int head = blockIdx.y;
+  int b = blockIdx.z;
+  if (gridDim.z < a.s.count) {
+    b = seq_last(a.s, [&](int64_t i, int64_t first) { return seq_first_state(a.s, i, first, a.piece) <= blockIdx.z; });
+    if (b < 0) return;
+  }
   const int64_t e = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
   if (e >= elems) return;
   const SeqPiece sp = seq_of(a.s, b);
   const int pieces = (int)(((int64_t)sp.len + a.piece - 1) / a.piece);
-  if (pieces < 2) return;
-  const int64_t slot = a.s.offsets ? sp.first / a.piece + b : b * ((a.s.rows + a.piece - 1) / a.piece);
+  const int64_t at0 = seq_first_state(a.s, b, sp.first, a.piece);
+  if (pieces < 2 || (gridDim.z < a.s.count && at0 != blockIdx.z)) return;
   const int64_t step = a.H * decay_state_floats(a.dk, a.dv);
-  float* x = a.states + slot * step + head * decay_state_floats(a.dk, a.dv) + e;
+  float* x = a.states + at0 * step + head * decay_state_floats(a.dk, a.dv) + e;
   const auto at = [&](int p) { return reinterpret_cast<f32x4*>(x + p * step); };
   const float f = exp2_raw(decay_log2(a.log_decay[head]) * (float)a.piece);
   f32x4 run = zero4(), next = *at(0);
@@ -102,7 +108,8 @@ hipError_t launch_decay_out(Dt dt, int mode, const DecayArgs& a, hipStream_t s) 
 
 hipError_t launch_decay_scan(const DecayArgs& a, hipStream_t s) {
   const int64_t elems = decay_state_floats(a.dk, a.dv);  // (a multiple of 4; unused ones of z too)
-  const dim3 grid((unsigned)((elems / 4 + 255) / 256), (unsigned)a.H, (unsigned)a.s.count);
+  const int64_t sequences = a.s.count < a.nstates ? a.s.count : a.nstates;
+  const dim3 grid((unsigned)((elems / 4 + 255) / 256), (unsigned)a.H, (unsigned)sequences);
   hipLaunchKernelGGL(decay_scan_kernel, grid, dim3(256), 0, s, a, elems);
   return hipGetLastError();
 }

@@ -214,7 +214,8 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
 
   // the state before the piece
   const int64_t sf = decay_state_floats(a.dk, a.dv), sheads = (int64_t)a.H * sf;
-  float* st = a.states ? a.states + ((int64_t)slot * a.H + head) * sf : nullptr;
+  const int state = __builtin_amdgcn_readfirstlane(packed ? (int)seq_first_state(a.s, sp.seq, sp.first, a.piece) + sp.index : slot);
+  float* st = a.states ? a.states + ((int64_t)state * a.H + head) * sf : nullptr;  // (not touched where the sequence has one piece)
   const int64_t user = (int64_t)sp.seq * a.H + head;
   const int mycol = wcol + c;
   f32x4 S[FT], za = zero4();  // za: row 0 is the further key component's row of S (kDecayAug)

@@ -29,6 +29,18 @@ inline int64_t seq_slots(const SeqSet& s, int64_t piece) {
   return s.offsets ? s.rows / piece + s.count : s.count * ((s.rows + piece - 1) / piece);
 }
 
+// States of pieces are numbered apart from the slots, so that short packed sequences take none: only sequences longer than a
+// piece have them, a state per piece.  With u = offsets[b] / piece, one's first state is floor(u) + min(b, floor(u)).  The next
+// such sequence starts len / piece > 1 pieces later or more and is a later one, so that its first state is at least
+// floor(len / piece) + 1 >= ceil(len / piece) further; and with u + len / piece <= rows / piece no state reaches
+// floor(rows / piece) + min(count, floor(rows / piece)).  Equal and padded sequences have theirs in the place of their slots.
+__host__ __device__ inline int64_t seq_first_state(const SeqSet& s, int64_t b, int64_t first, int piece) {
+  if (!s.offsets) return b * ((s.rows + piece - 1) / piece);
+  const int u = (int)first / piece;  // (at most 2^30 rows)
+  return u + (b < u ? b : u);
+}
+inline int64_t seq_states(const SeqSet& s, int piece) { return seq_first_state(s, s.count, s.rows, piece); }
+
 // One piece of one sequence.
 struct SeqPiece {
   int seq;      // -1: the slot holds no piece
@@ -55,22 +67,27 @@ __device__ __forceinline__ SeqPiece seq_of(const SeqSet& s, int b) {
   return p;
 }
 
+// The last packed sequence b with holds(b, offsets[b]), which holds up to some sequence and no further; -1: none (the whole
+// wave calls this).
+template <typename Holds>
+__device__ __forceinline__ int seq_last(const SeqSet& s, Holds holds) {
+  int below = 0;
+  const int lane = threadIdx.x % kWave;
+  for (int b0 = 0; b0 < s.count; b0 += kWave) {
+    const int b = b0 + lane;
+    const uint64_t m = __ballot(b < s.count && holds(b, seq_clamp(s.offsets[min((int64_t)b, s.count)], 0, s.rows)));
+    below += __popcll(m);
+    if (m != ~(uint64_t)0) break;
+  }
+  return __builtin_amdgcn_readfirstlane(below - 1);
+}
+
 // The piece of a slot (the whole wave calls this with one slot).
 __device__ __forceinline__ SeqPiece seq_piece(const SeqSet& s, int slot, int piece) {
   SeqPiece p;
   int first_slot;
   if (s.offsets) {
-    int below = 0;  // sequences whose first slot is not behind this one
-    const int lane = threadIdx.x % kWave;
-    for (int b0 = 0; b0 < s.count; b0 += kWave) {
-      const int b = b0 + lane;
-      const bool in = b < s.count;
-      const int at = in ? seq_clamp(s.offsets[b], 0, s.rows) / piece + b : 0;
-      const uint64_t m = __ballot(in && at <= slot);
-      below += __popcll(m);
-      if (m != ~(uint64_t)0) break;
-    }
-    p.seq = __builtin_amdgcn_readfirstlane(below - 1);
+    p.seq = seq_last(s, [&](int b, int first) { return first / piece + b <= slot; });
     if (p.seq < 0) return p;
     p = seq_of(s, p.seq);
     first_slot = (int)(p.first / piece) + p.seq;
@@ -146,10 +163,11 @@ struct DecayArgs {
   SeqSet s;
   const float* log_decay;  // [H]
   int H, dk, dv;
-  int piece, slots;        // tokens per piece (a multiple of 64)
+  int piece, slots;        // tokens per piece (a multiple of 64), and slots of pieces (workgroups)
+  int nstates;             // states (seq_states)
   int reverse;             // sums over later tokens instead of earlier ones
   int exact_state;         // the state to fp32 accuracy (it is returned)
-  float* states;           // [slots][H][decay_state_floats]: state before each piece; null: one piece per sequence
+  float* states;           // [nstates][H][decay_state_floats]: state before each piece; null: one piece per sequence
   int transposed;          // states: of k and v exchanged
   int guard;               // values that are not finite reach no earlier token
   float* S;                // [count][H][dk][dv] and z [count][H][dk], in and out, or null

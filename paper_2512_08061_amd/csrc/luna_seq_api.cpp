@@ -97,7 +97,7 @@ luna_status check_type(luna_dtype dt) {
 // ---------------------------------------------------------------------------
 
 struct DecayPlan {
-  int piece = 0, slots = 0;
+  int piece = 0, slots = 0, nstates = 0;
   bool many = false;  // some sequence may have more than one piece
   size_t states = 0, w = 0, delta = 0, total = 0;  // workspace offsets
 };
@@ -108,8 +108,9 @@ struct DecayPlan {
 // a compute unit (two with 64 features), and a sixth more while no second one fills its waits; 4.5 TB/s.  Measured, us a
 // call by piece: 8 x 16 heads of 16384 tokens, D = d = 128, one 1070, 4096 683, 2048 726, 1024 783; backward of 2 x 16
 // heads of 2048 tokens with 256 features 128 289, 256 214, 384 244, 512 222; fp32 backward of 4096 tokens in 12 heads, 64
-// features, 64 114, 128 101, 256 118.  How lengths fall into pieces is on the device and not known here (packed
-// prompts with 256 features: 384 us by the estimate's 1024, 353 by 576).
+// features, 64 114, 128 101, 256 118.  How lengths fall into pieces is on the device and not known here (six packed prompts
+// with 256 features: 384 us by the estimate's 512, 353 by 576): packed sequences are taken as of their mean length, one of
+// them as long as a piece.
 luna_status plan_decay(luna_dtype dt, const luna_seqs& s, int64_t H, int64_t D, int64_t d, bool backward, bool normalize,
                        DecayPlan* p) {
   const int64_t per = s.rows, all = s.offsets ? s.rows : s.count * s.rows;
@@ -121,10 +122,13 @@ luna_status plan_decay(luna_dtype dt, const luna_seqs& s, int64_t H, int64_t D, 
   double best = 0.0;
   for (int64_t piece = longest; piece >= 64; piece = piece > 64 && piece < 128 ? 64 : piece / 128 * 64) {
     // sequences of the same length, or packed ones, with half a piece left over at the end of each
-    const int64_t pieces = s.offsets ? ceil_div(all, piece) + s.count / 2 : s.count * ceil_div(per, piece);
+    const int64_t whole = s.offsets ? ceil_div(all, piece) : s.count * ceil_div(per, piece);
+    const int64_t pieces = whole + (s.offsets ? s.count / 2 : 0), full = ceil_div(piece, 64);
     const double groups = (double)(pieces * H);
-    const double one = (double)ceil_div(pieces * H, room) * (double)ceil_div(piece, 64) * chunk * (groups < 2 * room ? 1.17 : 1.0);
-    const double cost = piece == longest ? one : 1.4 * one + 8.0 + 4.0 * groups * state / 4.5e6;
+    const double mean = s.offsets ? std::min((double)full, ((double)all / 64 + (double)(s.count / 2)) / (double)pieces) : (double)full;
+    const double chunks = (double)ceil_div(pieces * H, room) * mean + ((double)full - mean);
+    const double one = chunks * chunk * (groups < 2 * room ? 1.17 : 1.0);
+    const double cost = piece == longest ? one : 1.4 * one + 8.0 + 4.0 * (double)(whole * H) * state / 4.5e6;
     if (p->piece == 0 || cost < best) {
       best = cost;
       p->piece = (int)piece;
@@ -142,7 +146,10 @@ luna_status plan_decay(luna_dtype dt, const luna_seqs& s, int64_t H, int64_t D, 
     at = off;
     off = align256(off + bytes);
   };
-  if (p->many) take(p->states, (size_t)slots * H * luna::decay_state_floats((int)D, (int)d) * 4);
+  if (p->many) {
+    p->nstates = (int)luna::seq_states(set, p->piece);
+    take(p->states, (size_t)p->nstates * H * luna::decay_state_floats((int)D, (int)d) * 4);
+  }
   if (backward && normalize) {
     take(p->w, (size_t)all * H * 4);
     take(p->delta, (size_t)all * H * 4);
@@ -177,6 +184,7 @@ luna_status check_state(const float* S, const float* z, int32_t normalize) {
 void set_plan(const DecayPlan& p, luna::DecayArgs& a, void* ws) {
   a.piece = p.piece;
   a.slots = p.slots;
+  a.nstates = p.nstates;
   a.states = p.many ? reinterpret_cast<float*>(static_cast<char*>(ws) + p.states) : nullptr;
 }
 luna_status run_decay_states(luna::Dt dt, int mode, const luna::DecayArgs& a, hipStream_t s) {

@@ -1,11 +1,14 @@
 """The sequence operators (include/luna_seq.h) at the ends of what they take: values, sizes and forms of a call that
 choose between kernels."""
+import ctypes
+
 import pytest
 import torch
 
 from gpu_util import say
 from paper_2512_08061_amd import luna
-from seq_util import device, rand, unit
+from seq_util import U32, assert_within, cut, decay_grads, device, packed_offsets, rand, unit
+from test_gpu_decay import EPS, check_forward as check_decay, decays
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +47,36 @@ def test_gradients_of_very_large_scores(H, Hk, d, dtype, size):
         assert torch.isfinite(got.float()).all(), name
         over = (got[0].double().abs() / bound).max().item()
         assert over <= 1 + 4 * unit(torch.bfloat16), f"{name}: {over} of the sum over weights of 1"
+
+
+@pytest.mark.parametrize("norm,dtype,D", [(True, "bf16", 64), (False, "bf16", 128), (True, "f32", 64)])
+def test_long_sequences_among_many_short_ones(norm, dtype, D):
+    """More packed sequences than states of pieces: only the long ones have states, wherever they lie."""
+    say(f"long among many short: norm={norm} {dtype} D={D}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    lens = [(7 * i) % 19 if i % 4 else 0 for i in range(400)]
+    for i, n in ((0, 1300), (57, 641), (58, 640), (200, 513), (399, 2100)):
+        lens[i] = n
+    H, d, T, off, g = 4, 64, sum(lens), packed_offsets(lens), decays(4)
+    opt = {"normalize": norm, "eps": EPS, "offsets": off}
+    at = lambda a: ctypes.addressof(a)  # noqa: E731
+    rows = (ctypes.c_int64 * 4)(len(lens), T, off.data_ptr(), 0)
+    nb = luna.load_library().luna_seq_workspace_bytes(luna.OP_DECAY_FWD, luna.LUNA_BF16 if dtype == "bf16" else luna.LUNA_F32, at(rows),
+                                                      None, H, H, D, d)
+    assert 0 < nb < len(lens) * H * (D * d + max(D, d)) * 4, "pieces, and fewer states than sequences"
+    gen = torch.Generator(device=device()).manual_seed(22)
+    Q, K = (rand((T, H, D), dt, gen, norm) for _ in range(2))
+    V, dO = (rand((T, H, d), dt, gen) for _ in range(2))
+    S = torch.randn((len(lens), H, D, d), generator=gen, device=device())
+    z = torch.rand((len(lens), H, D), generator=gen, device=device()) + 1.0 if norm else None
+    S0, z0 = S.clone(), None if z is None else z.clone()
+    out, den = luna.decay_attn(Q, K, V, g, S=S, z=z, **opt)
+    check_decay(Q, K, V, g, out, den, "packed", lens, norm, 1.0, S0, z0, S, z)
+    out, den = luna.decay_attn(Q, K, V, g, **opt)
+    grads = luna.decay_attn_bwd(Q, K, V, dO, g, out=out, den=den, **opt)
+    u = unit(dt) if dt == torch.bfloat16 else 0.0
+    for i, n in enumerate(lens):  # (the bounds of the operator's own test)
+        refs, sizes = decay_grads(*(cut(t, "packed", lens, i) for t in (Q, K, V, dO)), g, norm, 1.0, EPS)
+        for got, ref, size, name in zip(grads, refs, sizes, ("dQ", "dK", "dV")):
+            sums = (2 * n + D + d + 32) * U32 * (4 if norm else 1)
+            assert_within(cut(got, "packed", lens, i), ref, (5 * u + sums) * size + u * ref.abs() + 1e-30, f"{name}[{i}]")

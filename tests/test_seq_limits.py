@@ -1,5 +1,7 @@
 """Which sizes the operators over sequences (include/luna_seq.h) take and how much workspace they ask for, without a GPU."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 
@@ -64,3 +66,76 @@ def test_many_short_sequences_of_the_decay_operators(H, D, d, fits):
     """A workgroup of 256 or 512 threads per sequence and head."""
     _, why = workspace(luna.OP_DECAY_FWD, seqs(65535, 4), H=H, Dq=D, Dv=d)
     assert ("too many" in why) != fits and bool(why) != fits
+
+
+def state_bytes(H, D, d):
+    return H * (D * d + max(D, d)) * 4
+
+
+@pytest.mark.parametrize("op", [luna.OP_DECAY_FWD, luna.OP_DECAY_BWD])
+@pytest.mark.parametrize("count,rows,D,d,dt", [(8192, 131072, 256, 128, BF16), (8192, 131072, 128, 128, BF16),
+                                               (16384, 262144, 256, 128, BF16), (1000, 64000, 256, 128, BF16), (65535, 262140, 256, 128, BF16),
+                                               (6, 16384, 256, 128, BF16), (1, 65536, 128, 128, F32), (300, 70000, 64, 32, F32)])
+def test_states_of_packed_sequences_go_by_their_rows(op, count, rows, D, d, dt):
+    """Two states per 64 rows at most, however many sequences share them, and never more than a state per piece and sequence
+    (a piece has 64 rows or more)."""
+    nb, why = workspace(op, seqs(count, rows, offsets=True), H=16, Dq=D, Dv=d, dt=dt)
+    weights = 2 * rows * 16 * 4 if op == luna.OP_DECAY_BWD else 0
+    assert not why and nb <= min(2 * (rows // 64), rows // 64 + count) * state_bytes(16, D, d) + weights + 512
+    tensors = rows * 16 * (2 * D + 2 * d) * (2 if dt == BF16 else 4)
+    assert nb - weights <= 2.7 * tensors  # (64 rows of Q, K, V and out against two states)
+
+
+def test_states_do_not_grow_with_the_number_of_sequences():
+    """As many rows in ever more sequences; the states of the most are those of fewer rows each."""
+    sizes = [workspace(luna.OP_DECAY_FWD, seqs(n, 65536, offsets=True), Dq=256, Dv=128)[0] for n in (1024, 8192, 65535)]
+    assert all(0 < x <= 2 * 1024 * state_bytes(16, 256, 128) for x in sizes)
+
+
+NUMBERING = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "luna_seq.hpp"
+int main() {
+  srand(1);
+  long checked = 0;
+  for (int trial = 0; trial < 20000; ++trial) {
+    const int piece = 64 * (1 + rand() % 4), count = 1 + rand() % 40, kind = rand() % 3;
+    int32_t off[64];
+    off[0] = rand() % 3 ? 0 : rand() % 300;
+    for (int b = 0; b < count; ++b)
+      off[b + 1] = off[b] + (rand() % 4 == 0 ? 0 : kind == 0 ? rand() % (3 * piece) : kind == 1 ? rand() % 20 : piece * (rand() % 4) + rand() % 2);
+    luna::SeqSet s{count, off[count] + (rand() % 2 ? 0 : rand() % 200), off, nullptr};
+    const int64_t n = luna::seq_states(s, piece);
+    if (n > 2 * (s.rows / piece) || n > s.rows / piece + count) return printf("too many states\n"), 1;
+    int64_t next = 0;
+    for (int b = 0; b < count; ++b) {
+      const int len = off[b + 1] - off[b];
+      const int64_t at = luna::seq_first_state(s, b, off[b], piece);
+      if (len <= piece) continue;
+      const int64_t pieces = (len + piece - 1) / piece;
+      if (at < next || at + pieces > n) return printf("trial %d sequence %d: %ld .. %ld of %ld, the one before ends at %ld\n", trial, b, (long)at,
+                                                      (long)(at + pieces), (long)n, (long)next), 1;
+      int last = -1;  // the sequence that a state's workgroup of the scan finds
+      for (int i = 0; i < count; ++i)
+        if (luna::seq_first_state(s, i, off[i], piece) <= at) last = i;
+      if (last != b) return printf("trial %d: state %ld finds %d, not %d\n", trial, (long)at, last, b), 1;
+      next = at + pieces;
+      ++checked;
+    }
+  }
+  return checked > 10000 ? 0 : 1;
+}
+"""
+
+
+def test_states_of_sequences_are_apart_and_within(tmp_path):
+    """The numbering of states, on the host: long sequences among short and empty ones, of lengths around whole pieces."""
+    src, exe = tmp_path / "numbering.cpp", tmp_path / "numbering"
+    src.write_text(NUMBERING)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run(["/opt/rocm/bin/hipcc", "-x", "hip", "--offload-arch=gfx950", "-O1", "-std=c++17", "-Xclang", "-target-feature", "-Xclang",
+                    "-packed-fp32-ops", "-I", os.path.join(root, "include"), "-I", os.path.join(root, "paper_2512_08061_amd", "csrc"),
+                    str(src), "-o", str(exe)], check=True, capture_output=True)
+    p = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert p.returncode == 0, p.stdout
