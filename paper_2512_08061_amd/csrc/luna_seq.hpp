@@ -68,16 +68,16 @@ __device__ __forceinline__ SeqPiece seq_of(const SeqSet& s, int b) {
 }
 
 // The last packed sequence b with holds(b, offsets[b]), which holds up to some sequence and no further; -1: none (the whole
-// wave calls this).
+// wave calls this).  64 guesses at a time: every 4096th, 64th and single sequence.  (One look at each 64 after the other
+// took 24 ms for 16384 sequences of 8 tokens in 16 heads, of 1.6 ms for the same sequences without offsets.)
 template <typename Holds>
 __device__ __forceinline__ int seq_last(const SeqSet& s, Holds holds) {
-  int below = 0;
-  const int lane = threadIdx.x % kWave;
-  for (int b0 = 0; b0 < s.count; b0 += kWave) {
-    const int b = b0 + lane;
-    const uint64_t m = __ballot(b < s.count && holds(b, seq_clamp(s.offsets[min((int64_t)b, s.count)], 0, s.rows)));
-    below += __popcll(m);
-    if (m != ~(uint64_t)0) break;
+  const int lane = threadIdx.x % kWave, count = (int)s.count;
+  int below = 0, step = 1;  // sequences known to hold
+  while (step * kWave < count) step *= kWave;
+  for (; step > 0; step /= kWave) {
+    const int b = below + step * (lane + 1) - 1;
+    below += step * __popcll(__ballot(b < count && holds(b, seq_clamp(s.offsets[min(b, count)], 0, s.rows))));
   }
   return __builtin_amdgcn_readfirstlane(below - 1);
 }

@@ -80,3 +80,39 @@ def test_long_sequences_among_many_short_ones(norm, dtype, D):
         for got, ref, size, name in zip(grads, refs, sizes, ("dQ", "dK", "dV")):
             sums = (2 * n + D + d + 32) * U32 * (4 if norm else 1)
             assert_within(cut(got, "packed", lens, i), ref, (5 * u + sums) * size + u * ref.abs() + 1e-30, f"{name}[{i}]")
+
+
+@pytest.mark.parametrize("count", [65, 4097, 5000])
+def test_thousands_of_packed_sequences(count):
+    """Each packed sequence of thousands is found: the same bits as the padded batch of the same rows, forward and backward.
+    (The sequence of two chunks may be one piece in one form and two in the other.  A piece hands dK the state of dV's
+    product transposed, formed from other roundings than its own, so there dK is held to its bound instead.)"""
+    say(f"packed sequences: {count}")
+    H, Hk, d, most = 2, 1, 64, 70
+    gen = torch.Generator(device=device()).manual_seed(23)
+    lens = torch.randint(0, 6, (count,), generator=gen, device=device(), dtype=torch.int32)
+    lens[::61] = 0
+    lens[count // 2] = most
+    off = torch.cat([torch.zeros(1, dtype=torch.int32, device=device()), lens.cumsum(0).int()])
+    T, g = int(off[-1]), decays(H)
+    used = torch.arange(most, device=device())[None, :] < lens[:, None]  # [count, most]: row by row as packed
+    pad = {n: rand((count, h, most, d), torch.bfloat16, gen) for n, h in (("Q", H), ("K", H), ("V", H), ("dO", H), ("K2", Hk), ("V2", Hk))}
+    rows = lambda t: t.transpose(1, 2)[used].contiguous()  # noqa: E731
+    own = {n: rows(t) for n, t in pad.items()}
+    assert own["Q"].shape[0] == T
+
+    def call(x, **opt):
+        a, _ = luna.decay_attn(x["Q"], x["K"], x["V"], g, **opt)
+        out, lse = luna.softmax_attn(x["Q"], x["K2"], x["V2"], **opt)
+        return (a, out, *luna.decay_attn_bwd(x["Q"], x["K"], x["V"], x["dO"], g, **opt),
+                *luna.softmax_attn_bwd(x["Q"], x["K2"], x["V2"], out, lse, x["dO"], **opt))
+
+    at, u = int(off[count // 2]), unit(torch.bfloat16)
+    for i, (got, want) in enumerate(zip(call(own, offsets=off), call(pad, lens=lens))):
+        want = rows(want)
+        if i == 3:
+            ref, size = (x[1] for x in decay_grads(*(own[n][at:at + most].double().transpose(0, 1) for n in ("Q", "K", "V", "dO")), g))
+            for t in (got, want):
+                assert_within(t[at:at + most].transpose(0, 1), ref, (5 * u + (2 * most + 2 * d + 32) * U32) * size + u * ref.abs() + 1e-30, "dK")
+                t[at:at + most] = 0
+        assert torch.equal(got, want), i
