@@ -9,6 +9,7 @@ from gpu_util import say
 from paper_2512_08061_amd import luna
 from seq_util import U32, assert_within, cut, decay_grads, device, packed_offsets, rand, unit
 from test_gpu_decay import EPS, check_forward as check_decay, decays
+from test_gpu_softmax import check_backward as check_softmax_grads, check_forward as check_softmax
 
 pytestmark = pytest.mark.gpu
 
@@ -116,3 +117,59 @@ def test_thousands_of_packed_sequences(count):
                 assert_within(t[at:at + most].transpose(0, 1), ref, (5 * u + (2 * most + 2 * d + 32) * U32) * size + u * ref.abs() + 1e-30, "dK")
                 t[at:at + most] = 0
         assert torch.equal(got, want), i
+
+
+@pytest.mark.parametrize("H,d,layout", [(32, 64, "packed"), (32, 128, "packed"), (64, 64, "packed"), (48, 128, "batch")])
+def test_gradients_of_shared_key_heads_without_parts(H, d, layout):
+    """Enough key tiles that a workgroup takes all query heads of a key head, one after the other, instead of leaving fp32 parts."""
+    say(f"shared key heads without parts: H={H} d={d} {layout}")
+    Hk, lens = 16, [(29 * i) % 131 for i in range(70)]
+    gen = torch.Generator(device=device()).manual_seed(24)
+    shape = (lambda h: (sum(lens), h, d)) if layout == "packed" else (lambda h: (len(lens), h, max(lens), d))
+    Q, dO = (rand(shape(H), torch.bfloat16, gen) for _ in range(2))
+    K, V = (rand(shape(Hk), torch.bfloat16, gen) for _ in range(2))
+    index = packed_offsets(lens) if layout == "packed" else torch.tensor(lens, dtype=torch.int32, device=device())
+    opt = {"offsets" if layout == "packed" else "lens": index}
+    rows = sum(lens) if layout == "packed" else max(lens)
+    seqs = (ctypes.c_int64 * 4)(len(lens), rows, *((index.data_ptr(), 0) if layout == "packed" else (0, index.data_ptr())))
+    nb = luna.load_library().luna_seq_workspace_bytes(luna.OP_SOFTMAX_BWD, luna.LUNA_BF16, ctypes.addressof(seqs), None, H, Hk, d, d)
+    numbers = Q[..., 0].numel() * 4
+    assert nb == (numbers + 255) // 256 * 256, "dO.out per row and nothing else"
+    out, lse = luna.softmax_attn(Q, K, V, **opt)
+    check_softmax(Q, K, V, out, lse, layout, lens)
+    check_softmax_grads(Q, K, V, dO, luna.softmax_attn_bwd(Q, K, V, out, lse, dO, **opt), layout, lens)
+
+
+@pytest.mark.parametrize("m,H,Hk", [(4, 6, 1), (11, 4, 2), (1, 48, 1), (16, 4, 1), (64, 1, 1), (8, 16, 2)])
+@pytest.mark.parametrize("d,dtype", [(32, "bf16"), (64, "bf16"), (128, "bf16"), (32, "f32"), (64, "f32"), (128, "f32")])
+def test_rows_of_a_key_head_over_a_cache(m, H, Hk, d, dtype):
+    """24 to 64 query rows per key head (two and four tiles of rows), over caches of several pieces, short and empty ones."""
+    say(f"rows of a key head over a cache: m={m} H={H} Hk={Hk} d={d} {dtype}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    klens = [1300, 129, 40, 3, 0, 512]
+    gen = torch.Generator(device=device()).manual_seed(25)
+    Q = rand((len(klens), H, m, d), dt, gen)
+    K, V = (rand((len(klens), Hk, 1310, d), dt, gen) for _ in range(2))
+    for t in (K, V):
+        for i, n in enumerate(klens):
+            t[i, :, n:] = float("nan")
+    k_lens = torch.tensor(klens, dtype=torch.int32, device=device())
+    out, lse = luna.softmax_attn(Q, K, V, k_lens=k_lens)
+    check_softmax(Q, K, V, out, lse, "batch", [m] * len(klens), klens)
+    few = [min(m, i) for i in (1, 0, m, 3, 2, m)]  # padded queries
+    out, lse = luna.softmax_attn(Q, K, V, lens=torch.tensor(few, dtype=torch.int32, device=device()), k_lens=k_lens)
+    check_softmax(Q, K, V, out, lse, "batch", few, klens)
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "f32")])
+def test_many_query_heads_on_one_key_head(d, dtype):
+    """128 query heads of one key head, a token and three over a cache: more rows than the split form takes."""
+    say(f"many query heads on one: d={d} {dtype}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    klens = [700, 1, 130]
+    gen = torch.Generator(device=device()).manual_seed(26)
+    K, V = (rand((3, 1, 700, d), dt, gen) for _ in range(2))
+    for m in (1, 3):
+        Q = rand((3, 128, m, d), dt, gen)
+        out, lse = luna.softmax_attn(Q, K, V, k_lens=torch.tensor(klens, dtype=torch.int32, device=device()))
+        check_softmax(Q, K, V, out, lse, "batch", [m] * 3, klens)
