@@ -245,11 +245,6 @@ inline bool softmax_splits(const SeqSet& qs, const SeqSet& ks, int64_t H, int64_
   return !qs.offsets && qs.rows * (H / Hk) <= kSplitRows && ks.rows > 128;
 }
 hipError_t launch_softmax_split(Dt dt, const SoftmaxArgs& a, hipStream_t s);
-// Whether dK and dV are formed per query head, in fp32 parts that are added up: where key tiles and heads alone
-// would not fill the compute units a few times over (their work is very unequal: early keys are seen by more queries).
-inline bool softmax_head_parts(Dt dt, const SeqSet& ks, int64_t H, int64_t Hk, int64_t d) {
-  return dt == Dt::BF16 && d >= 64 && H > Hk && seq_slots(ks, 128) * Hk < 1024;
-}
 hipError_t launch_softmax_bwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 
 }  // namespace luna

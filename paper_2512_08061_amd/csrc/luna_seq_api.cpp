@@ -201,6 +201,27 @@ luna_status run_decay_rows(luna::Dt dt, int mode, const luna::DecayArgs& a, hipS
 // softmax
 // ---------------------------------------------------------------------------
 
+// Whether dK and dV are formed per query head, in fp32 parts that are added up.  Without parts a workgroup walks the queries
+// of a key tile for every head of the group: the longest chain is group * n / 64 steps of about 2.1 us (d = 128; 1.35 with 64).
+// Parts divide the chains by the group, down to the mean of all steps over 256 compute units.  They cost their bytes
+// (written and read, 1.7 MB a us), or at least the sum's chain of 32 (16) rounds of loads per head of the group, and 8 us per
+// workgroup and compute unit.  Packed sequences are taken as of their mean length.  Measured, us without and with parts, d = 128:
+// 8192 tokens, 16 heads on 4 1482 and 1097; 32 heads on 4, 4096 tokens 1261 and 637, 1024 tokens 313 and 173, but 256 tokens
+// 93 and 121, 16 x 512 tokens 259 and 459, 6 x 4096 3339 and 3780, 64 queries behind 16000 keys 598 and 915.  So the parts
+// never hold more than 512 key tiles' rows: 64 MiB (d = 128) times the query heads of a group.
+bool softmax_head_parts(luna::Dt dt, const luna::SeqSet& qs, const luna::SeqSet& ks, int64_t H, int64_t Hk, int64_t d) {
+  if (dt != luna::Dt::BF16 || d < 64 || H == Hk) return false;
+  const double group = (double)(H / Hk), width = (double)d / 128;
+  const double nq = qs.offsets ? (double)qs.rows / (double)qs.count : (double)qs.rows;
+  const double nk = ks.offsets ? (double)ks.rows / (double)ks.count : (double)ks.rows;
+  const double tiles = (double)ks.count * std::ceil(nk / 128);
+  const double seen = nq < nk ? 1.0 - nq / (2 * nk) : 0.5;  // of the queries, by a key tile in the mean
+  const double chain = group * nq / 64 * (d == 64 ? 1.35 : 2.1);
+  const double saved = chain * (1.0 - tiles * (double)Hk * seen / 256);
+  const double bytes = (double)ks.count * nk * (double)H * 2 * (double)d * 4;
+  return saved > std::max(bytes / 1.7e6, 11.5 * width * group) + 8.0 * tiles * (double)H / 256 + 6.0;
+}
+
 luna_status check_softmax(luna_dtype dt, const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d,
                           float scale, bool backward) {
   luna_status st = check_type(dt);
@@ -219,7 +240,7 @@ luna_status check_softmax(luna_dtype dt, const luna_seqs* seqs, const luna_seqs*
   bool fits;
   if (backward) {
     fits = launchable(qtiles * H, 256) &&
-           launchable(ktiles * (luna::softmax_head_parts(t, ks, H, Hk, d) ? H : Hk), tile == 128 ? 512 : 256);
+           launchable(ktiles * (softmax_head_parts(t, qs, ks, H, Hk, d) ? H : Hk), tile == 128 ? 512 : 256);
   } else if (luna::softmax_splits(qs, ks, H, Hk)) {
     fits = launchable(luna::seq_slots(ks, luna::kSplitKeys) * Hk, 256) && launchable(qs.count * H * qs.rows, (int)d);
   } else {
@@ -250,7 +271,7 @@ int64_t all_rows(const luna_seqs& s) { return s.offsets ? s.rows : s.count * s.r
 size_t delta_bytes(const luna_seqs* seqs, int64_t H) { return align256((size_t)all_rows(*seqs) * H * 4); }
 size_t head_part_bytes(luna_dtype dt, const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d) {
   const luna_seqs* ks = keys ? keys : seqs;
-  if (!luna::softmax_head_parts(type_of(dt), set_of(ks), H, Hk, d)) return 0;
+  if (!softmax_head_parts(type_of(dt), set_of(seqs), set_of(ks), H, Hk, d)) return 0;
   return align256((size_t)all_rows(*ks) * H * 2 * d * 4);
 }
 

@@ -173,3 +173,26 @@ def test_many_query_heads_on_one_key_head(d, dtype):
         Q = rand((3, 128, m, d), dt, gen)
         out, lse = luna.softmax_attn(Q, K, V, k_lens=torch.tensor(klens, dtype=torch.int32, device=device()))
         check_softmax(Q, K, V, out, lse, "batch", [m] * 3, klens)
+
+
+@pytest.mark.parametrize("lens,klens,H,Hk,d,layout", [([512], None, 32, 4, 128, "batch"), ([1024, 700], None, 16, 2, 64, "packed"),
+                                                      ([600], [1500], 16, 1, 128, "batch"), ([1100, 900], None, 12, 2, 128, "packed")])
+def test_gradients_of_shared_key_heads_from_parts(lens, klens, H, Hk, d, layout):
+    """Few key tiles and long chains: a workgroup per query head, whose fp32 parts are added up."""
+    say(f"shared key heads from parts: {lens} {klens} H={H} Hk={Hk} d={d} {layout}")
+    gen = torch.Generator(device=device()).manual_seed(27)
+    shape = (lambda ls, h: (sum(ls), h, d)) if layout == "packed" else (lambda ls, h: (len(ls), h, max(ls), d))
+    Q, dO = (rand(shape(lens, H), torch.bfloat16, gen) for _ in range(2))
+    K, V = (rand(shape(klens or lens, Hk), torch.bfloat16, gen) for _ in range(2))
+    opt = {"offsets": packed_offsets(lens)} if layout == "packed" else {}
+    if klens:
+        opt["k_lens"] = torch.tensor(klens, dtype=torch.int32, device=device())
+    seqs = (ctypes.c_int64 * 4)(len(lens), sum(lens) if layout == "packed" else max(lens), 1 if layout == "packed" else 0, 0)
+    keys = (ctypes.c_int64 * 4)(len(klens), max(klens), 0, 1) if klens else None
+    nb = luna.load_library().luna_seq_workspace_bytes(luna.OP_SOFTMAX_BWD, luna.LUNA_BF16, ctypes.addressof(seqs),
+                                                      None if keys is None else ctypes.addressof(keys), H, Hk, d, d)
+    assert nb > Q[..., 0].numel() * 4 + K[..., 0].numel() * (H // Hk) * 2 * d * 4 - 1, "fp32 rows of every query head"
+    out, lse = luna.softmax_attn(Q, K, V, **opt)
+    grads = luna.softmax_attn_bwd(Q, K, V, out, lse, dO, **opt)
+    check_softmax_grads(Q, K, V, dO, grads, layout, lens, klens)
+    assert all(torch.equal(a, b) for a, b in zip(grads, luna.softmax_attn_bwd(Q, K, V, out, lse, dO, **opt)))

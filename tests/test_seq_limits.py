@@ -139,3 +139,33 @@ def test_states_of_sequences_are_apart_and_within(tmp_path):
                     str(src), "-o", str(exe)], check=True, capture_output=True)
     p = subprocess.run([str(exe)], capture_output=True, text=True)
     assert p.returncode == 0, p.stdout
+
+
+def parts(q, keys, H, Hk, d):
+    """Bytes of the fp32 parts of the backward call beside one number per query row (a refused call: 2^32 threads, has none)."""
+    nb, why = workspace(luna.OP_SOFTMAX_BWD, q, keys, H, Hk, d)
+    if "too many" in why:
+        return 0
+    assert not why
+    rows = q[1] if q[2] else q[0] * q[1]
+    return nb - (rows * H * 4 + 255) // 256 * 256
+
+
+def test_parts_of_shared_key_heads_are_bounded():
+    """Never more than the rows of 512 key tiles, for any length, batch and group, and none where queries are few."""
+    taken = 0
+    for d in (64, 128):
+        for group in (2, 4, 8, 32):
+            for Hk in (1, 2, 8):
+                for count in (1, 3, 16, 200):
+                    for n in (64, 500, 2048, 8192, 30000, 130000):
+                        most = 512 * 128 * group * 2 * d * 4
+                        for packed in (False, True):
+                            nb = parts(seqs(count, n * count if packed else n, offsets=packed), None, group * Hk, Hk, d)
+                            assert 0 <= nb <= most
+                            taken += nb > 0
+                        if n > 2048:  # keys of a cache: queries see nearly all of them
+                            assert parts(seqs(count, 64), seqs(count, n, lens=True), group * Hk, Hk, d) <= most // 2
+    assert taken > 50
+    assert parts(seqs(1, 130000), None, 32, 1, 128) == 0 and parts(seqs(1, 64), seqs(1, 65000, lens=True), 32, 1, 128) == 0
+    assert parts(seqs(1, 8192), None, 16, 4, 128) == 8192 * 16 * 2 * 128 * 4
