@@ -66,7 +66,7 @@ struct DecayLds {
   float z[DK];
   int since[DVW];  // per column: the first token with a value that is not finite
   f32x4 o[FS > 1 ? DVW / 16 : 1][FS][C / 32][kWave];  // half of out's tiles, from one such wave to the other
-  T one[4][C];  // the parts of f^(m-1-j) w_j, times b_j in state passes, and zeros
+  T one[4][C];  // three parts and zeros: of f^(m-1-j) w_j, times b_j in state passes; kDecayAug: of b_j
 };
 
 // Rows of one tensor on their way from memory to LDS: C rows of width w (at most W), rows past m and columns past w as
@@ -218,7 +218,7 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
   float* st = a.states ? a.states + ((int64_t)state * a.H + head) * sf : nullptr;  // (not touched where the sequence has one piece)
   const int64_t user = (int64_t)sp.seq * a.H + head;
   const int mycol = wcol + c;
-  f32x4 S[FT], za = zero4();  // za: row 0 is the further key component's row of S (kDecayAug)
+  f32x4 S[FT], za = zero4();  // za: rows 0 to 2 add up to the further key component's row of S (kDecayAug; its parts, in bf16)
 #pragma unroll
   for (int ft = 0; ft < FT; ++ft) S[ft] = zero4();
   if (MODE == kDecayNorm) {
@@ -260,7 +260,7 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
           const int k = wfeat + 16 * ft + 4 * g + j;
           if (k < a.dk) S1[(int64_t)k * a.dv + col0 + mycol] = lost ? __builtin_nanf("") : S[ft][j];
         }
-      if (MODE == kDecayAug && g == 0) z1[col0 + mycol] = lost ? __builtin_nanf("") : za[0];
+      if (MODE == kDecayAug && g == 0) z1[col0 + mycol] = lost ? __builtin_nanf("") : za[0] + za[1] + za[2];
     }
     if (MODE == kDecayNorm && slice == 0)
       for (int k = tid; k < a.dk; k += THREADS) z1[k] = l.z[k];
@@ -280,8 +280,8 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
         l.ka[tid] = in ? ka : 0.0f;
         if (OUT) l.qa[tid] = in ? qa : 0.0f;
       }
-      if (MODE == kDecayNorm) {  // the discounts of z (times b_j), bf16: in three parts
-        const float x = l.dec[tid] * (OUT ? 1.0f : ka);
+      if (MODE != kDecayPlain) {  // the discounts of z (times b_j) or b_j, bf16: in three parts
+        const float x = MODE == kDecayAug ? l.ka[tid] : l.dec[tid] * (OUT ? 1.0f : ka);
         const T part0 = (T)x, part1 = (T)(x - (float)part0);
         l.one[0][tid] = part0;
         l.one[1][tid] = part1;
@@ -363,15 +363,20 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
         }
       }
       if (MODE == kDecayAug) {
-        Frag<T> zf;
+        const float z = g == 0 ? za[0] + za[1] + za[2] : 0.0f;
+        Frag<T> zf;  // (z and a_i in two parts each: one rounding of either would be 2^-9 of sums that nearly cancel)
         zf.zero();
-        zf.set(0, g == 0 ? za[0] : 0.0f);
+        zf.set(0, z);
+        zf.set(1, z);
+        zf.set(2, z - (float)(T)z);
 #pragma unroll
         for (int qt = 0; qt < KT; ++qt) {
-          const float x = l.qa[16 * qt + c];
           Frag<T> qf;
+          const float x = l.qa[16 * qt + c];
           qf.zero();
-          qf.set(0, g == 0 ? x : 0.0f);
+          qf.set(0, x);
+          qf.set(1, x - (float)(T)x);
+          qf.set(2, x);
           mma(o[qt], zf, qf);
         }
       }
@@ -391,7 +396,8 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
       for (int ft = 0; ft < FT; ++ft)
 #pragma unroll
         for (int j = 0; j < 4; ++j) S[ft][j] *= f;
-      za[0] *= f;
+#pragma unroll
+      for (int j = 0; j < 3; ++j) za[j] *= f;
     }
     constexpr int ZT = (FT + NW - 1) / NW;  // tiles of z per wave
     f32x4 zacc[ZT];
@@ -440,12 +446,7 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
       }
       if (MODE == kDecayAug) {
         Frag<T> kf;
-        kf.zero();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = l.ka[32 * ks + 8 * g + e];
-          kf.set(e, c == 0 ? x : 0.0f);
-        }
+        load8(kf, &l.one[min(c, 3)][32 * ks + 8 * g]);
         vs.mma_into(za, kf, EXACT);
       }
     }

@@ -196,3 +196,39 @@ def test_gradients_of_shared_key_heads_from_parts(lens, klens, H, Hk, d, layout)
     grads = luna.softmax_attn_bwd(Q, K, V, out, lse, dO, **opt)
     check_softmax_grads(Q, K, V, dO, grads, layout, lens, klens)
     assert all(torch.equal(a, b) for a, b in zip(grads, luna.softmax_attn_bwd(Q, K, V, out, lse, dO, **opt)))
+
+
+@pytest.mark.parametrize("n,D,d", [(200, 64, 64), (200, 128, 128), (250, 32, 64)])
+def test_gradients_where_values_are_equal(n, D, d):
+    """bf16, all values 1, so that out is 1 and dO.v - dO.out is 0 in every term: dQ and dK are 0 up to fp32 sums and the two
+    parts of 2^-9 each in which dO.out meets the state.  (Queries and keys are small whole numbers and nothing decays, so that
+    weights, sums of keys and the state are whole numbers up to 256: exact in bf16.)"""
+    say(f"gradients where values are equal: n={n} D={D} d={d}")
+    H, gen = 2, torch.Generator(device=device()).manual_seed(28)
+    Q, K = (torch.randint(0, 2, (1, H, n, D), generator=gen, device=device()).to(torch.bfloat16) for _ in range(2))
+    Q[..., 0], K[..., 0] = 1, 1
+    V, dO = torch.ones((1, H, n, d), dtype=torch.bfloat16, device=device()), rand((1, H, n, d), torch.bfloat16, gen)
+    g = torch.zeros(H, device=device())
+    out, den = luna.decay_attn(Q, K, V, g, normalize=True, eps=EPS)
+    assert (out == 1).all()
+    dQ, dK, _ = luna.decay_attn_bwd(Q, K, V, dO, g, out=out, den=den, normalize=True, eps=EPS)
+    q, k, do = (t[0].double() for t in (Q, K, dO))
+    z, w = k.cumsum(1), 1 / den[0].double()
+    total, size = do.sum(-1), do.abs().sum(-1)  # |dO.out| and the sum that forms it
+    # two parts of both factors leave 3 2^-18 of a product; P's terms are 2^-24 sums, rounded once more
+    each = 3 * 2.0 ** -18 * total.abs() + (n + 2 * d + 16) * U32 * size
+    assert_within(dQ[0], torch.zeros_like(q), (each * w)[..., None] * z + 1e-30, "dQ")
+
+    # dK behind one query with a weight of 2^-8: dO / 256 is exact in bf16 as the state, its sum is not
+    Q = torch.zeros_like(Q)
+    K = torch.zeros_like(K)
+    K[..., 0] = 1
+    at = 127
+    Q[:, :, at, 0] = 2
+    dO[:, :, at] = rand((1, H, d), torch.bfloat16, gen)
+    out, den = luna.decay_attn(Q, K, V, g, normalize=True, eps=1e-30)
+    assert (out[:, :, at] == 1).all() and (den[:, :, at] == 256).all()
+    _, dK, _ = luna.decay_attn_bwd(Q, K, V, dO, g, out=out, den=den, normalize=True, eps=1e-30)
+    do = dO[0, :, at].double()
+    each = (3 * 2.0 ** -18 * do.sum(-1).abs() + (n + 2 * d + 16) * U32 * do.abs().sum(-1)) * 2 / 256
+    assert_within(dK[0], torch.zeros_like(k), each[:, None, None].expand_as(k), "dK")
