@@ -239,6 +239,7 @@ __global__ __launch_bounds__(kCkThreads, KB <= 4 ? 4 : 2) void chunk_kernel(Chun
         mma(den, za, xb);
       }
     }
+    if (PASS == kPassQuery) mma_settle();
     if (dwave && g == 0) deni[16 * wave + r] = den[0];
   }
 

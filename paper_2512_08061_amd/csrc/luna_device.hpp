@@ -58,6 +58,14 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// Between fp32 matrix products (10 wait states until their results lie in the registers) and a conditional block or a
+// branch before those registers' first use: on a path around such a block the compiler has left out some of the waits.
+__device__ __forceinline__ void mma_settle() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 9");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // ---------------------------------------------------------------------------
 // piecewise-linear tables (layout shared with the host and luna_prepare.hip)
 // ---------------------------------------------------------------------------

@@ -264,6 +264,7 @@ __global__ __launch_bounds__((map_threads<T, DH, L, PACK>())) void map_bwd_kerne
         for (int cb = 0; cb < CB; ++cb) mma(dx[i][cb], wt[PACK ? i : mb / 2][cb][lane], di);
       }
     }
+    mma_settle();  // (no lane may have a row to store)
     if (!want_dx) continue;
     T* dX = reinterpret_cast<T*>(key ? a.dxk : a.dxq);
 #pragma unroll
