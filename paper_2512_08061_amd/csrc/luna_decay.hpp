@@ -118,14 +118,6 @@ struct DecayRows {
   }
 };
 
-// x summed over the four lane groups
-__device__ __forceinline__ float sum_groups(float x) {
-  auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-  p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
-}
-
 // The scaled values of a fragment as one operand (fp32) or in parts (bf16: two, or three where exact).
 template <typename T>
 struct DecayScaled;
@@ -339,7 +331,7 @@ __global__ __launch_bounds__((kDecayThreads<DK, DVW>), (kDecayWaves<T, DK, DVW, 
                    acc[2] - (float)(T)acc[2], acc[3] - (float)(T)acc[3]);
         }
         if (MODE == kDecayNorm) {
-          den = sum_groups(den);
+          den = groups_sum(den);
           if (g == 0) l.den[share][i] = den;
         }
       }

@@ -143,6 +143,14 @@ __device__ __forceinline__ int64_t seq_num(const SeqSet& s, const SeqPiece& p, i
 // compiler left out the wait states on the path around it, and the reads came too early.)
 __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// x summed over the four lane groups of 16
+__device__ __forceinline__ float groups_sum(float x) {
+  auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
 // Decay factor's exponent: log_decay within [-1e30, 0], so that multiples of it stay defined (0 times it
 // is 0), in base 2; NaN stays NaN.
 __device__ __forceinline__ float decay_log2(float g) {

@@ -30,12 +30,6 @@ __device__ __forceinline__ void softmax_load_frags(Frag<T> (&f)[DH / 32], const 
 }
 
 // x over the four lane groups
-__device__ __forceinline__ float groups_sum(float x) {
-  auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-  p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
-}
 __device__ __forceinline__ float groups_max(float x) {
   auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   x = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
