@@ -121,6 +121,8 @@ luna_status luna_decay_step(const luna_rows* Q, const luna_rows* K, const luna_r
  * Gradients of luna_decay_fwd from S == NULL: for dO = dL/dout writes dQ, dK (width D) and
  * dV (width d); log_decay gets none.  With normalize 1, out and den are what the forward call
  * wrote (out in the call's type); with normalize 0 they are not read and may be NULL.
+ * Precision as in the forward call; the weights and their gradients are rounded to bf16 once as operands, dO.out
+ * meets the sums before a chunk in parts (2^-17).
  */
 luna_status luna_decay_bwd(const luna_rows* Q, const luna_rows* K, const luna_rows* V, const luna_rows* dO,
                            luna_dtype dtype, const luna_seqs* seqs, int64_t H, int64_t D, int64_t d,
@@ -139,7 +141,11 @@ luna_status luna_decay_bwd(const luna_rows* Q, const luna_rows* K, const luna_ro
  * Q, K, V, out: width d in {32, 64, 128}; K and V have Hk heads (H a multiple of Hk).
  * lse (may be NULL): fp32 per query row, which the backward pass takes.
  * LUNA_BF16 rounds P to bf16 as an operand of the product with V; scores, maxima and
- * sums are fp32.  Calls with few queries over long keys (decoding) split the keys.
+ * sums are fp32.
+ * Calls of equal or padded query sequences with at most 64 query rows per key head (rows * H / Hk: the next tokens
+ * over a cache) and room for more than 128 keys read the keys in pieces of 512 side by side, each once for all
+ * query heads of a key head.  All others, among them packed queries and larger groups, take the keys one
+ * block after the other for 128 query rows of a head (64: LUNA_F32 and d = 32), however few of these there are.
  */
 luna_status luna_softmax_fwd(const luna_rows* Q, const luna_rows* K, const luna_rows* V, luna_dtype dtype,
                              const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d,

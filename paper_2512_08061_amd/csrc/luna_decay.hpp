@@ -33,10 +33,10 @@
 // fp32 accuracy.  With 256 features and up to 64 columns two waves share the features of 16 columns (four waves alone
 // leave a SIMD one each: 249 -> 157 us for 4 x 16 heads of 4096 tokens); with 128 columns that was no faster (384 -> 390).
 //
-// Measured: 8 x 16 heads of 16384 tokens, D = d = 128: 706 us, of which state pass 190, scan 11, row pass 500 (1.3 GB at
-// 2.6 TB/s; LDS active 68% of the time).  Six packed prompts, 16 heads, 256 features, with denominators: 342 us (78, 23,
-// 244); matrix cores 14% busy, bound by the chain of a chunk, one workgroup a compute unit, and the count of
-// pieces over the compute units.
+// Measured: 8 x 16 heads of 16384 tokens, D = d = 128: 708 us, of which state pass 190, scan 11, row pass 500 (2.1 GB at
+// 4.2 TB/s; LDS active 61% of all cycles).  Six packed prompts, 16 heads, 256 features, with denominators: 341 us (77, 23,
+// 242); matrix cores 14% busy, bound by the chain of a chunk, one workgroup a compute unit, and 560 pieces over 256
+// compute units.
 #pragma once
 
 #include "luna_seq.hpp"
@@ -149,9 +149,10 @@ struct DecayScaled<__bf16> {
 template <int DK, int DVW>
 constexpr int kDecayThreads = decay_threads(DK, DVW);
 
-// Waves per SIMD: two workgroups of a compute unit where the registers suffice (128 features without denominators: 546 ->
-// 487 us of the long batch's row pass).  The others would spill (128 features and 64 columns, whose half as many waves carry
-// twice the rows in flight: 254 -> 517 us for 8 x 16 heads of 8192 tokens).
+// Waves per SIMD: two workgroups of a compute unit where the registers suffice or nearly so (128 features without
+// denominators: 546 -> 487 us of the long batch's row pass, with 2 registers spilled; of those with 64 features up to 3 spill,
+// 10 of 64 plain bf16 columns that return a state).  The others would spill more (128 features and 64 columns, whose half as
+// many waves carry twice the rows in flight: 254 -> 517 us for 8 x 16 heads of 8192 tokens).
 template <typename T, int DK, int DVW, int MODE, bool EXACT>
 constexpr int kDecayWaves = DK <= 64 || (DK == 128 && DVW == 128 && MODE == kDecayPlain && !EXACT) ? 4 : 2;
 

@@ -7,7 +7,8 @@
 // S for the features group + 32 i in registers for the whole step, so that a call reads the state
 // once and writes it once with 16-byte accesses, which is what bounds it.  Every group has its
 // share of each sum over features; the shares are added within a wave by lane exchanges and over the
-// waves through LDS, in a fixed order.  Measured: 64 sequences of 16 heads, states of 256 x 128: 48 us for 270 MB (5.6 TB/s);
+// waves through LDS, in a fixed order.  Measured: 64 sequences of 16 heads, states of 256 x 128: 60 us for 270 MB (4.5 TB/s)
+// with other states in between, 48 us again and again on one state, half of which then lies in the last-level cache;
 // 8 sequences, 128 x 128: 5.5 us.  Normalised calls take all columns of a head in one
 // workgroup: each of several would read z while one of them writes it.
 #include "luna_seq.hpp"

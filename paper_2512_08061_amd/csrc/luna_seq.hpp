@@ -247,7 +247,8 @@ struct SoftmaxArgs {
 constexpr int softmax_tile(Dt dt, int64_t d) { return dt == Dt::BF16 && d >= 64 ? 128 : 64; }
 hipError_t launch_softmax_fwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 // Few queries over long keys: m tokens of equal or padded sequences, up to 64 rows per key head, whose keys
-// then share one read of the cache; cut in pieces of kSplitKeys keys.
+// then share one read of the cache; cut in pieces of kSplitKeys keys.  (Packed queries, whose lengths the host does not see,
+// and more rows take the tile kernels, a chain of all key blocks each.)
 constexpr int kSplitKeys = 512, kSplitRows = 64;
 inline bool softmax_splits(const SeqSet& qs, const SeqSet& ks, int64_t H, int64_t Hk) {
   return !qs.offsets && qs.rows * (H / Hk) <= kSplitRows && ks.rows > 128;

@@ -105,7 +105,8 @@ struct DecayPlan {
 // Tokens per piece.  A piece is a serial chain of chunks, so cutting sequences fills the device; but pieces cost a pass
 // over the keys and values of all but each sequence's last one, and their states written, scanned and read.  Estimated
 // from: a 64-token chunk about 4 us with 128 features and d = 128 in bf16, three times as much in fp32, one workgroup
-// a compute unit (two with 64 features), and a sixth more while no second one fills its waits; 4.5 TB/s.  Measured, us a
+// a compute unit (two with 64 features; the plain bf16 pass of 128 features and columns, which also runs two, is counted as
+// one), and a sixth more while no second one fills its waits; 4.5 TB/s.  Measured, us a
 // call by piece: 8 x 16 heads of 16384 tokens, D = d = 128, one 1070, 4096 683, 2048 726, 1024 783; backward of 2 x 16
 // heads of 2048 tokens with 256 features 128 289, 256 214, 384 244, 512 222; fp32 backward of 4096 tokens in 12 heads, 64
 // features, 64 114, 128 101, 256 118.  How lengths fall into pieces is on the device and not known here (six packed prompts

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256) void softmax_fwd_kernel(SoftmaxArgs a) {
 // are the k-slots of its half for the product with V.  The next block is on its way to registers while one is worked on.
 // The output is rescaled only when some row's maximum has grown by more than 2^8 since its last rescaling (a sum of
 // at most 2^8 times larger terms keeps its relative accuracy), which most blocks skip.
-// Packed prompts of up to 16384 tokens, 16 heads of 128 on 4: 1450 to 1490 us on different cards, 970 TFLOP/s over the
+// Packed prompts of up to 16384 tokens, 16 heads of 128 on 4: 1450 to 1550 us on different cards, 925 to 970 TFLOP/s over the
 // visible pairs; matrix cores 47% busy, the rest the exponentials and maxima between the two products, at two waves a SIMD.
 // With GROUPS = 2 two groups of four waves take the key blocks in turn, each with its own maxima, sums and rows, which are
 // joined at the end: the last tile of a sequence is a chain half as long.

@@ -342,7 +342,8 @@ __global__ __launch_bounds__(256, 2) void softmax_dq32_kernel(SoftmaxArgs a) {
 // that factor until the gradients are stored.  Either wave does the same two products (its rows against a tile, a
 // transposed tile against its result) with half of the operands and gradients, so that two
 // waves fit a SIMD; one wave with all of them took 490 registers, moved half of them about and reached 20% of the matrix
-// cores' time.  8192 tokens, 16 heads of 128 on 4: 585 us (the query pass 418, the sum 47), matrix cores 38% busy.  With parts a
+// cores' time.  8192 tokens, 16 heads of 128 on 4: 590 to 627 us on different cards (the query pass 425 to 456, the sum 46),
+// matrix cores 37% busy; with d = 128 3 registers spill (query pass: 5).  With parts a
 // workgroup takes one query head and leaves fp32 rows there, which softmax_sum_kernel adds up.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int kKeyShift = 15;  // P times 2^15 in the key pass

@@ -112,14 +112,14 @@ def test_the_walk_finds_what_it_looks_for():
     assert not list(early(blocks))
 
 
-SOURCES = ["luna_chunk_query.hip", "luna_chunk_key.hip", "luna_map_backward.hip", "luna_decay_bf16_aug.hip", "luna_decay_f32_aug.hip",
-           "luna_softmax.hip", "luna_softmax_split.hip", "luna_softmax_bwd.hip"]
+SOURCES = ["luna_chunk_query.hip", "luna_chunk_key.hip", "luna_map_backward.hip", "luna_softmax.hip", "luna_softmax_split.hip",
+           "luna_softmax_bwd.hip"] + [f"luna_decay_{t}_{m}.hip" for t in ("bf16", "f32") for m in ("plain", "norm", "aug")]
 
 
 @pytest.fixture(scope="module")
 def texts(tmp_path_factory):
     folder = tmp_path_factory.mktemp("assembly")
-    with cf.ThreadPoolExecutor(4) as pool:
+    with cf.ThreadPoolExecutor(8) as pool:
         return dict(zip(SOURCES, pool.map(lambda s: assembly(s, str(folder / (s + ".s"))), SOURCES)))
 
 
