@@ -139,7 +139,8 @@ luna_status plan_decay(luna_dtype dt, const luna_seqs& s, int64_t H, int64_t D, 
   const int64_t slots = luna::seq_slots(set, p->piece);
   const int dk = (int)D, dv = (int)d;  // (the other way round: dQ and dK)
   if (!launchable(luna::decay_groups(slots, H, dv), luna::decay_threads(dk, dv)) ||
-      (backward && !launchable(luna::decay_groups(slots, H, dk), luna::decay_threads(dv, dk))))
+      (backward && !launchable(luna::decay_groups(slots, H, dk), luna::decay_threads(dv, dk))) ||
+      (backward && normalize && !launchable(luna::seq_slots(set, 64), 256)))
     return set_error(LUNA_ERR_UNSUPPORTED, "too many pieces of sequences and heads");
   p->slots = (int)slots;
   size_t off = 0;

@@ -169,3 +169,11 @@ def test_parts_of_shared_key_heads_are_bounded():
     assert taken > 50
     assert parts(seqs(1, 130000), None, 32, 1, 128) == 0 and parts(seqs(1, 64), seqs(1, 65000, lens=True), 32, 1, 128) == 0
     assert parts(seqs(1, 8192), None, 16, 4, 128) == 8192 * 16 * 2 * 128 * 4
+
+
+def test_row_weights_of_very_long_sequences():
+    """The backward pass's weights take a workgroup of 256 threads per 64 rows."""
+    _, why = workspace(luna.OP_DECAY_BWD, seqs(1, (1 << 30) - 128, offsets=True), H=1, Dq=32, Dv=32)
+    assert not why
+    nb, why = workspace(luna.OP_DECAY_BWD, seqs(1, 1 << 30, offsets=True), H=1, Dq=32, Dv=32)
+    assert nb == 0 and "too many" in why
