@@ -203,25 +203,31 @@ luna_status run_decay_rows(luna::Dt dt, int mode, const luna::DecayArgs& a, hipS
 // softmax
 // ---------------------------------------------------------------------------
 
+// Pairs of a query and a key that it sees.
+double seen_pairs(double nq, double nk) { return nq <= nk ? nq * nk - nq * nq / 2 : nk * nk / 2; }
+
 // Whether dK and dV are formed per query head, in fp32 parts that are added up.  Without parts a workgroup walks the queries
 // of a key tile for every head of the group: the longest chain is group * n / 64 steps of about 2.1 us (d = 128; 1.35 with 64).
 // Parts divide the chains by the group, down to the mean of all steps over 256 compute units.  They cost their bytes
 // (written and read, 1.7 MB a us), or at least the sum's chain of 32 (16) rounds of loads per head of the group, and 8 us per
-// workgroup and compute unit.  Packed sequences are taken as of their mean length.  Measured, us without and with parts, d = 128:
-// 8192 tokens, 16 heads on 4 1482 and 1097; 32 heads on 4, 4096 tokens 1261 and 637, 1024 tokens 313 and 173, but 256 tokens
-// 93 and 121, 16 x 512 tokens 259 and 459, 6 x 4096 3339 and 3780, 64 queries behind 16000 keys 598 and 915.  So the parts
-// never hold more than 512 key tiles' rows: 64 MiB (d = 128) times the query heads of a group.
+// workgroup and compute unit.  Of packed sequences one is taken as three times as long as the mean (by this estimate the pass
+// then takes 1.04 times the better form's time in the mean of 750 random packings; 1.15 with all taken as equal, 1.57 with parts
+// up to 1024 key tiles).  Measured, us of the call without and with parts, d = 128: 8192 tokens, 16 heads on 4 1482 and 1097;
+// 32 heads on 4, 4096 tokens 1261 and 637, 1024 tokens 313 and 173, but 256 tokens 93 and 121, 16 x 512 tokens 259 and 459,
+// 6 x 4096 3339 and 3780, 64 queries behind 16000 keys 598 and 915; packed, 8192 and 50 times 100 tokens 1526 and 1207 (taken
+// without).  Parts hold the rows of 512 key tiles at most: 64 MiB (d = 128) times the query heads of a group.
 bool softmax_head_parts(luna::Dt dt, const luna::SeqSet& qs, const luna::SeqSet& ks, int64_t H, int64_t Hk, int64_t d) {
   if (dt != luna::Dt::BF16 || d < 64 || H == Hk) return false;
-  const double group = (double)(H / Hk), width = (double)d / 128;
-  const double nq = qs.offsets ? (double)qs.rows / (double)qs.count : (double)qs.rows;
-  const double nk = ks.offsets ? (double)ks.rows / (double)ks.count : (double)ks.rows;
-  const double tiles = (double)ks.count * std::ceil(nk / 128);
-  const double seen = nq < nk ? 1.0 - nq / (2 * nk) : 0.5;  // of the queries, by a key tile in the mean
-  const double chain = group * nq / 64 * (d == 64 ? 1.35 : 2.1);
-  const double saved = chain * (1.0 - tiles * (double)Hk * seen / 256);
-  const double bytes = (double)ks.count * nk * (double)H * 2 * (double)d * 4;
-  return saved > std::max(bytes / 1.7e6, 11.5 * width * group) + 8.0 * tiles * (double)H / 256 + 6.0;
+  const double count = (double)qs.count, group = (double)(H / Hk), width = (double)d / 128, step = d == 64 ? 1.35 : 2.1;
+  const auto all = [](const luna::SeqSet& s) { return (double)s.rows * (s.offsets ? 1.0 : (double)s.count); };
+  const auto longest = [&](const luna::SeqSet& s) { return s.offsets ? std::min(3.0 / count, 1.0) * (double)s.rows : (double)s.rows; };
+  const auto other = [&](const luna::SeqSet& s) { return s.count > 1 ? (all(s) - longest(s)) / (count - 1) : 0.0; };
+  const double tiles = count * std::ceil(all(ks) / count / 128);
+  const double pairs = seen_pairs(longest(qs), longest(ks)) + (count - 1) * seen_pairs(other(qs), other(ks));
+  const double chain = group * std::min(longest(qs), longest(ks)) / 64 * step, mean = pairs / (128 * 64) * (double)H / 256 * step;
+  const double bytes = all(ks) * (double)H * 2 * (double)d * 4;
+  return tiles * (double)Hk <= 512 && chain - std::max(chain / group, mean) >
+                                          std::max(bytes / 1.7e6, 11.5 * width * group) + 8.0 * tiles * (double)H / 256 + 6.0;
 }
 
 luna_status check_softmax(luna_dtype dt, const luna_seqs* seqs, const luna_seqs* keys, int64_t H, int64_t Hk, int64_t d,
