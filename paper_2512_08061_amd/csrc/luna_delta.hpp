@@ -1,0 +1,184 @@
+// luna_delta.hpp -- linear attention by the gated delta rule: what its kernels and the host share
+// (luna_delta_*.hip, luna_delta_api.cpp).
+//
+// Per sequence and head, with a_t = exp(log_decay) of the token and its beta,
+//
+//   u_t = beta_t (v_t - a_t S_{t-1}^T k_t),  S_t = a_t S_{t-1} + k_t u_t^T,  out_t = scale S_t^T q_t.
+//
+// A chunk of C = 64 tokens from the state S before it, with G the sums of log decays within it:
+//
+//   M_ij = e^(G_i - G_j) k_i.k_j  (j < i),   P_ij = scale e^(G_i - G_j) q_i.k_j  (j <= i),
+//   R = V - e^G K S,   E = R - M U,  U = beta E   =>   E = R + N (beta R),   N = -M (I + beta M)^-1,
+//   out = scale e^G Q S + P U,   S' = e^(G_C) S + K^T (e^(G_C - G) U).
+//
+// N is strictly lower triangular and so are its factors; it serves the backward pass as well, where from dS' (of the
+// state behind the chunk)
+//
+//   dU = P^T dO + e^(G_C - G) K dS',   X = dU + N^T (beta dU),   dV = beta X,   dbeta = X.E,
+//   dS = e^(G_C) dS' + Q^T (scale e^G dO) - K^T (e^G beta X).
+//
+// N, P and the factors of the gates are formed for all chunks at once (luna_delta_gates.hip); what is left is serial in
+// the chunks but independent for each value column, so a wave takes 16 columns of one head from the first chunk to the
+// last (luna_delta_scan.hip).
+#pragma once
+
+#include "luna_decay.hpp"
+
+namespace luna {
+
+constexpr int kDeltaChunk = 64;
+
+// Per chunk and head: rows of 64 numbers.
+constexpr int kDeltaFirst = 0;  // e^G
+constexpr int kDeltaLast = 1;   // e^(G_C - G)
+constexpr int kDeltaBeta = 2;
+constexpr int kDeltaMisc = 3;  // e^(G_C), then (an int) the first token with a key or gate that is not finite, or 64
+constexpr int kDeltaHigh = 4, kDeltaLow = 5;  // G / ln 2 in two parts, so that differences keep their accuracy
+constexpr int kDeltaGateRows = 6, kDeltaGates = kDeltaGateRows * kDeltaChunk;
+
+// Parts of bf16 that fp32 operands of bf16 calls are split in: two (2^-17 of each operand), three (2^-24) where the
+// state is returned and in the backward pass, whose gradients of the gates are fp32 sums that cancel in part.  P is an operand
+// of `out` alone in the forward pass and is rounded once there.
+constexpr int kDeltaParts = 2, kDeltaExactParts = 3, kDeltaBackParts = 3;
+
+struct DeltaArgs {
+  SeqRows q, k, v, o;  // widths D, D, d, d; o: out, or dO in the backward pass
+  SeqSet s;
+  const float* log_decay;  // per row
+  const float* beta;
+  int H, Hk, D, d;
+  int slots;    // chunks of all sequences (seq_slots)
+  float scale;
+  float* S;     // [count][H][D][d], in and out, or null
+  // workspace, per slot and head
+  char* n;      // [parts][64][64] of the call's type
+  char* p;      // the same
+  float* gates; // [kDeltaGates]
+  float* before;  // backward: [d][D] state before the chunk
+  float* after;   // [d][D] gradient of the state behind it
+  float* e;       // [d][64]
+  float* x;       // [d][64]
+  // gradients
+  SeqRows dq, dk, dv;
+  float* dlog_decay;
+  float* dbeta;
+};
+
+// Slot of the first chunk of a sequence.
+__device__ __forceinline__ int delta_first_slot(const SeqSet& s, const SeqPiece& p) {
+  return s.offsets ? (int)(p.first / kDeltaChunk) + p.seq : p.seq * (int)((s.rows + kDeltaChunk - 1) / kDeltaChunk);
+}
+
+// An fp32 operand as products of type T take it: itself, or P parts in bf16.
+template <typename T, int P>
+struct DeltaOp;
+template <int P>
+struct DeltaOp<float, P> {
+  Frag<float> x;
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x.v[e] = v[e];
+  }
+};
+template <int P>
+struct DeltaOp<__bf16, P> {
+  Frag<__bf16> p[P];
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = v[e];
+#pragma unroll
+    for (int k = 0; k < P; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        p[k].set2(e, r[e], r[e + 1]);
+        r[e] -= p[k].get(e);
+        r[e + 1] -= p[k].get(e + 1);
+      }
+  }
+};
+template <typename T, int P>
+__device__ __forceinline__ void set_tiles(DeltaOp<T, P>& o, const f32x4& lo, const f32x4& hi) {
+  const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  o.set(v);
+}
+template <int P>
+__device__ __forceinline__ void mma(f32x4& c, const Frag<float>& a, const DeltaOp<float, P>& b) { mma(c, a, b.x); }
+template <int P>
+__device__ __forceinline__ void mma(f32x4& c, const DeltaOp<float, P>& a, const Frag<float>& b) { mma(c, a.x, b); }
+template <int P>
+__device__ __forceinline__ void mma(f32x4& c, const Frag<__bf16>& a, const DeltaOp<__bf16, P>& b) {
+#pragma unroll
+  for (int k = P - 1; k >= 0; --k) mma(c, a, b.p[k]);
+}
+template <int P>
+__device__ __forceinline__ void mma(f32x4& c, const DeltaOp<__bf16, P>& a, const Frag<__bf16>& b) {
+#pragma unroll
+  for (int k = P - 1; k >= 0; --k) mma(c, a.p[k], b);
+}
+template <int P, int Q>
+__device__ __forceinline__ void mma(f32x4& c, const DeltaOp<float, P>& a, const DeltaOp<float, Q>& b) { mma(c, a.x, b.x); }
+// (products of parts that are below what the others leave out are left out)
+template <int P, int Q>
+__device__ __forceinline__ void mma(f32x4& c, const DeltaOp<__bf16, P>& a, const DeltaOp<__bf16, Q>& b) {
+  constexpr int MOST = (P > Q ? P : Q) - 1;
+#pragma unroll
+  for (int k = MOST; k >= 0; --k)
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (k - i >= 0 && k - i < Q) mma(c, a.p[i], b.p[k - i]);
+}
+
+// The parts of an operand in LDS: [parts][rows][pitch].
+template <typename T>
+constexpr int delta_parts(int p) { return sizeof(T) == 2 ? p : 1; }
+template <int P>
+__device__ __forceinline__ void load_op(DeltaOp<float, P>& o, const float* x, int) { load8(o.x, x); }
+template <int P>
+__device__ __forceinline__ void load_op(DeltaOp<__bf16, P>& o, const __bf16* x, int part) {
+#pragma unroll
+  for (int k = 0; k < P; ++k) load8(o.p[k], x + k * part);
+}
+// slots e0 .. e0 + 3 from four rows of a column (see load_tr4_at)
+template <int P, typename F>
+__device__ __forceinline__ void load_op_tr4(DeltaOp<float, P>& o, int e0, int lane, int, F at) { load_tr4_at(o.x, e0, lane, at); }
+template <int P, typename F>
+__device__ __forceinline__ void load_op_tr4(DeltaOp<__bf16, P>& o, int e0, int lane, int part, F at) {
+#pragma unroll
+  for (int k = 0; k < P; ++k) load_tr4_at(o.p[k], e0, lane, [&](int kk, int col) { return at(kk, col) + k * part; });
+}
+// four consecutive elements as parts
+template <int P>
+__device__ __forceinline__ void store_parts4(float* x, int, float a, float b, float c, float d) { store4(x, a, b, c, d); }
+template <int P>
+__device__ __forceinline__ void store_parts4(__bf16* x, int part, float a, float b, float c, float d) {
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    store4(x + k * part, a, b, c, d);
+    a -= (float)(__bf16)a, b -= (float)(__bf16)b, c -= (float)(__bf16)c, d -= (float)(__bf16)d;
+  }
+}
+
+// parts: of N and of P
+hipError_t launch_delta_gates(Dt dt, int n_parts, int p_parts, const DeltaArgs& a, hipStream_t s);
+// out and the state
+hipError_t launch_delta_out(Dt dt, bool exact, const DeltaArgs& a, hipStream_t s);
+// the backward pass: E and the states before the chunks; X and the gradients of the states behind them; the gradients
+hipError_t launch_delta_record(Dt dt, const DeltaArgs& a, hipStream_t s);
+hipError_t launch_delta_back(Dt dt, const DeltaArgs& a, hipStream_t s);
+hipError_t launch_delta_grads(Dt dt, const DeltaArgs& a, hipStream_t s);
+// Value columns of a workgroup of the serial passes.
+constexpr int delta_columns(int64_t d) { return d < 64 ? 32 : 64; }
+
+struct DeltaStepArgs {
+  SeqRows q, k, v, o;
+  const float* log_decay;  // [count][H][m]
+  const float* beta;
+  int64_t count;
+  int m, H, Hk, D, d;
+  float scale;
+  float* S;
+};
+hipError_t launch_delta_step(Dt dt, const DeltaStepArgs& a, hipStream_t s);
+
+}  // namespace luna

@@ -1,0 +1,359 @@
+// luna_delta_grads.hip -- the gradients of the gated delta rule within each chunk (luna_delta.hpp), for all chunks side by side,
+// from the states before the chunks S, the gradients of the states behind them dS', E and X.  With U = beta E and
+// dR = beta X (dV), Gamma_ij = e^(G_i - G_j):
+//
+//   dbeta_i = X_i.E_i,   dP_ij = dO_i.U_j (j <= i),   dM_ij = -dR_i.U_j (j < i),
+//   dQ = scale e^G (dO S^T) + (scale dP Gamma) K,
+//   dK = e^(G_C - G) (U dS'^T) - e^G (dR S^T) + (scale dP Gamma)^T Q + (dM Gamma) K + (dM Gamma)^T K,
+//   dG_i = q_i.(scale e^G dO S^T)_i - k_i.(e^G dR S^T)_i - k_i.(e^(G_C - G) U dS'^T)_i
+//          + sum_j w_ij - sum_j w_ji,   w = dP P + dM M,
+//   dG_C = sum_i k_i.(e^(G_C - G) U dS'^T)_i + e^(G_C) <dS', S>,
+//   dlog_decay_t = sum_{i >= t} dG_i + dG_C.
+//
+// A workgroup takes a chunk of one key head and adds up over the value heads of its group, in their order; a wave has 16
+// features of dQ and dK, formed transposed, so that a lane holds four neighbouring features of a token.
+#include "luna_delta.hpp"
+
+namespace luna {
+
+namespace {
+
+constexpr int C = kDeltaChunk, KT = C / 16, KS = C / 32;
+
+template <int DK>
+constexpr int kGradWaves = DK == 128 ? 8 : 4;
+
+template <typename T, int DK, int DV, int NP>
+struct GradLds {
+  static constexpr int PAD = 16 / (int)sizeof(T), PK = DK + PAD, PT = C + PAD, W = kGradWaves<DK>;
+  T k[C][PK], q[C][PK];
+  union {
+    struct {
+      T u[NP][DV][PT], r[NP][DV][PT];  // U and dR, transposed
+    };
+    struct {
+      T ap[NP][C][PT], am[NP][C][PT];  // scale dP Gamma and dM Gamma
+    };
+  };
+  float gates[kDeltaGateRows][C];
+  union {
+    float beta[4 * W][C];  // shares of dbeta
+    struct {
+      float row[KT][C], col[KT][C];  // sums of w over the columns of block jt, and over the rows of block it
+      float dots[W][2][C];
+    };
+  };
+  float state[W];               // shares of <dS', S>
+};
+
+// sum over the 16 lanes of a group
+__device__ __forceinline__ float lanes_sum(float x) {
+#pragma unroll
+  for (int w = 1; w < 16; w *= 2) x += __shfl_xor(x, w);
+  return x;
+}
+
+template <typename T, int DK, int DV, int NP>
+__global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(DeltaArgs a) {
+  using Lds = GradLds<T, DK, DV, NP>;
+  constexpr int W = Lds::W, THREADS = 64 * W, PK = Lds::PK, PT = Lds::PT, esz = (int)sizeof(T), FS = DK / 32, VS = DV / 32;
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  Lds& l = *reinterpret_cast<Lds*>(raw);
+  const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
+  const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk, group = a.H / a.Hk;
+  const SeqPiece sp = seq_piece(a.s, slot, C);
+  if (sp.seq < 0) return;
+  const bool packed = a.s.offsets != nullptr, mine = wave < DK / 16;
+  const int t0 = sp.index * C, m = min(C, sp.len - t0), feat = mine ? 16 * wave : 0;
+  {
+    DecayRows<T, C, DK, PK, THREADS> x;
+    x.load(seq_row(a.k, sp, packed, hk, t0, esz), a.k.row, m, DK, false);
+    x.store(&l.k[0][0]);
+    x.load(seq_row(a.q, sp, packed, hk, t0, esz), a.q.row, m, DK, false);
+    x.store(&l.q[0][0]);
+  }
+  f32x4 dq[KT], dk[KT];
+#pragma unroll
+  for (int i = 0; i < KT; ++i) dq[i] = zero4(), dk[i] = zero4();
+
+  for (int h = 0; h < group; ++h) {
+    const int head = hk * group + h;
+    const int64_t at = (int64_t)slot * a.H + head;
+    const Buf bo = buffer(seq_row(a.o, sp, packed, head, t0, esz), (int)(((m - 1) * a.o.row + DV) * esz));
+    const auto load_do = [&](Frag<T>& f, int it, int s) {
+      const int i = 16 * it + c;
+      buf_load8(f, bo, i < m ? (i * (int)a.o.row + 32 * s + 8 * g) * esz : kPastEnd);
+    };
+    __syncthreads();  // the head before is no longer read
+    for (int i = tid; i < kDeltaGates; i += THREADS) (&l.gates[0][0])[i] = a.gates[at * kDeltaGates + i];
+    __syncthreads();
+    {  // U, dR and dbeta: four tokens of a column a thread
+      const float* e = a.e + at * DV * C;
+      const float* x = a.x + at * DV * C;
+      const int i = 4 * (tid % 16);
+      const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][i]);
+      f32x4 sum = zero4();
+#pragma unroll
+      for (int col = tid / 16; col < DV; col += THREADS / 16) {
+        const f32x4 ev = *reinterpret_cast<const f32x4*>(e + col * C + i), xv = *reinterpret_cast<const f32x4*>(x + col * C + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] = fmaf(ev[j], xv[j], sum[j]);
+        store_parts4<NP>(&l.u[0][col][i], DV * PT, beta[0] * ev[0], beta[1] * ev[1], beta[2] * ev[2], beta[3] * ev[3]);
+        store_parts4<NP>(&l.r[0][col][i], DV * PT, beta[0] * xv[0], beta[1] * xv[1], beta[2] * xv[2], beta[3] * xv[3]);
+      }
+      *reinterpret_cast<f32x4*>(&l.beta[tid / 16][i]) = sum;
+    }
+    __syncthreads();
+    float dbeta = 0.0f;
+    if (wave == 0)
+#pragma unroll
+      for (int w = 0; w < 4 * W; ++w) dbeta += l.beta[w][lane];
+    __syncthreads();  // the shares are no longer read
+    {  // dV
+      const Buf b = buffer(seq_row(a.dv, sp, packed, head, t0, esz), (int)(((m - 1) * a.dv.row + DV) * esz));
+#pragma unroll
+      for (int idx = tid; idx < C * DV / 4; idx += THREADS) {
+        const int i = idx % C, col = idx / C * 4;
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[j] = 0.0f;
+#pragma unroll
+          for (int p = delta_parts<T>(NP) - 1; p >= 0; --p) x[j] += (float)l.r[p][col + j][i];
+        }
+        buf_store4<T>(b, i < m ? (i * (int)a.dv.row + col) * esz : kPastEnd, x[0], x[1], x[2], x[3]);
+      }
+    }
+    // this wave's features of dO S^T, dR S^T and U dS'^T, transposed
+    f32x4 zq[KT], zr[KT], zk[KT];
+    float both = 0.0f;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) zq[i] = zero4(), zr[i] = zero4(), zk[i] = zero4();
+    {
+      const float* before = a.before + at * DV * DK + feat + c;
+      const float* after = a.after + at * DV * DK + feat + c;
+#pragma unroll 1
+      for (int s = 0; s < VS; ++s) {
+        float x[8], y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] = before[(32 * s + 8 * g + e) * DK];
+          y[e] = after[(32 * s + 8 * g + e) * DK];
+        }
+        DeltaOp<T, NP> sf, df;
+        sf.set(x);
+        df.set(y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) both = fmaf(x[e], y[e], both);
+#pragma unroll
+        for (int it = 0; it < KT; ++it) {
+          Frag<T> of;
+          DeltaOp<T, NP> rf, uf;
+          load_do(of, it, s);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int row = 32 * s + 8 * g + 4 * half;
+            load_op_tr4(rf, 4 * half, lane, DV * PT, [&](int kk, int col) { return &l.r[0][row + kk][16 * it + col]; });
+            load_op_tr4(uf, 4 * half, lane, DV * PT, [&](int kk, int col) { return &l.u[0][row + kk][16 * it + col]; });
+          }
+          mma(zq[it], sf, of);
+          mma(zr[it], sf, rf);
+          mma(zk[it], df, uf);
+        }
+      }
+    }
+    // blocks of dP and dM: rows j of block jt (4 g + e), column i of block it
+    constexpr int ROUNDS = (10 + W - 1) / W;
+    f32x4 ap[ROUNDS], am[ROUNDS];
+    int its[ROUNDS], jts[ROUNDS];
+#pragma unroll
+    for (int n = 0; n < ROUNDS; ++n) {
+      const int tile = wave + W * n;  // (0,0) (1,0) (1,1) (2,0) ..; behind the last one: again, unused
+      const int it = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, jt = min(tile - it * (it + 1) / 2, it);
+      its[n] = it;
+      jts[n] = jt;
+      f32x4 p = zero4(), r = zero4(), kk = zero4(), qk = zero4();
+#pragma unroll 2
+      for (int s = 0; s < VS; ++s) {
+        Frag<T> of;
+        DeltaOp<T, NP> rf, uf;
+        load_do(of, it, s);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int row = 32 * s + 8 * g + 4 * half;
+          load_op_tr4(rf, 4 * half, lane, DV * PT, [&](int kk2, int col) { return &l.r[0][row + kk2][16 * it + col]; });
+          load_op_tr4(uf, 4 * half, lane, DV * PT, [&](int kk2, int col) { return &l.u[0][row + kk2][16 * jt + col]; });
+        }
+        mma(p, uf, of);
+        mma(r, uf, rf);
+      }
+#pragma unroll
+      for (int t = 0; t < FS; ++t) {
+        Frag<T> kj, ki, qi;
+        load8(kj, &l.k[16 * jt + c][32 * t + 8 * g]);
+        load8(ki, &l.k[16 * it + c][32 * t + 8 * g]);
+        load8(qi, &l.q[16 * it + c][32 * t + 8 * g]);
+        mma(kk, kj, ki);
+        mma(qk, kj, qi);
+      }
+      const int i = 16 * it + c, j0 = 16 * jt + 4 * g;
+      const float high = l.gates[kDeltaHigh][i], low = l.gates[kDeltaLow][i];
+      const f32x4 hj = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaHigh][j0]);
+      const f32x4 lj = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaLow][j0]);
+      f32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int j = j0 + e;
+        const float f = exp2_raw((high - hj[e]) + (low - lj[e]));
+        ap[n][e] = j <= i ? a.scale * p[e] * f : 0.0f;
+        am[n][e] = j < i ? -r[e] * f : 0.0f;
+        w[e] = fmaf(ap[n][e], qk[e], am[n][e] * kk[e]);
+      }
+      const float over = groups_sum(w[0] + w[1] + w[2] + w[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = lanes_sum(w[e]);
+      if (tile < 10) {
+        if (g == 0) l.row[jt][i] = over;
+        if (c == 0) *reinterpret_cast<f32x4*>(&l.col[it][j0]) = w;
+      }
+    }
+    __syncthreads();  // U and dR are no longer read
+#pragma unroll
+    for (int n = 0; n < ROUNDS; ++n) {
+      if (wave + W * n < 10) {
+        const int i = 16 * its[n] + c, j = 16 * jts[n] + 4 * g;
+        store_parts4<NP>(&l.ap[0][i][j], C * PT, ap[n][0], ap[n][1], ap[n][2], ap[n][3]);
+        store_parts4<NP>(&l.am[0][i][j], C * PT, am[n][0], am[n][1], am[n][2], am[n][3]);
+      }
+    }
+    if (wave < 2) {  // the blocks beside the diagonal that products of 32 columns meet
+      const int i = 32 * wave + c, j = 32 * wave + 16 + 4 * g;
+      store_parts4<NP>(&l.ap[0][i][j], C * PT, 0.0f, 0.0f, 0.0f, 0.0f);
+      store_parts4<NP>(&l.am[0][i][j], C * PT, 0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    __syncthreads();
+    {
+#pragma unroll
+      for (int it = 0; it < KT; ++it) {
+        const int i = 16 * it + c;
+        const float first = l.gates[kDeltaFirst][i], last = l.gates[kDeltaLast][i];
+        Frag<T> qf, kf;
+        load4(qf, 0, &l.q[i][feat + 4 * g]);
+        load4(kf, 0, &l.k[i][feat + 4 * g]);
+        float sum = 0.0f, ends = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = a.scale * first * zq[it][e], y = first * zr[it][e], z = last * zk[it][e];
+          dq[it][e] += x;
+          dk[it][e] += z - y;
+          sum = fmaf(qf.get(e), x, sum);
+          sum = fmaf(-kf.get(e), y, sum);
+          ends = fmaf(kf.get(e), z, ends);
+        }
+        sum = groups_sum(sum);
+        ends = groups_sum(ends);
+        if (mine && g == 0) {
+          l.dots[wave][0][i] = sum - ends;
+          l.dots[wave][1][i] = ends;
+        }
+      }
+#pragma unroll
+      for (int w = 1; w < kWave; w *= 2) both += __shfl_xor(both, w);
+      if (mine && lane == 0) l.state[wave] = both;
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      Frag<T> kf, qf;  // features (rows) over the tokens 32 s + 8 g ..
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        load_tr4(kf, 4 * half, &l.k[0][0], PK, 32 * s + 8 * g + 4 * half, feat, lane);
+        load_tr4(qf, 4 * half, &l.q[0][0], PK, 32 * s + 8 * g + 4 * half, feat, lane);
+      }
+#pragma unroll
+      for (int it = 0; it < KT; ++it) {
+        if (it / 2 >= s) {  // over j
+          DeltaOp<T, NP> pf, mf;
+          load_op(pf, &l.ap[0][16 * it + c][32 * s + 8 * g], C * PT);
+          load_op(mf, &l.am[0][16 * it + c][32 * s + 8 * g], C * PT);
+          mma(dq[it], kf, pf);
+          mma(dk[it], kf, mf);
+        }
+        if (it / 2 <= s) {  // over i
+          DeltaOp<T, NP> pf, mf;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int row = 32 * s + 8 * g + 4 * half;
+            load_op_tr4(pf, 4 * half, lane, C * PT, [&](int kk, int col) { return &l.ap[0][row + kk][16 * it + col]; });
+            load_op_tr4(mf, 4 * half, lane, C * PT, [&](int kk, int col) { return &l.am[0][row + kk][16 * it + col]; });
+          }
+          mma(dk[it], qf, pf);
+          mma(dk[it], kf, mf);
+        }
+      }
+    }
+    __syncthreads();  // the sums are whole
+    if (wave == 0) {
+      float sum = 0.0f, ends = 0.0f, whole = 0.0f;
+#pragma unroll
+      for (int w = 0; w < DK / 16; ++w) {
+        sum += l.dots[w][0][lane];
+        ends += l.dots[w][1][lane];
+        whole += l.state[w];
+      }
+#pragma unroll
+      for (int b = 0; b < KT; ++b) {
+        sum += b <= lane / 16 ? l.row[b][lane] : 0.0f;
+        sum -= b >= lane / 16 ? l.col[b][lane] : 0.0f;
+      }
+#pragma unroll
+      for (int w = 1; w < kWave; w *= 2) {
+        const float other = __shfl_down(sum, w);
+        sum += lane + w < kWave ? other : 0.0f;
+        ends += __shfl_xor(ends, w);
+      }
+      if (lane < m) {
+        const int64_t num = seq_num(a.s, sp, a.H, head, t0 + lane);
+        // (above 0 a log decay counts as 0)
+        a.dlog_decay[num] = a.log_decay[num] > 0.0f ? 0.0f : sum + ends + l.gates[kDeltaMisc][0] * whole;
+        a.dbeta[num] = dbeta;
+      }
+    }
+  }
+  if (mine) {
+    const Buf bq = buffer(seq_row(a.dq, sp, packed, hk, t0, esz), (int)(((m - 1) * a.dq.row + DK) * esz));
+    const Buf bk = buffer(seq_row(a.dk, sp, packed, hk, t0, esz), (int)(((m - 1) * a.dk.row + DK) * esz));
+#pragma unroll
+    for (int it = 0; it < KT; ++it) {
+      const int i = 16 * it + c;
+      buf_store4<T>(bq, i < m ? (i * (int)a.dq.row + feat + 4 * g) * esz : kPastEnd, dq[it][0], dq[it][1], dq[it][2], dq[it][3]);
+      buf_store4<T>(bk, i < m ? (i * (int)a.dk.row + feat + 4 * g) * esz : kPastEnd, dk[it][0], dk[it][1], dk[it][2], dk[it][3]);
+    }
+  }
+}
+
+template <typename T, int DK, int DV, int NP>
+hipError_t launch_one(const DeltaArgs& a, hipStream_t s) {
+  constexpr int bytes = (int)sizeof(GradLds<T, DK, DV, NP>);
+  static_assert(bytes <= 160 * 1024, "one workgroup's LDS");
+  const hipError_t e = allow_lds<delta_grads_kernel<T, DK, DV, NP>>(bytes);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((delta_grads_kernel<T, DK, DV, NP>), dim3((unsigned)((int64_t)a.slots * a.Hk)), dim3(64 * kGradWaves<DK>),
+                     bytes, s, a);
+  return hipGetLastError();
+}
+template <typename T, int DK, int NP>
+hipError_t launch_columns(const DeltaArgs& a, hipStream_t s) {
+  return a.d == 32 ? launch_one<T, DK, 32, NP>(a, s) : a.d == 64 ? launch_one<T, DK, 64, NP>(a, s) : launch_one<T, DK, 128, NP>(a, s);
+}
+template <typename T, int NP>
+hipError_t launch_grads(const DeltaArgs& a, hipStream_t s) {
+  return a.D == 32 ? launch_columns<T, 32, NP>(a, s) : a.D == 64 ? launch_columns<T, 64, NP>(a, s) : launch_columns<T, 128, NP>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_delta_grads(Dt dt, const DeltaArgs& a, hipStream_t s) {
+  return dt == Dt::BF16 ? launch_grads<__bf16, kDeltaBackParts>(a, s) : launch_grads<float, 1>(a, s);
+}
+
+}  // namespace luna

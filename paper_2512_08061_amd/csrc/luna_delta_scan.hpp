@@ -1,0 +1,462 @@
+// luna_delta_scan.hpp -- the passes of the gated delta rule that are serial in the chunks (luna_delta.hpp): a wave takes 16
+// value columns of one sequence and head from the first chunk to the last (the backward pass: from the last to the first),
+// with its columns of the state in registers, as the accumulator tiles of S' = .. + K^T U.
+//
+// Every product's result is the next one's operand as it lies in the registers, so that a chunk needs no exchange between
+// lanes: rows 4g + e of a pair of tiles 2s, 2s + 1 stand for features (and tokens) 32 s + 8 g + e and 32 s + 8 g + 4 + e, the
+// eight k-slots of lane group g.  K S and N (beta R) take such pairs as their B operand, out^T = S^T Q^T + U^T P^T the same
+// registers as its A operand.  K and Q lie in LDS as their rows; K^T is read transposed.
+#pragma once
+
+#include "luna_delta.hpp"
+
+namespace luna {
+
+// Forward: FWD_OUT writes out and returns the state; RECORD leaves E and the states before the chunks for the backward pass.
+template <typename T, int DK, int DVW, int NP, int PP, bool OUT>
+struct ScanLds {
+  static constexpr int C = kDeltaChunk, PAD = 16 / (int)sizeof(T), PK = DK + PAD, PV = DVW + PAD, PN = C + PAD;
+  T k[C][PK];
+  T q[OUT ? C : 1][PK];
+  T v[C][PV];
+  T n[NP][C][PN];
+  T p[OUT ? PP : 1][OUT ? C : 1][PN];
+  float gates[4][C];
+  int since[DVW];  // per column: the first token with a value that is not finite
+};
+
+// Token (feature) of row r of tile i of such pairs, and of rows 4 g .. 4 g + 3.
+__device__ __forceinline__ int pair_row(int i, int r) { return 32 * (i / 2) + 8 * (r / 4) + 4 * (i % 2) + r % 4; }
+__device__ __forceinline__ int pair_rows(int i, int g) { return 32 * (i / 2) + 8 * g + 4 * (i % 2); }
+
+// N x [64][64] from the workspace to LDS, a chunk ahead.
+template <typename T, int N, int PN, int THREADS>
+struct ScanMatrix {
+  DecayRows<T, kDeltaChunk, kDeltaChunk, PN, THREADS> x[N];
+  __device__ __forceinline__ void load(const char* from) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      x[i].load(from + (int64_t)i * kDeltaChunk * kDeltaChunk * sizeof(T), kDeltaChunk, kDeltaChunk, kDeltaChunk, false);
+  }
+  __device__ __forceinline__ void store(T (*to)[kDeltaChunk][PN]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i].store(&to[i][0][0]);
+  }
+};
+
+// rows from `first` on as zeros
+template <typename T, int C, int W, int P, int THREADS>
+__device__ __forceinline__ void clear_rows(DecayRows<T, C, W, P, THREADS>& x, int first) {
+  using R = DecayRows<T, C, W, P, THREADS>;
+#pragma unroll
+  for (int i = 0; i < R::N; ++i)
+    if ((threadIdx.x + THREADS * i) / R::PER >= (unsigned)first) x.x[i] = i32x4{0, 0, 0, 0};
+}
+
+// The transposed operand of tile i (16 features or tokens as pair_row says) over rows k0 + 8 g .. + 7 of an LDS tile.
+template <typename T>
+__device__ __forceinline__ void load_pair_tr(Frag<T>& f, const T* x, int pitch, int i, int k0, int lane) {
+  const int first = 32 * (i / 2) + 4 * (i % 2), row = k0 + 8 * (lane / 16);
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+    load_tr4_at(f, 4 * half, lane, [&](int kk, int col) { return x + (row + 4 * half + kk) * pitch + first + 8 * (col / 4) + col % 4; });
+}
+template <typename T, int P>
+__device__ __forceinline__ void load_op_pair_tr(DeltaOp<T, P>& f, const T* x, int part, int pitch, int i, int k0, int lane) {
+  const int first = 32 * (i / 2) + 4 * (i % 2), row = k0 + 8 * (lane / 16);
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+    load_op_tr4(f, 4 * half, lane, part,
+                [&](int kk, int col) { return x + (row + 4 * half + kk) * pitch + first + 8 * (col / 4) + col % 4; });
+}
+
+template <typename T, int DK, int DVW, int NP, bool OUT>
+__global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
+  using Lds = ScanLds<T, DK, DVW, NP, 1, OUT>;
+  constexpr int C = Lds::C, FT = DK / 16, FS = DK / 32, KT = C / 16, KS = C / 32, esz = (int)sizeof(T), THREADS = 4 * DVW;
+  constexpr int UP = sizeof(T) == 2 ? 2 : 1;  // parts of U in the product with P
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  Lds& l = *reinterpret_cast<Lds*>(raw);
+  const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
+  const int slices = a.d / DVW;
+  const int slice = blockIdx.x % slices, head = (blockIdx.x / slices) % a.H, b = blockIdx.x / slices / a.H;
+  const SeqPiece sp = seq_of(a.s, b);
+  if (sp.len == 0) return;
+  const bool packed = a.s.offsets != nullptr;
+  const int hk = head / (a.H / a.Hk), col0 = slice * DVW, wcol = 16 * wave;
+  const int slot0 = delta_first_slot(a.s, sp), chunks = (sp.len + C - 1) / C;
+  constexpr int64_t nbytes = (int64_t)delta_parts<T>(NP) * C * C * esz, pbytes = (int64_t)C * C * esz;
+  constexpr int kNever = 1 << 30;
+
+  DecayRows<T, C, DK, Lds::PK, THREADS> kr, qr;
+  DecayRows<T, C, DVW, Lds::PV, THREADS> vr;
+  ScanMatrix<T, NP, Lds::PN, THREADS> nr;
+  ScanMatrix<T, 1, Lds::PN, THREADS> pr;
+  constexpr int GN = 4 * C / THREADS;
+  float gr[GN];
+  int bad = C;
+  const auto load = [&](int chunk) {
+    const int t0 = chunk * C, m = min(C, sp.len - t0);
+    const int64_t at = (int64_t)(slot0 + chunk) * a.H + head;
+    kr.load(seq_row(a.k, sp, packed, hk, t0, esz), a.k.row, m, DK, false);
+    vr.load(seq_row(a.v, sp, packed, head, t0, esz) + col0 * esz, a.v.row, m, DVW, false);
+    nr.load(a.n + at * nbytes);
+    if constexpr (OUT) {
+      qr.load(seq_row(a.q, sp, packed, hk, t0, esz), a.q.row, m, DK, false);
+      pr.load(a.p + at * pbytes);
+    }
+    const float* gates = a.gates + at * kDeltaGates;
+#pragma unroll
+    for (int i = 0; i < GN; ++i) gr[i] = gates[tid + THREADS * i];
+    bad = __builtin_amdgcn_readfirstlane(__float_as_int(gates[kDeltaMisc * C + 1]));
+  };
+  load(0);
+  for (int i = tid; i < DVW; i += THREADS) l.since[i] = kNever;
+
+  f32x4 S[FT];
+  const int64_t state = ((int64_t)b * a.H + head) * a.D * a.d + col0 + wcol + c;
+#pragma unroll
+  for (int ft = 0; ft < FT; ++ft)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) S[ft][j] = OUT && a.S ? a.S[state + (int64_t)(pair_rows(ft, g) + j) * a.d] : 0.0f;
+
+  int lost = kNever;  // the first token with a key or gate that is not finite
+  for (int chunk = 0; chunk < chunks; ++chunk) {
+    const int t0 = chunk * C, m = min(C, sp.len - t0);
+    const int64_t at = (int64_t)(slot0 + chunk) * a.H + head;
+    __syncthreads();  // the chunk before is no longer read
+    if (bad < C) {
+      clear_rows(kr, bad);
+      lost = min(lost, t0 + bad);
+    }
+    kr.store(&l.k[0][0]);
+    if constexpr (OUT) {
+      vr.clean(l.since, t0);
+      qr.store(&l.q[0][0]);
+      pr.store(l.p);
+    }
+    vr.store(&l.v[0][0]);
+    nr.store(l.n);
+#pragma unroll
+    for (int i = 0; i < GN; ++i) (&l.gates[0][0])[tid + THREADS * i] = gr[i];
+    if (chunk + 1 < chunks) load(chunk + 1);
+    __syncthreads();
+
+    if (!OUT) {  // the state before the chunk, [d][D]
+      float* to = a.before + (at * a.d + col0 + wcol + c) * DK;
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(to + pair_rows(ft, g)) = S[ft];
+    }
+    f32x4 r[KT], o[KT];
+#pragma unroll
+    for (int i = 0; i < KT; ++i) r[i] = zero4(), o[i] = zero4();
+#pragma unroll
+    for (int t = 0; t < FS; ++t) {
+      DeltaOp<T, NP> sf;
+      set_tiles(sf, S[2 * t], S[2 * t + 1]);
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        Frag<T> f;
+        load8(f, &l.k[pair_row(i, c)][32 * t + 8 * g]);
+        mma(r[i], f, sf);
+      }
+      if constexpr (OUT) {
+#pragma unroll
+        for (int i = 0; i < KT; ++i) {
+          Frag<T> f;
+          load8(f, &l.q[16 * i + c][32 * t + 8 * g]);
+          if constexpr (sizeof(T) == 2) {  // (two parts of S suffice for out)
+            mma(o[i], sf.p[1], f);
+            mma(o[i], sf.p[0], f);
+          } else {
+            mma(o[i], sf, f);
+          }
+        }
+      }
+    }
+    // R and beta R
+    DeltaOp<T, NP> br[KS];
+    {
+      f32x4 x[KT];
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        const int row = pair_rows(i, g);
+        Frag<T> v;
+        load_tr4(v, 0, &l.v[0][0], Lds::PV, row, wcol, lane);
+        const f32x4 first = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaFirst][row]);
+        const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][row]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          r[i][e] = fmaf(-first[e], r[i][e], v.get(e));
+          x[i][e] = beta[e] * r[i][e];
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s) set_tiles(br[s], x[2 * s], x[2 * s + 1]);
+    }
+    // E = R + N (beta R), of whose rows 32 s .. the columns up to 32 s + 31
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+#pragma unroll
+      for (int s = 0; s <= i / 2; ++s) {
+        DeltaOp<T, NP> f;
+        load_op(f, &l.n[0][pair_row(i, c)][32 * s + 8 * g], C * Lds::PN);
+        mma(r[i], f, br[s]);
+      }
+    if (!OUT) {
+      float* to = a.e + (at * a.d + col0 + wcol + c) * C;
+#pragma unroll
+      for (int i = 0; i < KT; ++i) *reinterpret_cast<f32x4*>(to + pair_rows(i, g)) = r[i];
+    }
+    // U, and U discounted to the chunk's end
+    DeltaOp<T, UP> uf[KS];
+    DeltaOp<T, NP> ul[KS];
+    {
+      f32x4 x[KT];
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        const int row = pair_rows(i, g);
+        const f32x4 last = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaLast][row]);
+        const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][row]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          r[i][e] *= beta[e];
+          x[i][e] = last[e] * r[i][e];
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        if constexpr (OUT) set_tiles(uf[s], r[2 * s], r[2 * s + 1]);
+        set_tiles(ul[s], x[2 * s], x[2 * s + 1]);
+      }
+    }
+    {
+      const float whole = l.gates[kDeltaMisc][0];
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) S[ft][j] *= whole;
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft) {
+        Frag<T> f;
+        load_pair_tr(f, &l.k[0][0], Lds::PK, ft, 32 * s, lane);
+        mma(S[ft], f, ul[s]);
+      }
+    if constexpr (OUT) {
+      const Buf to = buffer(seq_row(a.o, sp, packed, head, t0, esz) + col0 * esz, (int)(((m - 1) * a.o.row + DVW) * esz));
+      const i32x4 since = *reinterpret_cast<const i32x4*>(&l.since[wcol + 4 * g]);
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        const int row = 16 * i + c;
+        const float first = a.scale * l.gates[kDeltaFirst][row];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][e] *= first;
+#pragma unroll
+        for (int s = 0; s <= i / 2; ++s) {
+          Frag<T> f;
+          load8(f, &l.p[0][row][32 * s + 8 * g]);
+          mma(o[i], uf[s], f);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        const int row = 16 * i + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][e] = t0 + row >= min(since[e], lost) ? __builtin_nanf("") : o[i][e];
+        buf_store4<T>(to, row < m ? (row * (int)a.o.row + wcol + 4 * g) * esz : kPastEnd, o[i][0], o[i][1], o[i][2], o[i][3]);
+      }
+    }
+  }
+  if (OUT && a.S) {
+    const bool gone = min(l.since[wcol + c], lost) != kNever;
+#pragma unroll
+    for (int ft = 0; ft < FT; ++ft)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) a.S[state + (int64_t)(pair_rows(ft, g) + j) * a.d] = gone ? __builtin_nanf("") : S[ft][j];
+  }
+}
+
+// The gradients of the states and X, from the last chunk to the first.
+template <typename T, int DK, int DVW, int NP>
+__global__ __launch_bounds__(4 * DVW, 1) void delta_back_kernel(DeltaArgs a) {
+  using Lds = ScanLds<T, DK, DVW, NP, NP, true>;
+  constexpr int C = Lds::C, FT = DK / 16, FS = DK / 32, KT = C / 16, KS = C / 32, esz = (int)sizeof(T), THREADS = 4 * DVW;
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  Lds& l = *reinterpret_cast<Lds*>(raw);
+  const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
+  const int slices = a.d / DVW;
+  const int slice = blockIdx.x % slices, head = (blockIdx.x / slices) % a.H, b = blockIdx.x / slices / a.H;
+  const SeqPiece sp = seq_of(a.s, b);
+  if (sp.len == 0) return;
+  const bool packed = a.s.offsets != nullptr;
+  const int hk = head / (a.H / a.Hk), col0 = slice * DVW, wcol = 16 * wave;
+  const int slot0 = delta_first_slot(a.s, sp), chunks = (sp.len + C - 1) / C;
+  constexpr int64_t nbytes = (int64_t)NP * C * C * esz;
+
+  DecayRows<T, C, DK, Lds::PK, THREADS> kr, qr;
+  DecayRows<T, C, DVW, Lds::PV, THREADS> vr;
+  ScanMatrix<T, NP, Lds::PN, THREADS> nr, pr;
+  constexpr int GN = 4 * C / THREADS;
+  float gr[GN];
+  const auto load = [&](int chunk) {
+    const int t0 = chunk * C, m = min(C, sp.len - t0);
+    const int64_t at = (int64_t)(slot0 + chunk) * a.H + head;
+    kr.load(seq_row(a.k, sp, packed, hk, t0, esz), a.k.row, m, DK, false);
+    qr.load(seq_row(a.q, sp, packed, hk, t0, esz), a.q.row, m, DK, false);
+    vr.load(seq_row(a.o, sp, packed, head, t0, esz) + col0 * esz, a.o.row, m, DVW, false);
+    nr.load(a.n + at * nbytes);
+    pr.load(a.p + at * nbytes);
+    const float* gates = a.gates + at * kDeltaGates;
+#pragma unroll
+    for (int i = 0; i < GN; ++i) gr[i] = gates[tid + THREADS * i];
+  };
+  load(chunks - 1);
+  f32x4 S[FT];
+#pragma unroll
+  for (int ft = 0; ft < FT; ++ft) S[ft] = zero4();
+  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+    const int64_t at = (int64_t)(slot0 + chunk) * a.H + head;
+    __syncthreads();  // the chunk behind is no longer read
+    kr.store(&l.k[0][0]);
+    qr.store(&l.q[0][0]);
+    vr.store(&l.v[0][0]);
+    nr.store(l.n);
+    pr.store(l.p);
+#pragma unroll
+    for (int i = 0; i < GN; ++i) (&l.gates[0][0])[tid + THREADS * i] = gr[i];
+    if (chunk > 0) load(chunk - 1);
+    __syncthreads();
+
+    {  // [d][D]
+      float* to = a.after + (at * a.d + col0 + wcol + c) * DK;
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(to + pair_rows(ft, g)) = S[ft];
+    }
+    f32x4 x[KT];
+#pragma unroll
+    for (int i = 0; i < KT; ++i) x[i] = zero4();
+#pragma unroll
+    for (int t = 0; t < FS; ++t) {
+      DeltaOp<T, NP> sf;
+      set_tiles(sf, S[2 * t], S[2 * t + 1]);
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        Frag<T> f;
+        load8(f, &l.k[pair_row(i, c)][32 * t + 8 * g]);
+        mma(x[i], f, sf);
+      }
+    }
+    // dO as an operand, and scale e^G dO
+    Frag<T> of[KS];
+    DeltaOp<T, NP> os[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      load_tr4(of[s], 0, &l.v[0][0], Lds::PV, 32 * s + 8 * g, wcol, lane);
+      load_tr4(of[s], 4, &l.v[0][0], Lds::PV, 32 * s + 8 * g + 4, wcol, lane);
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = a.scale * l.gates[kDeltaFirst][32 * s + 8 * g + e] * of[s].get(e);
+      os[s].set(y);
+    }
+    // dU
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      const f32x4 last = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaLast][pair_rows(i, g)]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i][e] *= last[e];
+#pragma unroll
+      for (int s = i / 2; s < KS; ++s) {
+        DeltaOp<T, NP> f;
+        load_op_pair_tr(f, &l.p[0][0][0], C * Lds::PN, Lds::PN, i, 32 * s, lane);
+        mma(x[i], f, of[s]);
+      }
+    }
+    // X = dU + N^T (beta dU)
+    DeltaOp<T, NP> bu[KS];
+    {
+      f32x4 y[KT];
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][pair_rows(i, g)]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[i][e] = beta[e] * x[i][e];
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s) set_tiles(bu[s], y[2 * s], y[2 * s + 1]);
+    }
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+#pragma unroll
+      for (int s = i / 2; s < KS; ++s) {
+        DeltaOp<T, NP> f;
+        load_op_pair_tr(f, &l.n[0][0][0], C * Lds::PN, Lds::PN, i, 32 * s, lane);
+        mma(x[i], f, bu[s]);
+      }
+    {
+      float* to = a.x + (at * a.d + col0 + wcol + c) * C;
+#pragma unroll
+      for (int i = 0; i < KT; ++i) *reinterpret_cast<f32x4*>(to + pair_rows(i, g)) = x[i];
+    }
+    // - e^G beta X
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      const int row = pair_rows(i, g);
+      const f32x4 first = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaFirst][row]);
+      const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][row]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i][e] *= -first[e] * beta[e];
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) set_tiles(bu[s], x[2 * s], x[2 * s + 1]);
+    {
+      const float whole = l.gates[kDeltaMisc][0];
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) S[ft][j] *= whole;
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft) {
+        Frag<T> f;
+        load_pair_tr(f, &l.q[0][0], Lds::PK, ft, 32 * s, lane);
+        mma(S[ft], f, os[s]);
+        load_pair_tr(f, &l.k[0][0], Lds::PK, ft, 32 * s, lane);
+        mma(S[ft], f, bu[s]);
+      }
+  }
+}
+
+template <typename T, int DK, int DVW, int NP, bool OUT>
+hipError_t launch_scan_one(const DeltaArgs& a, hipStream_t s) {
+  constexpr int bytes = (int)sizeof(ScanLds<T, DK, DVW, NP, 1, OUT>);
+  static_assert(bytes <= 160 * 1024, "one workgroup's LDS");
+  const hipError_t e = allow_lds<delta_scan_kernel<T, DK, DVW, NP, OUT>>(bytes);
+  if (e != hipSuccess) return e;
+  const int64_t groups = a.s.count * a.H * (a.d / DVW);
+  hipLaunchKernelGGL((delta_scan_kernel<T, DK, DVW, NP, OUT>), dim3((unsigned)groups), dim3(4 * DVW), bytes, s, a);
+  return hipGetLastError();
+}
+template <typename T, int DK, int DVW, int NP>
+hipError_t launch_back_one(const DeltaArgs& a, hipStream_t s) {
+  constexpr int bytes = (int)sizeof(ScanLds<T, DK, DVW, NP, NP, true>);
+  static_assert(bytes <= 160 * 1024, "one workgroup's LDS");
+  const hipError_t e = allow_lds<delta_back_kernel<T, DK, DVW, NP>>(bytes);
+  if (e != hipSuccess) return e;
+  const int64_t groups = a.s.count * a.H * (a.d / DVW);
+  hipLaunchKernelGGL((delta_back_kernel<T, DK, DVW, NP>), dim3((unsigned)groups), dim3(4 * DVW), bytes, s, a);
+  return hipGetLastError();
+}
+
+#define LUNA_DELTA_WIDTHS(LAUNCH, T, ...)                                                                            \
+  if (delta_columns(a.d) == 32)                                                                                      \
+    return a.D == 32 ? LAUNCH<T, 32, 32, __VA_ARGS__>(a, s) : a.D == 64 ? LAUNCH<T, 64, 32, __VA_ARGS__>(a, s)       \
+                                                            : LAUNCH<T, 128, 32, __VA_ARGS__>(a, s);                 \
+  return a.D == 32 ? LAUNCH<T, 32, 64, __VA_ARGS__>(a, s) : a.D == 64 ? LAUNCH<T, 64, 64, __VA_ARGS__>(a, s)         \
+                                                          : LAUNCH<T, 128, 64, __VA_ARGS__>(a, s)
+
+}  // namespace luna

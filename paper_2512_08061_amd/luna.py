@@ -17,6 +17,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libluna.so")
 HEADER = os.path.join(os.path.dirname(PKG), "include", "luna.h")
 SEQ_HEADER = os.path.join(os.path.dirname(PKG), "include", "luna_seq.h")
+DELTA_HEADER = os.path.join(os.path.dirname(PKG), "include", "luna_delta.h")
 
 LUNA_OK, LUNA_ERR_INVALID_ARG, LUNA_ERR_UNSUPPORTED, LUNA_ERR_WORKSPACE, LUNA_ERR_HIP = range(5)
 LUNA_F32, LUNA_BF16 = 0, 1
@@ -109,6 +110,15 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.luna_softmax_fwd.restype = i32
     lib.luna_softmax_bwd.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, vp, i64, i64, i64, f32, vp, vp, vp, vp, sz, vp]
     lib.luna_softmax_bwd.restype = i32
+    # luna_delta.h
+    lib.luna_delta_workspace_bytes.argtypes = [i32, i32, vp, i64, i64, i64, i64]
+    lib.luna_delta_workspace_bytes.restype = sz
+    lib.luna_delta_fwd.argtypes = [vp, vp, vp, i32, vp, i64, i64, i64, i64, vp, vp, f32, vp, vp, vp, sz, vp]
+    lib.luna_delta_fwd.restype = i32
+    lib.luna_delta_step.argtypes = [vp, vp, vp, i32, i64, i64, i64, i64, i64, i64, vp, vp, f32, vp, vp, vp]
+    lib.luna_delta_step.restype = i32
+    lib.luna_delta_bwd.argtypes = [vp, vp, vp, vp, i32, vp, i64, i64, i64, i64, vp, vp, f32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.luna_delta_bwd.restype = i32
     lib.luna_status_string.argtypes = [i32]
     lib.luna_status_string.restype = ctypes.c_char_p
     lib.luna_last_error.argtypes = []
@@ -841,3 +851,81 @@ def softmax_attn_bwd(Q, K, V, out, lse, dO, scale: float | None = None, offsets=
                                     d ** -0.5 if scale is None else scale, at + 96, ak + 64, ak + 96, wsp, wsn,
                                     _seq_torch.stream(seqs.device)))
     return dQ, dK, dV
+
+
+# ---------------------------------------------------------------------------
+# linear attention by the gated delta rule (include/luna_delta.h)
+# ---------------------------------------------------------------------------
+
+OP_DELTA_FWD, OP_DELTA_BWD = range(2)
+
+
+def _delta_workspace(op, seqs, H, Hk, D, d, dt):
+    nb = int(_seq_torch.lib.luna_delta_workspace_bytes(op, dt, ctypes.addressof(seqs.c), H, Hk, D, d))
+    return (None, None, 0) if nb == 0 else _workspace(nb, seqs.device)
+
+
+def delta_attn(Q, K, V, log_decay, beta, S=None, scale: float = 1.0, offsets=None, lens=None, out=None):
+    """Causal linear attention by the gated delta rule (luna_delta_fwd):
+    u = beta (v - exp(log_decay) S^T k), S = exp(log_decay) S + k u^T, out = scale S^T q per token.
+
+    Q, K [B, Hk, n, D] and V [B, H, n, d] (H a multiple of Hk; lens [B]: the rows used of each sequence), or packed
+    [T, Hk, D] and [T, H, d] with offsets [B + 1] (int32 tensors on the device); any strides that keep rows contiguous and
+    16-byte aligned.  log_decay and beta: fp32 [B, H, n], or [H, T] for packed sequences.  S [B, H, D, d] (fp32): the
+    state before the first token, overwritten by the state after the last.  Returns out, like V.  Rows of no sequence are
+    not written: zeros in a new out for lens, undefined in one for offsets."""
+    lib = (_seq_torch or _seq_init()).lib
+    seqs = _Seqs(Q, offsets, lens, "Q")
+    H, Hk, D, d = V.shape[1], Q.shape[1], Q.shape[-1], V.shape[-1]
+    out = _new(V, lens) if out is None else out
+    rows = _seq_rows(seqs, (Q, K, V, out), (Hk, Hk, H, H), (D, D, d, d), ("Q", "K", "V", "out"))
+    gp = _f32_ptr(log_decay, seqs.numbers(H), seqs.device, "log_decay")
+    bp = _f32_ptr(beta, seqs.numbers(H), seqs.device, "beta")
+    sp = None if S is None else _f32_ptr(S, (seqs.count, H, D, d), seqs.device, "S")
+    dt, at = _dt(Q), ctypes.addressof(rows)
+    with _on_device(seqs.device):
+        ws, wsp, wsn = _delta_workspace(OP_DELTA_FWD, seqs, H, Hk, D, d, dt)
+        _check(lib.luna_delta_fwd(at, at + 32, at + 64, dt, ctypes.addressof(seqs.c), H, Hk, D, d, gp, bp, scale, sp, at + 96, wsp,
+                                  wsn, _seq_torch.stream(seqs.device)))
+    return out
+
+
+def delta_attn_step(Q, K, V, log_decay, beta, S, scale: float = 1.0, out=None):
+    """The m next tokens of every sequence (luna_delta_step): Q, K [B, Hk, m, D], V [B, H, m, d], log_decay and beta
+    [B, H, m] from the state S [B, H, D, d], which is updated in place; returns out like V."""
+    lib = (_seq_torch or _seq_init()).lib
+    if Q.dim() != 4:
+        raise LunaError(LUNA_ERR_INVALID_ARG, "Q must be [B, Hk, m, D]")
+    seqs = _Seqs(Q, None, None, "Q")
+    H, Hk, D, d = V.shape[1], Q.shape[1], Q.shape[-1], V.shape[-1]
+    out = _new(V, None) if out is None else out
+    rows = _seq_rows(seqs, (Q, K, V, out), (Hk, Hk, H, H), (D, D, d, d), ("Q", "K", "V", "out"))
+    gp = _f32_ptr(log_decay, seqs.numbers(H), seqs.device, "log_decay")
+    bp = _f32_ptr(beta, seqs.numbers(H), seqs.device, "beta")
+    sp = _f32_ptr(S, (seqs.count, H, D, d), seqs.device, "S")
+    at = ctypes.addressof(rows)
+    with _on_device(seqs.device):
+        _check(lib.luna_delta_step(at, at + 32, at + 64, _dt(Q), seqs.count, seqs.rows, H, Hk, D, d, gp, bp, scale, sp, at + 96,
+                                   _seq_torch.stream(seqs.device)))
+    return out
+
+
+def delta_attn_bwd(Q, K, V, dO, log_decay, beta, scale: float = 1.0, offsets=None, lens=None, grads=None):
+    """Backward pass of delta_attn from an empty state (luna_delta_bwd): returns (dQ, dK, dV, dlog_decay, dbeta), into
+    grads when given; dQ and dK are summed over the value heads of each key head."""
+    lib = (_seq_torch or _seq_init()).lib
+    seqs = _Seqs(Q, offsets, lens, "Q")
+    H, Hk, D, d = V.shape[1], Q.shape[1], Q.shape[-1], V.shape[-1]
+    gp = _f32_ptr(log_decay, seqs.numbers(H), seqs.device, "log_decay")
+    bp = _f32_ptr(beta, seqs.numbers(H), seqs.device, "beta")
+    dQ, dK, dV, dg, db = tuple(_new(t, lens) for t in (Q, K, V, log_decay, beta)) if grads is None else grads
+    rows = _seq_rows(seqs, (Q, K, V, dO, dQ, dK, dV), (Hk, Hk, H, H, Hk, Hk, H), (D, D, d, d, D, D, d),
+                     ("Q", "K", "V", "dO", "dQ", "dK", "dV"))
+    dgp = _f32_ptr(dg, seqs.numbers(H), seqs.device, "dlog_decay")
+    dbp = _f32_ptr(db, seqs.numbers(H), seqs.device, "dbeta")
+    dt, at = _dt(Q), ctypes.addressof(rows)
+    with _on_device(seqs.device):
+        ws, wsp, wsn = _delta_workspace(OP_DELTA_BWD, seqs, H, Hk, D, d, dt)
+        _check(lib.luna_delta_bwd(at, at + 32, at + 64, at + 96, dt, ctypes.addressof(seqs.c), H, Hk, D, d, gp, bp, scale, at + 128,
+                                  at + 160, at + 192, dgp, dbp, wsp, wsn, _seq_torch.stream(seqs.device)))
+    return dQ, dK, dV, dg, db
