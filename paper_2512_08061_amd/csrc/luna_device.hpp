@@ -58,11 +58,12 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Between fp32 matrix products (10 wait states until their results lie in the registers) and a conditional block or a
-// branch before those registers' first use: on a path around such a block the compiler has left out some of the waits.
+// Between matrix products (10 wait states until fp32 results lie in the registers, 12 for 32 x 32 bf16 ones) and a conditional
+// block or a branch before those registers' first use: on a path around such a block the compiler has left out some of the waits.
+template <int STATES = 10>
 __device__ __forceinline__ void mma_settle() {
   __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_nop 9");
+  asm volatile("s_nop %0" ::"n"(STATES - 1));
   __builtin_amdgcn_sched_barrier(0);
 }
 

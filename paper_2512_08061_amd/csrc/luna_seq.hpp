@@ -227,8 +227,21 @@ struct DecayStepArgs {
 hipError_t launch_decay_step(Dt dt, const DecayStepArgs& a, hipStream_t s);
 
 // ---------------------------------------------------------------------------
-// softmax (luna_softmax*.hip)
+// softmax (luna_softmax*.hip, luna_paged_*.hip)
 // ---------------------------------------------------------------------------
+
+// luna_pages: token i of sequence b lies in row i % 2^shift of page table[b][i / 2^shift].  A page has at least 16 rows, so that
+// 16 keys from a multiple of 16 on lie in one.
+struct PageSet {
+  const int32_t* table;  // [count][width]
+  int64_t pool;
+  int width, shift;
+};
+// The page of a token of a sequence (which has room for it), or -1 where the table holds none of the pool.
+__host__ __device__ inline int page_of(const PageSet& p, int seq, int token) {
+  const int page = p.table[(int64_t)seq * p.width + (token >> p.shift)];
+  return page >= 0 && page < p.pool ? page : -1;
+}
 
 struct SoftmaxArgs {
   SeqRows q, k, v, o;
@@ -241,6 +254,7 @@ struct SoftmaxArgs {
   float* parts;  // few queries over long keys: [slots][Hk][rows][d + 2], see luna_softmax_split.hip;
                  // backward: [H] numbers per key row of 2 d floats, see softmax_head_parts
   float* delta;  // per query row: dO.out, written by the query pass and read by the key pass
+  PageSet pages;  // calls over pages: k.seq and v.seq are those of pages
 };
 // Query rows of a workgroup of the forward call and of the backward pass over queries, and key rows of one of the pass over
 // keys: four waves of 32 or 16.
@@ -255,5 +269,45 @@ inline bool softmax_splits(const SeqSet& qs, const SeqSet& ks, int64_t H, int64_
 }
 hipError_t launch_softmax_split(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 hipError_t launch_softmax_bwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
+// Over pages: the tile kernels, and the kernel for few rows (luna_paged_split.hip) of a key head.
+hipError_t launch_paged_tiles(Dt dt, const SoftmaxArgs& a, hipStream_t s);
+inline bool paged_splits(const SeqSet& qs, int64_t H, int64_t Hk) { return !qs.offsets && qs.rows * (H / Hk) <= kSplitRows; }
+// Keys of a unit of work of that kernel, which a wave takes at a time, and the workgroups that share the units of a key
+// head (room: of the sequences' rows of the table).
+constexpr int paged_unit(Dt dt) { return dt == Dt::BF16 ? 64 : 32; }
+int64_t paged_shares(Dt dt, int64_t count, int64_t room, int64_t Hk);
+hipError_t launch_paged_split(Dt dt, const SoftmaxArgs& a, hipStream_t s);
+
+// The line of all sequences' units in equal shares: units of a share; the units u0 .. u1 - 1 of a sequence with `before` units
+// before it that a share holds; the shares that hold units of a sequence; the number of a share's part of a sequence, below
+// shares + count (from part to part of the line the share or the sequence grows, or both).
+struct PagedUnits {
+  int u0, u1;
+};
+__host__ __device__ inline int64_t paged_per(int64_t all, int shares) {
+  const int64_t per = (all + shares - 1) / shares;
+  return per < 4 ? 4 : per;
+}
+__host__ __device__ inline PagedUnits paged_held(int64_t before, int units, int64_t per, int share, int64_t all) {
+  const int64_t begin = share * per, end = begin + per < all ? begin + per : all;
+  return PagedUnits{(int)(begin > before ? begin - before : 0), (int)(end - before < units ? end - before : units)};
+}
+__host__ __device__ inline PagedUnits paged_holders(int64_t before, int units, int64_t per) {  // (first, last; none: last < first)
+  const int first = (int)(before / per);
+  return PagedUnits{first, units ? (int)((before + units - 1) / per) : first - 1};
+}
+__host__ __device__ inline int64_t paged_part(int share, int seq) { return (int64_t)share + seq; }
+
+struct AppendArgs {
+  SeqRows k, v, q, o;     // new rows, o: rotated queries; q.data null: no queries
+  SeqRows kp, vp;         // pages
+  SeqSet s;               // the new tokens
+  PageSet pages;
+  const int32_t* lens;    // [count], these tokens included
+  const float* inv_freq;  // [rot / 2]
+  int H, Hk, d, rot, interleaved;
+};
+hipError_t launch_append(Dt dt, const AppendArgs& a, hipStream_t s);
+bool append_launchable(const SeqSet& s);
 
 }  // namespace luna

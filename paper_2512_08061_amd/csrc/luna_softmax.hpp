@@ -20,6 +20,49 @@ __device__ __forceinline__ void softmax_load_rows(T* dst, const char* base, int6
   }
 }
 
+// The pages of N groups of 16 keys from k0 (a multiple of 16) on, up to kend; none: a bit for each group without one.
+template <int N>
+struct KeyPages {
+  int page[N], none;
+  __device__ __forceinline__ int at(int i) const {
+    int p = 0;  // (selects became a load at an address that depends on i, and the pages went to scratch memory)
+#pragma unroll
+    for (int k = 0; k < N; ++k) p |= page[k] & -(int)(i == k);
+    return p;
+  }
+};
+template <int N>
+__device__ __forceinline__ KeyPages<N> key_pages(const SoftmaxArgs& a, int seq, int k0, int kend) {
+  KeyPages<N> p;
+  p.none = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int key = k0 + 16 * i;
+    p.page[i] = __builtin_amdgcn_readfirstlane(page_of(a.pages, seq, max(min(key, kend - 1), 0)));
+    if (p.page[i] < 0 && key < kend) p.none |= 1 << i;
+  }
+  return p;
+}
+// Rows key .. key + 15 (key a multiple of 16) of a page, up to kend; none of a page that is none of the pool.
+__device__ __forceinline__ Buf key_group(const SoftmaxArgs& a, const SeqRows& r, int page, int hk, int key, int kend, int width, int esz) {
+  const int n = page < 0 ? 0 : min(16, kend - key);
+  const char* base = r.data + (max(page, 0) * r.seq + hk * r.head + (key & ((1 << a.pages.shift) - 1)) * r.row) * esz;
+  return buffer(base, n > 0 ? (int)(((n - 1) * r.row + width) * esz) : 0);
+}
+// As softmax_load_rows, group(i): rows 16 i .. 16 i + 15.
+template <typename T, int R, int DH, int P, typename F>
+__device__ __forceinline__ void softmax_load_pages(T* dst, F group, int64_t row) {
+  constexpr int E = 16 / (int)sizeof(T), PER = DH / E;
+  static_assert(R * PER % 256 == 0 && (kWave <= 16 * PER), "a wave's rows lie in one group");
+#pragma unroll
+  for (int i = 0; i < R * PER / 256; ++i) {
+    const int idx = threadIdx.x + 256 * i, r = idx / PER, c = (idx % PER) * E;
+    const Buf b = group((kWave * wave_id() + 256 * i) / PER / 16);
+    const auto x = __builtin_amdgcn_raw_buffer_load_b128(b, (r % 16 * (int)row + c) * (int)sizeof(T), 0, 0);
+    *reinterpret_cast<i32x4*>(&dst[r * P + c]) = __builtin_bit_cast(i32x4, x);
+  }
+}
+
 // This lane's row (of m, from base) as operand fragments; a row past m as zeros.
 template <typename T, int DH>
 __device__ __forceinline__ void softmax_load_frags(Frag<T> (&f)[DH / 32], const char* base, int64_t row, int m, int r, int g) {
@@ -69,6 +112,16 @@ struct Tile {
       const int at = tid + THREADS * j, r = at / PIECES, piece = at % PIECES;
       t.x[j] = __builtin_bit_cast(
           i32x4, __builtin_amdgcn_raw_buffer_load_b128(b, r < n ? (r * (int)row + piece * 8) * 2 : kPastEnd, 0, 0));
+    }
+  }
+  // by four waves, group(i): rows 16 i .. 16 i + 15
+  template <typename F>
+  static __device__ __forceinline__ void load_pages(TileRegs<DH, 256>& t, int wave, int lane, F group, int64_t row) {
+#pragma unroll
+    for (int j = 0; j < 64 * PIECES / 256; ++j) {
+      const int first = kWave * wave + 256 * j, at = first + lane, r = at / PIECES, piece = at % PIECES;
+      t.x[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(group(first / PIECES / 16),
+                                                                               (r % 16 * (int)row + piece * 8) * 2, 0, 0));
     }
   }
   template <int THREADS>
@@ -123,13 +176,25 @@ __device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) < __buil
 // forms it again from the keys that it sees.  Tiles of finite values pay one test of their results, and rows that see what
 // is not finite, far from the tile where it lies, one more.  (The log-sum is right as it is: scores are masked one by one.)
 
+// Row of a key among keys or values; null where its page is none of the pool (whose keys no row sees).
+template <bool PAGED>
+__device__ __forceinline__ char* softmax_key_row(const SoftmaxArgs& a, const SeqRows& r, const SeqPiece& sk, int hk, int key, int esz) {
+  if constexpr (!PAGED) {
+    return seq_row(r, sk, a.ks.offsets != nullptr, hk, key, esz);
+  } else {
+    const int page = page_of(a.pages, sk.seq, key);
+    return page < 0 ? nullptr : r.data + (page * r.seq + hk * r.head + (key & ((1 << a.pages.shift) - 1)) * r.row) * esz;
+  }
+}
+
 // Whether the values of keys first .. end - 1 hold any that is not finite (for all lanes).
-template <typename T, int DH, int LANES>
+template <typename T, int DH, int LANES, bool PAGED = false>
 __device__ __forceinline__ bool softmax_odd_values(const SoftmaxArgs& a, const SeqPiece& sk, int hk, int first, int end) {
   bool odd = false;
 #pragma unroll 1
   for (int key = max(first, 0) + (int)threadIdx.x % LANES; key < end; key += LANES) {
-    const T* v = reinterpret_cast<const T*>(seq_row(a.v, sk, a.ks.offsets != nullptr, hk, key, (int)sizeof(T)));
+    const T* v = reinterpret_cast<const T*>(softmax_key_row<PAGED>(a, a.v, sk, hk, key, (int)sizeof(T)));
+    if (PAGED && !v) continue;
 #pragma unroll 4
     for (int c = 0; c < DH; c += 8) {
       Frag<T> f;
@@ -141,11 +206,21 @@ __device__ __forceinline__ bool softmax_odd_values(const SoftmaxArgs& a, const S
   return __any(odd);
 }
 
-// One query row by itself, key by key in fp32, by LANES lanes of a wave.
+// The same for the LANES lanes of a row, where a wave may have rows of its own in each.
 template <typename T, int DH, int LANES>
+__device__ __forceinline__ bool softmax_odd_row(const SoftmaxArgs& a, const SeqPiece& sk, int hk, int first, int end) {
+  if constexpr (LANES == kWave) {
+    return softmax_odd_values<T, DH, LANES, true>(a, sk, hk, first, end);
+  } else {
+    return true;  // (two rows of a wave may go different ways: formed again in any case)
+  }
+}
+
+// One query row by itself, key by key in fp32, by LANES lanes of a wave.
+template <typename T, int DH, int LANES, bool PAGED = false>
 __device__ __forceinline__ void softmax_row(const SoftmaxArgs& a, const SeqPiece& sq, const SeqPiece& sk, int head, int i) {
   constexpr int PER = (DH + LANES - 1) / LANES, esz = (int)sizeof(T);
-  const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
+  const bool pq = a.qs.offsets != nullptr;
   const int lane = threadIdx.x % LANES, hk = head / (a.H / a.Hk), last = min(sk.len - 1, i + sk.len - sq.len);
   const T* q = reinterpret_cast<const T*>(seq_row(a.q, sq, pq, head, i, esz));
   float top = -__builtin_inff(), sum = 0.0f, acc[PER];
@@ -154,7 +229,9 @@ __device__ __forceinline__ void softmax_row(const SoftmaxArgs& a, const SeqPiece
 #pragma unroll 1
   for (int k0 = 0; k0 <= last; k0 += LANES) {
     const int n = min(LANES, last - k0 + 1);
-    const T* k = reinterpret_cast<const T*>(seq_row(a.k, sk, pk, hk, k0 + min(lane, n - 1), esz));
+    const T* k = reinterpret_cast<const T*>(softmax_key_row<PAGED>(a, a.k, sk, hk, k0 + min(lane, n - 1), esz));
+    const bool seen = lane < n && (!PAGED || k);
+    if (PAGED && !k) k = q;
     float s = 0.0f;
 #pragma unroll 4
     for (int c = 0; c < DH; c += 8) {
@@ -164,7 +241,7 @@ __device__ __forceinline__ void softmax_row(const SoftmaxArgs& a, const SeqPiece
 #pragma unroll
       for (int e = 0; e < 8; ++e) s = fmaf(qf.get(e), kf.get(e), s);
     }
-    s = lane < n ? s * (a.scale * kLog2e) : -__builtin_inff();
+    s = seen ? s * (a.scale * kLog2e) : -__builtin_inff();
     float most = fmaxf(top, s);
 #pragma unroll
     for (int x = LANES / 2; x > 0; x /= 2) most = fmaxf(most, __shfl_xor(most, x));
@@ -177,8 +254,9 @@ __device__ __forceinline__ void softmax_row(const SoftmaxArgs& a, const SeqPiece
     for (int j0 = 0; j0 < n; j0 += 8)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {  // (behind the last key: the last one again, times 0)
-        const T* v = reinterpret_cast<const T*>(seq_row(a.v, sk, pk, hk, k0 + min(j0 + j, n - 1), esz));
-        const float pj = __shfl(p, j0 + j);
+        const T* v = reinterpret_cast<const T*>(softmax_key_row<PAGED>(a, a.v, sk, hk, k0 + min(j0 + j, n - 1), esz));
+        const float pj = __shfl(p, j0 + j, LANES);
+        if (PAGED && !v) continue;
 #pragma unroll
         for (int c = 0; c < PER; ++c) acc[c] = fmaf(pj, (float)v[min(lane + LANES * c, DH - 1)], acc[c]);
       }

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(PKG, "libluna.so")
 HEADER = os.path.join(os.path.dirname(PKG), "include", "luna.h")
 SEQ_HEADER = os.path.join(os.path.dirname(PKG), "include", "luna_seq.h")
 DELTA_HEADER = os.path.join(os.path.dirname(PKG), "include", "luna_delta.h")
+PAGED_HEADER = os.path.join(os.path.dirname(PKG), "include", "luna_paged.h")
 
 LUNA_OK, LUNA_ERR_INVALID_ARG, LUNA_ERR_UNSUPPORTED, LUNA_ERR_WORKSPACE, LUNA_ERR_HIP = range(5)
 LUNA_F32, LUNA_BF16 = 0, 1
@@ -119,6 +120,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.luna_delta_step.restype = i32
     lib.luna_delta_bwd.argtypes = [vp, vp, vp, vp, i32, vp, i64, i64, i64, i64, vp, vp, f32, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.luna_delta_bwd.restype = i32
+    # luna_paged.h
+    lib.luna_paged_append.argtypes = [vp, vp, vp, i32, vp, vp, i64, i64, i64, i64, vp, i32, vp, vp, vp, vp]
+    lib.luna_paged_append.restype = i32
+    lib.luna_paged_workspace_bytes.argtypes = [i32, vp, vp, i64, i64, i64]
+    lib.luna_paged_workspace_bytes.restype = sz
+    lib.luna_paged_fwd.argtypes = [vp, vp, vp, i32, vp, vp, i64, i64, i64, f32, vp, vp, vp, sz, vp]
+    lib.luna_paged_fwd.restype = i32
     lib.luna_status_string.argtypes = [i32]
     lib.luna_status_string.restype = ctypes.c_char_p
     lib.luna_last_error.argtypes = []
@@ -929,3 +937,81 @@ def delta_attn_bwd(Q, K, V, dO, log_decay, beta, scale: float = 1.0, offsets=Non
         _check(lib.luna_delta_bwd(at, at + 32, at + 64, at + 96, dt, ctypes.addressof(seqs.c), H, Hk, D, d, gp, bp, scale, at + 128,
                                   at + 160, at + 192, dgp, dbp, wsp, wsn, _seq_torch.stream(seqs.device)))
     return dQ, dK, dV, dg, db
+
+
+# ---------------------------------------------------------------------------
+# softmax attention over a cache in pages (include/luna_paged.h)
+# ---------------------------------------------------------------------------
+
+def _paged(seqs, k_pages, v_pages, table, lens, Hk, d):
+    """(luna_pages, luna_rows of both tensors of pages) of a call."""
+    T = _seq_torch
+    if k_pages.dim() != 4:
+        raise LunaError(LUNA_ERR_INVALID_ARG, "k_pages must be [pages, Hk, rows, d]")
+    pool = _Seqs(k_pages, None, None, "k_pages")
+    if pool.dtype != seqs.dtype or pool.device != seqs.device:
+        raise LunaError(LUNA_ERR_INVALID_ARG, "the pages must share the other tensors' dtype and GPU")
+    rows = _seq_rows(pool, (k_pages, v_pages), (Hk, Hk), (d, d), ("k_pages", "v_pages"))
+    for t, dim, name in ((table, 2, "table [B, width]"), (lens, 1, "lens [B]")):
+        if t.dtype != T.i32 or t.device != seqs.device or t.dim() != dim or t.shape[0] != seqs.count or not t.is_contiguous():
+            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} must be a contiguous int32 tensor on the tensors' device")
+    return (ctypes.c_int64 * 5)(pool.count, pool.rows, table.shape[1], table.data_ptr(), lens.data_ptr()), rows
+
+
+def paged_append(K, V, k_pages, v_pages, table, lens, Q=None, inv_freq=None, interleaved: bool = False, offsets=None,
+                 new_lens=None, q_out=None):
+    """New keys and values into the pages of a cache (luna_paged_append).
+
+    K, V [B, Hk, m, d] (new_lens [B]: the rows used of each sequence), or packed [T, Hk, d] with offsets [B + 1]: the last of the
+    lens [B] tokens that each sequence then has.  k_pages, v_pages [pages, Hk, rows, d] (any strides that keep rows contiguous;
+    rows a power of two from 16 on), table [B, width]: the pages of each sequence (int32 tensors on the device).  inv_freq
+    (fp32 [rot / 2], rot a multiple of 16): the first rot components of keys and queries are rotated by position times inv_freq, as
+    pairs of halves or, interleaved, of neighbours.  Returns Q (H heads, a multiple of Hk) rotated, into q_out (which may be Q)
+    when given, or None without Q.  What a table entry outside of the pool stands for is not written."""
+    lib = (_seq_torch or _seq_init()).lib
+    seqs = _Seqs(K, offsets, new_lens, "K")
+    Hk, d = K.shape[1], K.shape[-1]
+    H = Hk if Q is None else Q.shape[1]
+    pages, prows = _paged(seqs, k_pages, v_pages, table, lens, Hk, d)
+    if Q is None:
+        if q_out is not None:
+            raise LunaError(LUNA_ERR_INVALID_ARG, "q_out goes with Q")
+        rows = _seq_rows(seqs, (K, V), (Hk, Hk), (d, d), ("K", "V"))
+    else:
+        q_out = _new(Q, new_lens) if q_out is None else q_out
+        rows = _seq_rows(seqs, (K, V, Q, q_out), (Hk, Hk, H, H), (d, d, d, d), ("K", "V", "Q", "q_out"))
+    fp, rot = None, 0
+    if inv_freq is not None:
+        if inv_freq.dim() != 1:
+            raise LunaError(LUNA_ERR_INVALID_ARG, "inv_freq must be [rot / 2]")
+        fp, rot = _f32_ptr(inv_freq, (inv_freq.shape[0],), seqs.device, "inv_freq"), 2 * inv_freq.shape[0]
+    at, ap = ctypes.addressof(rows), ctypes.addressof(prows)
+    with _on_device(seqs.device):
+        _check(lib.luna_paged_append(at, at + 32, None if Q is None else at + 64, _dt(K), ctypes.addressof(seqs.c),
+                                     ctypes.addressof(pages), H, Hk, d, rot, fp, int(interleaved), ap, ap + 32,
+                                     None if Q is None else at + 96, _seq_torch.stream(seqs.device)))
+    return q_out
+
+
+def paged_attn(Q, k_pages, v_pages, table, lens, scale: float | None = None, offsets=None, q_lens=None, out=None, lse=None):
+    """Causal softmax attention over a cache in pages (luna_paged_fwd), scale 1 / sqrt(d) unless given.
+
+    Q [B, H, m, d] (q_lens [B]: the rows used), or packed [T, H, d] with offsets [B + 1]: the last tokens of sequences of
+    lens [B] tokens in all, whose keys and values lie in the pages k_pages, v_pages [pages, Hk, rows, d] that table
+    [B, width] assigns to them (int32 tensors on the device).  Returns (out, lse) as softmax_attn does."""
+    lib = (_seq_torch or _seq_init()).lib
+    seqs = _Seqs(Q, offsets, q_lens, "Q")
+    H, d = Q.shape[1], Q.shape[-1]
+    Hk = k_pages.shape[1] if k_pages.dim() == 4 else 1
+    pages, prows = _paged(seqs, k_pages, v_pages, table, lens, Hk, d)
+    out = _new(Q, q_lens) if out is None else out
+    rows = _seq_rows(seqs, (Q, out), (H, H), (d, d), ("Q", "out"))
+    lse = _seq_torch.empty(seqs.numbers(H), dtype=_seq_torch.f32, device=seqs.device) if lse is None else lse
+    lp = _f32_ptr(lse, seqs.numbers(H), seqs.device, "lse")
+    dt, at, ap, pp = _dt(Q), ctypes.addressof(rows), ctypes.addressof(prows), ctypes.addressof(pages)
+    with _on_device(seqs.device):
+        nb = int(lib.luna_paged_workspace_bytes(dt, ctypes.addressof(seqs.c), pp, H, Hk, d))
+        ws, wsp, wsn = (None, None, 0) if nb == 0 else _workspace(nb, seqs.device)
+        _check(lib.luna_paged_fwd(at, ap, ap + 32, dt, ctypes.addressof(seqs.c), pp, H, Hk, d, d ** -0.5 if scale is None else scale,
+                                  at + 32, lp, wsp, wsn, _seq_torch.stream(seqs.device)))
+    return out, lse
