@@ -25,7 +25,7 @@ SOURCES = ["luna_prepare.hip", "luna_featuremap.hip", "luna_noncausal.hip", "lun
            "luna_backward.hip", "luna_map_backward.hip", "luna_features.hip", "luna_chunk_query.hip", "luna_chunk_key.hip",
            "luna_decay_bf16_plain.hip", "luna_decay_bf16_norm.hip", "luna_decay_bf16_aug.hip", "luna_decay_f32_plain.hip",
            "luna_decay_f32_norm.hip", "luna_decay_f32_aug.hip", "luna_decay.hip", "luna_decay_step.hip", "luna_softmax.hip",
-           "luna_softmax_split.hip", "luna_softmax_bwd.hip", "luna_delta_gates.hip", "luna_delta_bf16.hip",
+           "luna_softmax_split.hip", "luna_softmax_bwd.hip", "luna_delta_gates.hip", "luna_delta_fwd.hip", "luna_delta_bf16.hip",
            "luna_delta_f32.hip", "luna_delta_grads.hip", "luna_delta_step.hip", "luna_delta_api.cpp", "luna_paged_tiles.hip",
            "luna_paged_split.hip", "luna_paged_append.hip", "luna_paged_api.cpp", "luna_seq_api.cpp", "luna_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

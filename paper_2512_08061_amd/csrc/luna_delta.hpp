@@ -17,9 +17,10 @@
 //   dU = P^T dO + e^(G_C - G) K dS',   X = dU + N^T (beta dU),   dV = beta X,   dbeta = X.E,
 //   dS = e^(G_C) dS' + Q^T (scale e^G dO) - K^T (e^G beta X).
 //
-// N, P and the factors of the gates are formed for all chunks at once (luna_delta_gates.hip); what is left is serial in
-// the chunks but independent for each value column, so a wave takes 16 columns of one head from the first chunk to the
-// last (luna_delta_scan.hip).
+// N, P and the factors of the gates need no state; what is left is serial in the chunks but independent for each value
+// column, so a wave takes 16 columns of one head from the first chunk to the last.  The bf16 forward pass forms the matrices in
+// the workgroups that use them (luna_delta_fwd.hip); the fp32 and backward passes for all chunks at once before
+// (luna_delta_gates.hip, luna_delta_scan.hpp, luna_delta_grads.hip).
 #pragma once
 
 #include "luna_decay.hpp"
@@ -159,10 +160,11 @@ __device__ __forceinline__ void store_parts4(__bf16* x, int part, float a, float
   }
 }
 
-// parts: of N and of P
-hipError_t launch_delta_gates(Dt dt, int n_parts, int p_parts, const DeltaArgs& a, hipStream_t s);
-// out and the state
-hipError_t launch_delta_out(Dt dt, bool exact, const DeltaArgs& a, hipStream_t s);
+// N, P and the gates' factors of all chunks to the workspace
+hipError_t launch_delta_gates(Dt dt, const DeltaArgs& a, hipStream_t s);
+// out and the state: in bf16 all in one launch (exact: the state to fp32 accuracy), in fp32 behind the gates' launch
+hipError_t launch_delta_fwd_bf16(bool exact, const DeltaArgs& a, hipStream_t s);
+hipError_t launch_delta_fwd_f32(const DeltaArgs& a, hipStream_t s);
 // the backward pass: E and the states before the chunks; X and the gradients of the states behind them; the gradients
 hipError_t launch_delta_record(Dt dt, const DeltaArgs& a, hipStream_t s);
 hipError_t launch_delta_back(Dt dt, const DeltaArgs& a, hipStream_t s);

@@ -41,7 +41,7 @@ luna_status plan_delta(luna_dtype dt, const luna_seqs& s, int64_t H, int64_t Hk,
   const luna::SeqSet set = set_of(&s);
   p->slots = luna::seq_slots(set, luna::kDeltaChunk);
   if (!launchable(p->slots * Hk, 512) || p->slots >= ((int64_t)1 << 31) ||
-      !launchable(s.count * H * (d / luna::delta_columns(d)), 4 * luna::delta_columns(d)))
+      !launchable(s.count * H * (d / luna::delta_columns(d)), 512))
     return set_error(LUNA_ERR_UNSUPPORTED, "too many chunks of sequences and heads");
   const size_t all = (size_t)p->slots * H, matrix = (size_t)luna::kDeltaChunk * luna::kDeltaChunk * (dt == LUNA_BF16 ? 2 : 4);
   const auto parts = [&](int n) { return (size_t)(dt == LUNA_BF16 ? n : 1); };
@@ -49,8 +49,9 @@ luna_status plan_delta(luna_dtype dt, const luna_seqs& s, int64_t H, int64_t Hk,
     at = p->total;
     p->total = align256(p->total + all * bytes);
   };
-  take(p->n, parts(backward ? luna::kDeltaBackParts : luna::kDeltaExactParts) * matrix);
-  take(p->p, parts(backward ? luna::kDeltaBackParts : 1) * matrix);
+  if (!backward && dt == LUNA_BF16) return LUNA_OK;  // (one launch, all in LDS)
+  take(p->n, parts(luna::kDeltaBackParts) * matrix);
+  take(p->p, parts(luna::kDeltaBackParts) * matrix);
   take(p->gates, luna::kDeltaGates * 4);
   if (backward) {
     take(p->before, (size_t)(D * d) * 4);
@@ -130,9 +131,9 @@ luna_status luna_delta_fwd(const luna_rows* Q, const luna_rows* K, const luna_ro
   a.S = S;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const luna::Dt dt = type_of(dtype);
-  st = hip_status(luna::launch_delta_gates(dt, S ? luna::kDeltaExactParts : luna::kDeltaParts, 1, a, s), "delta gate launch");
-  if (st != LUNA_OK) return st;
-  return hip_status(luna::launch_delta_out(dt, S != nullptr, a, s), "delta launch");
+  if (dt == luna::Dt::BF16) return hip_status(luna::launch_delta_fwd_bf16(S != nullptr, a, s), "delta launch");
+  if ((st = hip_status(luna::launch_delta_gates(dt, a, s), "delta gate launch")) != LUNA_OK) return st;
+  return hip_status(luna::launch_delta_fwd_f32(a, s), "delta launch");
 }
 
 luna_status luna_delta_step(const luna_rows* Q, const luna_rows* K, const luna_rows* V, luna_dtype dtype, int64_t count,
@@ -203,7 +204,7 @@ luna_status luna_delta_bwd(const luna_rows* Q, const luna_rows* K, const luna_ro
   a.dbeta = dbeta;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const luna::Dt dt = type_of(dtype);
-  if ((st = hip_status(luna::launch_delta_gates(dt, luna::kDeltaBackParts, luna::kDeltaBackParts, a, s), "delta gate launch")) != LUNA_OK)
+  if ((st = hip_status(luna::launch_delta_gates(dt, a, s), "delta gate launch")) != LUNA_OK)
     return st;
   if ((st = hip_status(luna::launch_delta_record(dt, a, s), "delta state launch")) != LUNA_OK) return st;
   if ((st = hip_status(luna::launch_delta_back(dt, a, s), "delta backward launch")) != LUNA_OK) return st;

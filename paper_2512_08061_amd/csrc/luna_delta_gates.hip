@@ -42,7 +42,7 @@ __device__ __forceinline__ bool odd(const Frag<float>& f) {
   return bad;
 }
 
-template <typename T, int DK, int NP, int PP>
+template <typename T, int DK, int NP>
 __global__ __launch_bounds__(256) void delta_gates_kernel(DeltaArgs a) {
   using Lds = GatesLds<T, DK>;
   constexpr int esz = (int)sizeof(T), KS = DK / 32;
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256) void delta_gates_kernel(DeltaArgs a) {
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
   const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk, group = a.H / a.Hk;
-  const SeqPiece sp = seq_piece(a.s, slot, C);
+  const SeqPiece sp = seq_uniform(seq_piece(a.s, slot, C));
   if (sp.seq < 0) return;
   const bool packed = a.s.offsets != nullptr;
   const int t0 = sp.index * C, m = min(C, sp.len - t0);
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256) void delta_gates_kernel(DeltaArgs a) {
     __syncthreads();
     const int bad = l.gate, i = 16 * wave + c;
     const float high = l.high[i], low = l.low[i];
-    T* p = reinterpret_cast<T*>(a.p) + at * delta_parts<T>(PP) * C * C;
+    T* p = reinterpret_cast<T*>(a.p) + at * delta_parts<T>(NP) * C * C;
 #pragma unroll
     for (int jt = 0; jt < 4; ++jt) {
       f32x4 mm, pp;
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(256) void delta_gates_kernel(DeltaArgs a) {
         pp[e] = j <= i && j < bad ? a.scale * qk[jt][e] * f : 0.0f;
       }
       *reinterpret_cast<f32x4*>(&l.m[i][16 * jt + 4 * g]) = mm;
-      store_parts4<PP>(p + i * C + 16 * jt + 4 * g, C * C, pp[0], pp[1], pp[2], pp[3]);
+      store_parts4<NP>(p + i * C + 16 * jt + 4 * g, C * C, pp[0], pp[1], pp[2], pp[3]);
     }
     __syncthreads();
     {  // diagonal blocks
@@ -212,13 +212,13 @@ __global__ __launch_bounds__(256) void delta_gates_kernel(DeltaArgs a) {
   }
 }
 
-template <typename T, int NP, int PP>
+template <typename T, int NP>
 hipError_t launch_gates(const DeltaArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)a.slots * a.Hk)), block(256);
   switch (a.D) {
-    case 32: hipLaunchKernelGGL((delta_gates_kernel<T, 32, NP, PP>), grid, block, 0, s, a); break;
-    case 64: hipLaunchKernelGGL((delta_gates_kernel<T, 64, NP, PP>), grid, block, 0, s, a); break;
-    case 128: hipLaunchKernelGGL((delta_gates_kernel<T, 128, NP, PP>), grid, block, 0, s, a); break;
+    case 32: hipLaunchKernelGGL((delta_gates_kernel<T, 32, NP>), grid, block, 0, s, a); break;
+    case 64: hipLaunchKernelGGL((delta_gates_kernel<T, 64, NP>), grid, block, 0, s, a); break;
+    case 128: hipLaunchKernelGGL((delta_gates_kernel<T, 128, NP>), grid, block, 0, s, a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
@@ -226,11 +226,8 @@ hipError_t launch_gates(const DeltaArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_delta_gates(Dt dt, int n_parts, int p_parts, const DeltaArgs& a, hipStream_t s) {
-  if (dt == Dt::F32) return launch_gates<float, 1, 1>(a, s);
-  if (p_parts == 1)
-    return n_parts == kDeltaParts ? launch_gates<__bf16, kDeltaParts, 1>(a, s) : launch_gates<__bf16, kDeltaExactParts, 1>(a, s);
-  return launch_gates<__bf16, kDeltaBackParts, kDeltaBackParts>(a, s);
+hipError_t launch_delta_gates(Dt dt, const DeltaArgs& a, hipStream_t s) {
+  return dt == Dt::F32 ? launch_gates<float, 1>(a, s) : launch_gates<__bf16, kDeltaBackParts>(a, s);
 }
 
 }  // namespace luna

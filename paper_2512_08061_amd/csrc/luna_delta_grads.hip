@@ -61,7 +61,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
   const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk, group = a.H / a.Hk;
-  const SeqPiece sp = seq_piece(a.s, slot, C);
+  const SeqPiece sp = seq_uniform(seq_piece(a.s, slot, C));
   if (sp.seq < 0) return;
   const bool packed = a.s.offsets != nullptr, mine = wave < DK / 16;
   const int t0 = sp.index * C, m = min(C, sp.len - t0), feat = mine ? 16 * wave : 0;

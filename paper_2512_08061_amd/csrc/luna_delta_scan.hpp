@@ -74,13 +74,13 @@ template <typename T, int DK, int DVW, int NP, bool OUT>
 __global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
   using Lds = ScanLds<T, DK, DVW, NP, 1, OUT>;
   constexpr int C = Lds::C, FT = DK / 16, FS = DK / 32, KT = C / 16, KS = C / 32, esz = (int)sizeof(T), THREADS = 4 * DVW;
-  constexpr int UP = sizeof(T) == 2 ? 2 : 1;  // parts of U in the product with P
+  static_assert(!OUT || sizeof(T) == 4, "bf16 has a forward kernel of its own");
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
   const int slices = a.d / DVW;
   const int slice = blockIdx.x % slices, head = (blockIdx.x / slices) % a.H, b = blockIdx.x / slices / a.H;
-  const SeqPiece sp = seq_of(a.s, b);
+  const SeqPiece sp = seq_uniform(seq_of(a.s, b));
   if (sp.len == 0) return;
   const bool packed = a.s.offsets != nullptr;
   const int hk = head / (a.H / a.Hk), col0 = slice * DVW, wcol = 16 * wave;
@@ -165,12 +165,7 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
         for (int i = 0; i < KT; ++i) {
           Frag<T> f;
           load8(f, &l.q[16 * i + c][32 * t + 8 * g]);
-          if constexpr (sizeof(T) == 2) {  // (two parts of S suffice for out)
-            mma(o[i], sf.p[1], f);
-            mma(o[i], sf.p[0], f);
-          } else {
-            mma(o[i], sf, f);
-          }
+          mma(o[i], sf, f);
         }
       }
     }
@@ -209,7 +204,7 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
       for (int i = 0; i < KT; ++i) *reinterpret_cast<f32x4*>(to + pair_rows(i, g)) = r[i];
     }
     // U, and U discounted to the chunk's end
-    DeltaOp<T, UP> uf[KS];
+    DeltaOp<T, NP> uf[KS];
     DeltaOp<T, NP> ul[KS];
     {
       f32x4 x[KT];
@@ -289,7 +284,7 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_back_kernel(DeltaArgs a) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
   const int slices = a.d / DVW;
   const int slice = blockIdx.x % slices, head = (blockIdx.x / slices) % a.H, b = blockIdx.x / slices / a.H;
-  const SeqPiece sp = seq_of(a.s, b);
+  const SeqPiece sp = seq_uniform(seq_of(a.s, b));
   if (sp.len == 0) return;
   const bool packed = a.s.offsets != nullptr;
   const int hk = head / (a.H / a.Hk), col0 = slice * DVW, wcol = 16 * wave;

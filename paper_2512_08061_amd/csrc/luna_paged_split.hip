@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void paged_split_kernel(SoftmaxArgs a, int sha
   const float scale = a.scale * kLog2e;
 
   for (; b < a.ks.count && first < end; ++b) {
-    const SeqPiece sk = seq_of(a.ks, b), sq = seq_of(a.qs, b);
+    const SeqPiece sk = seq_uniform(seq_of(a.ks, b)), sq = seq_uniform(seq_of(a.qs, b));
     const int units = (sk.len + KB - 1) / KB, shift = sk.len - sq.len;
     const PagedUnits held = paged_held(first, units, per, share, all);
     const int u0 = held.u0, u1 = held.u1;

@@ -67,6 +67,16 @@ __device__ __forceinline__ SeqPiece seq_of(const SeqSet& s, int b) {
   return p;
 }
 
+// The same in scalar registers (a sequence that the whole workgroup has: what is read from memory lies in vector registers, and a
+// buffer whose address does is tried lane by lane).
+__device__ __forceinline__ SeqPiece seq_uniform(SeqPiece p) {
+  p.seq = __builtin_amdgcn_readfirstlane(p.seq);
+  p.index = __builtin_amdgcn_readfirstlane(p.index);
+  p.len = __builtin_amdgcn_readfirstlane(p.len);
+  p.first = __builtin_amdgcn_readfirstlane((int)p.first);  // (at most 2^30)
+  return p;
+}
+
 // The last packed sequence b with holds(b, offsets[b]), which holds up to some sequence and no further; -1: none (the whole
 // wave calls this).  64 guesses at a time: every 4096th, 64th and single sequence.  (One look at each 64 after the other
 // took 24 ms for 16384 sequences of 8 tokens in 16 heads, of 1.6 ms for the same sequences without offsets.)
@@ -126,6 +136,20 @@ __device__ __forceinline__ SeqPiece seq_piece_by_work(const SeqSet& s, int slot,
   p = seq_of(s, __builtin_ctzll(__ballot(hit)));
   p.index = late ? far : __builtin_amdgcn_readlane(mine, p.seq) - 1 - far;
   return p;
+}
+
+// The sequence of a rank by length, the longest first, of up to 64 sequences (the whole wave calls this with one rank); of more:
+// of that number.
+__device__ __forceinline__ int seq_by_length(const SeqSet& s, int rank) {
+  if (s.count > kWave) return rank;
+  const int lane = threadIdx.x % kWave, count = (int)s.count;
+  const int mine = lane < count ? seq_of(s, lane).len : -1;
+  int before = 0;
+  for (int b = 0; b < count; ++b) {
+    const int other = __builtin_amdgcn_readlane(mine, b);
+    before += other > mine || (other == mine && b < lane);
+  }
+  return __builtin_ctzll(__ballot(lane < count && before == rank));
 }
 
 // Address of row i of a sequence and head.

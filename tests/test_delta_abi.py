@@ -77,9 +77,9 @@ def test_refuses_arguments(lib, op):
         refused(lib, op, INV, n=-1)
         refused(lib, op, UNS, n=(1 << 30) + 64)
         refused(lib, op, INV, off=FAKE, lens=FAKE)
-        refused(lib, op, WS, wsn=256)
-        refused(lib, op, INV, ws=FAKE + 16)
-        refused(lib, op, INV, ws=0)
+        refused(lib, op, WS, wsn=256, dt=luna.LUNA_F32)
+        refused(lib, op, INV, ws=FAKE + 16, dt=luna.LUNA_F32)
+        refused(lib, op, INV, ws=0, dt=luna.LUNA_F32)
     if op == "bwd":
         refused(lib, op, INV, dg=0)
         refused(lib, op, INV, db=0)
@@ -94,15 +94,16 @@ def test_refuses_rows(lib, op, names, outputs):
 
 
 def test_workspace_sizes(lib):
-    def nb(op, seqs, H=16, Hk=16, D=128, d=128, dt=luna.LUNA_BF16):
+    def nb(op, seqs, H=16, Hk=16, D=128, d=128, dt=luna.LUNA_F32):
         return lib.luna_delta_workspace_bytes(op, dt, ref(seqs), H, Hk, D, d)
 
-    chunk = 64 * 64 * 2
-    for op, least in ((luna.OP_DELTA_FWD, 3 * chunk), (luna.OP_DELTA_BWD, 3 * chunk + 2 * 128 * 128 * 4 + 2 * 64 * 128 * 4)):
+    chunk = 64 * 64 * 4
+    for op, least in ((luna.OP_DELTA_FWD, 2 * chunk), (luna.OP_DELTA_BWD, 2 * chunk + 2 * 128 * 128 * 4 + 2 * 64 * 128 * 4)):
         one = nb(op, i64(1, 64, 0, 0), H=1, Hk=1)
         assert one >= least and one % 256 == 0
         assert nb(op, i64(2, 2048, 0, 0)) >= 2 * 32 * 16 * least
         assert nb(op, i64(7, 5000, FAKE, 0)) >= 7 * 16 * least
+        assert (nb(op, i64(2, 2048, 0, 0), dt=luna.LUNA_BF16) > 0) == (op == luna.OP_DELTA_BWD) and not lib.luna_last_error()
         for kw in (dict(D=48), dict(dt=5), dict(Hk=3)):
             assert nb(op, i64(2, 64, 0, 0), **kw) == 0 and lib.luna_last_error()
     assert nb(9, i64(1, 64, 0, 0)) == 0 and nb(0, None) == 0
@@ -136,7 +137,7 @@ def test_binding_refuses():
     bad(luna.delta_attn_step, q4, q4, q4, g, g, S)
 
 
-SOURCES = ["luna_delta_gates.hip", "luna_delta_bf16.hip", "luna_delta_f32.hip", "luna_delta_grads.hip"]
+SOURCES = ["luna_delta_gates.hip", "luna_delta_fwd.hip", "luna_delta_bf16.hip", "luna_delta_f32.hip", "luna_delta_grads.hip"]
 
 
 def test_results_of_matrix_products_are_waited_for(tmp_path):
