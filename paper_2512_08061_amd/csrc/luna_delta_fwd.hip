@@ -90,9 +90,9 @@ struct GateWave {
   const int g0, c0;
   unsigned rows[2][FS];  // row c of tiles 0 and 1 of K
 
-  // The rows 16 W .. of K K^T and Q K^T, of M and P, and N's diagonal block.
+  // The rows 16 W .. of K K^T and Q K^T, of M and P; returns N's diagonal block (rows 4 g + e of column c).
   template <int W>
-  __device__ __forceinline__ void rows_of(int buf, const float (&gates)[4][C], int bad) const {
+  __device__ __forceinline__ f32x4 rows_of(int buf, const float (&gates)[4][C]) const {
     const int g = anew(g0), c = anew(c0);
     const unsigned kb = lds_address(l.k[buf]), qb = lds_address(l.q[buf]);
     const auto row = [&](Frag<__bf16>& f, unsigned base, int tile, int t) { lds8(f, base + rows[tile % 2][t] + tile / 2 * 32 * DK * 2); };
@@ -105,18 +105,22 @@ struct GateWave {
     if (W > 0)
 #pragma unroll
       for (int t = 0; t < FS; ++t) row(kj[0][t], kb, 0, t);
+    const int key = l.key[buf], gate = l.gate;
     const float high = l.high[i], low = l.low[i], first = l.high[16 * W], first_low = l.low[16 * W];
     const f32x4 hj = lds4(lds_address(&l.high[16 * W + 4 * g])), lj = lds4(lds_address(&l.low[16 * W + 4 * g]));
+    const f32x4 beta = lds4(lds_address(&gates[kDeltaBeta][16 * W + 4 * g]));
     f32x4 from[KT], kk[KT], qk[KT];
 #pragma unroll
     for (int jt = 0; jt < W; ++jt) from[jt] = lds4(lds_address(&l.from[W][16 * jt + 4 * g]));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int jt = 0; jt <= W; ++jt) {
+    for (int n = 0; n <= W; ++n) {  // (the diagonal block first: its operands arrive first)
+      const int jt = n == 0 ? W : n - 1;
       kk[jt] = zero4();
       qk[jt] = zero4();
-      if (jt + 1 < W)
+      if (n > 0 && n < W)
 #pragma unroll
-        for (int t = 0; t < FS; ++t) row(kj[(jt + 1) % 2][t], kb, jt + 1, t);
+        for (int t = 0; t < FS; ++t) row(kj[n % 2][t], kb, n, t);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < FS; ++t) {
@@ -124,81 +128,96 @@ struct GateWave {
         mma(qk[jt], jt == W ? kf[t] : kj[jt % 2][t], qf[t]);
       }
     }
-    // e^(G_i - G_j): before the diagonal block as a product over the block's first row, in it directly
+    const int bad = __builtin_amdgcn_readfirstlane(min(key, gate));
+    // e^(G_i - G_j): before the diagonal block as a product over the block's first row, in it directly.  M's diagonal block comes
+    // as M^T and, K K^T being symmetric, as M.
     const float to = exp2_raw((high - first) + (low - first_low)), scaled = a.scale * to;
-    f32x4 mm[KT];
+    f32x4 mm[KT], pp[KT], z;
 #pragma unroll
-    for (int jt = 0; jt <= W; ++jt) {
-      f32x4 pp;
+    for (int jt = 0; jt <= W; ++jt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (jt < W) {
           mm[jt][e] = kk[jt][e] * (to * from[jt][e]);
-          pp[e] = qk[jt][e] * (scaled * from[jt][e]);
+          pp[jt][e] = qk[jt][e] * (scaled * from[jt][e]);
         } else {
-          const float f = exp2_raw((high - hj[e]) + (low - lj[e]));
+          const float d = (high - hj[e]) + (low - lj[e]), f = exp2_raw(fminf(d, 0.0f)), f2 = exp2_raw(fminf(-d, 0.0f));
           mm[jt][e] = 4 * g + e < c ? kk[jt][e] * f : 0.0f;
-          pp[e] = 4 * g + e <= c ? a.scale * f * qk[jt][e] : 0.0f;
+          pp[jt][e] = 4 * g + e <= c ? a.scale * f * qk[jt][e] : 0.0f;
+          z[e] = 4 * g + e > c ? kk[jt][e] * f2 : 0.0f;
         }
       }
-      if (bad < C)
+    if (bad < C)
+#pragma unroll
+      for (int jt = 0; jt <= W; ++jt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           mm[jt][e] = i < bad ? mm[jt][e] : 0.0f;
-          pp[e] = 16 * jt + 4 * g + e < bad ? pp[e] : 0.0f;
+          pp[jt][e] = 16 * jt + 4 * g + e < bad ? pp[jt][e] : 0.0f;
+          if (jt == W) z[e] = 16 * W + 4 * g + e < bad ? z[e] : 0.0f;
         }
+#pragma unroll
+    for (int n = 0; n <= W; ++n) {
+      const int jt = W - n;
       *reinterpret_cast<f32x4*>(&l.m[i][16 * jt + 4 * g]) = mm[jt];
-      store4(&l.p[buf][Rows<C>::at(i, 16 * jt + 4 * g)], pp[0], pp[1], pp[2], pp[3]);
     }
     wave_lds_fence();
-    // the diagonal block, a column a lane
-    float n[16], bn[16];
-    f32x4 beta[4];
+    f32x4 m4[4];  // M's blocks of 4 on the diagonal: row e of this lane group's
 #pragma unroll
-    for (int r = 0; r < 4; ++r) beta[r] = lds4(lds_address(&gates[kDeltaBeta][16 * W + 4 * r]));
-    constexpr int AHEAD = 4;  // rows read before their use
-    f32x4 m[16][4];
-    const auto read_m = [&](int r) {
+    for (int e = 1; e < 4; ++e) m4[e] = lds4(lds_address(&l.m[16 * W + 4 * g + e][16 * W + 4 * g]));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int p = 0; p < 4; ++p)
-        if (4 * p < r) m[r][p] = lds4(lds_address(&l.m[16 * W + r][16 * W + 4 * p]));
-    };
+    for (int jt = 0; jt <= W; ++jt) store4(&l.p[buf][Rows<C>::at(i, 16 * jt + 4 * g)], pp[jt][0], pp[jt][1], pp[jt][2], pp[jt][3]);
+    // The diagonal block by substitution, four rows at a time: lane group p's rows are solved among themselves, and
+    // all rows take what these contribute as a product (its own among them).
 #pragma unroll
-    for (int r = 0; r < 16; ++r) n[r] = l.m[16 * W + r][16 * W + c];
+    for (int p = 0; p < 4; ++p) {
+      f32x4 t = z, bn;
 #pragma unroll
-    for (int r = 1; r < AHEAD; ++r) read_m(r);
+      for (int e = 0; e < 4; ++e) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if (r + AHEAD < 16) read_m(r + AHEAD);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int k = 0; k < e; ++k) t[e] = fmaf(m4[e][k], bn[k], t[e]);
+        bn[e] = -beta[e] * t[e];
+      }
+      if (p == 3) {
 #pragma unroll
-      for (int p = 0; p < r; ++p) n[r] = fmaf(m[r][p / 4][p % 4], bn[p], n[r]);
-      bn[r] = -beta[r / 4][r % 4] * n[r];
+        for (int e = 0; e < 4; ++e) z[e] = g == p ? t[e] : z[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bn[e] = g == p ? bn[e] : 0.0f;
+        mma16(z, mm[W], bn);
+      }
     }
-    float x[4];  // rows 4 g + e
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      x[e] = g == 0 ? n[e] : g == 1 ? n[4 + e] : g == 2 ? n[8 + e] : n[12 + e];
-      x[e] = 4 * g + e > c ? -x[e] : 0.0f;
-      l.nd[W][4 * g + e][c] = x[e];
+      z[e] = -z[e];
+      l.nd[W][4 * g + e][c] = z[e];
     }
-    store_parts4<NP>(&l.n[buf][0][Rows<C>::at(16 * W + c, 16 * W + 4 * g)], C * C, x[0], x[1], x[2], x[3]);
+    store_parts4<NP>(&l.n[buf][0][Rows<C>::at(16 * W + c, 16 * W + 4 * g)], C * C, z[0], z[1], z[2], z[3]);
+    return z;
   }
 
-  // The blocks of N below the diagonal one of block column W: what each takes from the finished ones above it.
+  // The blocks of N below the diagonal one (x) of block column W: what each takes from the finished ones above it.
   template <int W>
-  __device__ __forceinline__ void column_of(int buf, const float (&gates)[4][C]) const {
+  __device__ __forceinline__ void column_of(int buf, const float (&gates)[4][C], const f32x4& x) const {
     const int g = anew(g0), c = anew(c0);
     f32x4 z[KT], an[KT], am[KT][KT], beta[KT], bn;
+    z[W] = x;
+    beta[W] = lds4(lds_address(&gates[kDeltaBeta][16 * W + 4 * g]));
 #pragma unroll
-    for (int i = W; i < KT; ++i) {
+    for (int i = W + 1; i < KT; ++i) am[i][W] = lds4(lds_address(&l.m[16 * i + c][16 * W + 4 * g]));
+#pragma unroll
+    for (int i = W + 1; i < KT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[i][e] = l.m[16 * i + 4 * g + e][16 * W + c];
+#pragma unroll
+    for (int i = W + 1; i < KT; ++i) {
       beta[i] = lds4(lds_address(&gates[kDeltaBeta][16 * i + 4 * g]));
+      an[i] = lds4(lds_address(&l.nd[i][c][4 * g]));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) z[i][e] = i == W ? l.nd[i][4 * g + e][c] : l.m[16 * i + 4 * g + e][16 * W + c];
-#pragma unroll
-      for (int p = W; p < i; ++p) am[i][p] = lds4(lds_address(&l.m[16 * i + c][16 * p + 4 * g]));
-      if (i > W) an[i] = lds4(lds_address(&l.nd[i][c][4 * g]));
+      for (int p = W + 1; p < i; ++p) am[i][p] = lds4(lds_address(&l.m[16 * i + c][16 * p + 4 * g]));
     }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int p = W; p < KT; ++p) {
       if (p == W) {
@@ -214,12 +233,34 @@ struct GateWave {
         store_parts4<NP>(&l.n[buf][0][Rows<C>::at(16 * W + c, 16 * p + 4 * g)], C * C, -y[0], -y[1], -y[2], -y[3]);
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int i = p + 1; i < KT; ++i) z[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(am[i][p][e], bn[e], z[i], 0, 0, 0);
+      for (int i = p + 1; i < KT; ++i) mma16(z[i], am[i][p], bn);
     }
   }
 };
+
+// x of the lanes of a row, or of a row's last lane, that a DPP control names; zeros where there is none.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double dpp(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, ROWS, 0xf, ROWS == 0xf);
+  const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, ROWS, 0xf, ROWS == 0xf);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Sums over the lanes up to this one.
+__device__ __forceinline__ double lane_sums(double x) {
+  x += dpp<0x111>(x);       // a lane before in the row of 16
+  x += dpp<0x112>(x);       // two
+  x += dpp<0x114>(x);       // four
+  x += dpp<0x118>(x);       // eight
+  x += dpp<0x142, 0xa>(x);  // the last lane of the row before, for rows 1 and 3
+  x += dpp<0x143, 0xc>(x);  // lane 31, for rows 2 and 3
+  return x;
+}
+__device__ __forceinline__ double of_lane(double x, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)u, lane), hi = __builtin_amdgcn_readlane((int)(unsigned)(u >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 
 template <int DK, int DVW, int NP>
 __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a) {
@@ -284,7 +325,7 @@ __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a
         qr[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(bq, qat[j], 0, 0));
       }
     };
-    const auto load_gates = [&](int chunk) {  // (by the last wave, a chunk before they are formed)
+    const auto load_gates = [&](int chunk) {  // (a chunk before the last wave forms them)
       const int64_t num = seq_num(a.s, sp, a.H, head, min(chunk * C + lane, sp.len - 1));
       gr = a.log_decay[num];
       br = a.beta[num];
@@ -297,13 +338,7 @@ __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a
       const int bad = lost ? (int)__builtin_ctzll(lost) : C;
       if (lane >= bad) x = beta = 0.0f;
       // (e^-128 is 0 in fp32; in base 2)
-      double sum = (double)fminf(fmaxf(x, -128.0f), 0.0f) * 1.4426950408889634;
-#pragma unroll
-      for (int s = 1; s < kWave; s *= 2) {
-        const double other = __shfl_up(sum, s);
-        sum += lane >= s ? other : 0.0;
-      }
-      const double whole = __shfl(sum, kWave - 1);
+      const double sum = lane_sums((double)fminf(fmaxf(x, -128.0f), 0.0f) * 1.4426950408889634), whole = of_lane(sum, kWave - 1);
       const float high = (float)sum;
       l.high[lane] = high;
       l.low[lane] = (float)(sum - (double)high);
@@ -311,18 +346,16 @@ __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a
       gates[kDeltaLast][lane] = exp2_raw((float)(whole - sum));
       gates[kDeltaBeta][lane] = beta;
 #pragma unroll
-      for (int t = 1; t < KT; ++t) l.from[t][lane] = exp2_raw((float)fmin(__shfl(sum, 16 * t) - sum, 0.0));
+      for (int t = 1; t < KT; ++t) l.from[t][lane] = exp2_raw((float)fmin(of_lane(sum, 16 * t) - sum, 0.0));
       if (lane == 0) {
         gates[kDeltaMisc][0] = exp2_raw((float)whole);
         l.gate = bad;
       }
     };
     load(0);
-    if (w == KT - 1) {
-      load_gates(0);
-      form_gates(0, 0);
-      load_gates(min(1, chunks - 1));
-    }
+    load_gates(0);
+    if (w == KT - 1) form_gates(0, 0);
+    load_gates(min(1, chunks - 1));
     int slot = 0;
     for (int chunk = 0; chunk <= chunks; ++chunk) {  // (beside the scan of chunk - 1)
       const int buf = chunk % 2, next = slot == 2 ? 0 : slot + 1;
@@ -347,30 +380,28 @@ __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a
           }
       }
       __syncthreads();
+      f32x4 diag = zero4();
       if (chunk < chunks) {
-        const int bad = __builtin_amdgcn_readfirstlane(min(l.key[buf], l.gate));
         if (tid == 0) {
           l.key[1 - buf] = C;
-          reinterpret_cast<int&>(gates[kDeltaMisc][1]) = bad;
+          reinterpret_cast<int&>(gates[kDeltaMisc][1]) = min(l.key[buf], l.gate);
         }
+        diag = w == 0 ? gate.template rows_of<0>(buf, gates) : w == 1 ? gate.template rows_of<1>(buf, gates)
+             : w == 2 ? gate.template rows_of<2>(buf, gates) : gate.template rows_of<3>(buf, gates);
         if (chunk + 1 < chunks) load(chunk + 1);
-        if (w == 0) gate.template rows_of<0>(buf, gates, bad);
-        else if (w == 1) gate.template rows_of<1>(buf, gates, bad);
-        else if (w == 2) gate.template rows_of<2>(buf, gates, bad);
-        else gate.template rows_of<3>(buf, gates, bad);
       }
       __syncthreads();
       if (chunk < chunks) {
         if (w == 0) {
-          gate.template column_of<0>(buf, gates);
+          gate.template column_of<0>(buf, gates, diag);
         } else if (w == 1) {
-          gate.template column_of<1>(buf, gates);
+          gate.template column_of<1>(buf, gates, diag);
         } else if (w == 2) {
-          gate.template column_of<2>(buf, gates);
-        } else if (chunk + 1 < chunks) {  // the gates of the next chunk
+          gate.template column_of<2>(buf, gates, diag);
+        } else if (chunk + 1 < chunks) {
           form_gates(chunk + 1, next);
-          load_gates(min(chunk + 2, chunks - 1));
         }
+        load_gates(min(chunk + 2, chunks - 1));
       }
       __syncthreads();
       slot = next;
