@@ -41,11 +41,12 @@ template <int DK, int NP>
 struct FwdLds {
   __bf16 k[2][C * DK], q[2][C * DK];
   __bf16 n[2][NP][C * C], p[2][C * C];  // N transposed
-  float m[C][C + 4];
-  float nd[KT][16][20];  // diagonal blocks of N
-  float gates[3][4][C];  // (formed while the two chunks before are at work)
+  // M below its diagonal blocks, in parts: of a row the first two parts of four columns, and the third of them
+  __bf16 m[C][2 * C + 8], m3[NP == 3 ? C : 2][C + 4];
+  alignas(16) float gates[3][4][C];  // (formed while the two chunks before are at work)
   float high[C], low[C];
   float from[KT][C];  // e^(G_i0 - G_j) for the rows i0 = 16 w
+  float to[C];        // e^(G_i - G_i0) for i's block's first row i0
   int since[64];      // per column: the first token with a value that is not finite
   int key[2], gate;   // the first row with a key, or gate, that is not finite
 };
@@ -58,6 +59,7 @@ __device__ __forceinline__ unsigned lds_address(const void* p) {
 __device__ __forceinline__ void lds8(Frag<__bf16>& f, unsigned at) {
   f.v = *(__attribute__((address_space(3))) const bf16x8*)(uintptr_t)at;
 }
+__device__ __forceinline__ void lds8_store(unsigned at, const Frag<__bf16>& f) { *(__attribute__((address_space(3))) bf16x8*)(uintptr_t)at = f.v; }
 __device__ __forceinline__ f32x4 lds4(unsigned at) { return *(__attribute__((address_space(3))) const f32x4*)(uintptr_t)at; }
 // eight rows of a column, four and four `step` bytes apart
 __device__ __forceinline__ void lds_tr(Frag<__bf16>& f, unsigned at, int step) {
@@ -74,11 +76,43 @@ __device__ __forceinline__ int anew(int x) {
   return x;
 }
 
-// c += A B of fp32 blocks of 16: row c of A (four numbers from 4 g on), and B as a sum's registers are.
-__device__ __forceinline__ void mma16(f32x4& c, const f32x4& a, const f32x4& b) {
+// Four numbers in parts.
+template <int NP>
+struct Parts4 {
+  bf16x4 p[NP];
+};
+template <int NP>
+__device__ __forceinline__ Parts4<NP> parts_of(f32x4 x) {
+  Parts4<NP> r;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+  for (int k = 0; k < NP; ++k) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.p[k][e] = (__bf16)x[e];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] -= (float)r.p[k][e];
+  }
+  return r;
 }
+// c += A B of fp32 blocks of 16, both in parts: row c of A (four numbers from 4 g on), and B as a sum's registers are.  A bf16
+// product has room for two of the products of parts.  (As fp32 products, 128 cycles each instead of 32 or 48, the blocks of N
+// below its diagonal ones took 4100 cycles a chunk beside the scan's products.)
+template <int NP>
+__device__ __forceinline__ void mma16(f32x4& c, const Parts4<NP>& a, const Parts4<NP>& b) {
+  const auto two = [](const bf16x4& x, const bf16x4& y) {
+    Frag<__bf16> f;
+    f.v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    return f;
+  };
+  if constexpr (NP == 3) mma(c, two(a.p[0], a.p[2]), two(b.p[2], b.p[0]));
+  mma(c, two(a.p[0], a.p[1]), two(b.p[1], b.p[1]));
+  mma(c, two(a.p[0], a.p[1]), two(b.p[0], b.p[0]));
+}
+// four rows of a column
+__device__ __forceinline__ bf16x4 lds_tr4(unsigned at) {
+  typedef __attribute__((ext_vector_type(4))) short i16x4;
+  return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(uintptr_t)at));
+}
+__device__ __forceinline__ bf16x4 lds_b4(unsigned at) { return *(__attribute__((address_space(3))) const bf16x4*)(uintptr_t)at; }
 
 // What every gate wave has.
 template <int DK, int NP>
@@ -90,86 +124,110 @@ struct GateWave {
   const int g0, c0;
   unsigned rows[2][FS];  // row c of tiles 0 and 1 of K
 
-  // The rows 16 W .. of K K^T and Q K^T, of M and P; returns N's diagonal block (rows 4 g + e of column c).
+  // Of K K^T and Q K^T, M and P: the diagonal block W (kf, qf: its rows of K and Q) and one or two of those below the
+  // diagonal, (3, 0) | (1, 0) | (2, 0), (2, 1) | (3, 1), (3, 2), so that no wave has more than three.  Returns N's diagonal block
+  // (rows 4 g + e of column c).
   template <int W>
-  __device__ __forceinline__ f32x4 rows_of(int buf, const float (&gates)[4][C]) const {
+  __device__ __forceinline__ f32x4 blocks_of(int buf, const float (&gates)[4][C], const Frag<__bf16> (&kf)[FS],
+                                             const Frag<__bf16> (&qf)[FS]) const {
+    constexpr int OFF = W < 2 ? 1 : 2, I = W == 0 ? KT - 1 : W, J0 = W == 3 ? 1 : 0;  // blocks (I, J0 ..)
     const int g = anew(g0), c = anew(c0);
     const unsigned kb = lds_address(l.k[buf]), qb = lds_address(l.q[buf]);
     const auto row = [&](Frag<__bf16>& f, unsigned base, int tile, int t) { lds8(f, base + rows[tile % 2][t] + tile / 2 * 32 * DK * 2); };
-    const int i = 16 * W + c;
-    Frag<__bf16> kf[FS], qf[FS], kj[2][FS];
+    const int i = 16 * I + c;
+    Frag<__bf16> ki[FS], qi[FS], kj[OFF][FS];
 #pragma unroll
-    for (int t = 0; t < FS; ++t) row(kf[t], kb, W, t);
-#pragma unroll
-    for (int t = 0; t < FS; ++t) row(qf[t], qb, W, t);
-    if (W > 0)
-#pragma unroll
-      for (int t = 0; t < FS; ++t) row(kj[0][t], kb, 0, t);
+    for (int t = 0; t < FS; ++t) {
+      if (W == 0) {
+        row(ki[t], kb, I, t);
+        row(qi[t], qb, I, t);
+        kj[0][t] = kf[t];
+      } else {
+        ki[t] = kf[t];
+        qi[t] = qf[t];
+        row(kj[0][t], kb, J0, t);
+      }
+    }
     const int key = l.key[buf], gate = l.gate;
-    const float high = l.high[i], low = l.low[i], first = l.high[16 * W], first_low = l.low[16 * W];
     const f32x4 hj = lds4(lds_address(&l.high[16 * W + 4 * g])), lj = lds4(lds_address(&l.low[16 * W + 4 * g]));
+    const float high = l.high[16 * W + c], low = l.low[16 * W + c];
     const f32x4 beta = lds4(lds_address(&gates[kDeltaBeta][16 * W + 4 * g]));
-    f32x4 from[KT], kk[KT], qk[KT];
+    const float to_row = l.to[i];
+    f32x4 from[OFF], kk[OFF], qk[OFF], kd = zero4(), qd = zero4();
 #pragma unroll
-    for (int jt = 0; jt < W; ++jt) from[jt] = lds4(lds_address(&l.from[W][16 * jt + 4 * g]));
+    for (int n = 0; n < OFF; ++n) from[n] = lds4(lds_address(&l.from[I][16 * (J0 + n) + 4 * g]));
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int n = 0; n <= W; ++n) {  // (the diagonal block first: its operands arrive first)
-      const int jt = n == 0 ? W : n - 1;
-      kk[jt] = zero4();
-      qk[jt] = zero4();
-      if (n > 0 && n < W)
+    for (int t = 0; t < FS; ++t) {
+      mma(kd, kf[t], kf[t]);
+      mma(qd, kf[t], qf[t]);
+    }
 #pragma unroll
-        for (int t = 0; t < FS; ++t) row(kj[n % 2][t], kb, n, t);
+    for (int n = 0; n < OFF; ++n) {
+      kk[n] = zero4();
+      qk[n] = zero4();
+      if (n + 1 < OFF)
+#pragma unroll
+        for (int t = 0; t < FS; ++t) row(kj[n + 1][t], kb, J0 + n + 1, t);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < FS; ++t) {
-        mma(kk[jt], jt == W ? kf[t] : kj[jt % 2][t], kf[t]);
-        mma(qk[jt], jt == W ? kf[t] : kj[jt % 2][t], qf[t]);
+        mma(kk[n], kj[n][t], ki[t]);
+        mma(qk[n], kj[n][t], qi[t]);
       }
     }
     const int bad = __builtin_amdgcn_readfirstlane(min(key, gate));
-    // e^(G_i - G_j): before the diagonal block as a product over the block's first row, in it directly.  M's diagonal block comes
+    // e^(G_i - G_j): in the diagonal block directly, below it as a product over the first row of i's block.  M's diagonal block comes
     // as M^T and, K K^T being symmetric, as M.
-    const float to = exp2_raw((high - first) + (low - first_low)), scaled = a.scale * to;
-    f32x4 mm[KT], pp[KT], z;
+    f32x4 md, pd, mm[OFF], pp[OFF], z;
 #pragma unroll
-    for (int jt = 0; jt <= W; ++jt)
+    for (int e = 0; e < 4; ++e) {
+      const float d = (high - hj[e]) + (low - lj[e]), f = exp2_raw(fminf(d, 0.0f)), f2 = exp2_raw(fminf(-d, 0.0f));
+      md[e] = 4 * g + e < c ? kd[e] * f : 0.0f;
+      pd[e] = 4 * g + e <= c ? a.scale * f * qd[e] : 0.0f;
+      z[e] = 4 * g + e > c ? kd[e] * f2 : 0.0f;
+    }
+#pragma unroll
+    for (int n = 0; n < OFF; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (jt < W) {
-          mm[jt][e] = kk[jt][e] * (to * from[jt][e]);
-          pp[jt][e] = qk[jt][e] * (scaled * from[jt][e]);
-        } else {
-          const float d = (high - hj[e]) + (low - lj[e]), f = exp2_raw(fminf(d, 0.0f)), f2 = exp2_raw(fminf(-d, 0.0f));
-          mm[jt][e] = 4 * g + e < c ? kk[jt][e] * f : 0.0f;
-          pp[jt][e] = 4 * g + e <= c ? a.scale * f * qk[jt][e] : 0.0f;
-          z[e] = 4 * g + e > c ? kk[jt][e] * f2 : 0.0f;
+        const float f = to_row * from[n][e];
+        mm[n][e] = kk[n][e] * f;
+        pp[n][e] = qk[n][e] * (a.scale * f);
+      }
+    if (bad < C) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        md[e] = 16 * W + c < bad ? md[e] : 0.0f;
+        pd[e] = 16 * W + 4 * g + e < bad ? pd[e] : 0.0f;
+        z[e] = 16 * W + 4 * g + e < bad ? z[e] : 0.0f;
+#pragma unroll
+        for (int n = 0; n < OFF; ++n) {
+          mm[n][e] = i < bad ? mm[n][e] : 0.0f;
+          pp[n][e] = 16 * (J0 + n) + 4 * g + e < bad ? pp[n][e] : 0.0f;
         }
       }
-    if (bad < C)
-#pragma unroll
-      for (int jt = 0; jt <= W; ++jt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          mm[jt][e] = i < bad ? mm[jt][e] : 0.0f;
-          pp[jt][e] = 16 * jt + 4 * g + e < bad ? pp[jt][e] : 0.0f;
-          if (jt == W) z[e] = 16 * W + 4 * g + e < bad ? z[e] : 0.0f;
-        }
-#pragma unroll
-    for (int n = 0; n <= W; ++n) {
-      const int jt = W - n;
-      *reinterpret_cast<f32x4*>(&l.m[i][16 * jt + 4 * g]) = mm[jt];
     }
-    wave_lds_fence();
-    f32x4 m4[4];  // M's blocks of 4 on the diagonal: row e of this lane group's
+    // M's blocks of 4 on the diagonal: of this lane group's, row e
+    f32x4 m4[4];
 #pragma unroll
-    for (int e = 1; e < 4; ++e) m4[e] = lds4(lds_address(&l.m[16 * W + 4 * g + e][16 * W + 4 * g]));
+    for (int e = 1; e < 4; ++e)
+#pragma unroll
+      for (int k = 0; k < e; ++k) m4[e][k] = __shfl(z[e], 20 * g + k);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int jt = 0; jt <= W; ++jt) store4(&l.p[buf][Rows<C>::at(i, 16 * jt + 4 * g)], pp[jt][0], pp[jt][1], pp[jt][2], pp[jt][3]);
+    for (int n = 0; n < OFF; ++n) {
+      const Parts4<NP> x = parts_of<NP>(mm[n]);
+      Frag<__bf16> f;
+      f.v = __builtin_shufflevector(x.p[0], x.p[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      *reinterpret_cast<bf16x8*>(&l.m[i][32 * (J0 + n) + 8 * g]) = f.v;
+      if constexpr (NP == 3) *reinterpret_cast<bf16x4*>(&l.m3[i][16 * (J0 + n) + 4 * g]) = x.p[2];
+      store4(&l.p[buf][Rows<C>::at(i, 16 * (J0 + n) + 4 * g)], pp[n][0], pp[n][1], pp[n][2], pp[n][3]);
+    }
+    store4(&l.p[buf][Rows<C>::at(16 * W + c, 16 * W + 4 * g)], pd[0], pd[1], pd[2], pd[3]);
     // The diagonal block by substitution, four rows at a time: lane group p's rows are solved among themselves, and
     // all rows take what these contribute as a product (its own among them).
+    const Parts4<NP> mp = parts_of<NP>(md);
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
       f32x4 t = z, bn;
@@ -185,14 +243,11 @@ struct GateWave {
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) bn[e] = g == p ? bn[e] : 0.0f;
-        mma16(z, mm[W], bn);
+        mma16(z, mp, parts_of<NP>(bn));
       }
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      z[e] = -z[e];
-      l.nd[W][4 * g + e][c] = z[e];
-    }
+    for (int e = 0; e < 4; ++e) z[e] = -z[e];
     store_parts4<NP>(&l.n[buf][0][Rows<C>::at(16 * W + c, 16 * W + 4 * g)], C * C, z[0], z[1], z[2], z[3]);
     return z;
   }
@@ -200,24 +255,43 @@ struct GateWave {
   // The blocks of N below the diagonal one (x) of block column W: what each takes from the finished ones above it.
   template <int W>
   __device__ __forceinline__ void column_of(int buf, const float (&gates)[4][C], const f32x4& x) const {
-    const int g = anew(g0), c = anew(c0);
-    f32x4 z[KT], an[KT], am[KT][KT], beta[KT], bn;
+    const int g = anew(g0), c = anew(c0), tr = 4 * g + c / 4, q = c % 4;
+    const auto block = [&](Parts4<NP>& y, int i, int p) {  // row c of a block of M
+      Frag<__bf16> f;
+      lds8(f, lds_address(&l.m[c][8 * g]) + 16 * i * (2 * C + 8) * 2 + 16 * p * 4);
+      y.p[0] = __builtin_shufflevector(f.v, f.v, 0, 1, 2, 3);
+      y.p[1] = __builtin_shufflevector(f.v, f.v, 4, 5, 6, 7);
+      if constexpr (NP == 3) y.p[2] = lds_b4(lds_address(&l.m3[c][4 * g]) + 16 * i * (C + 4) * 2 + 16 * p * 2);
+    };
+    Parts4<NP> an[KT], am[KT][KT], zp[KT];
+    f32x4 z[KT], beta[KT], bn;
     z[W] = x;
     beta[W] = lds4(lds_address(&gates[kDeltaBeta][16 * W + 4 * g]));
 #pragma unroll
-    for (int i = W + 1; i < KT; ++i) am[i][W] = lds4(lds_address(&l.m[16 * i + c][16 * W + 4 * g]));
+    for (int i = W + 1; i < KT; ++i) block(am[i][W], i, W);
 #pragma unroll
-    for (int i = W + 1; i < KT; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) z[i][e] = l.m[16 * i + 4 * g + e][16 * W + c];
+    for (int i = W + 1; i < KT; ++i) {  // four rows of column c
+      const unsigned at = lds_address(&l.m[tr][8 * q]) + 16 * i * (2 * C + 8) * 2 + 16 * W * 4;
+      zp[i].p[0] = lds_tr4(at);
+      zp[i].p[1] = lds_tr4(at + 8);
+      if constexpr (NP == 3) zp[i].p[2] = lds_tr4(lds_address(&l.m3[tr][4 * q]) + 16 * i * (C + 4) * 2 + 16 * W * 2);
+    }
 #pragma unroll
     for (int i = W + 1; i < KT; ++i) {
       beta[i] = lds4(lds_address(&gates[kDeltaBeta][16 * i + 4 * g]));
-      an[i] = lds4(lds_address(&l.nd[i][c][4 * g]));
 #pragma unroll
-      for (int p = W + 1; p < i; ++p) am[i][p] = lds4(lds_address(&l.m[16 * i + c][16 * p + 4 * g]));
+      for (int k = 0; k < NP; ++k) an[i].p[k] = lds_tr4(lds_address(&l.n[buf][k][Rows<C>::at(16 * i + tr, 16 * i + 4 * q)]));
+#pragma unroll
+      for (int p = W + 1; p < i; ++p) block(am[i][p], i, p);
     }
     __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = W + 1; i < KT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        z[i][e] = (float)zp[i].p[0][e] + (float)zp[i].p[1][e];
+        if constexpr (NP == 3) z[i][e] = (float)zp[i].p[0][e] + ((float)zp[i].p[1][e] + (float)zp[i].p[2][e]);
+      }
 #pragma unroll
     for (int p = W; p < KT; ++p) {
       if (p == W) {
@@ -227,13 +301,16 @@ struct GateWave {
         f32x4 bz, y = z[p];
 #pragma unroll
         for (int e = 0; e < 4; ++e) bz[e] = beta[p][e] * z[p][e];
-        mma16(y, an[p], bz);
+        mma16(y, an[p], parts_of<NP>(bz));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bn[e] = -beta[p][e] * y[e];
-        store_parts4<NP>(&l.n[buf][0][Rows<C>::at(16 * W + c, 16 * p + 4 * g)], C * C, -y[0], -y[1], -y[2], -y[3]);
+        for (int e = 0; e < 4; ++e) y[e] = -y[e], bn[e] = beta[p][e] * y[e];
+        store_parts4<NP>(&l.n[buf][0][Rows<C>::at(16 * W + c, 16 * p + 4 * g)], C * C, y[0], y[1], y[2], y[3]);
       }
+      if (p + 1 < KT) {
+        const Parts4<NP> b = parts_of<NP>(bn);
 #pragma unroll
-      for (int i = p + 1; i < KT; ++i) mma16(z[i], am[i][p], bn);
+        for (int i = p + 1; i < KT; ++i) mma16(z[i], am[i][p], b);
+      }
     }
   }
 };
@@ -266,7 +343,6 @@ template <int DK, int DVW, int NP>
 __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a) {
   using Lds = FwdLds<DK, NP>;
   constexpr int FT = DK / 16, FS = DK / 32, SCAN = DVW / 16;  // feature tiles, and scan waves
-  constexpr int TL = C * DK / 8 / 256;                        // 16-byte pieces of a tile per gate thread
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
@@ -299,30 +375,27 @@ __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a
   if (wave >= SCAN) {
     // ------------------------------------------------------------------ gate waves
     const int w = wave - SCAN, tid = threadIdx.x - 64 * SCAN;
+    if constexpr (NP == 2) __builtin_amdgcn_s_setprio(3);
     GateWave<DK, NP> gate{a, l, g, c, {}};
 #pragma unroll
     for (int t = 0; t < FS; ++t) {
       gate.rows[0][t] = Rows<DK>::byte(c, 32 * t + 8 * g);
       gate.rows[1][t] = Rows<DK>::byte(16 + c, 32 * t + 8 * g);
     }
-    i32x4 kr[TL], qr[TL];
-    int kat[TL], qat[TL], to[TL];
+    unsigned to_row[FS];
 #pragma unroll
-    for (int j = 0; j < TL; ++j) {
-      const int at = tid + 256 * j, r = at / (DK / 8), col = at % (DK / 8) * 8;
-      kat[j] = (r * (int)a.k.row + col) * 2;
-      qat[j] = (r * (int)a.q.row + col) * 2;
-      to[j] = Rows<DK>::at(r, col);
-    }
+    for (int t = 0; t < FS; ++t) to_row[t] = Rows<DK>::byte(16 * w + c, 32 * t + 8 * g);
+    Frag<__bf16> kr[FS], qr[FS];  // this wave's 16 rows
+    const int kat = ((16 * w + c) * (int)a.k.row + 8 * g) * 2, qat = ((16 * w + c) * (int)a.q.row + 8 * g) * 2;
     float gr = 0.0f, br = 0.0f;
     const auto load = [&](int chunk) {
       const int t0 = chunk * C, m = min(C, sp.len - t0);  // (rows from m on lie behind the buffers)
       const Buf bk = buffer(seq_row(a.k, sp, packed, hk, t0, 2), (int)(((m - 1) * a.k.row + DK) * 2));
       const Buf bq = buffer(seq_row(a.q, sp, packed, hk, t0, 2), (int)(((m - 1) * a.q.row + DK) * 2));
 #pragma unroll
-      for (int j = 0; j < TL; ++j) {
-        kr[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(bk, kat[j], 0, 0));
-        qr[j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(bq, qat[j], 0, 0));
+      for (int t = 0; t < FS; ++t) {
+        buf_load8(kr[t], bk, kat + 64 * t);
+        buf_load8(qr[t], bq, qat + 64 * t);
       }
     };
     const auto load_gates = [&](int chunk) {  // (a chunk before the last wave forms them)
@@ -347,6 +420,10 @@ __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a
       gates[kDeltaBeta][lane] = beta;
 #pragma unroll
       for (int t = 1; t < KT; ++t) l.from[t][lane] = exp2_raw((float)fmin(of_lane(sum, 16 * t) - sum, 0.0));
+      double row0 = of_lane(sum, 0);
+#pragma unroll
+      for (int t = 1; t < KT; ++t) row0 = lane >= 16 * t ? of_lane(sum, 16 * t) : row0;
+      l.to[lane] = exp2_raw((float)(sum - row0));
       if (lane == 0) {
         gates[kDeltaMisc][0] = exp2_raw((float)whole);
         l.gate = bad;
@@ -364,20 +441,12 @@ __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a
       if (chunk < chunks) {
         bool odd = false;
 #pragma unroll
-        for (int j = 0; j < TL; ++j) {
-          Frag<__bf16> f;
-          f.v = __builtin_bit_cast(bf16x8, kr[j]);
-          odd |= not_finite(f);
-          *reinterpret_cast<i32x4*>(&l.k[buf][to[j]]) = kr[j];
-          *reinterpret_cast<i32x4*>(&l.q[buf][to[j]]) = qr[j];
+        for (int t = 0; t < FS; ++t) {
+          odd |= not_finite(kr[t]);
+          lds8_store(lds_address(l.k[buf]) + to_row[t], kr[t]);
+          lds8_store(lds_address(l.q[buf]) + to_row[t], qr[t]);
         }
-        if (__any(odd))
-#pragma unroll
-          for (int j = 0; j < TL; ++j) {
-            Frag<__bf16> f;
-            f.v = __builtin_bit_cast(bf16x8, kr[j]);
-            if (not_finite(f)) atomicMin(&l.key[buf], (tid + 256 * j) / (DK / 8));
-          }
+        if (__any(odd) && odd) atomicMin(&l.key[buf], 16 * w + c);
       }
       __syncthreads();
       f32x4 diag = zero4();
@@ -386,8 +455,8 @@ __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a
           l.key[1 - buf] = C;
           reinterpret_cast<int&>(gates[kDeltaMisc][1]) = min(l.key[buf], l.gate);
         }
-        diag = w == 0 ? gate.template rows_of<0>(buf, gates) : w == 1 ? gate.template rows_of<1>(buf, gates)
-             : w == 2 ? gate.template rows_of<2>(buf, gates) : gate.template rows_of<3>(buf, gates);
+        diag = w == 0 ? gate.template blocks_of<0>(buf, gates, kr, qr) : w == 1 ? gate.template blocks_of<1>(buf, gates, kr, qr)
+             : w == 2 ? gate.template blocks_of<2>(buf, gates, kr, qr) : gate.template blocks_of<3>(buf, gates, kr, qr);
         if (chunk + 1 < chunks) load(chunk + 1);
       }
       __syncthreads();
@@ -474,11 +543,11 @@ __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < KT; ++i) mma(r[i], kf[t % 2][i], sf[t]);
+      if (t == (FS - 1) / 2) __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < KT; ++i) first[i] = gate4(kDeltaFirst, i), beta[i] = gate4(kDeltaBeta, i);
     const int bad = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int&>(gates[kDeltaMisc][1]));
-    __syncthreads();
     // R and beta R
     DeltaOp<__bf16, NP> br[KS];
     {
