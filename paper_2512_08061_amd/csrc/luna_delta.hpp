@@ -165,9 +165,8 @@ hipError_t launch_delta_gates(Dt dt, const DeltaArgs& a, hipStream_t s);
 // out and the state: in bf16 all in one launch (exact: the state to fp32 accuracy), in fp32 behind the gates' launch
 hipError_t launch_delta_fwd_bf16(bool exact, const DeltaArgs& a, hipStream_t s);
 hipError_t launch_delta_fwd_f32(const DeltaArgs& a, hipStream_t s);
-// the backward pass: E and the states before the chunks; X and the gradients of the states behind them; the gradients
-hipError_t launch_delta_record(Dt dt, const DeltaArgs& a, hipStream_t s);
-hipError_t launch_delta_back(Dt dt, const DeltaArgs& a, hipStream_t s);
+// the backward pass: E and the states before the chunks, X and the gradients of the states behind them; the gradients
+hipError_t launch_delta_both(Dt dt, const DeltaArgs& a, hipStream_t s);
 hipError_t launch_delta_grads(Dt dt, const DeltaArgs& a, hipStream_t s);
 // Value columns of a workgroup of the serial passes.
 constexpr int delta_columns(int64_t d) { return d < 64 ? 32 : 64; }

@@ -3,7 +3,6 @@
 
 namespace luna {
 
-hipError_t launch_delta_record_bf16(const DeltaArgs& a, hipStream_t s) { LUNA_DELTA_WIDTHS(launch_scan_one, __bf16, kDeltaBackParts, false); }
-hipError_t launch_delta_back_bf16(const DeltaArgs& a, hipStream_t s) { LUNA_DELTA_WIDTHS(launch_back_one, __bf16, kDeltaBackParts); }
+hipError_t launch_delta_both_bf16(const DeltaArgs& a, hipStream_t s) { LUNA_DELTA_WIDTHS(launch_both_one, __bf16, , kDeltaBackParts); }
 
 }  // namespace luna

@@ -71,15 +71,15 @@ __device__ __forceinline__ void load_op_pair_tr(DeltaOp<T, P>& f, const T* x, in
 }
 
 template <typename T, int DK, int DVW, int NP, bool OUT>
-__global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
+__device__ __forceinline__ void delta_scan(const DeltaArgs& a, int block, char* raw) {
   using Lds = ScanLds<T, DK, DVW, NP, 1, OUT>;
   constexpr int C = Lds::C, FT = DK / 16, FS = DK / 32, KT = C / 16, KS = C / 32, esz = (int)sizeof(T), THREADS = 4 * DVW;
+  constexpr int TI = FT < 4 ? FT : 4, TN = FT * KS / TI;  // tiles of a batch of transposed reads, and batches
   static_assert(!OUT || sizeof(T) == 4, "bf16 has a forward kernel of its own");
-  extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
   const int slices = a.d / DVW;
-  const int slice = blockIdx.x % slices, head = (blockIdx.x / slices) % a.H, b = blockIdx.x / slices / a.H;
+  const int slice = block % slices, head = (block / slices) % a.H, b = block / slices / a.H;
   const SeqPiece sp = seq_uniform(seq_of(a.s, b));
   if (sp.len == 0) return;
   const bool packed = a.s.offsets != nullptr;
@@ -147,26 +147,47 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
 #pragma unroll
       for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(to + pair_rows(ft, g)) = S[ft];
     }
+    // (operands are read from LDS a batch before their products)
     f32x4 r[KT], o[KT];
+    Frag<T> kf[2][KT], qf[2][OUT ? KT : 1], tf[2][TI];
+    DeltaOp<T, NP> nf[KT][KS];
+    const auto read_k = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        load8(kf[t % 2][i], &l.k[pair_row(i, c)][32 * t + 8 * g]);
+        if constexpr (OUT) load8(qf[t % 2][i], &l.q[16 * i + c][32 * t + 8 * g]);
+      }
+    };
+    const auto read_t = [&](int n) {
+#pragma unroll
+      for (int i = 0; i < TI; ++i) load_pair_tr(tf[n % 2][i], &l.k[0][0], Lds::PK, (TI * n + i) % FT, 32 * ((TI * n + i) / FT), lane);
+    };
+    const auto gate4 = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&l.gates[which][pair_rows(i, g)]); };
+    f32x4 first[KT], beta[KT], last[KT];
+    Frag<T> v[KT];
+    read_k(0);
 #pragma unroll
     for (int i = 0; i < KT; ++i) r[i] = zero4(), o[i] = zero4();
 #pragma unroll
     for (int t = 0; t < FS; ++t) {
-      DeltaOp<T, NP> sf;
-      set_tiles(sf, S[2 * t], S[2 * t + 1]);
-#pragma unroll
-      for (int i = 0; i < KT; ++i) {
-        Frag<T> f;
-        load8(f, &l.k[pair_row(i, c)][32 * t + 8 * g]);
-        mma(r[i], f, sf);
-      }
-      if constexpr (OUT) {
+      if (t + 1 < FS) read_k(t + 1);
+      else
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
-          Frag<T> f;
-          load8(f, &l.q[16 * i + c][32 * t + 8 * g]);
-          mma(o[i], sf, f);
+          first[i] = gate4(kDeltaFirst, i);
+          beta[i] = gate4(kDeltaBeta, i);
+          last[i] = gate4(kDeltaLast, i);
+          load_tr4(v[i], 0, &l.v[0][0], Lds::PV, pair_rows(i, g), wcol, lane);
+#pragma unroll
+          for (int s = 0; s <= i / 2; ++s) load_op(nf[i][s], &l.n[0][pair_row(i, c)][32 * s + 8 * g], C * Lds::PN);
         }
+      DeltaOp<T, NP> sf;
+      set_tiles(sf, S[2 * t], S[2 * t + 1]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        mma(r[i], kf[t % 2][i], sf);
+        if constexpr (OUT) mma(o[i], sf, qf[t % 2][i]);
       }
     }
     // R and beta R
@@ -174,30 +195,22 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
     {
       f32x4 x[KT];
 #pragma unroll
-      for (int i = 0; i < KT; ++i) {
-        const int row = pair_rows(i, g);
-        Frag<T> v;
-        load_tr4(v, 0, &l.v[0][0], Lds::PV, row, wcol, lane);
-        const f32x4 first = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaFirst][row]);
-        const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][row]);
+      for (int i = 0; i < KT; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          r[i][e] = fmaf(-first[e], r[i][e], v.get(e));
-          x[i][e] = beta[e] * r[i][e];
+          r[i][e] = fmaf(-first[i][e], r[i][e], v[i].get(e));
+          x[i][e] = beta[i][e] * r[i][e];
         }
-      }
 #pragma unroll
       for (int s = 0; s < KS; ++s) set_tiles(br[s], x[2 * s], x[2 * s + 1]);
     }
+    read_t(0);
+    __builtin_amdgcn_sched_barrier(0);
     // E = R + N (beta R), of whose rows 32 s .. the columns up to 32 s + 31
 #pragma unroll
-    for (int i = 0; i < KT; ++i)
+    for (int s = 0; s < KS; ++s)
 #pragma unroll
-      for (int s = 0; s <= i / 2; ++s) {
-        DeltaOp<T, NP> f;
-        load_op(f, &l.n[0][pair_row(i, c)][32 * s + 8 * g], C * Lds::PN);
-        mma(r[i], f, br[s]);
-      }
+      for (int i = 2 * s; i < KT; ++i) mma(r[i], nf[i][s], br[s]);
     if (!OUT) {
       float* to = a.e + (at * a.d + col0 + wcol + c) * C;
 #pragma unroll
@@ -209,16 +222,12 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
     {
       f32x4 x[KT];
 #pragma unroll
-      for (int i = 0; i < KT; ++i) {
-        const int row = pair_rows(i, g);
-        const f32x4 last = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaLast][row]);
-        const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][row]);
+      for (int i = 0; i < KT; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          r[i][e] *= beta[e];
-          x[i][e] = last[e] * r[i][e];
+          r[i][e] *= beta[i][e];
+          x[i][e] = last[i][e] * r[i][e];
         }
-      }
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         if constexpr (OUT) set_tiles(uf[s], r[2 * s], r[2 * s + 1]);
@@ -233,13 +242,12 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
         for (int j = 0; j < 4; ++j) S[ft][j] *= whole;
     }
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
+    for (int n = 0; n < TN; ++n) {
+      if (n + 1 < TN) read_t(n + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int ft = 0; ft < FT; ++ft) {
-        Frag<T> f;
-        load_pair_tr(f, &l.k[0][0], Lds::PK, ft, 32 * s, lane);
-        mma(S[ft], f, ul[s]);
-      }
+      for (int i = 0; i < TI; ++i) mma(S[(TI * n + i) % FT], tf[n % 2][i], ul[(TI * n + i) / FT]);
+    }
     if constexpr (OUT) {
       const Buf to = buffer(seq_row(a.o, sp, packed, head, t0, esz) + col0 * esz, (int)(((m - 1) * a.o.row + DVW) * esz));
       const i32x4 since = *reinterpret_cast<const i32x4*>(&l.since[wcol + 4 * g]);
@@ -276,14 +284,14 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
 
 // The gradients of the states and X, from the last chunk to the first.
 template <typename T, int DK, int DVW, int NP>
-__global__ __launch_bounds__(4 * DVW, 1) void delta_back_kernel(DeltaArgs a) {
+__device__ __forceinline__ void delta_back(const DeltaArgs& a, int block, char* raw) {
   using Lds = ScanLds<T, DK, DVW, NP, NP, true>;
   constexpr int C = Lds::C, FT = DK / 16, FS = DK / 32, KT = C / 16, KS = C / 32, esz = (int)sizeof(T), THREADS = 4 * DVW;
-  extern __shared__ __attribute__((aligned(16))) char raw[];
+  constexpr int TI = FT < 4 ? FT : 4, TN = FT * KS / TI;  // tiles of a batch of transposed reads, and batches
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
   const int slices = a.d / DVW;
-  const int slice = blockIdx.x % slices, head = (blockIdx.x / slices) % a.H, b = blockIdx.x / slices / a.H;
+  const int slice = block % slices, head = (block / slices) % a.H, b = block / slices / a.H;
   const SeqPiece sp = seq_uniform(seq_of(a.s, b));
   if (sp.len == 0) return;
   const bool packed = a.s.offsets != nullptr;
@@ -330,66 +338,86 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_back_kernel(DeltaArgs a) {
 #pragma unroll
       for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(to + pair_rows(ft, g)) = S[ft];
     }
+    // (operands are read from LDS a batch before their products)
     f32x4 x[KT];
+    Frag<T> kf[2][KT], qt[2][TI], kt[2][TI], of[KS];
+    DeltaOp<T, NP> pf[KT][KS], nf[KT][KS], os[KS];
+    const auto read_k = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < KT; ++i) load8(kf[t % 2][i], &l.k[pair_row(i, c)][32 * t + 8 * g]);
+    };
+    const auto read_t = [&](int n) {
+#pragma unroll
+      for (int i = 0; i < TI; ++i) {
+        load_pair_tr(qt[n % 2][i], &l.q[0][0], Lds::PK, (TI * n + i) % FT, 32 * ((TI * n + i) / FT), lane);
+        load_pair_tr(kt[n % 2][i], &l.k[0][0], Lds::PK, (TI * n + i) % FT, 32 * ((TI * n + i) / FT), lane);
+      }
+    };
+    const auto gate4 = [&](int which, int i) { return *reinterpret_cast<const f32x4*>(&l.gates[which][pair_rows(i, g)]); };
+    f32x4 first[KT], beta[KT], last[KT];
+    read_k(0);
 #pragma unroll
     for (int i = 0; i < KT; ++i) x[i] = zero4();
 #pragma unroll
     for (int t = 0; t < FS; ++t) {
+      if (t + 1 < FS) {
+        read_k(t + 1);
+      } else {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          load_tr4(of[s], 0, &l.v[0][0], Lds::PV, 32 * s + 8 * g, wcol, lane);
+          load_tr4(of[s], 4, &l.v[0][0], Lds::PV, 32 * s + 8 * g + 4, wcol, lane);
+        }
+#pragma unroll
+        for (int i = 0; i < KT; ++i) {
+          first[i] = gate4(kDeltaFirst, i);
+          beta[i] = gate4(kDeltaBeta, i);
+          last[i] = gate4(kDeltaLast, i);
+#pragma unroll
+          for (int s = i / 2; s < KS; ++s) load_op_pair_tr(pf[i][s], &l.p[0][0][0], C * Lds::PN, Lds::PN, i, 32 * s, lane);
+        }
+      }
       DeltaOp<T, NP> sf;
       set_tiles(sf, S[2 * t], S[2 * t + 1]);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < KT; ++i) {
-        Frag<T> f;
-        load8(f, &l.k[pair_row(i, c)][32 * t + 8 * g]);
-        mma(x[i], f, sf);
-      }
-    }
-    // dO as an operand, and scale e^G dO
-    Frag<T> of[KS];
-    DeltaOp<T, NP> os[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      load_tr4(of[s], 0, &l.v[0][0], Lds::PV, 32 * s + 8 * g, wcol, lane);
-      load_tr4(of[s], 4, &l.v[0][0], Lds::PV, 32 * s + 8 * g + 4, wcol, lane);
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = a.scale * l.gates[kDeltaFirst][32 * s + 8 * g + e] * of[s].get(e);
-      os[s].set(y);
+      for (int i = 0; i < KT; ++i) mma(x[i], kf[t % 2][i], sf);
     }
     // dU
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
-      const f32x4 last = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaLast][pair_rows(i, g)]);
+      x[i] *= last[i];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] *= last[e];
+      for (int s = i / 2; s < KS; ++s) load_op_pair_tr(nf[i][s], &l.n[0][0][0], C * Lds::PN, Lds::PN, i, 32 * s, lane);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int s = i / 2; s < KS; ++s) {
-        DeltaOp<T, NP> f;
-        load_op_pair_tr(f, &l.p[0][0][0], C * Lds::PN, Lds::PN, i, 32 * s, lane);
-        mma(x[i], f, of[s]);
-      }
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int i = 0; i < 2 * s + 2; ++i) mma(x[i], pf[i][s], of[s]);
+    // scale e^G dO
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = a.scale * first[2 * s + e / 4][e % 4] * of[s].get(e);
+      os[s].set(y);
     }
     // X = dU + N^T (beta dU)
     DeltaOp<T, NP> bu[KS];
     {
       f32x4 y[KT];
 #pragma unroll
-      for (int i = 0; i < KT; ++i) {
-        const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][pair_rows(i, g)]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[i][e] = beta[e] * x[i][e];
-      }
+      for (int i = 0; i < KT; ++i) y[i] = beta[i] * x[i];
 #pragma unroll
       for (int s = 0; s < KS; ++s) set_tiles(bu[s], y[2 * s], y[2 * s + 1]);
     }
+    read_t(0);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < KT; ++i)
+    for (int s = 0; s < KS; ++s)
 #pragma unroll
-      for (int s = i / 2; s < KS; ++s) {
-        DeltaOp<T, NP> f;
-        load_op_pair_tr(f, &l.n[0][0][0], C * Lds::PN, Lds::PN, i, 32 * s, lane);
-        mma(x[i], f, bu[s]);
-      }
+      for (int i = 0; i < 2 * s + 2; ++i) mma(x[i], nf[i][s], bu[s]);
     {
       float* to = a.x + (at * a.d + col0 + wcol + c) * C;
 #pragma unroll
@@ -397,13 +425,9 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_back_kernel(DeltaArgs a) {
     }
     // - e^G beta X
 #pragma unroll
-    for (int i = 0; i < KT; ++i) {
-      const int row = pair_rows(i, g);
-      const f32x4 first = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaFirst][row]);
-      const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][row]);
+    for (int i = 0; i < KT; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] *= -first[e] * beta[e];
-    }
+      for (int e = 0; e < 4; ++e) x[i][e] *= -first[i][e] * beta[i][e];
 #pragma unroll
     for (int s = 0; s < KS; ++s) set_tiles(bu[s], x[2 * s], x[2 * s + 1]);
     {
@@ -414,44 +438,57 @@ __global__ __launch_bounds__(4 * DVW, 1) void delta_back_kernel(DeltaArgs a) {
         for (int j = 0; j < 4; ++j) S[ft][j] *= whole;
     }
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
+    for (int n = 0; n < TN; ++n) {
+      if (n + 1 < TN) read_t(n + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int ft = 0; ft < FT; ++ft) {
-        Frag<T> f;
-        load_pair_tr(f, &l.q[0][0], Lds::PK, ft, 32 * s, lane);
-        mma(S[ft], f, os[s]);
-        load_pair_tr(f, &l.k[0][0], Lds::PK, ft, 32 * s, lane);
-        mma(S[ft], f, bu[s]);
-      }
+      for (int i = 0; i < TI; ++i) mma(S[(TI * n + i) % FT], qt[n % 2][i], os[(TI * n + i) / FT]);
+#pragma unroll
+      for (int i = 0; i < TI; ++i) mma(S[(TI * n + i) % FT], kt[n % 2][i], bu[(TI * n + i) / FT]);
+    }
   }
 }
 
-template <typename T, int DK, int DVW, int NP, bool OUT>
+template <typename T, int DK, int DVW>
+__global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  delta_scan<T, DK, DVW, 1, true>(a, blockIdx.x, raw);
+}
+// Both passes of the backward half: neither needs what the other writes, and each alone has few workgroups.
+template <typename T, int DK, int DVW, int NP>
+__global__ __launch_bounds__(4 * DVW, 1) void delta_both_kernel(DeltaArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  const int half = gridDim.x / 2;
+  if ((int)blockIdx.x < half) delta_back<T, DK, DVW, NP>(a, blockIdx.x, raw);
+  else delta_scan<T, DK, DVW, NP, false>(a, blockIdx.x - half, raw);
+}
+
+template <typename T, int DK, int DVW>
 hipError_t launch_scan_one(const DeltaArgs& a, hipStream_t s) {
-  constexpr int bytes = (int)sizeof(ScanLds<T, DK, DVW, NP, 1, OUT>);
+  constexpr int bytes = (int)sizeof(ScanLds<T, DK, DVW, 1, 1, true>);
   static_assert(bytes <= 160 * 1024, "one workgroup's LDS");
-  const hipError_t e = allow_lds<delta_scan_kernel<T, DK, DVW, NP, OUT>>(bytes);
+  const hipError_t e = allow_lds<delta_scan_kernel<T, DK, DVW>>(bytes);
   if (e != hipSuccess) return e;
   const int64_t groups = a.s.count * a.H * (a.d / DVW);
-  hipLaunchKernelGGL((delta_scan_kernel<T, DK, DVW, NP, OUT>), dim3((unsigned)groups), dim3(4 * DVW), bytes, s, a);
+  hipLaunchKernelGGL((delta_scan_kernel<T, DK, DVW>), dim3((unsigned)groups), dim3(4 * DVW), bytes, s, a);
   return hipGetLastError();
 }
 template <typename T, int DK, int DVW, int NP>
-hipError_t launch_back_one(const DeltaArgs& a, hipStream_t s) {
+hipError_t launch_both_one(const DeltaArgs& a, hipStream_t s) {
   constexpr int bytes = (int)sizeof(ScanLds<T, DK, DVW, NP, NP, true>);
-  static_assert(bytes <= 160 * 1024, "one workgroup's LDS");
-  const hipError_t e = allow_lds<delta_back_kernel<T, DK, DVW, NP>>(bytes);
+  static_assert(bytes <= 160 * 1024 && bytes >= (int)sizeof(ScanLds<T, DK, DVW, NP, 1, false>), "one workgroup's LDS");
+  const hipError_t e = allow_lds<delta_both_kernel<T, DK, DVW, NP>>(bytes);
   if (e != hipSuccess) return e;
-  const int64_t groups = a.s.count * a.H * (a.d / DVW);
-  hipLaunchKernelGGL((delta_back_kernel<T, DK, DVW, NP>), dim3((unsigned)groups), dim3(4 * DVW), bytes, s, a);
+  const int64_t groups = 2 * a.s.count * a.H * (a.d / DVW);
+  hipLaunchKernelGGL((delta_both_kernel<T, DK, DVW, NP>), dim3((unsigned)groups), dim3(4 * DVW), bytes, s, a);
   return hipGetLastError();
 }
 
 #define LUNA_DELTA_WIDTHS(LAUNCH, T, ...)                                                                            \
   if (delta_columns(a.d) == 32)                                                                                      \
-    return a.D == 32 ? LAUNCH<T, 32, 32, __VA_ARGS__>(a, s) : a.D == 64 ? LAUNCH<T, 64, 32, __VA_ARGS__>(a, s)       \
-                                                            : LAUNCH<T, 128, 32, __VA_ARGS__>(a, s);                 \
-  return a.D == 32 ? LAUNCH<T, 32, 64, __VA_ARGS__>(a, s) : a.D == 64 ? LAUNCH<T, 64, 64, __VA_ARGS__>(a, s)         \
-                                                          : LAUNCH<T, 128, 64, __VA_ARGS__>(a, s)
+    return a.D == 32 ? LAUNCH<T, 32, 32 __VA_ARGS__>(a, s) : a.D == 64 ? LAUNCH<T, 64, 32 __VA_ARGS__>(a, s)         \
+                                                           : LAUNCH<T, 128, 32 __VA_ARGS__>(a, s);                   \
+  return a.D == 32 ? LAUNCH<T, 32, 64 __VA_ARGS__>(a, s) : a.D == 64 ? LAUNCH<T, 64, 64 __VA_ARGS__>(a, s)           \
+                                                         : LAUNCH<T, 128, 64 __VA_ARGS__>(a, s)
 
 }  // namespace luna
