@@ -69,13 +69,6 @@ __device__ __forceinline__ void lds_tr(Frag<__bf16>& f, unsigned at, int step) {
   f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// The same number, of which the compiler knows nothing: what is worked out from it is worked out there, not once before the
-// loop over the chunks, where 100 such numbers would be written to memory and read back in every chunk.
-__device__ __forceinline__ int anew(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
 // Four numbers in parts.
 template <int NP>
 struct Parts4 {

@@ -59,50 +59,87 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
   constexpr int W = Lds::W, THREADS = 64 * W, PK = Lds::PK, PT = Lds::PT, esz = (int)sizeof(T), FS = DK / 32, VS = DV / 32;
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
-  const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
+  const int tid0 = threadIdx.x, wave = wave_id();
   const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk, group = a.H / a.Hk;
   const SeqPiece sp = seq_uniform(seq_piece(a.s, slot, C));
   if (sp.seq < 0) return;
   const bool packed = a.s.offsets != nullptr, mine = wave < DK / 16;
   const int t0 = sp.index * C, m = min(C, sp.len - t0), feat = mine ? 16 * wave : 0;
+  // What a head needs from memory is asked for before the head before it is done, or as early in it as registers allow: a load
+  // takes 2000 cycles and more.
+  constexpr int NC = DV * 16 / THREADS, NG = (kDeltaGates + THREADS - 1) / THREADS;
+  f32x4 ev[NC], xv[NC];
+  float gv[NG], lv = 0.0f;
+  const auto load_head = [&](int head) {
+    const int tid = anew(tid0), lane = tid % kWave, i4 = 4 * (tid % 16);  // U, dR and dbeta: four tokens of a column a thread
+    const int64_t at = (int64_t)slot * a.H + head;
+    const Buf be = buffer(a.e + at * DV * C, DV * C * 4), bx = buffer(a.x + at * DV * C, DV * C * 4);
+    const Buf bg = buffer(a.gates + at * kDeltaGates, kDeltaGates * 4);
+    const int off = (tid / 16 * C + i4) * 4;
+#pragma unroll
+    for (int n = 0; n < NG; ++n) gv[n] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(bg, (tid + THREADS * n) * 4, 0, 0));
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      ev[n] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(be, off, n * (THREADS / 16) * C * 4, 0));
+      xv[n] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(bx, off, n * (THREADS / 16) * C * 4, 0));
+    }
+    lv = a.log_decay[seq_num(a.s, sp, a.H, head, t0 + min(lane, m - 1))];
+  };
   {
-    DecayRows<T, C, DK, PK, THREADS> x;
+    DecayRows<T, C, DK, PK, THREADS> x, y;
     x.load(seq_row(a.k, sp, packed, hk, t0, esz), a.k.row, m, DK, false);
+    y.load(seq_row(a.q, sp, packed, hk, t0, esz), a.q.row, m, DK, false);
+    load_head(hk * group);
     x.store(&l.k[0][0]);
-    x.load(seq_row(a.q, sp, packed, hk, t0, esz), a.q.row, m, DK, false);
-    x.store(&l.q[0][0]);
+    y.store(&l.q[0][0]);
   }
   f32x4 dq[KT], dk[KT];
 #pragma unroll
   for (int i = 0; i < KT; ++i) dq[i] = zero4(), dk[i] = zero4();
 
   for (int h = 0; h < group; ++h) {
+    const int tid = anew(tid0), lane = tid % kWave, g = lane / 16, c = lane % 16, i4 = 4 * (tid % 16);
     const int head = hk * group + h;
     const int64_t at = (int64_t)slot * a.H + head;
     const Buf bo = buffer(seq_row(a.o, sp, packed, head, t0, esz), (int)(((m - 1) * a.o.row + DV) * esz));
-    const auto load_do = [&](Frag<T>& f, int it, int s) {
-      const int i = 16 * it + c;
-      buf_load8(f, bo, i < m ? (i * (int)a.o.row + 32 * s + 8 * g) * esz : kPastEnd);
+    const int orow = (c * (int)a.o.row + 8 * g) * esz;
+    const auto load_do = [&](Frag<T>& f, int it, int s) {  // (rows from m on lie behind the buffer)
+      buf_load8(f, bo, orow + 16 * it * (int)a.o.row * esz + 32 * s * esz);
+    };
+    // this wave's features of the states, 32 columns of d at a time, and rows of dO
+    const Buf before = buffer(a.before + at * DV * DK, DV * DK * 4), after = buffer(a.after + at * DV * DK, DV * DK * 4);
+    const int state = (feat + c + 8 * g * DK) * 4;
+    float sx[2][8], sy[2][8];
+    Frag<T> of[2][KT];
+    const auto load_states = [&](int s) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sx[s % 2][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(before, state, (32 * s + e) * DK * 4, 0));
+        sy[s % 2][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(after, state, (32 * s + e) * DK * 4, 0));
+      }
+#pragma unroll
+      for (int it = 0; it < KT; ++it) load_do(of[s % 2][it], it, s);
     };
     __syncthreads();  // the head before is no longer read
-    for (int i = tid; i < kDeltaGates; i += THREADS) (&l.gates[0][0])[i] = a.gates[at * kDeltaGates + i];
+#pragma unroll
+    for (int n = 0; n < NG; ++n)
+      if (tid + THREADS * n < kDeltaGates) (&l.gates[0][0])[tid + THREADS * n] = gv[n];
+    const float log_decay = lv;
     __syncthreads();
-    {  // U, dR and dbeta: four tokens of a column a thread
-      const float* e = a.e + at * DV * C;
-      const float* x = a.x + at * DV * C;
-      const int i = 4 * (tid % 16);
-      const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][i]);
+    {
+      const f32x4 beta = *reinterpret_cast<const f32x4*>(&l.gates[kDeltaBeta][i4]);
       f32x4 sum = zero4();
 #pragma unroll
-      for (int col = tid / 16; col < DV; col += THREADS / 16) {
-        const f32x4 ev = *reinterpret_cast<const f32x4*>(e + col * C + i), xv = *reinterpret_cast<const f32x4*>(x + col * C + i);
+      for (int n = 0; n < NC; ++n) {
+        const int col = tid / 16 + n * (THREADS / 16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] = fmaf(ev[j], xv[j], sum[j]);
-        store_parts4<NP>(&l.u[0][col][i], DV * PT, beta[0] * ev[0], beta[1] * ev[1], beta[2] * ev[2], beta[3] * ev[3]);
-        store_parts4<NP>(&l.r[0][col][i], DV * PT, beta[0] * xv[0], beta[1] * xv[1], beta[2] * xv[2], beta[3] * xv[3]);
+        for (int j = 0; j < 4; ++j) sum[j] = fmaf(ev[n][j], xv[n][j], sum[j]);
+        store_parts4<NP>(&l.u[0][col][i4], DV * PT, beta[0] * ev[n][0], beta[1] * ev[n][1], beta[2] * ev[n][2], beta[3] * ev[n][3]);
+        store_parts4<NP>(&l.r[0][col][i4], DV * PT, beta[0] * xv[n][0], beta[1] * xv[n][1], beta[2] * xv[n][2], beta[3] * xv[n][3]);
       }
-      *reinterpret_cast<f32x4*>(&l.beta[tid / 16][i]) = sum;
+      *reinterpret_cast<f32x4*>(&l.beta[tid / 16][i4]) = sum;
     }
+    load_states(0);
     __syncthreads();
     float dbeta = 0.0f;
     if (wave == 0)
@@ -112,8 +149,8 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     {  // dV
       const Buf b = buffer(seq_row(a.dv, sp, packed, head, t0, esz), (int)(((m - 1) * a.dv.row + DV) * esz));
 #pragma unroll
-      for (int idx = tid; idx < C * DV / 4; idx += THREADS) {
-        const int i = idx % C, col = idx / C * 4;
+      for (int n = 0; n < C * DV / 4 / THREADS; ++n) {
+        const int idx = tid + n * THREADS, i = idx % C, col = idx / C * 4;
         float x[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -130,35 +167,33 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
 #pragma unroll
     for (int i = 0; i < KT; ++i) zq[i] = zero4(), zr[i] = zero4(), zk[i] = zero4();
     {
-      const float* before = a.before + at * DV * DK + feat + c;
-      const float* after = a.after + at * DV * DK + feat + c;
-#pragma unroll 1
-      for (int s = 0; s < VS; ++s) {
-        float x[8], y[8];
+      const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
+      DeltaOp<T, NP> rf[2], uf[2];
+      const auto read = [&](int n) {  // of tile n % KT and columns 32 (n / KT) ..
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] = before[(32 * s + 8 * g + e) * DK];
-          y[e] = after[(32 * s + 8 * g + e) * DK];
+        for (int half = 0; half < 2; ++half) {
+          const int row = 32 * (n / KT) + 8 * g + 4 * half;
+          load_op_tr4(rf[n % 2], 4 * half, lane, DV * PT, [&](int kk, int col) { return &l.r[0][row + kk][16 * (n % KT) + col]; });
+          load_op_tr4(uf[n % 2], 4 * half, lane, DV * PT, [&](int kk, int col) { return &l.u[0][row + kk][16 * (n % KT) + col]; });
         }
-        DeltaOp<T, NP> sf, df;
-        sf.set(x);
-        df.set(y);
+      };
+      read(0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) both = fmaf(x[e], y[e], both);
+      for (int s = 0; s < VS; ++s) {
+        if (s + 1 < VS) load_states(s + 1);
+        DeltaOp<T, NP> sf, df;
+        sf.set(sx[s % 2]);
+        df.set(sy[s % 2]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) both = fmaf(sx[s % 2][e], sy[s % 2][e], both);
 #pragma unroll
         for (int it = 0; it < KT; ++it) {
-          Frag<T> of;
-          DeltaOp<T, NP> rf, uf;
-          load_do(of, it, s);
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int row = 32 * s + 8 * g + 4 * half;
-            load_op_tr4(rf, 4 * half, lane, DV * PT, [&](int kk, int col) { return &l.r[0][row + kk][16 * it + col]; });
-            load_op_tr4(uf, 4 * half, lane, DV * PT, [&](int kk, int col) { return &l.u[0][row + kk][16 * it + col]; });
-          }
-          mma(zq[it], sf, of);
-          mma(zr[it], sf, rf);
-          mma(zk[it], df, uf);
+          const int n = s * KT + it;
+          if (n + 1 < VS * KT) read(n + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          mma(zq[it], sf, of[s % 2][it]);
+          mma(zr[it], sf, rf[n % 2]);
+          mma(zk[it], df, uf[n % 2]);
         }
       }
     }
@@ -168,24 +203,31 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     int its[ROUNDS], jts[ROUNDS];
 #pragma unroll
     for (int n = 0; n < ROUNDS; ++n) {
+      const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
       const int tile = wave + W * n;  // (0,0) (1,0) (1,1) (2,0) ..; behind the last one: again, unused
       const int it = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, jt = min(tile - it * (it + 1) / 2, it);
       its[n] = it;
       jts[n] = jt;
       f32x4 p = zero4(), r = zero4(), kk = zero4(), qk = zero4();
-#pragma unroll 2
-      for (int s = 0; s < VS; ++s) {
-        Frag<T> of;
-        DeltaOp<T, NP> rf, uf;
-        load_do(of, it, s);
+      Frag<T> oi[VS];
+      DeltaOp<T, NP> rf[2], uf[2];
+      const auto read = [&](int s) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const int row = 32 * s + 8 * g + 4 * half;
-          load_op_tr4(rf, 4 * half, lane, DV * PT, [&](int kk2, int col) { return &l.r[0][row + kk2][16 * it + col]; });
-          load_op_tr4(uf, 4 * half, lane, DV * PT, [&](int kk2, int col) { return &l.u[0][row + kk2][16 * jt + col]; });
+          load_op_tr4(rf[s % 2], 4 * half, lane, DV * PT, [&](int kk2, int col) { return &l.r[0][row + kk2][16 * it + col]; });
+          load_op_tr4(uf[s % 2], 4 * half, lane, DV * PT, [&](int kk2, int col) { return &l.u[0][row + kk2][16 * jt + col]; });
         }
-        mma(p, uf, of);
-        mma(r, uf, rf);
+      };
+#pragma unroll
+      for (int s = 0; s < VS; ++s) load_do(oi[s], it, s);
+      read(0);
+#pragma unroll
+      for (int s = 0; s < VS; ++s) {
+        if (s + 1 < VS) read(s + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        mma(r, uf[s % 2], rf[s % 2]);
+        mma(p, uf[s % 2], oi[s]);
       }
 #pragma unroll
       for (int t = 0; t < FS; ++t) {
@@ -233,6 +275,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     }
     __syncthreads();
     {
+      const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
 #pragma unroll
       for (int it = 0; it < KT; ++it) {
         const int i = 16 * it + c;
@@ -261,8 +304,10 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
       for (int w = 1; w < kWave; w *= 2) both += __shfl_xor(both, w);
       if (mine && lane == 0) l.state[wave] = both;
     }
+    if (h + 1 < group) load_head(head + 1);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
+      const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
       Frag<T> kf, qf;  // features (rows) over the tokens 32 s + 8 g ..
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -314,12 +359,13 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
       if (lane < m) {
         const int64_t num = seq_num(a.s, sp, a.H, head, t0 + lane);
         // (above 0 a log decay counts as 0)
-        a.dlog_decay[num] = a.log_decay[num] > 0.0f ? 0.0f : sum + ends + l.gates[kDeltaMisc][0] * whole;
+        a.dlog_decay[num] = log_decay > 0.0f ? 0.0f : sum + ends + l.gates[kDeltaMisc][0] * whole;
         a.dbeta[num] = dbeta;
       }
     }
   }
   if (mine) {
+    const int lane = tid0 % kWave, g = lane / 16, c = lane % 16;
     const Buf bq = buffer(seq_row(a.dq, sp, packed, hk, t0, esz), (int)(((m - 1) * a.dq.row + DK) * esz));
     const Buf bk = buffer(seq_row(a.dk, sp, packed, hk, t0, esz), (int)(((m - 1) * a.dk.row + DK) * esz));
 #pragma unroll
