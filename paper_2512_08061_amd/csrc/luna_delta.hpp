@@ -65,13 +65,6 @@ struct DeltaArgs {
   float* dbeta;
 };
 
-// The same number, of which the compiler knows nothing: what is worked out from it is worked out there, not once before a
-// loop, where 100 such numbers and more would be written to memory and read back in every turn.
-__device__ __forceinline__ int anew(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
 // Slot of the first chunk of a sequence.
 __device__ __forceinline__ int delta_first_slot(const SeqSet& s, const SeqPiece& p) {
   return s.offsets ? (int)(p.first / kDeltaChunk) + p.seq : p.seq * (int)((s.rows + kDeltaChunk - 1) / kDeltaChunk);

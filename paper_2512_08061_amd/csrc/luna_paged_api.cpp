@@ -45,8 +45,9 @@ luna_status check_pages(const luna_rows* r, const char* what, luna_dtype dt, con
 
 // bytes of the parts of rows whose keys lie in several shares, or 0 where the tile kernels take the call
 size_t part_bytes(luna_dtype dt, const luna_seqs& s, const luna_pages& p, int64_t H, int64_t Hk, int64_t d) {
-  if (!luna::paged_splits(set_of(&s), H, Hk)) return 0;
-  const int64_t shares = luna::paged_shares(type_of(dt), s.count, p.width * p.rows, Hk);
+  const int64_t shares = luna::paged_splits(set_of(&s), H, Hk) ? luna::paged_shares(type_of(dt), s.count, p.width * p.rows, Hk)
+                                                               : luna::paged_tile_shares(type_of(dt), set_of(&s), H, Hk, d);
+  if (!shares) return 0;
   return align256((size_t)(shares + s.count) * H * (s.rows < 1 ? 1 : s.rows) * (d + 2) * 4);
 }
 
@@ -142,7 +143,8 @@ luna_status luna_paged_fwd(const luna_rows* Q, const luna_rows* k_pages, const l
   a.lse = lse;
   a.parts = static_cast<float*>(ws);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  return hip_status(need ? luna::launch_paged_split(type_of(dtype), a, s) : luna::launch_paged_tiles(type_of(dtype), a, s),
+  return hip_status(luna::paged_splits(a.qs, H, Hk) ? luna::launch_paged_split(type_of(dtype), a, s)
+                                                          : luna::launch_paged_tiles(type_of(dtype), a, s),
                     "paged attention launch");
 }
 

@@ -27,53 +27,6 @@ struct PagedLds {
   int64_t scan[4];
 };
 
-__device__ __forceinline__ int units_of(const SeqSet& s, int b, int unit) {
-  return (seq_clamp(s.lens[b], 0, s.rows) + unit - 1) / unit;
-}
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
-#pragma unroll
-  for (int w = 1; w < kWave; w *= 2) x += __shfl_xor(x, w);
-  return x;
-}
-// Sum over the threads of a workgroup of four waves.
-__device__ __forceinline__ int64_t group_sum(int64_t x, int64_t* scan) {
-  x = wave_sum(x);
-  __syncthreads();
-  if (threadIdx.x % kWave == 0) scan[threadIdx.x / kWave] = x;
-  __syncthreads();
-  return scan[0] + scan[1] + scan[2] + scan[3];
-}
-// Units of the sequences before `end`, by the whole workgroup.
-__device__ __forceinline__ int64_t units_before(const SeqSet& s, int end, int unit, int64_t* scan) {
-  int64_t x = 0;
-  for (int b = threadIdx.x; b < end; b += 256) x += units_of(s, b, unit);
-  return group_sum(x, scan);
-}
-
-// The last sequence with at most `at` units before it, and these units (at is below the sum of all).
-__device__ __forceinline__ int sequence_at(const SeqSet& s, int64_t at, int unit, int64_t* before) {
-  const int lane = threadIdx.x % kWave, count = (int)s.count;
-  int64_t sum = 0;
-  for (int b0 = 0; b0 < count; b0 += kWave) {
-    const int64_t mine = b0 + lane < count ? units_of(s, b0 + lane, unit) : 0;
-    int64_t to = mine;  // units up to this sequence's end
-#pragma unroll
-    for (int w = 1; w < kWave; w *= 2) {
-      const int64_t other = __shfl_up(to, w);
-      to += lane >= w ? other : 0;
-    }
-    const uint64_t behind = __ballot(b0 + lane < count && sum + to > at);
-    if (behind) {
-      const int i = __builtin_ctzll(behind);
-      *before = sum + __shfl(to - mine, i);
-      return __builtin_amdgcn_readfirstlane(b0 + i);
-    }
-    sum += __shfl(to, kWave - 1);
-  }
-  *before = sum;
-  return count;
-}
-
 template <typename T, int DH, int RT>
 __global__ __launch_bounds__(256) void paged_split_kernel(SoftmaxArgs a, int shares) {
   using Lds = PagedLds<T, DH>;
@@ -83,7 +36,7 @@ __global__ __launch_bounds__(256) void paged_split_kernel(SoftmaxArgs a, int sha
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
   const int hk = blockIdx.x % a.Hk, share = blockIdx.x / a.Hk;
-  const int64_t all = units_before(a.ks, (int)a.ks.count, KB, l.scan), per = paged_per(all, shares);
+  const int64_t all = units_before(a.ks, (int)a.ks.count, KB, l.scan), per = paged_per(all, shares, kPagedLeast);
   const int64_t begin = share * per, end = min(all, begin + per);
   if (begin >= end) return;
   int64_t first;  // units before sequence b
@@ -267,50 +220,52 @@ __global__ __launch_bounds__(256) void paged_split_kernel(SoftmaxArgs a, int sha
   }
 }
 
-// Rows whose keys lie in several shares joined; rows of sequences without any key as zeros.
+// Rows whose keys lie in several shares joined, `times` rows a thread group; rows of sequences without any key as zeros.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void paged_join_kernel(SoftmaxArgs a, int shares) {
-  constexpr int KB = PagedLds<T, DH>::KB, LANES = DH < kWave ? DH : kWave, ROWS = 256 / LANES, N = DH / LANES;
+__global__ __launch_bounds__(256) void paged_join_kernel(SoftmaxArgs a, int shares, int unit, int least, int times) {
+  constexpr int LANES = DH < kWave ? DH : kWave, ROWS = 256 / LANES, N = DH / LANES;
   __shared__ int64_t scan[4];
-  const int group = a.H / a.Hk, rows = (int)a.qs.rows * group, tiles = (rows + ROWS - 1) / ROWS;
+  const int group = a.H / a.Hk, rows = (int)a.qs.rows * group, tiles = (rows + ROWS * times - 1) / (ROWS * times);
   const int tile = blockIdx.x % tiles, hk = blockIdx.x / tiles % a.Hk, b = blockIdx.x / tiles / a.Hk;
   const SeqPiece sq = seq_of(a.qs, b), sk = seq_of(a.ks, b);
-  const int64_t all = units_before(a.ks, (int)a.ks.count, KB, scan), before = units_before(a.ks, b, KB, scan);
-  const PagedUnits holders = paged_holders(before, (sk.len + KB - 1) / KB, paged_per(all, shares));
+  const int64_t all = units_before(a.ks, (int)a.ks.count, unit, scan), before = units_before(a.ks, b, unit, scan);
+  const PagedUnits holders = paged_holders(before, (sk.len + unit - 1) / unit, paged_per(all, shares, least));
   const int s0 = holders.u0, s1 = holders.u1;
   if (s0 == s1) return;  // (finished there)
-  const int row = tile * ROWS + (int)threadIdx.x / LANES, x = threadIdx.x % LANES, lane = threadIdx.x % kWave;
-  const int t = row / group, head = hk * group + row % group;
-  if (row >= rows || t >= sq.len) return;
+  const int x = threadIdx.x % LANES, lane = threadIdx.x % kWave;
   const int64_t step = (int64_t)a.Hk * rows * (DH + 2);
-  const float* part = a.parts + (paged_part(s0, b) * a.Hk + hk) * rows * (DH + 2) + (int64_t)row * (DH + 2);
-  float most = -__builtin_inff(), total = 0.0f, y[N];
+  for (int n = 0; n < times; ++n) {
+    const int row = (tile * times + n) * ROWS + (int)threadIdx.x / LANES, t = row / group, head = hk * group + row % group;
+    if (row >= rows || t >= sq.len) return;
+    const float* part = a.parts + (paged_part(s0, b) * a.Hk + hk) * rows * (DH + 2) + (int64_t)row * (DH + 2);
+    float most = -__builtin_inff(), total = 0.0f, y[N];
 #pragma unroll
-  for (int e = 0; e < N; ++e) y[e] = 0.0f;
+    for (int e = 0; e < N; ++e) y[e] = 0.0f;
 #pragma unroll 4
-  for (int i = 0; i <= s1 - s0; ++i) most = fmaxf(most, part[i * step + DH + 1]);
-  const float base = most == -__builtin_inff() ? 0.0f : most;
+    for (int i = 0; i <= s1 - s0; ++i) most = fmaxf(most, part[i * step + DH + 1]);
+    const float base = most == -__builtin_inff() ? 0.0f : most;
 #pragma unroll 4
-  for (int i = 0; i <= s1 - s0; ++i) {
-    const float f = exp2_raw(part[i * step + DH + 1] - base);
-    total = fmaf(f, part[i * step + DH], total);
+    for (int i = 0; i <= s1 - s0; ++i) {
+      const float f = exp2_raw(part[i * step + DH + 1] - base);
+      total = fmaf(f, part[i * step + DH], total);
 #pragma unroll
-    for (int e = 0; e < N; ++e) y[e] = fmaf(f, part[i * step + x + LANES * e], y[e]);
+      for (int e = 0; e < N; ++e) y[e] = fmaf(f, part[i * step + x + LANES * e], y[e]);
+    }
+    const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) odd |= not_finite(y[e] * inv);
+    uint64_t lost = __ballot(odd);
+    if constexpr (LANES < kWave) lost = lost >> (lane / LANES * LANES) & (((uint64_t)1 << LANES) - 1);
+    if (a.lse && x == 0) a.lse[seq_num(a.qs, sq, a.H, head, t)] = (most + log2f(total)) * kLn2;
+    if (lost && softmax_odd_row<T, DH, LANES>(a, sk, hk, t + sk.len - sq.len + 1, sk.len)) {
+      softmax_row<T, DH, LANES, true>(a, sq, sk, head, t);
+      continue;
+    }
+    T* to = reinterpret_cast<T*>(seq_row(a.o, sq, false, head, t, (int)sizeof(T)));
+#pragma unroll
+    for (int e = 0; e < N; ++e) to[x + LANES * e] = (T)(y[e] * inv);
   }
-  const float inv = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
-  bool odd = false;
-#pragma unroll
-  for (int e = 0; e < N; ++e) odd |= not_finite(y[e] * inv);
-  uint64_t lost = __ballot(odd);
-  if constexpr (LANES < kWave) lost = lost >> (lane / LANES * LANES) & (((uint64_t)1 << LANES) - 1);
-  if (a.lse && x == 0) a.lse[seq_num(a.qs, sq, a.H, head, t)] = (most + log2f(total)) * kLn2;
-  if (lost && softmax_odd_row<T, DH, LANES>(a, sk, hk, t + sk.len - sq.len + 1, sk.len)) {
-    softmax_row<T, DH, LANES, true>(a, sq, sk, head, t);
-    return;
-  }
-  T* to = reinterpret_cast<T*>(seq_row(a.o, sq, false, head, t, (int)sizeof(T)));
-#pragma unroll
-  for (int e = 0; e < N; ++e) to[x + LANES * e] = (T)(y[e] * inv);
 }
 
 template <typename T, int DH, int RT>
@@ -323,17 +278,21 @@ hipError_t launch_rows(const SoftmaxArgs& a, int shares, hipStream_t s) {
 }
 
 template <typename T, int DH>
+hipError_t launch_join(const SoftmaxArgs& a, int rows, int shares, int unit, int least, int times, hipStream_t s) {
+  const int each = 256 / (DH < kWave ? DH : kWave) * times;
+  const int64_t groups = a.qs.count * a.Hk * ((rows + each - 1) / each);
+  hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3((unsigned)groups), dim3(256), 0, s, a, shares, unit, least, times);
+  return hipGetLastError();
+}
+
+template <typename T, int DH>
 hipError_t launch_width(const SoftmaxArgs& a, hipStream_t s) {
   const int rows = (int)a.qs.rows * (a.H / a.Hk);
   const int shares = (int)paged_shares(sizeof(T) == 2 ? Dt::BF16 : Dt::F32, a.ks.count, a.ks.rows, a.Hk);
   const hipError_t e = rows <= 16   ? launch_rows<T, DH, 1>(a, shares, s)
                        : rows <= 32 ? launch_rows<T, DH, 2>(a, shares, s)
                                     : launch_rows<T, DH, 4>(a, shares, s);
-  if (e != hipSuccess) return e;
-  constexpr int ROWS = 256 / (DH < kWave ? DH : kWave);
-  const int64_t groups = a.qs.count * a.Hk * ((rows + ROWS - 1) / ROWS);
-  hipLaunchKernelGGL((paged_join_kernel<T, DH>), dim3((unsigned)groups), dim3(256), 0, s, a, shares);
-  return hipGetLastError();
+  return e != hipSuccess ? e : launch_join<T, DH>(a, rows, shares, PagedLds<T, DH>::KB, kPagedLeast, 1, s);
 }
 
 template <typename T>
@@ -351,6 +310,11 @@ int64_t paged_shares(Dt dt, int64_t count, int64_t room, int64_t Hk) {
 
 hipError_t launch_paged_split(Dt dt, const SoftmaxArgs& a, hipStream_t s) {
   return dt == Dt::BF16 ? launch_split<__bf16>(a, s) : launch_split<float>(a, s);
+}
+
+hipError_t launch_paged_tile_join(const SoftmaxArgs& a, int shares, hipStream_t s) {
+  const int rows = (int)a.qs.rows * (a.H / a.Hk);
+  return a.d == 64 ? launch_join<__bf16, 64>(a, rows, shares, kPagedTileUnit, 1, 8, s) : launch_join<__bf16, 128>(a, rows, shares, kPagedTileUnit, 1, 8, s);
 }
 
 }  // namespace luna

@@ -77,6 +77,13 @@ __device__ __forceinline__ SeqPiece seq_uniform(SeqPiece p) {
   return p;
 }
 
+// The same number, of which the compiler knows nothing: what is worked out from it is worked out there, not once before a
+// loop, where 100 such numbers and more would be written to memory and read back in every turn.
+__device__ __forceinline__ int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // The last packed sequence b with holds(b, offsets[b]), which holds up to some sequence and no further; -1: none (the whole
 // wave calls this).  64 guesses at a time: every 4096th, 64th and single sequence.  (One look at each 64 after the other
 // took 24 ms for 16384 sequences of 8 tokens in 16 heads, of 1.6 ms for the same sequences without offsets.)
@@ -296,6 +303,15 @@ hipError_t launch_softmax_bwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 // Over pages: the tile kernels, and the kernel for few rows (luna_paged_split.hip) of a key head.
 hipError_t launch_paged_tiles(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 inline bool paged_splits(const SeqSet& qs, int64_t H, int64_t Hk) { return !qs.offsets && qs.rows * (H / Hk) <= kSplitRows; }
+// Tiles (bf16 with d = 64 and 128) whose keys are cut in shares as well: calls of so few tiles that the longest sequence alone would keep
+// some of the device busy to the end.  Shares of the keys, in units of kPagedTileUnit; 0: no cut.
+constexpr int kPagedTileUnit = 512;
+inline int paged_tile_shares(Dt dt, const SeqSet& qs, int64_t H, int64_t Hk, int64_t d) {
+  if (dt != Dt::BF16 || d < 64 || qs.offsets || paged_splits(qs, H, Hk)) return 0;
+  const int64_t tiles = (qs.rows + 127) / 128;
+  return qs.count * tiles * H > 512 ? 0 : (int)(512 / (tiles * H));
+}
+hipError_t launch_paged_tile_join(const SoftmaxArgs& a, int shares, hipStream_t s);
 // Keys of a unit of work of that kernel, which a wave takes at a time, and the workgroups that share the units of a key
 // head (room: of the sequences' rows of the table).
 constexpr int paged_unit(Dt dt) { return dt == Dt::BF16 ? 64 : 32; }
@@ -308,15 +324,17 @@ hipError_t launch_paged_split(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 struct PagedUnits {
   int u0, u1;
 };
-__host__ __device__ inline int64_t paged_per(int64_t all, int shares) {
+// (at least `least` units: a share of fewer costs more than it saves)
+constexpr int kPagedLeast = 4;  // of the kernel for few rows
+__host__ __device__ inline int64_t paged_per(int64_t all, int shares, int least = kPagedLeast) {
   const int64_t per = (all + shares - 1) / shares;
-  return per < 4 ? 4 : per;
+  return per < least ? least : per;
 }
 __host__ __device__ inline PagedUnits paged_held(int64_t before, int units, int64_t per, int share, int64_t all) {
   const int64_t begin = share * per, end = begin + per < all ? begin + per : all;
   return PagedUnits{(int)(begin > before ? begin - before : 0), (int)(end - before < units ? end - before : units)};
 }
-__host__ __device__ inline PagedUnits paged_holders(int64_t before, int units, int64_t per) {  // (first, last; none: last < first)
+__host__ __device__ inline PagedUnits paged_holders(int64_t before, int units, int64_t per) {  // (first, last; none: last = first - 1)
   const int first = (int)(before / per);
   return PagedUnits{first, units ? (int)((before + units - 1) / per) : first - 1};
 }

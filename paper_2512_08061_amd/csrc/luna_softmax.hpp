@@ -274,4 +274,100 @@ __device__ __forceinline__ void softmax_row(const SoftmaxArgs& a, const SeqPiece
     if (lane + LANES * c < DH) o[lane + LANES * c] = (T)(acc[c] * inv);
 }
 
+// The keys of padded sequences as one line of units of `unit` keys, cut in equal shares (see PagedUnits).
+__device__ __forceinline__ int units_of(const SeqSet& s, int b, int unit) {
+  return (seq_clamp(s.lens[b], 0, s.rows) + unit - 1) / unit;
+}
+__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+#pragma unroll
+  for (int w = 1; w < kWave; w *= 2) x += __shfl_xor(x, w);
+  return x;
+}
+template <typename I>
+__device__ __forceinline__ I lanes_up_to(I x) {
+  const int lane = threadIdx.x % kWave;
+#pragma unroll
+  for (int w = 1; w < kWave; w *= 2) {
+    const I other = __shfl_up(x, w);
+    x += lane >= w ? other : 0;
+  }
+  return x;
+}
+// The parts of the line (what a share holds of a sequence) by size: whole shares first, then the others.  The sequence of the part
+// of a rank, its share and the units that this holds; -1: no such part (the whole wave calls this; units of all below 2^31).
+__device__ __forceinline__ int sequence_of_part(const SeqSet& s, int rank, int shares, int unit, int* share, PagedUnits* held) {
+  const int lane = threadIdx.x % kWave, count = (int)s.count;
+  int64_t sum = 0;
+  for (int b = lane; b < count; b += kWave) sum += units_of(s, b, unit);
+  const int all = (int)wave_sum(sum), per = (int)paged_per(all, shares, 1);
+#pragma unroll 1
+  for (int rest = 0; rest < 2; ++rest) {
+    int before0 = 0;
+#pragma unroll 1
+    for (int b0 = 0; b0 < count; b0 += kWave) {
+      const int b = b0 + lane, mine = b < count ? units_of(s, b, unit) : 0, to = before0 + lanes_up_to(mine), before = to - mine;
+      const PagedUnits in = paged_holders(before, mine, per);
+      const int lo = (before + per - 1) / per, hi = to / per;  // whole ones: lo .. hi - 1
+      const int whole = hi > lo ? hi - lo : 0, n = rest ? in.u1 - in.u0 + 1 - whole : whole;
+      const int until = lanes_up_to(n);
+      const uint64_t found = __ballot(rank < until);
+      if (found) {
+        const int i = __builtin_ctzll(found), k = rank - (until - n);
+        const int mine_share = !rest ? lo + k : !whole ? in.u0 + k : k == 0 && in.u0 < lo ? in.u0 : in.u1;
+        const PagedUnits u = paged_held(before, mine, per, mine_share, all);
+        *share = __builtin_amdgcn_readlane(mine_share, i);
+        held->u0 = __builtin_amdgcn_readlane(u.u0, i);
+        held->u1 = __builtin_amdgcn_readlane(u.u1, i);
+        return b0 + i;
+      }
+      rank -= __builtin_amdgcn_readlane(until, kWave - 1);
+      before0 = __builtin_amdgcn_readlane(to, kWave - 1);
+    }
+  }
+  return -1;
+}
+// Sum over the threads of a workgroup.
+template <int THREADS>
+__device__ __forceinline__ int64_t group_sum(int64_t x, int64_t* scan) {
+  x = wave_sum(x);
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) scan[threadIdx.x / kWave] = x;
+  __syncthreads();
+  int64_t sum = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / kWave; ++w) sum += scan[w];
+  return sum;
+}
+// Units of the sequences before `end`, by the whole workgroup.
+template <int THREADS = 256>
+__device__ __forceinline__ int64_t units_before(const SeqSet& s, int end, int unit, int64_t* scan) {
+  int64_t x = 0;
+  for (int b = threadIdx.x; b < end; b += THREADS) x += units_of(s, b, unit);
+  return group_sum<THREADS>(x, scan);
+}
+
+// The last sequence with at most `at` units before it, and these units (at is below the sum of all).
+__device__ __forceinline__ int sequence_at(const SeqSet& s, int64_t at, int unit, int64_t* before) {
+  const int lane = threadIdx.x % kWave, count = (int)s.count;
+  int64_t sum = 0;
+  for (int b0 = 0; b0 < count; b0 += kWave) {
+    const int64_t mine = b0 + lane < count ? units_of(s, b0 + lane, unit) : 0;
+    int64_t to = mine;  // units up to this sequence's end
+#pragma unroll
+    for (int w = 1; w < kWave; w *= 2) {
+      const int64_t other = __shfl_up(to, w);
+      to += lane >= w ? other : 0;
+    }
+    const uint64_t behind = __ballot(b0 + lane < count && sum + to > at);
+    if (behind) {
+      const int i = __builtin_ctzll(behind);
+      *before = sum + __shfl(to - mine, i);
+      return __builtin_amdgcn_readfirstlane(b0 + i);
+    }
+    sum += __shfl(to, kWave - 1);
+  }
+  *before = sum;
+  return count;
+}
+
 }  // namespace luna

@@ -155,21 +155,19 @@ struct SoftmaxLds32 {
   Tile<DH> k[GROUPS][2], v[GROUPS][2];  // per group of waves, twice
 };
 
+// A tile and the keys first (a multiple of 64) .. end - 1 that it sees; part: where its rows go that are part of the sequence's
+// ([token][head of the key head][d + 2]: unnormalised, then the sum and the maximum), null: to out.
 template <int DH, int GROUPS, bool PAGED>
-__global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
+__device__ __forceinline__ void softmax_tile32(const SoftmaxArgs& a, char* raw, int head, const SeqPiece& sq, const SeqPiece& sk,
+                                               int first, int end, float* part_rows) {
   constexpr int KB = 64, KS = DH / 16, CT = DH / 32, esz = 2;
-  extern __shared__ __attribute__((aligned(16))) char raw[];
   SoftmaxLds32<DH, GROUPS>& l = *reinterpret_cast<SoftmaxLds32<DH, GROUPS>*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id() % 4, h = lane / 32, c = lane % 32;
   const int group = GROUPS == 1 ? 0 : wave_id() / 4, tid = threadIdx.x % 256;
-  const int head = head_of(blockIdx.x % a.H, a.H);
-  const SeqPiece sq = seq_piece_by_work(a.qs, blockIdx.x / a.H, gridDim.x / a.H, 128, true);
-  if (sq.seq < 0) return;
-  const SeqPiece sk = seq_of(a.ks, sq.seq);
   const bool pq = a.qs.offsets != nullptr, pk = a.ks.offsets != nullptr;
   const int q0 = sq.index * 128, m = min(128, sq.len - q0);
   const int shift = sk.len - sq.len;
-  const int kend = min(sk.len, max(0, q0 + m + shift));
+  const int kend = min(end, max(0, q0 + m + shift));
   const int i = 32 * wave + c, last = q0 + i + shift;
   const int wfirst = q0 + 32 * wave + shift, wlast = min(wfirst + 31, kend - 1);  // the wave's rows see all keys up to / none behind
   const int hk = head / (a.H / a.Hk);
@@ -207,11 +205,11 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxA
     Tile<DH>::load(kr, tid, seq_row(a.k, sk, pk, hk, k0, esz), a.k.row, min(KB, kend - k0));
     Tile<DH>::load(vr, tid, seq_row(a.v, sk, pk, hk, k0, esz), a.v.row, min(KB, kend - k0));
   };
-  load(KB * group);
+  load(first + KB * group);
   l.k[group][0].store(kr, tid);
   l.v[group][0].store(vr, tid);
   int buf = 0;
-  for (int k0 = KB * group; k0 - KB * group < kend; k0 += GROUPS * KB, buf ^= 1) {
+  for (int k0 = first + KB * group; k0 - KB * group < kend; k0 += GROUPS * KB, buf ^= 1) {
     __syncthreads();  // this block is whole, and the one before no longer read
     const int without = none;
     load(k0 + GROUPS * KB);
@@ -318,6 +316,19 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxA
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[t][e] = fmaf(o[t][e], f, g * rows[((t * 4 + e / 4) * 4 + wave) * kWave + lane][e % 4]);
   }
+  if (PAGED && part_rows) {
+    const int heads = a.H / a.Hk;
+    float* to = part_rows + (int64_t)((q0 + i) * heads + head % heads) * (DH + 2);
+    if (i < m) {
+#pragma unroll
+      for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2)  // (rows of d + 2 numbers begin at multiples of 8 bytes)
+          *reinterpret_cast<float2*>(to + 32 * t + 2 * (e - e % 4) + 4 * h + e % 4) = float2{o[t][e], o[t][e + 1]};
+      if (h == 0) to[DH] = sum, to[DH + 1] = base;
+    }
+    return;
+  }
   const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;  // (NaN stays)
   bool bad = false;
 #pragma unroll
@@ -343,6 +354,36 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxA
 }
 
 template <int DH, int GROUPS, bool PAGED>
+__global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  const int head = head_of(blockIdx.x % a.H, a.H);
+  const SeqPiece sq = seq_piece_by_work(a.qs, blockIdx.x / a.H, gridDim.x / a.H, 128, true);
+  if (sq.seq < 0) return;
+  const SeqPiece sk = seq_of(a.ks, sq.seq);
+  softmax_tile32<DH, GROUPS, PAGED>(a, raw, head, sq, sk, 0, sk.len, nullptr);
+}
+
+// Over pages, what a share of the line of all sequences' keys holds of one sequence (see PagedUnits), for the tiles of one number
+// and head: whole sequences are finished here, the parts of others are joined by a launch behind it.
+template <int DH, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, 2) void softmax_part32_kernel(SoftmaxArgs a, int shares) {
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  const int tiles = (int)((a.qs.rows + 127) / 128), tile = blockIdx.x / a.H % tiles, rank = blockIdx.x / (tiles * a.H);
+  const int head = head_of(blockIdx.x % a.H, a.H), heads = a.H / a.Hk;
+  int share;
+  PagedUnits held;
+  const int b = sequence_of_part(a.ks, rank, shares, kPagedTileUnit, &share, &held);
+  if (b < 0) return;
+  const SeqPiece sk = seq_uniform(seq_of(a.ks, b));
+  SeqPiece sq = seq_uniform(seq_of(a.qs, b));
+  if (128 * tile >= sq.len) return;
+  sq.index = tile;
+  const bool whole = held.u0 == 0 && held.u1 * kPagedTileUnit >= sk.len;
+  float* rows = a.parts + (paged_part(share, b) * a.Hk + head / heads) * (a.qs.rows * heads) * (DH + 2);
+  softmax_tile32<DH, GROUPS, true>(a, raw, head, sq, sk, kPagedTileUnit * held.u0, min(sk.len, kPagedTileUnit * held.u1), whole ? nullptr : rows);
+}
+
+template <int DH, int GROUPS, bool PAGED>
 hipError_t launch_groups(const SoftmaxArgs& a, hipStream_t s) {
   constexpr int bytes = (int)sizeof(SoftmaxLds32<DH, GROUPS>);
   const hipError_t e = allow_lds<softmax_fwd32_kernel<DH, GROUPS, PAGED>>(bytes);
@@ -360,6 +401,17 @@ hipError_t launch_fwd32(const SoftmaxArgs& a, hipStream_t s) {
   return seq_slots(a.qs, 128) * a.H <= 512 ? launch_groups<DH, 2, PAGED>(a, s) : launch_groups<DH, 1, PAGED>(a, s);
 }
 
+template <int DH>
+hipError_t launch_shares(const SoftmaxArgs& a, int shares, hipStream_t s) {
+  constexpr int GROUPS = 1, bytes = (int)sizeof(SoftmaxLds32<DH, GROUPS>);
+  hipError_t e = allow_lds<softmax_part32_kernel<DH, GROUPS>>(bytes);
+  if (e != hipSuccess) return e;
+  const dim3 grid((unsigned)((shares + a.qs.count) * ((a.qs.rows + 127) / 128) * a.H));
+  hipLaunchKernelGGL((softmax_part32_kernel<DH, GROUPS>), grid, dim3(256 * GROUPS), bytes, s, a, shares);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  return launch_paged_tile_join(a, shares, s);
+}
+
 template <typename T, int DH, bool PAGED>
 hipError_t launch_fwd(const SoftmaxArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((softmax_fwd_kernel<T, DH, PAGED>), dim3((unsigned)(seq_slots(a.qs, kSoftmaxTile) * a.H)), dim3(256), 0, s, a);
@@ -370,6 +422,9 @@ template <bool PAGED>
 hipError_t launch_tiles(Dt dt, const SoftmaxArgs& a, hipStream_t s) {
   if (dt == Dt::F32)
     return a.d == 32 ? launch_fwd<float, 32, PAGED>(a, s) : a.d == 64 ? launch_fwd<float, 64, PAGED>(a, s) : launch_fwd<float, 128, PAGED>(a, s);
+  if constexpr (PAGED)
+    if (const int shares = paged_tile_shares(dt, a.qs, a.H, a.Hk, a.d))
+      return a.d == 64 ? launch_shares<64>(a, shares, s) : launch_shares<128>(a, shares, s);
   return a.d == 32 ? launch_fwd<__bf16, 32, PAGED>(a, s) : a.d == 64 ? launch_fwd32<64, PAGED>(a, s) : launch_fwd32<128, PAGED>(a, s);
 }
 

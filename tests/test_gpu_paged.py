@@ -100,6 +100,44 @@ def test_many_sequences(count, most, m):
     check_forward(Q, K, V, out, lse, "batch", [m] * count, klens)
 
 
+@pytest.mark.parametrize("m,klens,H,Hk,d", [
+    (130, [0, 1, 511, 512, 513, 3000, 1024, 9000], 2, 1, 128), (300, [512, 512, 512, 512], 4, 4, 64), (65, [20000, 130], 16, 4, 128),
+    (500, [1536, 5], 32, 8, 64), (129, [4096], 1, 1, 128)])
+def test_tiles_of_long_and_short_caches(m, klens, H, Hk, d):
+    """Few tiles, whose keys are cut in shares: sequences of one share, of several, and none."""
+    say(f"paged tiles m={m} {klens} H={H} Hk={Hk} d={d}")
+    Q, K, V, kp, vp, table, _ = make(m, klens, H, Hk, d, torch.bfloat16, 64, seed=31)
+    out, lse = luna.paged_attn(Q, kp, vp, table, i32(klens))
+    check_forward(Q, K, V, out, lse, "batch", [m] * len(klens), klens)
+
+
+def test_tiles_of_many_sequences():
+    gen = torch.Generator(device=device()).manual_seed(32)
+    klens = torch.randint(0, 1500, (200,), generator=gen, device=device()).tolist()
+    klens[::9] = [0] * len(klens[::9])
+    klens[77] = 9000
+    Q, K, V, kp, vp, table, _ = make(66, klens, 2, 2, 64, torch.bfloat16, 32, seed=33)
+    out, lse = luna.paged_attn(Q, kp, vp, table, i32(klens))
+    check_forward(Q, K, V, out, lse, "batch", [66] * 200, klens)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_values_in_other_shares(bad):
+    """A value of a later token reaches no earlier row, and one of an early token all of them, where they lie in other shares."""
+    m, n = 140, 2600
+    Q, K, V, _, _, table, _ = make(m, [n], 2, 1, 64, torch.bfloat16, 16, seed=34)
+    V[0, 0, n - 3, 5] = bad
+    kp, vp = (pages_of(t, [n], table, int(table.max()) + 4, 16, False) for t in (K, V))
+    out, lse = luna.paged_attn(Q, kp, vp, table, i32([n]))
+    assert torch.isfinite(out[:, :, :m - 3]).all() and torch.isfinite(lse).all()
+    assert not torch.isfinite(out[:, :, m - 3:, 5]).any() and torch.isfinite(out[:, :, m - 3:, 6]).all()
+    check_forward(Q[:, :, :m - 3], K[:, :, :n - 3], V[:, :, :n - 3], out[:, :, :m - 3], lse[:, :, :m - 3], "batch", [m - 3], [n - 3])
+    V[0, 0, n - 3, 5], V[0, 0, 700, 5] = 0.0, bad
+    vp = pages_of(V, [n], table, int(table.max()) + 4, 16, False)
+    out, lse = luna.paged_attn(Q, kp, vp, table, i32([n]))
+    assert not torch.isfinite(out[..., 5]).any() and torch.isfinite(out[..., 6]).all() and torch.isfinite(lse).all()
+
+
 @pytest.mark.parametrize("m,H,d,dtype", [(3, 2, 64, "bf16"), (3, 2, 32, "bf16"), (90, 2, 128, "bf16"), (3, 2, 32, "f32")])
 def test_padded_queries_keep_other_rows(m, H, d, dtype):
     qlens, klens = [m, 0, m - 1, 1], [m + 60, 90, m - 1, 300]
