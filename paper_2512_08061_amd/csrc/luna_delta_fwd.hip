@@ -706,7 +706,9 @@ hipError_t launch_one(const DeltaArgs& a, hipStream_t s) {
 }
 template <int DK, int NP>
 hipError_t launch_columns(const DeltaArgs& a, hipStream_t s) {
-  return delta_columns(a.d) == 32 ? launch_one<DK, 32, NP>(a, s) : launch_one<DK, 64, NP>(a, s);
+  // 32 columns where workgroups of 64 would leave half of the device idle: a chunk passes in less time (2000 tokens, 16 heads, D = d = 128:
+  // 118 and 127 us, with a state 141 and 162)
+  return a.d == 32 || a.s.count * a.H * (a.d / 64) <= 128 ? launch_one<DK, 32, NP>(a, s) : launch_one<DK, 64, NP>(a, s);
 }
 template <int NP>
 hipError_t launch_parts(const DeltaArgs& a, hipStream_t s) {
