@@ -57,7 +57,8 @@ luna_status check_attn(luna_dtype dt, const luna_seqs* seqs, const luna_pages* p
   const luna::SeqSet qs = set_of(seqs);
   bool fits;
   if (luna::paged_splits(qs, H, Hk)) {  // (a join takes two rows of a key head or more)
-    fits = launchable(qs.count * H * qs.rows, 256);
+    fits = launchable(qs.count * H * qs.rows, 256) &&
+           launchable((luna::paged_shares(type_of(dt), qs.count, pages->width * pages->rows, Hk) + qs.count) * Hk, 256);
   } else {
     fits = launchable(luna::seq_slots(qs, luna::softmax_tile(type_of(dt), d)) * H, 256);
   }

@@ -35,16 +35,25 @@ __global__ __launch_bounds__(256) void paged_split_kernel(SoftmaxArgs a, int sha
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
-  const int hk = blockIdx.x % a.Hk, share = blockIdx.x / a.Hk;
+  const int hk = blockIdx.x % a.Hk, number = blockIdx.x / a.Hk;
   const int64_t all = units_before(a.ks, (int)a.ks.count, KB, l.scan), per = paged_per(all, shares, kPagedLeast);
-  const int64_t begin = share * per, end = min(all, begin + per);
-  if (begin >= end) return;
   int64_t first;  // units before sequence b
-  int b = sequence_at(a.ks, begin, KB, &first);
+  int b, share, stop = (int)a.ks.count;
+  if (per > kPagedLeast || gridDim.x == (unsigned)(shares * a.Hk)) {  // a share
+    share = number;
+    if (share >= shares || share * per >= all) return;
+    b = sequence_at(a.ks, share * per, KB, &first);
+  } else {  // of a short line what a share holds of one sequence, so that no sequence waits for another
+    b = sequence_of_number(a.ks, number, shares, KB, per, all, &first);
+    if (b < 0) return;
+    share = number - b;
+    stop = b + 1;
+  }
+  const int64_t end = min(all, (share + 1) * per);
   const int group = a.H / a.Hk, rows = (int)a.qs.rows * group;
   const float scale = a.scale * kLog2e;
 
-  for (; b < a.ks.count && first < end; ++b) {
+  for (; b < stop && first < end; ++b) {
     const SeqPiece sk = seq_uniform(seq_of(a.ks, b)), sq = seq_uniform(seq_of(a.qs, b));
     const int units = (sk.len + KB - 1) / KB, shift = sk.len - sq.len;
     const PagedUnits held = paged_held(first, units, per, share, all);
@@ -273,7 +282,10 @@ hipError_t launch_rows(const SoftmaxArgs& a, int shares, hipStream_t s) {
   constexpr int bytes = (int)sizeof(PagedLds<T, DH>);
   const hipError_t e = allow_lds<paged_split_kernel<T, DH, RT>>(bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_split_kernel<T, DH, RT>), dim3((unsigned)((int64_t)shares * a.Hk)), dim3(256), bytes, s, a, shares);
+  // Of a short line a sequence of a share each, as long as these run side by side: caches of 11, 10, 510 and 19 tokens, d = 128, 15.5
+  // instead of 27.3 us; eight of up to 3371, 12 heads, fp32, 21 and 42; but 200 of 30 tokens, four key heads, 44 and 35.
+  const int64_t groups = (shares + (a.ks.count * a.Hk <= 512 ? a.ks.count : 0)) * a.Hk;
+  hipLaunchKernelGGL((paged_split_kernel<T, DH, RT>), dim3((unsigned)groups), dim3(256), bytes, s, a, shares);
   return hipGetLastError();
 }
 

@@ -326,6 +326,24 @@ __device__ __forceinline__ int sequence_of_part(const SeqSet& s, int rank, int s
   }
   return -1;
 }
+// The sequence b of which share number - b holds units, and the units before it; -1: none (the whole wave calls this).
+__device__ __forceinline__ int sequence_of_number(const SeqSet& s, int number, int shares, int unit, int64_t per, int64_t all, int64_t* first) {
+  const int lane = threadIdx.x % kWave, count = (int)s.count;
+  int64_t sum = 0;
+  for (int b0 = 0; b0 < count && b0 <= number; b0 += kWave) {
+    const int b = b0 + lane, mine = b < count ? units_of(s, b, unit) : 0, share = number - b;
+    const int64_t to = sum + lanes_up_to((int64_t)mine);
+    const PagedUnits u = paged_held(to - mine, mine, per, share, all);
+    const uint64_t found = __ballot(mine > 0 && share >= 0 && share < shares && share * per < all && u.u0 < u.u1);
+    if (found) {
+      const int i = __builtin_ctzll(found);
+      *first = __shfl(to - mine, i);
+      return __builtin_amdgcn_readfirstlane(b0 + i);
+    }
+    sum = __shfl(to, kWave - 1);
+  }
+  return -1;
+}
 // Sum over the threads of a workgroup.
 template <int THREADS>
 __device__ __forceinline__ int64_t group_sum(int64_t x, int64_t* scan) {
