@@ -168,9 +168,6 @@ hipError_t launch_delta_fwd_f32(const DeltaArgs& a, hipStream_t s);
 // the backward pass: E and the states before the chunks, X and the gradients of the states behind them; the gradients
 hipError_t launch_delta_both(Dt dt, const DeltaArgs& a, hipStream_t s);
 hipError_t launch_delta_grads(Dt dt, const DeltaArgs& a, hipStream_t s);
-// Value columns of a workgroup of the serial passes.
-constexpr int delta_columns(int64_t d) { return d < 64 ? 32 : 64; }
-
 struct DeltaStepArgs {
   SeqRows q, k, v, o;
   const float* log_decay;  // [count][H][m]

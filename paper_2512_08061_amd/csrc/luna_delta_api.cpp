@@ -41,7 +41,7 @@ luna_status plan_delta(luna_dtype dt, const luna_seqs& s, int64_t H, int64_t Hk,
   const luna::SeqSet set = set_of(&s);
   p->slots = luna::seq_slots(set, luna::kDeltaChunk);
   if (!launchable(p->slots * Hk, 512) || p->slots >= ((int64_t)1 << 31) ||
-      !launchable((backward ? 2 : 1) * s.count * H * (d / luna::delta_columns(d)), 512))
+      !launchable((backward ? 2 : 1) * s.count * H * (d / 32), 512))
     return set_error(LUNA_ERR_UNSUPPORTED, "too many chunks of sequences and heads");
   const size_t all = (size_t)p->slots * H, matrix = (size_t)luna::kDeltaChunk * luna::kDeltaChunk * (dt == LUNA_BF16 ? 2 : 4);
   const auto parts = [&](int n) { return (size_t)(dt == LUNA_BF16 ? n : 1); };

@@ -3,6 +3,6 @@
 
 namespace luna {
 
-hipError_t launch_delta_both_bf16(const DeltaArgs& a, hipStream_t s) { LUNA_DELTA_WIDTHS(launch_both_one, __bf16, , kDeltaBackParts); }
+hipError_t launch_delta_both_bf16(const DeltaArgs& a, hipStream_t s) { return launch_scan_all<__bf16, kDeltaBackParts, true>(a, s); }
 
 }  // namespace luna

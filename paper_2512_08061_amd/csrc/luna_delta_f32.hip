@@ -3,9 +3,9 @@
 
 namespace luna {
 
-hipError_t launch_delta_fwd_f32(const DeltaArgs& a, hipStream_t s) { LUNA_DELTA_WIDTHS(launch_scan_one, float, ); }
+hipError_t launch_delta_fwd_f32(const DeltaArgs& a, hipStream_t s) { return launch_scan_all<float, 1, false>(a, s); }
 
-static hipError_t both(const DeltaArgs& a, hipStream_t s) { LUNA_DELTA_WIDTHS(launch_both_one, float, , 1); }
+static hipError_t both(const DeltaArgs& a, hipStream_t s) { return launch_scan_all<float, 1, true>(a, s); }
 
 hipError_t launch_delta_both_bf16(const DeltaArgs& a, hipStream_t s);
 

@@ -70,14 +70,14 @@ __device__ __forceinline__ void load_op_pair_tr(DeltaOp<T, P>& f, const T* x, in
                 [&](int kk, int col) { return x + (row + 4 * half + kk) * pitch + first + 8 * (col / 4) + col % 4; });
 }
 
-template <typename T, int DK, int DVW, int NP, bool OUT>
+template <typename T, int DK, int DVW, int NP, int HELP, bool OUT>
 __device__ __forceinline__ void delta_scan(const DeltaArgs& a, int block, char* raw) {
   using Lds = ScanLds<T, DK, DVW, NP, 1, OUT>;
-  constexpr int C = Lds::C, FT = DK / 16, FS = DK / 32, KT = C / 16, KS = C / 32, esz = (int)sizeof(T), THREADS = 4 * DVW;
+  constexpr int C = Lds::C, FT = DK / 16, FS = DK / 32, KT = C / 16, KS = C / 32, esz = (int)sizeof(T), THREADS = HELP ? 64 * HELP : 4 * DVW;  // (those that load)
   constexpr int TI = FT < 4 ? FT : 4, TN = FT * KS / TI;  // tiles of a batch of transposed reads, and batches
   static_assert(!OUT || sizeof(T) == 4, "bf16 has a forward kernel of its own");
   Lds& l = *reinterpret_cast<Lds*>(raw);
-  const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id() - HELP, g = lane / 16, c = lane % 16;
   const int slices = a.d / DVW;
   const int slice = block % slices, head = (block / slices) % a.H, b = block / slices / a.H;
   const SeqPiece sp = seq_uniform(seq_of(a.s, b));
@@ -94,7 +94,7 @@ __device__ __forceinline__ void delta_scan(const DeltaArgs& a, int block, char* 
   ScanMatrix<T, 1, Lds::PN, THREADS> pr;
   constexpr int GN = 4 * C / THREADS;
   float gr[GN];
-  int bad = C;
+  int br = C;
   const auto load = [&](int chunk) {
     const int t0 = chunk * C, m = min(C, sp.len - t0);
     const int64_t at = (int64_t)(slot0 + chunk) * a.H + head;
@@ -108,10 +108,34 @@ __device__ __forceinline__ void delta_scan(const DeltaArgs& a, int block, char* 
     const float* gates = a.gates + at * kDeltaGates;
 #pragma unroll
     for (int i = 0; i < GN; ++i) gr[i] = gates[tid + THREADS * i];
-    bad = __builtin_amdgcn_readfirstlane(__float_as_int(gates[kDeltaMisc * C + 1]));
+    br = __float_as_int(gates[kDeltaMisc * C + 1]);
   };
-  load(0);
   for (int i = tid; i < DVW; i += THREADS) l.since[i] = kNever;
+
+  const auto put = [&](int t0) {
+    const int bad = __builtin_amdgcn_readfirstlane(br);
+    if (bad < C) clear_rows(kr, bad);
+    kr.store(&l.k[0][0]);
+    if constexpr (OUT) {
+      vr.clean(l.since, t0);
+      qr.store(&l.q[0][0]);
+      pr.store(l.p);
+    }
+    vr.store(&l.v[0][0]);
+    nr.store(l.n);
+#pragma unroll
+    for (int i = 0; i < GN; ++i) (&l.gates[0][0])[tid + THREADS * i] = gr[i];
+  };
+  if (!HELP || wave < 0) load(0);
+  if (HELP && wave < 0) {
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+      __syncthreads();
+      put(chunk * C);
+      __syncthreads();
+      if (chunk + 1 < chunks) load(chunk + 1);
+    }
+    return;
+  }
 
   f32x4 S[FT];
   const int64_t state = ((int64_t)b * a.H + head) * a.D * a.d + col0 + wcol + c;
@@ -125,22 +149,15 @@ __device__ __forceinline__ void delta_scan(const DeltaArgs& a, int block, char* 
     const int t0 = chunk * C, m = min(C, sp.len - t0);
     const int64_t at = (int64_t)(slot0 + chunk) * a.H + head;
     __syncthreads();  // the chunk before is no longer read
-    if (bad < C) {
-      clear_rows(kr, bad);
-      lost = min(lost, t0 + bad);
+    if constexpr (!HELP) {
+      put(t0);
+      if (chunk + 1 < chunks) load(chunk + 1);
     }
-    kr.store(&l.k[0][0]);
-    if constexpr (OUT) {
-      vr.clean(l.since, t0);
-      qr.store(&l.q[0][0]);
-      pr.store(l.p);
-    }
-    vr.store(&l.v[0][0]);
-    nr.store(l.n);
-#pragma unroll
-    for (int i = 0; i < GN; ++i) (&l.gates[0][0])[tid + THREADS * i] = gr[i];
-    if (chunk + 1 < chunks) load(chunk + 1);
     __syncthreads();
+    if constexpr (OUT) {
+      const int bad = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int&>(l.gates[kDeltaMisc][1]));
+      if (bad < C) lost = min(lost, t0 + bad);
+    }
 
     if (!OUT) {  // the state before the chunk, [d][D]
       float* to = a.before + (at * a.d + col0 + wcol + c) * DK;
@@ -283,13 +300,13 @@ __device__ __forceinline__ void delta_scan(const DeltaArgs& a, int block, char* 
 }
 
 // The gradients of the states and X, from the last chunk to the first.
-template <typename T, int DK, int DVW, int NP>
+template <typename T, int DK, int DVW, int NP, int HELP>
 __device__ __forceinline__ void delta_back(const DeltaArgs& a, int block, char* raw) {
   using Lds = ScanLds<T, DK, DVW, NP, NP, true>;
-  constexpr int C = Lds::C, FT = DK / 16, FS = DK / 32, KT = C / 16, KS = C / 32, esz = (int)sizeof(T), THREADS = 4 * DVW;
+  constexpr int C = Lds::C, FT = DK / 16, FS = DK / 32, KT = C / 16, KS = C / 32, esz = (int)sizeof(T), THREADS = HELP ? 64 * HELP : 4 * DVW;  // (those that load)
   constexpr int TI = FT < 4 ? FT : 4, TN = FT * KS / TI;  // tiles of a batch of transposed reads, and batches
   Lds& l = *reinterpret_cast<Lds*>(raw);
-  const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = wave_id() - HELP, g = lane / 16, c = lane % 16;
   const int slices = a.d / DVW;
   const int slice = block % slices, head = (block / slices) % a.H, b = block / slices / a.H;
   const SeqPiece sp = seq_uniform(seq_of(a.s, b));
@@ -316,13 +333,7 @@ __device__ __forceinline__ void delta_back(const DeltaArgs& a, int block, char* 
 #pragma unroll
     for (int i = 0; i < GN; ++i) gr[i] = gates[tid + THREADS * i];
   };
-  load(chunks - 1);
-  f32x4 S[FT];
-#pragma unroll
-  for (int ft = 0; ft < FT; ++ft) S[ft] = zero4();
-  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
-    const int64_t at = (int64_t)(slot0 + chunk) * a.H + head;
-    __syncthreads();  // the chunk behind is no longer read
+  const auto put = [&] {
     kr.store(&l.k[0][0]);
     qr.store(&l.q[0][0]);
     vr.store(&l.v[0][0]);
@@ -330,7 +341,27 @@ __device__ __forceinline__ void delta_back(const DeltaArgs& a, int block, char* 
     pr.store(l.p);
 #pragma unroll
     for (int i = 0; i < GN; ++i) (&l.gates[0][0])[tid + THREADS * i] = gr[i];
-    if (chunk > 0) load(chunk - 1);
+  };
+  if (!HELP || wave < 0) load(chunks - 1);
+  if (HELP && wave < 0) {
+    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+      __syncthreads();
+      put();
+      __syncthreads();
+      if (chunk > 0) load(chunk - 1);
+    }
+    return;
+  }
+  f32x4 S[FT];
+#pragma unroll
+  for (int ft = 0; ft < FT; ++ft) S[ft] = zero4();
+  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+    const int64_t at = (int64_t)(slot0 + chunk) * a.H + head;
+    __syncthreads();  // the chunk behind is no longer read
+    if constexpr (!HELP) {
+      put();
+      if (chunk > 0) load(chunk - 1);
+    }
     __syncthreads();
 
     {  // [d][D]
@@ -449,46 +480,59 @@ __device__ __forceinline__ void delta_back(const DeltaArgs& a, int block, char* 
   }
 }
 
-template <typename T, int DK, int DVW>
-__global__ __launch_bounds__(4 * DVW, 1) void delta_scan_kernel(DeltaArgs a) {
+template <typename T, int DK, int DVW, int HELP>
+__global__ __launch_bounds__(4 * DVW + 64 * HELP, 1) void delta_scan_kernel(DeltaArgs a) {
   extern __shared__ __attribute__((aligned(16))) char raw[];
-  delta_scan<T, DK, DVW, 1, true>(a, blockIdx.x, raw);
+  delta_scan<T, DK, DVW, 1, HELP, true>(a, blockIdx.x, raw);
 }
 // Both passes of the backward half: neither needs what the other writes, and each alone has few workgroups.
-template <typename T, int DK, int DVW, int NP>
-__global__ __launch_bounds__(4 * DVW, 1) void delta_both_kernel(DeltaArgs a) {
+template <typename T, int DK, int DVW, int NP, int HELP>
+__global__ __launch_bounds__(4 * DVW + 64 * HELP, 1) void delta_both_kernel(DeltaArgs a) {
   extern __shared__ __attribute__((aligned(16))) char raw[];
   const int half = gridDim.x / 2;
-  if ((int)blockIdx.x < half) delta_back<T, DK, DVW, NP>(a, blockIdx.x, raw);
-  else delta_scan<T, DK, DVW, NP, false>(a, blockIdx.x - half, raw);
+  if ((int)blockIdx.x < half) delta_back<T, DK, DVW, NP, HELP>(a, blockIdx.x, raw);
+  else delta_scan<T, DK, DVW, NP, HELP, false>(a, blockIdx.x - half, raw);
 }
 
-template <typename T, int DK, int DVW>
+template <typename T, int DK, int DVW, int HELP>
 hipError_t launch_scan_one(const DeltaArgs& a, hipStream_t s) {
   constexpr int bytes = (int)sizeof(ScanLds<T, DK, DVW, 1, 1, true>);
   static_assert(bytes <= 160 * 1024, "one workgroup's LDS");
-  const hipError_t e = allow_lds<delta_scan_kernel<T, DK, DVW>>(bytes);
+  const hipError_t e = allow_lds<delta_scan_kernel<T, DK, DVW, HELP>>(bytes);
   if (e != hipSuccess) return e;
   const int64_t groups = a.s.count * a.H * (a.d / DVW);
-  hipLaunchKernelGGL((delta_scan_kernel<T, DK, DVW>), dim3((unsigned)groups), dim3(4 * DVW), bytes, s, a);
+  hipLaunchKernelGGL((delta_scan_kernel<T, DK, DVW, HELP>), dim3((unsigned)groups), dim3(4 * DVW + 64 * HELP), bytes, s, a);
   return hipGetLastError();
 }
-template <typename T, int DK, int DVW, int NP>
+template <typename T, int DK, int DVW, int NP, int HELP>
 hipError_t launch_both_one(const DeltaArgs& a, hipStream_t s) {
   constexpr int bytes = (int)sizeof(ScanLds<T, DK, DVW, NP, NP, true>);
   static_assert(bytes <= 160 * 1024 && bytes >= (int)sizeof(ScanLds<T, DK, DVW, NP, 1, false>), "one workgroup's LDS");
-  const hipError_t e = allow_lds<delta_both_kernel<T, DK, DVW, NP>>(bytes);
+  const hipError_t e = allow_lds<delta_both_kernel<T, DK, DVW, NP, HELP>>(bytes);
   if (e != hipSuccess) return e;
   const int64_t groups = 2 * a.s.count * a.H * (a.d / DVW);
-  hipLaunchKernelGGL((delta_both_kernel<T, DK, DVW, NP>), dim3((unsigned)groups), dim3(4 * DVW), bytes, s, a);
+  hipLaunchKernelGGL((delta_both_kernel<T, DK, DVW, NP, HELP>), dim3((unsigned)groups), dim3(4 * DVW + 64 * HELP), bytes, s, a);
   return hipGetLastError();
 }
 
-#define LUNA_DELTA_WIDTHS(LAUNCH, T, ...)                                                                            \
-  if (delta_columns(a.d) == 32)                                                                                      \
-    return a.D == 32 ? LAUNCH<T, 32, 32 __VA_ARGS__>(a, s) : a.D == 64 ? LAUNCH<T, 64, 32 __VA_ARGS__>(a, s)         \
-                                                           : LAUNCH<T, 128, 32 __VA_ARGS__>(a, s);                   \
-  return a.D == 32 ? LAUNCH<T, 32, 64 __VA_ARGS__>(a, s) : a.D == 64 ? LAUNCH<T, 64, 64 __VA_ARGS__>(a, s)           \
-                                                         : LAUNCH<T, 128, 64 __VA_ARGS__>(a, s)
+// 32 columns and two waves that load, or 64 columns of which all waves load: the first where its workgroups run side by side.
+constexpr int kScanHelp = 2;
+template <typename T, int DK, int DVW, int NP, bool BOTH>
+hipError_t launch_scan_width(const DeltaArgs& a, hipStream_t s) {
+  constexpr int help = DVW == 32 ? kScanHelp : 0;
+  if constexpr (BOTH) return launch_both_one<T, DK, DVW, NP, help>(a, s);
+  else return launch_scan_one<T, DK, DVW, help>(a, s);
+}
+template <typename T, int DK, int NP, bool BOTH>
+hipError_t launch_scan_feature(const DeltaArgs& a, hipStream_t s) {
+  constexpr int at_once = 256 * (160 * 1024 / (int)sizeof(ScanLds<T, DK, 32, NP, NP, true>));
+  return a.d == 32 || (BOTH ? 2 : 1) * a.s.count * a.H * (a.d / 32) <= at_once ? launch_scan_width<T, DK, 32, NP, BOTH>(a, s)
+                                                                              : launch_scan_width<T, DK, 64, NP, BOTH>(a, s);
+}
+template <typename T, int NP, bool BOTH>
+hipError_t launch_scan_all(const DeltaArgs& a, hipStream_t s) {
+  return a.D == 32 ? launch_scan_feature<T, 32, NP, BOTH>(a, s) : a.D == 64 ? launch_scan_feature<T, 64, NP, BOTH>(a, s)
+                                                                            : launch_scan_feature<T, 128, NP, BOTH>(a, s);
+}
 
 }  // namespace luna
