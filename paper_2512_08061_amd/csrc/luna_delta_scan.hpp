@@ -515,7 +515,8 @@ hipError_t launch_both_one(const DeltaArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// 32 columns and two waves that load, or 64 columns of which all waves load: the first where its workgroups run side by side.
+// 32 columns and two waves that load, or 64 columns of which all waves load: the first where its workgroups run side by side
+// (backward in bf16, 16 heads, D = d = 128: 2 x 2048 tokens 301 and 366 us, but 8 x 2048 1138 and 1057).
 constexpr int kScanHelp = 2;
 template <typename T, int DK, int DVW, int NP, bool BOTH>
 hipError_t launch_scan_width(const DeltaArgs& a, hipStream_t s) {
