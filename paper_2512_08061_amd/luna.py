@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+from array import array
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libluna.so")
@@ -609,7 +610,7 @@ def _seq_init():
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     stream = (lambda device: raw(device.index)) if raw is not None else _stream_ptr
     _seq_torch = types.SimpleNamespace(
-        f32=torch.float32, i32=torch.int32, bf16=torch.bfloat16, empty=torch.empty, empty_like=torch.empty_like,
+        f32=torch.float32, i32=torch.int32, bf16=torch.bfloat16, u8=torch.uint8, empty=torch.empty, empty_like=torch.empty_like,
         zeros_like=torch.zeros_like, device=torch.cuda.device, current=torch.cuda.current_device, stream=stream,
         lib=load_library())
     return _seq_torch
@@ -619,29 +620,33 @@ class _Seqs:
     """The sequences of a call (luna_seqs): of 4-dim tensors [B, H, n, width], with lens [B]
     where fewer than n rows of each are used, or of 3-dim packed tensors [T, H, width] with offsets [B + 1]."""
 
+    __slots__ = ("count", "rows", "packed", "device", "dtype", "c", "at")
+
     def __init__(self, t, offsets, lens, what):
         T = _seq_torch or _seq_init()
-        if t.dim() == 3:
-            if offsets is None or lens is not None:
-                raise LunaError(LUNA_ERR_INVALID_ARG, f"{what}: packed [T, H, width] tensors take offsets, and no lens")
-            self.count, self.rows = offsets.shape[0] - 1 if offsets.dim() == 1 else -1, t.shape[0]
-        elif t.dim() == 4:
+        shape, device = t.shape, t.device
+        dim = len(shape)
+        if dim == 4:
             if offsets is not None:
                 raise LunaError(LUNA_ERR_INVALID_ARG, f"{what}: offsets go with packed [T, H, width] tensors")
-            self.count, self.rows = t.shape[0], t.shape[2]
+            count, rows, index = shape[0], shape[2], lens
+        elif dim == 3:
+            if offsets is None or lens is not None:
+                raise LunaError(LUNA_ERR_INVALID_ARG, f"{what}: packed [T, H, width] tensors take offsets, and no lens")
+            count, rows, index = offsets.shape[0] - 1 if offsets.dim() == 1 else -1, shape[0], offsets
         else:
             raise LunaError(LUNA_ERR_INVALID_ARG, f"{what} must be [B, H, n, width] or packed [T, H, width]")
-        self.packed, self.device, self.dtype = t.dim() == 3, t.device, t.dtype
-        index = offsets if self.packed else lens
+        self.count, self.rows, self.packed, self.device, self.dtype = count, rows, dim == 3, device, t.dtype
         at = 0
         if index is not None:
-            want = self.count + 1 if self.packed else self.count
-            if index.dtype != T.i32 or index.device != t.device or not index.is_contiguous() or \
-                    index.dim() != 1 or index.shape[0] != want or self.count < 1:
+            want = count + 1 if dim == 3 else count
+            if index.dtype != T.i32 or index.device != device or not index.is_contiguous() or \
+                    index.dim() != 1 or index.shape[0] != want or count < 1:
                 raise LunaError(LUNA_ERR_INVALID_ARG, "offsets [B + 1] and lens [B] must be contiguous int32 tensors on "
                                                       "the tensors' device")
             at = index.data_ptr()
-        self.c = (ctypes.c_int64 * 4)(self.count, self.rows, at if self.packed else 0, 0 if self.packed else at)
+        self.c = array("q", (count, rows, at, 0) if dim == 3 else (count, rows, 0, at))
+        self.at = self.c.buffer_info()[0]
 
     def same(self, t) -> bool:
         """Whether t lies in this form's sequences."""
@@ -657,20 +662,22 @@ def _seq_rows(seqs, ts, heads, widths, names):
     """luna_rows of each tensor, one behind the other, as an array of whole numbers."""
     v = []
     dtype, device, packed, count, rows = seqs.dtype, seqs.device, seqs.packed, seqs.count, seqs.rows
+    if ts and not ts[0].is_cuda:
+        raise LunaError(LUNA_ERR_INVALID_ARG, f"{names[0]} must share the other tensors' dtype and GPU")
     for t, H, w, name in zip(ts, heads, widths, names):
-        if t.dtype != dtype or t.device != device or not t.is_cuda:
+        if t.dtype is not dtype or t.device != device:
             raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} must share the other tensors' dtype and GPU")
-        shape, st = t.shape, t.stride()
-        if shape != ((rows, H, w) if packed else (count, H, rows, w)):
-            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} has shape {tuple(shape)}: its sequences, {H} heads or width "
+        if t.shape != ((rows, H, w) if packed else (count, H, rows, w)):
+            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} has shape {tuple(t.shape)}: its sequences, {H} heads or width "
                                                   f"{w} do not match")
-        if w > 1 and st[-1] != 1:
+        st = t.stride()
+        if st[-1] != 1 and w > 1:
             raise LunaError(LUNA_ERR_INVALID_ARG, f"{name}'s rows must be contiguous")
         if packed:  # (a stride of an extent of one is never used)
             v += (t.data_ptr(), 0, st[1] if H > 1 else 0, st[0] if rows > 1 else w)
         else:
             v += (t.data_ptr(), st[0] if count > 1 else 0, st[1] if H > 1 else 0, st[2] if rows > 1 else w)
-    return (ctypes.c_int64 * len(v))(*v)
+    return array("q", v)
 
 
 def _f32_ptr(t, shape, device, name):
@@ -700,11 +707,24 @@ def _new(t, lens):
     return _seq_torch.empty_like(t) if lens is None else _seq_torch.zeros_like(t)
 
 
+def _seq_bytes(nbytes, device):
+    """(tensor to keep, address, bytes) of a workspace."""
+    if nbytes == 0:
+        return None, None, 0
+    ws = _seq_torch.empty(nbytes + 256, dtype=_seq_torch.u8, device=device)
+    at = ws.data_ptr()
+    return ws, at + -at % 256, nbytes
+
+
+def _seq_dt(seqs, t):
+    return LUNA_BF16 if seqs.dtype is _seq_torch.bf16 else _dt(t)
+
+
 def _seq_workspace(op, seqs, keys, H, Hk, Dq, Dv, dt):
     """(tensor to keep, address, bytes) of an operation's workspace."""
-    nb = int(_seq_torch.lib.luna_seq_workspace_bytes(op, dt, ctypes.addressof(seqs.c), None if keys is None else ctypes.addressof(keys.c),
+    nb = int(_seq_torch.lib.luna_seq_workspace_bytes(op, dt, seqs.at, None if keys is None else keys.at,
                                           H, Hk, Dq, Dv))
-    return (None, None, 0) if nb == 0 else _workspace(nb, seqs.device)
+    return _seq_bytes(nb, seqs.device)
 
 
 def _decay_state(S, z, count, H, D, d, normalize, device):
@@ -745,10 +765,10 @@ def decay_attn(Q, K, V, log_decay, S=None, z=None, normalize: bool = False, scal
         dp = _f32_ptr(den, seqs.numbers(H), seqs.device, "den")
     elif den is not None:
         raise LunaError(LUNA_ERR_INVALID_ARG, "den goes with normalize")
-    dt, at = _dt(Q), ctypes.addressof(rows)
+    dt, at = _seq_dt(seqs, Q), rows.buffer_info()[0]
     with _on_device(seqs.device):
         ws, wsp, wsn = _seq_workspace(OP_DECAY_FWD, seqs, None, H, H, D, d, dt)
-        _check(lib.luna_decay_fwd(at, at + 32, at + 64, dt, ctypes.addressof(seqs.c), H, D, d, gp, int(normalize), scale, eps,
+        _check(lib.luna_decay_fwd(at, at + 32, at + 64, dt, seqs.at, H, D, d, gp, int(normalize), scale, eps,
                                   sp, zp, at + 96, dp, wsp, wsn, _seq_torch.stream(seqs.device)))
     return out, den
 
@@ -765,9 +785,9 @@ def decay_attn_step(Q, K, V, log_decay, S, z=None, normalize: bool = False, scal
     rows = _seq_rows(seqs, (Q, K, V, out), (H, H, H, H), (D, D, d, d), ("Q", "K", "V", "out"))
     gp = _f32_ptr(log_decay, (H,), seqs.device, "log_decay")
     sp, zp = _decay_state(S, z, seqs.count, H, D, d, normalize, seqs.device)
-    at = ctypes.addressof(rows)
+    at = rows.buffer_info()[0]
     with _on_device(seqs.device):
-        _check(lib.luna_decay_step(at, at + 32, at + 64, _dt(Q), seqs.count, seqs.rows, H, D, d, gp, int(normalize), scale, eps,
+        _check(lib.luna_decay_step(at, at + 32, at + 64, _seq_dt(seqs, Q), seqs.count, seqs.rows, H, D, d, gp, int(normalize), scale, eps,
                                    sp, zp, at + 96, _seq_torch.stream(seqs.device)))
     return out
 
@@ -787,10 +807,10 @@ def decay_attn_bwd(Q, K, V, dO, log_decay, out=None, den=None, normalize: bool =
                      ("Q", "K", "V", "dO", "out", "dQ", "dK", "dV"))
     gp = _f32_ptr(log_decay, (H,), seqs.device, "log_decay")
     dp = _f32_ptr(den, seqs.numbers(H), seqs.device, "den") if normalize else None
-    dt, at = _dt(Q), ctypes.addressof(rows)
+    dt, at = _seq_dt(seqs, Q), rows.buffer_info()[0]
     with _on_device(seqs.device):
         ws, wsp, wsn = _seq_workspace(OP_DECAY_BWD, seqs, None, H, H, D, d, dt)
-        _check(lib.luna_decay_bwd(at, at + 32, at + 64, at + 96, dt, ctypes.addressof(seqs.c), H, D, d, gp, int(normalize),
+        _check(lib.luna_decay_bwd(at, at + 32, at + 64, at + 96, dt, seqs.at, H, D, d, gp, int(normalize),
                                   scale, eps, at + 128 if normalize else None, dp, at + 160, at + 192, at + 224, wsp, wsn,
                                   _seq_torch.stream(seqs.device)))
     return dQ, dK, dV
@@ -827,11 +847,11 @@ def softmax_attn(Q, K, V, scale: float | None = None, offsets=None, lens=None, k
         raise LunaError(LUNA_ERR_INVALID_ARG, "Q and K must share dtype and GPU")
     lse = _seq_torch.empty(seqs.numbers(H), dtype=_seq_torch.f32, device=seqs.device) if lse is None else lse
     lp = _f32_ptr(lse, seqs.numbers(H), seqs.device, "lse")
-    dt, at, ak = _dt(Q), ctypes.addressof(rows), ctypes.addressof(krows)
+    dt, at, ak = _seq_dt(seqs, Q), rows.buffer_info()[0], krows.buffer_info()[0]
     with _on_device(seqs.device):
         ws, wsp, wsn = _seq_workspace(OP_SOFTMAX_FWD, seqs, keys, H, Hk, d, d, dt)
-        _check(lib.luna_softmax_fwd(at, ak, ak + 32, dt, ctypes.addressof(seqs.c),
-                                    None if keys is None else ctypes.addressof(keys.c), H, Hk, d,
+        _check(lib.luna_softmax_fwd(at, ak, ak + 32, dt, seqs.at,
+                                    None if keys is None else keys.at, H, Hk, d,
                                     d ** -0.5 if scale is None else scale, at + 32, lp, wsp, wsn, _seq_torch.stream(seqs.device)))
     return out, lse
 
@@ -851,11 +871,11 @@ def softmax_attn_bwd(Q, K, V, out, lse, dO, scale: float | None = None, offsets=
     if keys is not None and (keys.dtype != seqs.dtype or keys.device != seqs.device):
         raise LunaError(LUNA_ERR_INVALID_ARG, "Q and K must share dtype and GPU")
     lp = _f32_ptr(lse, seqs.numbers(H), seqs.device, "lse")
-    dt, at, ak = _dt(Q), ctypes.addressof(rows), ctypes.addressof(krows)
+    dt, at, ak = _seq_dt(seqs, Q), rows.buffer_info()[0], krows.buffer_info()[0]
     with _on_device(seqs.device):
         ws, wsp, wsn = _seq_workspace(OP_SOFTMAX_BWD, seqs, keys, H, Hk, d, d, dt)
-        _check(lib.luna_softmax_bwd(at, ak, ak + 32, at + 32, lp, at + 64, dt, ctypes.addressof(seqs.c),
-                                    None if keys is None else ctypes.addressof(keys.c), H, Hk, d,
+        _check(lib.luna_softmax_bwd(at, ak, ak + 32, at + 32, lp, at + 64, dt, seqs.at,
+                                    None if keys is None else keys.at, H, Hk, d,
                                     d ** -0.5 if scale is None else scale, at + 96, ak + 64, ak + 96, wsp, wsn,
                                     _seq_torch.stream(seqs.device)))
     return dQ, dK, dV
@@ -869,8 +889,8 @@ OP_DELTA_FWD, OP_DELTA_BWD = range(2)
 
 
 def _delta_workspace(op, seqs, H, Hk, D, d, dt):
-    nb = int(_seq_torch.lib.luna_delta_workspace_bytes(op, dt, ctypes.addressof(seqs.c), H, Hk, D, d))
-    return (None, None, 0) if nb == 0 else _workspace(nb, seqs.device)
+    nb = int(_seq_torch.lib.luna_delta_workspace_bytes(op, dt, seqs.at, H, Hk, D, d))
+    return _seq_bytes(nb, seqs.device)
 
 
 def delta_attn(Q, K, V, log_decay, beta, S=None, scale: float = 1.0, offsets=None, lens=None, out=None):
@@ -890,10 +910,10 @@ def delta_attn(Q, K, V, log_decay, beta, S=None, scale: float = 1.0, offsets=Non
     gp = _f32_ptr(log_decay, seqs.numbers(H), seqs.device, "log_decay")
     bp = _f32_ptr(beta, seqs.numbers(H), seqs.device, "beta")
     sp = None if S is None else _f32_ptr(S, (seqs.count, H, D, d), seqs.device, "S")
-    dt, at = _dt(Q), ctypes.addressof(rows)
+    dt, at = _seq_dt(seqs, Q), rows.buffer_info()[0]
     with _on_device(seqs.device):
         ws, wsp, wsn = _delta_workspace(OP_DELTA_FWD, seqs, H, Hk, D, d, dt)
-        _check(lib.luna_delta_fwd(at, at + 32, at + 64, dt, ctypes.addressof(seqs.c), H, Hk, D, d, gp, bp, scale, sp, at + 96, wsp,
+        _check(lib.luna_delta_fwd(at, at + 32, at + 64, dt, seqs.at, H, Hk, D, d, gp, bp, scale, sp, at + 96, wsp,
                                   wsn, _seq_torch.stream(seqs.device)))
     return out
 
@@ -911,9 +931,9 @@ def delta_attn_step(Q, K, V, log_decay, beta, S, scale: float = 1.0, out=None):
     gp = _f32_ptr(log_decay, seqs.numbers(H), seqs.device, "log_decay")
     bp = _f32_ptr(beta, seqs.numbers(H), seqs.device, "beta")
     sp = _f32_ptr(S, (seqs.count, H, D, d), seqs.device, "S")
-    at = ctypes.addressof(rows)
+    at = rows.buffer_info()[0]
     with _on_device(seqs.device):
-        _check(lib.luna_delta_step(at, at + 32, at + 64, _dt(Q), seqs.count, seqs.rows, H, Hk, D, d, gp, bp, scale, sp, at + 96,
+        _check(lib.luna_delta_step(at, at + 32, at + 64, _seq_dt(seqs, Q), seqs.count, seqs.rows, H, Hk, D, d, gp, bp, scale, sp, at + 96,
                                    _seq_torch.stream(seqs.device)))
     return out
 
@@ -931,10 +951,10 @@ def delta_attn_bwd(Q, K, V, dO, log_decay, beta, scale: float = 1.0, offsets=Non
                      ("Q", "K", "V", "dO", "dQ", "dK", "dV"))
     dgp = _f32_ptr(dg, seqs.numbers(H), seqs.device, "dlog_decay")
     dbp = _f32_ptr(db, seqs.numbers(H), seqs.device, "dbeta")
-    dt, at = _dt(Q), ctypes.addressof(rows)
+    dt, at = _seq_dt(seqs, Q), rows.buffer_info()[0]
     with _on_device(seqs.device):
         ws, wsp, wsn = _delta_workspace(OP_DELTA_BWD, seqs, H, Hk, D, d, dt)
-        _check(lib.luna_delta_bwd(at, at + 32, at + 64, at + 96, dt, ctypes.addressof(seqs.c), H, Hk, D, d, gp, bp, scale, at + 128,
+        _check(lib.luna_delta_bwd(at, at + 32, at + 64, at + 96, dt, seqs.at, H, Hk, D, d, gp, bp, scale, at + 128,
                                   at + 160, at + 192, dgp, dbp, wsp, wsn, _seq_torch.stream(seqs.device)))
     return dQ, dK, dV, dg, db
 
@@ -944,18 +964,27 @@ def delta_attn_bwd(Q, K, V, dO, log_decay, beta, scale: float = 1.0, offsets=Non
 # ---------------------------------------------------------------------------
 
 def _paged(seqs, k_pages, v_pages, table, lens, Hk, d):
-    """(luna_pages, luna_rows of both tensors of pages) of a call."""
-    T = _seq_torch
-    if k_pages.dim() != 4:
+    """luna_pages and the luna_rows of both tensors of pages of a call, one behind the other."""
+    i32, dtype, device, count = _seq_torch.i32, seqs.dtype, seqs.device, seqs.count
+    shape = k_pages.shape
+    if len(shape) != 4:
         raise LunaError(LUNA_ERR_INVALID_ARG, "k_pages must be [pages, Hk, rows, d]")
-    pool = _Seqs(k_pages, None, None, "k_pages")
-    if pool.dtype != seqs.dtype or pool.device != seqs.device:
-        raise LunaError(LUNA_ERR_INVALID_ARG, "the pages must share the other tensors' dtype and GPU")
-    rows = _seq_rows(pool, (k_pages, v_pages), (Hk, Hk), (d, d), ("k_pages", "v_pages"))
+    pool, rows = shape[0], shape[2]
+    v = [pool, rows, 0, 0, 0]
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        if t.dtype is not dtype or t.device != device:
+            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} must share the other tensors' dtype and GPU")
+        if t.shape != (pool, Hk, rows, d):
+            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} has shape {tuple(t.shape)}: its pages, {Hk} heads or width {d} do not match")
+        st = t.stride()
+        if st[3] != 1 and d > 1:
+            raise LunaError(LUNA_ERR_INVALID_ARG, f"{name}'s rows must be contiguous")
+        v += (t.data_ptr(), st[0] if pool > 1 else 0, st[1] if Hk > 1 else 0, st[2] if rows > 1 else d)
     for t, dim, name in ((table, 2, "table [B, width]"), (lens, 1, "lens [B]")):
-        if t.dtype != T.i32 or t.device != seqs.device or t.dim() != dim or t.shape[0] != seqs.count or not t.is_contiguous():
+        if t.dtype != i32 or t.device != device or t.dim() != dim or t.shape[0] != count or not t.is_contiguous():
             raise LunaError(LUNA_ERR_INVALID_ARG, f"{name} must be a contiguous int32 tensor on the tensors' device")
-    return (ctypes.c_int64 * 5)(pool.count, pool.rows, table.shape[1], table.data_ptr(), lens.data_ptr()), rows
+    v[2], v[3], v[4] = table.shape[1], table.data_ptr(), lens.data_ptr()
+    return array("q", v)
 
 
 def paged_append(K, V, k_pages, v_pages, table, lens, Q=None, inv_freq=None, interleaved: bool = False, offsets=None,
@@ -972,7 +1001,7 @@ def paged_append(K, V, k_pages, v_pages, table, lens, Q=None, inv_freq=None, int
     seqs = _Seqs(K, offsets, new_lens, "K")
     Hk, d = K.shape[1], K.shape[-1]
     H = Hk if Q is None else Q.shape[1]
-    pages, prows = _paged(seqs, k_pages, v_pages, table, lens, Hk, d)
+    pages = _paged(seqs, k_pages, v_pages, table, lens, Hk, d)
     if Q is None:
         if q_out is not None:
             raise LunaError(LUNA_ERR_INVALID_ARG, "q_out goes with Q")
@@ -985,10 +1014,11 @@ def paged_append(K, V, k_pages, v_pages, table, lens, Q=None, inv_freq=None, int
         if inv_freq.dim() != 1:
             raise LunaError(LUNA_ERR_INVALID_ARG, "inv_freq must be [rot / 2]")
         fp, rot = _f32_ptr(inv_freq, (inv_freq.shape[0],), seqs.device, "inv_freq"), 2 * inv_freq.shape[0]
-    at, ap = ctypes.addressof(rows), ctypes.addressof(prows)
+    at, pp = rows.buffer_info()[0], pages.buffer_info()[0]
+    ap = pp + 40
     with _on_device(seqs.device):
-        _check(lib.luna_paged_append(at, at + 32, None if Q is None else at + 64, _dt(K), ctypes.addressof(seqs.c),
-                                     ctypes.addressof(pages), H, Hk, d, rot, fp, int(interleaved), ap, ap + 32,
+        _check(lib.luna_paged_append(at, at + 32, None if Q is None else at + 64, _seq_dt(seqs, K), seqs.at,
+                                     pp, H, Hk, d, rot, fp, int(interleaved), ap, ap + 32,
                                      None if Q is None else at + 96, _seq_torch.stream(seqs.device)))
     return q_out
 
@@ -1003,15 +1033,18 @@ def paged_attn(Q, k_pages, v_pages, table, lens, scale: float | None = None, off
     seqs = _Seqs(Q, offsets, q_lens, "Q")
     H, d = Q.shape[1], Q.shape[-1]
     Hk = k_pages.shape[1] if k_pages.dim() == 4 else 1
-    pages, prows = _paged(seqs, k_pages, v_pages, table, lens, Hk, d)
+    pages = _paged(seqs, k_pages, v_pages, table, lens, Hk, d)
     out = _new(Q, q_lens) if out is None else out
     rows = _seq_rows(seqs, (Q, out), (H, H), (d, d), ("Q", "out"))
-    lse = _seq_torch.empty(seqs.numbers(H), dtype=_seq_torch.f32, device=seqs.device) if lse is None else lse
-    lp = _f32_ptr(lse, seqs.numbers(H), seqs.device, "lse")
-    dt, at, ap, pp = _dt(Q), ctypes.addressof(rows), ctypes.addressof(prows), ctypes.addressof(pages)
+    if lse is None:
+        lse = _seq_torch.empty(seqs.numbers(H), dtype=_seq_torch.f32, device=seqs.device)
+        lp = lse.data_ptr()
+    else:
+        lp = _f32_ptr(lse, seqs.numbers(H), seqs.device, "lse")
+    dt, at, pp = _seq_dt(seqs, Q), rows.buffer_info()[0], pages.buffer_info()[0]
+    ap = pp + 40
     with _on_device(seqs.device):
-        nb = int(lib.luna_paged_workspace_bytes(dt, ctypes.addressof(seqs.c), pp, H, Hk, d))
-        ws, wsp, wsn = (None, None, 0) if nb == 0 else _workspace(nb, seqs.device)
-        _check(lib.luna_paged_fwd(at, ap, ap + 32, dt, ctypes.addressof(seqs.c), pp, H, Hk, d, d ** -0.5 if scale is None else scale,
+        ws, wsp, wsn = _seq_bytes(int(lib.luna_paged_workspace_bytes(dt, seqs.at, pp, H, Hk, d)), seqs.device)
+        _check(lib.luna_paged_fwd(at, ap, ap + 32, dt, seqs.at, pp, H, Hk, d, d ** -0.5 if scale is None else scale,
                                   at + 32, lp, wsp, wsn, _seq_torch.stream(seqs.device)))
     return out, lse
