@@ -85,6 +85,52 @@ def test_backward(layout, lens, H, Hk, D, d, dtype, state):
     check_backward(Q, K, V, dO, g, beta, grads, layout, lens, D ** -0.5)
 
 
+@pytest.mark.parametrize("Hk,D,d,dtype,state", [(32, 128, 128, "bf16", True), (16, 64, 64, "bf16", False), (32, 32, 128, "bf16", False),
+                                                (16, 128, 128, "f32", True), (32, 32, 128, "f32", False)])
+def test_many_heads(Hk, D, d, dtype, state):
+    """Heads and sequences that fill the device, where workgroups take 64 columns of d instead of 32."""
+    say(f"delta, many heads: Hk={Hk} D={D} d={d} {dtype} state={state}")
+    lens, H = [70, 1, 130, 64, 65], 32
+    Q, K, V, dO, g, beta, gen = make("packed", lens, H, Hk, D, d, of(dtype), seed=12)
+    S = torch.randn((len(lens), H, D, d), generator=gen, device=device()) if state else None
+    S0 = S.clone() if state else None
+    out = luna.delta_attn(Q, K, V, g, beta, S=S, scale=D ** -0.5, **kw("packed", lens))
+    check_forward(Q, K, V, g, beta, out, "packed", lens, D ** -0.5, S0, S)
+    grads = luna.delta_attn_bwd(Q, K, V, dO, g, beta, scale=D ** -0.5, **kw("packed", lens))
+    check_backward(Q, K, V, dO, g, beta, grads, "packed", lens, D ** -0.5)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_what_is_not_finite_with_many_heads(bad):
+    """The forward call's rules for 64 columns a workgroup: a value's column, a key's and a gate's heads, each from its token on."""
+    lens, H, D, d = [100, 140, 30], 32, 64, 128
+    Q, K, V, _, g, beta, gen = make("packed", lens, H, H, D, d, torch.bfloat16, seed=13)
+    S = torch.randn((len(lens), H, D, d), generator=gen, device=device())
+    want, WS = luna.delta_attn(Q, K, V, g, beta, S=(S0 := S.clone()), offsets=packed_offsets(lens)), S0
+    V[40, 3, 77], K[100 + 90, 5, 9], g[7, 100 + 20], Q[70, 9, 2] = bad, bad, math.nan, bad
+    out = luna.delta_attn(Q, K, V, g, beta, S=S, offsets=packed_offsets(lens))
+    lost = torch.zeros(out.shape, dtype=torch.bool, device=device())
+    lost[40:100, 3, 77] = lost[190:240, 5] = lost[120:240, 7] = True
+    lost[70, 9] = True
+    assert torch.isnan(out.float()[lost & (torch.arange(out.shape[0], device=device()) != 70)[:, None, None]]).all()
+    assert not torch.isfinite(out[70, 9].float()).any() and torch.equal(out[~lost], want[~lost])
+    gone = torch.zeros(S.shape, dtype=torch.bool, device=device())
+    gone[0, 3, :, 77] = gone[1, 5] = gone[1, 7] = True
+    assert torch.isnan(S[gone]).all() and torch.equal(S[~gone], WS[~gone])
+
+
+def test_more_sequences_than_lanes():
+    gen = torch.Generator(device=device()).manual_seed(14)
+    lens = torch.randint(0, 90, (70,), generator=gen, device=device()).tolist()
+    lens[33] = 200
+    for dtype in (torch.bfloat16, torch.float32):
+        Q, K, V, dO, g, beta, _ = make("packed", lens, 2, 1, 32, 64, dtype, seed=15)
+        out = luna.delta_attn(Q, K, V, g, beta, offsets=packed_offsets(lens))
+        check_forward(Q, K, V, g, beta, out, "packed", lens, 1.0)
+        grads = luna.delta_attn_bwd(Q, K, V, dO, g, beta, offsets=packed_offsets(lens))
+        check_backward(Q, K, V, dO, g, beta, grads, "packed", lens, 1.0)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_padded_batch_and_packed_gap(dtype):
     """Unused rows hold NaN, in the gates too: they are not read, and what is written keeps what it held there."""
