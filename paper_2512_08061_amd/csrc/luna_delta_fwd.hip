@@ -51,24 +51,6 @@ struct FwdLds {
   int key[2], gate;   // the first row with a key, or gate, that is not finite
 };
 
-// LDS by byte addresses: what differs between lanes is worked out once, the rest lies in the instructions' offsets.
-typedef __attribute__((address_space(3))) char* LdsPtr;
-__device__ __forceinline__ unsigned lds_address(const void* p) {
-  return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
-}
-__device__ __forceinline__ void lds8(Frag<__bf16>& f, unsigned at) {
-  f.v = *(__attribute__((address_space(3))) const bf16x8*)(uintptr_t)at;
-}
-__device__ __forceinline__ void lds8_store(unsigned at, const Frag<__bf16>& f) { *(__attribute__((address_space(3))) bf16x8*)(uintptr_t)at = f.v; }
-__device__ __forceinline__ f32x4 lds4(unsigned at) { return *(__attribute__((address_space(3))) const f32x4*)(uintptr_t)at; }
-// eight rows of a column, four and four `step` bytes apart
-__device__ __forceinline__ void lds_tr(Frag<__bf16>& f, unsigned at, int step) {
-  typedef __attribute__((ext_vector_type(4))) short i16x4;
-  const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(uintptr_t)at);
-  const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(uintptr_t)(at + step));
-  f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
 // Four numbers in parts.
 template <int NP>
 struct Parts4 {

@@ -25,16 +25,21 @@ constexpr int kGradWaves = DK == 128 ? 8 : 4;
 
 template <typename T, int DK, int DV, int NP>
 struct GradLds {
-  static constexpr int PAD = 16 / (int)sizeof(T), PK = DK + PAD, PT = C + PAD, W = kGradWaves<DK>;
+  static constexpr int PAD = 16 / (int)sizeof(T), PK = DK + PAD, PA = C + PAD, PT = sizeof(T) == 2 ? C : PA, W = kGradWaves<DK>;
   T k[C][PK], q[C][PK];
   union {
     struct {
       T u[NP][DV][PT], r[NP][DV][PT];  // U and dR, transposed
     };
     struct {
-      T ap[NP][C][PT], am[NP][C][PT];  // scale dP Gamma and dM Gamma
+      T ap[NP][C][PA], am[NP][C][PA];  // scale dP Gamma and dM Gamma
     };
   };
+  // Place of a column's token in u and r: in bf16 the 16-byte pieces are swapped by the row's number, so that the two pieces of eight
+  // rows that half a wave of transposing reads meets lie in different banks (padded rows: 40% of the LDS's cycles were conflicts).
+  static __device__ __forceinline__ int at(int row, int col) {
+    return sizeof(T) == 2 ? row * PT + ((col / 8 ^ (4 * (row / 2 % 2) + 2 * (row / 8 % 2))) * 8) + col % 8 : row * PT + col;
+  }
   float gates[kDeltaGateRows][C];
   union {
     float beta[4 * W][C];  // shares of dbeta
@@ -44,6 +49,25 @@ struct GradLds {
     };
   };
   float state[W];               // shares of <dS', S>
+};
+
+// A tile of 16 tokens of U or dR as an operand over the columns 32 s + 8 g .. + 7 of d.
+template <typename Lds, typename T, int NP, int DV>
+struct GradTile {
+  unsigned at;  // this lane's place in tile `it` of u, or of r
+  __device__ __forceinline__ GradTile(const T* x, int it, int lane) {
+    const int g = lane / 16, c = lane % 16;
+    at = lds_address(x) + (sizeof(T) == 2 ? Lds::at(8 * g + c / 4, 16 * it + 4 * (c % 4)) : Lds::at(8 * g, 16 * it + c)) * (int)sizeof(T);
+  }
+  __device__ __forceinline__ void read(DeltaOp<T, NP>& f, int s) const {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int k = 0; k < NP; ++k) lds_tr(f.p[k], at + (k * DV + 32 * s) * Lds::PT * 2, 4 * Lds::PT * 2);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f.x.v[e] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(at + (32 * s + e) * Lds::PT * 4);
+    }
+  }
 };
 
 // sum over the 16 lanes of a group
@@ -56,7 +80,7 @@ __device__ __forceinline__ float lanes_sum(float x) {
 template <typename T, int DK, int DV, int NP>
 __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(DeltaArgs a) {
   using Lds = GradLds<T, DK, DV, NP>;
-  constexpr int W = Lds::W, THREADS = 64 * W, PK = Lds::PK, PT = Lds::PT, esz = (int)sizeof(T), FS = DK / 32, VS = DV / 32;
+  constexpr int W = Lds::W, THREADS = 64 * W, PK = Lds::PK, PA = Lds::PA, PT = Lds::PT, esz = (int)sizeof(T), FS = DK / 32, VS = DV / 32;
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int tid0 = threadIdx.x, wave = wave_id();
@@ -93,7 +117,12 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     x.store(&l.k[0][0]);
     y.store(&l.q[0][0]);
   }
+  // The sums over the value heads, in registers or, where these do not suffice for them beside the rest, from head to head in
+  // the place of the first one's states, which have been read by then.
+  constexpr bool PARK = DK == 128 && DV == 128;
+  static_assert(!PARK || DV * DK >= 2 * C * DK, "room for both");
   f32x4 dq[KT], dk[KT];
+  const Buf parked = buffer(a.before + ((int64_t)slot * a.H + hk * group) * DV * DK, PARK ? 2 * KT * THREADS * 16 : 0);
 #pragma unroll
   for (int i = 0; i < KT; ++i) dq[i] = zero4(), dk[i] = zero4();
 
@@ -110,15 +139,13 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     const Buf before = buffer(a.before + at * DV * DK, DV * DK * 4), after = buffer(a.after + at * DV * DK, DV * DK * 4);
     const int state = (feat + c + 8 * g * DK) * 4;
     float sx[2][8], sy[2][8];
-    Frag<T> of[2][KT];
+    Frag<T> of[2];
     const auto load_states = [&](int s) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         sx[s % 2][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(before, state, (32 * s + e) * DK * 4, 0));
         sy[s % 2][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(after, state, (32 * s + e) * DK * 4, 0));
       }
-#pragma unroll
-      for (int it = 0; it < KT; ++it) load_do(of[s % 2][it], it, s);
     };
     __syncthreads();  // the head before is no longer read
 #pragma unroll
@@ -134,12 +161,13 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
         const int col = tid / 16 + n * (THREADS / 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum[j] = fmaf(ev[n][j], xv[n][j], sum[j]);
-        store_parts4<NP>(&l.u[0][col][i4], DV * PT, beta[0] * ev[n][0], beta[1] * ev[n][1], beta[2] * ev[n][2], beta[3] * ev[n][3]);
-        store_parts4<NP>(&l.r[0][col][i4], DV * PT, beta[0] * xv[n][0], beta[1] * xv[n][1], beta[2] * xv[n][2], beta[3] * xv[n][3]);
+        store_parts4<NP>(&l.u[0][0][0] + Lds::at(col, i4), DV * PT, beta[0] * ev[n][0], beta[1] * ev[n][1], beta[2] * ev[n][2], beta[3] * ev[n][3]);
+        store_parts4<NP>(&l.r[0][0][0] + Lds::at(col, i4), DV * PT, beta[0] * xv[n][0], beta[1] * xv[n][1], beta[2] * xv[n][2], beta[3] * xv[n][3]);
       }
       *reinterpret_cast<f32x4*>(&l.beta[tid / 16][i4]) = sum;
     }
     load_states(0);
+    load_do(of[0], 0, 0);
     __syncthreads();
     float dbeta = 0.0f;
     if (wave == 0)
@@ -156,7 +184,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
         for (int j = 0; j < 4; ++j) {
           x[j] = 0.0f;
 #pragma unroll
-          for (int p = delta_parts<T>(NP) - 1; p >= 0; --p) x[j] += (float)l.r[p][col + j][i];
+          for (int p = delta_parts<T>(NP) - 1; p >= 0; --p) x[j] += (float)(&l.r[p][0][0])[Lds::at(col + j, i)];
         }
         buf_store4<T>(b, i < m ? (i * (int)a.dv.row + col) * esz : kPastEnd, x[0], x[1], x[2], x[3]);
       }
@@ -169,13 +197,11 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     {
       const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
       DeltaOp<T, NP> rf[2], uf[2];
+      const GradTile<Lds, T, NP, DV> r0(&l.r[0][0][0], 0, lane), r1(&l.r[0][0][0], 1, lane), r2(&l.r[0][0][0], 2, lane), r3(&l.r[0][0][0], 3, lane);
+      const GradTile<Lds, T, NP, DV> u0(&l.u[0][0][0], 0, lane), u1(&l.u[0][0][0], 1, lane), u2(&l.u[0][0][0], 2, lane), u3(&l.u[0][0][0], 3, lane);
       const auto read = [&](int n) {  // of tile n % KT and columns 32 (n / KT) ..
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int row = 32 * (n / KT) + 8 * g + 4 * half;
-          load_op_tr4(rf[n % 2], 4 * half, lane, DV * PT, [&](int kk, int col) { return &l.r[0][row + kk][16 * (n % KT) + col]; });
-          load_op_tr4(uf[n % 2], 4 * half, lane, DV * PT, [&](int kk, int col) { return &l.u[0][row + kk][16 * (n % KT) + col]; });
-        }
+        (n % KT == 0 ? r0 : n % KT == 1 ? r1 : n % KT == 2 ? r2 : r3).read(rf[n % 2], n / KT);
+        (n % KT == 0 ? u0 : n % KT == 1 ? u1 : n % KT == 2 ? u2 : u3).read(uf[n % 2], n / KT);
       };
       read(0);
 #pragma unroll
@@ -189,9 +215,12 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
 #pragma unroll
         for (int it = 0; it < KT; ++it) {
           const int n = s * KT + it;
-          if (n + 1 < VS * KT) read(n + 1);
+          if (n + 1 < VS * KT) {
+            read(n + 1);
+            load_do(of[(n + 1) % 2], (n + 1) % KT, (n + 1) / KT);
+          }
           __builtin_amdgcn_sched_barrier(0);
-          mma(zq[it], sf, of[s % 2][it]);
+          mma(zq[it], sf, of[n % 2]);
           mma(zr[it], sf, rf[n % 2]);
           mma(zk[it], df, uf[n % 2]);
         }
@@ -211,13 +240,10 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
       f32x4 p = zero4(), r = zero4(), kk = zero4(), qk = zero4();
       Frag<T> oi[VS];
       DeltaOp<T, NP> rf[2], uf[2];
+      const GradTile<Lds, T, NP, DV> ri(&l.r[0][0][0], it, lane), uj(&l.u[0][0][0], jt, lane);
       const auto read = [&](int s) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int row = 32 * s + 8 * g + 4 * half;
-          load_op_tr4(rf[s % 2], 4 * half, lane, DV * PT, [&](int kk2, int col) { return &l.r[0][row + kk2][16 * it + col]; });
-          load_op_tr4(uf[s % 2], 4 * half, lane, DV * PT, [&](int kk2, int col) { return &l.u[0][row + kk2][16 * jt + col]; });
-        }
+        ri.read(rf[s % 2], s);
+        uj.read(uf[s % 2], s);
       };
 #pragma unroll
       for (int s = 0; s < VS; ++s) load_do(oi[s], it, s);
@@ -264,18 +290,30 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     for (int n = 0; n < ROUNDS; ++n) {
       if (wave + W * n < 10) {
         const int i = 16 * its[n] + c, j = 16 * jts[n] + 4 * g;
-        store_parts4<NP>(&l.ap[0][i][j], C * PT, ap[n][0], ap[n][1], ap[n][2], ap[n][3]);
-        store_parts4<NP>(&l.am[0][i][j], C * PT, am[n][0], am[n][1], am[n][2], am[n][3]);
+        store_parts4<NP>(&l.ap[0][i][j], C * PA, ap[n][0], ap[n][1], ap[n][2], ap[n][3]);
+        store_parts4<NP>(&l.am[0][i][j], C * PA, am[n][0], am[n][1], am[n][2], am[n][3]);
       }
     }
     if (wave < 2) {  // the blocks beside the diagonal that products of 32 columns meet
       const int i = 32 * wave + c, j = 32 * wave + 16 + 4 * g;
-      store_parts4<NP>(&l.ap[0][i][j], C * PT, 0.0f, 0.0f, 0.0f, 0.0f);
-      store_parts4<NP>(&l.am[0][i][j], C * PT, 0.0f, 0.0f, 0.0f, 0.0f);
+      store_parts4<NP>(&l.ap[0][i][j], C * PA, 0.0f, 0.0f, 0.0f, 0.0f);
+      store_parts4<NP>(&l.am[0][i][j], C * PA, 0.0f, 0.0f, 0.0f, 0.0f);
     }
     __syncthreads();
     {
       const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
+      if constexpr (PARK) {
+#pragma unroll
+        for (int i = 0; i < KT; ++i) dq[i] = zero4(), dk[i] = zero4();
+        if (h > 0) {
+          const int off = anew(tid0) * 16;
+#pragma unroll
+          for (int i = 0; i < KT; ++i) {
+            dq[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(parked, off, i * THREADS * 16, 0));
+            dk[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(parked, off, (KT + i) * THREADS * 16, 0));
+          }
+        }
+      }
 #pragma unroll
       for (int it = 0; it < KT; ++it) {
         const int i = 16 * it + c;
@@ -318,8 +356,8 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
       for (int it = 0; it < KT; ++it) {
         if (it / 2 >= s) {  // over j
           DeltaOp<T, NP> pf, mf;
-          load_op(pf, &l.ap[0][16 * it + c][32 * s + 8 * g], C * PT);
-          load_op(mf, &l.am[0][16 * it + c][32 * s + 8 * g], C * PT);
+          load_op(pf, &l.ap[0][16 * it + c][32 * s + 8 * g], C * PA);
+          load_op(mf, &l.am[0][16 * it + c][32 * s + 8 * g], C * PA);
           mma(dq[it], kf, pf);
           mma(dk[it], kf, mf);
         }
@@ -328,12 +366,32 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
             const int row = 32 * s + 8 * g + 4 * half;
-            load_op_tr4(pf, 4 * half, lane, C * PT, [&](int kk, int col) { return &l.ap[0][row + kk][16 * it + col]; });
-            load_op_tr4(mf, 4 * half, lane, C * PT, [&](int kk, int col) { return &l.am[0][row + kk][16 * it + col]; });
+            load_op_tr4(pf, 4 * half, lane, C * PA, [&](int kk, int col) { return &l.ap[0][row + kk][16 * it + col]; });
+            load_op_tr4(mf, 4 * half, lane, C * PA, [&](int kk, int col) { return &l.am[0][row + kk][16 * it + col]; });
           }
           mma(dk[it], qf, pf);
           mma(dk[it], kf, mf);
         }
+      }
+    }
+    if (PARK && h + 1 < group) {
+      typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+      const int off = anew(tid0) * 16;
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, dq[i]), parked, off, i * THREADS * 16, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, dk[i]), parked, off, (KT + i) * THREADS * 16, 0);
+      }
+    }
+    if (mine && h + 1 == group) {
+      const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
+      const Buf bq = buffer(seq_row(a.dq, sp, packed, hk, t0, esz), (int)(((m - 1) * a.dq.row + DK) * esz));
+      const Buf bk = buffer(seq_row(a.dk, sp, packed, hk, t0, esz), (int)(((m - 1) * a.dk.row + DK) * esz));
+#pragma unroll
+      for (int it = 0; it < KT; ++it) {
+        const int i = 16 * it + c;
+        buf_store4<T>(bq, i < m ? (i * (int)a.dq.row + feat + 4 * g) * esz : kPastEnd, dq[it][0], dq[it][1], dq[it][2], dq[it][3]);
+        buf_store4<T>(bk, i < m ? (i * (int)a.dk.row + feat + 4 * g) * esz : kPastEnd, dk[it][0], dk[it][1], dk[it][2], dk[it][3]);
       }
     }
     __syncthreads();  // the sums are whole
@@ -362,17 +420,6 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
         a.dlog_decay[num] = log_decay > 0.0f ? 0.0f : sum + ends + l.gates[kDeltaMisc][0] * whole;
         a.dbeta[num] = dbeta;
       }
-    }
-  }
-  if (mine) {
-    const int lane = tid0 % kWave, g = lane / 16, c = lane % 16;
-    const Buf bq = buffer(seq_row(a.dq, sp, packed, hk, t0, esz), (int)(((m - 1) * a.dq.row + DK) * esz));
-    const Buf bk = buffer(seq_row(a.dk, sp, packed, hk, t0, esz), (int)(((m - 1) * a.dk.row + DK) * esz));
-#pragma unroll
-    for (int it = 0; it < KT; ++it) {
-      const int i = 16 * it + c;
-      buf_store4<T>(bq, i < m ? (i * (int)a.dq.row + feat + 4 * g) * esz : kPastEnd, dq[it][0], dq[it][1], dq[it][2], dq[it][3]);
-      buf_store4<T>(bk, i < m ? (i * (int)a.dk.row + feat + 4 * g) * esz : kPastEnd, dk[it][0], dk[it][1], dk[it][2], dk[it][3]);
     }
   }
 }
