@@ -70,6 +70,44 @@ __device__ __forceinline__ int delta_first_slot(const SeqSet& s, const SeqPiece&
   return s.offsets ? (int)(p.first / kDeltaChunk) + p.seq : p.seq * (int)((s.rows + kDeltaChunk - 1) / kDeltaChunk);
 }
 
+// x of the lanes of a row of 16, or of a row's last lane, that a DPP control names; zeros where there is none.  (No LDS, unlike a shuffle.)
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float dpp(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROWS, 0xf, ROWS == 0xf));
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double dpp(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, ROWS, 0xf, ROWS == 0xf);
+  const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, ROWS, 0xf, ROWS == 0xf);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Sums over the lanes up to this one.
+template <typename F>
+__device__ __forceinline__ F lane_sums(F x) {
+  x += dpp<0x111>(x);       // a lane before in the row
+  x += dpp<0x112>(x);       // two
+  x += dpp<0x114>(x);       // four
+  x += dpp<0x118>(x);       // eight
+  x += dpp<0x142, 0xa>(x);  // the last lane of the row before, for rows 1 and 3
+  x += dpp<0x143, 0xc>(x);  // lane 31, for rows 2 and 3
+  return x;
+}
+// Sum over the 16 lanes of a row.
+__device__ __forceinline__ float row_sum(float x) {
+  x += dpp<0xb1>(x);   // lane 1, 0, 3, 2 of four
+  x += dpp<0x4e>(x);   // lane 2, 3, 0, 1
+  x += dpp<0x141>(x);  // the other four of eight
+  x += dpp<0x140>(x);  // the other eight
+  return x;
+}
+__device__ __forceinline__ double of_lane(double x, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)u, lane), hi = __builtin_amdgcn_readlane((int)(unsigned)(u >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ float of_lane(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
+
 // An fp32 operand as products of type T take it: itself, or P parts in bf16.
 template <typename T, int P>
 struct DeltaOp;

@@ -290,30 +290,6 @@ struct GateWave {
   }
 };
 
-// x of the lanes of a row, or of a row's last lane, that a DPP control names; zeros where there is none.
-template <int CTRL, int ROWS = 0xf>
-__device__ __forceinline__ double dpp(double x) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, x);
-  const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, ROWS, 0xf, ROWS == 0xf);
-  const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, ROWS, 0xf, ROWS == 0xf);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-// Sums over the lanes up to this one.
-__device__ __forceinline__ double lane_sums(double x) {
-  x += dpp<0x111>(x);       // a lane before in the row of 16
-  x += dpp<0x112>(x);       // two
-  x += dpp<0x114>(x);       // four
-  x += dpp<0x118>(x);       // eight
-  x += dpp<0x142, 0xa>(x);  // the last lane of the row before, for rows 1 and 3
-  x += dpp<0x143, 0xc>(x);  // lane 31, for rows 2 and 3
-  return x;
-}
-__device__ __forceinline__ double of_lane(double x, int lane) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, x);
-  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)u, lane), hi = __builtin_amdgcn_readlane((int)(unsigned)(u >> 32), lane);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-
 template <int DK, int DVW, int NP>
 __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a) {
   using Lds = FwdLds<DK, NP>;

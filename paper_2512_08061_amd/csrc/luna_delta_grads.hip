@@ -70,13 +70,6 @@ struct GradTile {
   }
 };
 
-// sum over the 16 lanes of a group
-__device__ __forceinline__ float lanes_sum(float x) {
-#pragma unroll
-  for (int w = 1; w < 16; w *= 2) x += __shfl_xor(x, w);
-  return x;
-}
-
 template <typename T, int DK, int DV, int NP>
 __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(DeltaArgs a) {
   using Lds = GradLds<T, DK, DV, NP>;
@@ -89,6 +82,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
   if (sp.seq < 0) return;
   const bool packed = a.s.offsets != nullptr, mine = wave < DK / 16;
   const int t0 = sp.index * C, m = min(C, sp.len - t0), feat = mine ? 16 * wave : 0;
+  constexpr bool PARK = DK == 128 && DV == 128;  // (registers are short)
   // What a head needs from memory is asked for before the head before it is done, or as early in it as registers allow: a load
   // takes 2000 cycles and more.
   constexpr int NC = DV * 16 / THREADS, NG = (kDeltaGates + THREADS - 1) / THREADS;
@@ -107,7 +101,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
       ev[n] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(be, off, n * (THREADS / 16) * C * 4, 0));
       xv[n] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(bx, off, n * (THREADS / 16) * C * 4, 0));
     }
-    lv = a.log_decay[seq_num(a.s, sp, a.H, head, t0 + min(lane, m - 1))];
+    lv = a.log_decay[seq_num(a.s, sp, a.H, head, t0 + min(kWave - 1 - lane, m - 1))];
   };
   {
     DecayRows<T, C, DK, PK, THREADS> x, y;
@@ -119,7 +113,6 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
   }
   // The sums over the value heads, in registers or, where these do not suffice for them beside the rest, from head to head in
   // the place of the first one's states, which have been read by then.
-  constexpr bool PARK = DK == 128 && DV == 128;
   static_assert(!PARK || DV * DK >= 2 * C * DK, "room for both");
   f32x4 dq[KT], dk[KT];
   const Buf parked = buffer(a.before + ((int64_t)slot * a.H + hk * group) * DV * DK, PARK ? 2 * KT * THREADS * 16 : 0);
@@ -138,15 +131,16 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     // this wave's features of the states, 32 columns of d at a time, and rows of dO
     const Buf before = buffer(a.before + at * DV * DK, DV * DK * 4), after = buffer(a.after + at * DV * DK, DV * DK * 4);
     const int state = (feat + c + 8 * g * DK) * 4;
-    float sx[2][8], sy[2][8];
+    float sx[8], sy[8];
     Frag<T> of[2];
     const auto load_states = [&](int s) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        sx[s % 2][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(before, state, (32 * s + e) * DK * 4, 0));
-        sy[s % 2][e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(after, state, (32 * s + e) * DK * 4, 0));
+        sx[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(before, state, (32 * s + e) * DK * 4, 0));
+        sy[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(after, state, (32 * s + e) * DK * 4, 0));
       }
     };
+    if (PARK && h > 0) load_head(head);
     __syncthreads();  // the head before is no longer read
 #pragma unroll
     for (int n = 0; n < NG; ++n)
@@ -172,7 +166,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     float dbeta = 0.0f;
     if (wave == 0)
 #pragma unroll
-      for (int w = 0; w < 4 * W; ++w) dbeta += l.beta[w][lane];
+      for (int w = 0; w < 4 * W; ++w) dbeta += l.beta[w][kWave - 1 - lane];
     __syncthreads();  // the shares are no longer read
     {  // dV
       const Buf b = buffer(seq_row(a.dv, sp, packed, head, t0, esz), (int)(((m - 1) * a.dv.row + DV) * esz));
@@ -206,12 +200,12 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
       read(0);
 #pragma unroll
       for (int s = 0; s < VS; ++s) {
-        if (s + 1 < VS) load_states(s + 1);
         DeltaOp<T, NP> sf, df;
-        sf.set(sx[s % 2]);
-        df.set(sy[s % 2]);
+        sf.set(sx);
+        df.set(sy);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) both = fmaf(sx[s % 2][e], sy[s % 2][e], both);
+        for (int e = 0; e < 8; ++e) both = fmaf(sx[e], sy[e], both);
+        if (s + 1 < VS) load_states(s + 1);
 #pragma unroll
         for (int it = 0; it < KT; ++it) {
           const int n = s * KT + it;
@@ -255,6 +249,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
         mma(r, uf[s % 2], rf[s % 2]);
         mma(p, uf[s % 2], oi[s]);
       }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < FS; ++t) {
         Frag<T> kj, ki, qi;
@@ -279,7 +274,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
       }
       const float over = groups_sum(w[0] + w[1] + w[2] + w[3]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = lanes_sum(w[e]);
+      for (int e = 0; e < 4; ++e) w[e] = row_sum(w[e]);
       if (tile < 10) {
         if (g == 0) l.row[jt][i] = over;
         if (c == 0) *reinterpret_cast<f32x4*>(&l.col[it][j0]) = w;
@@ -296,8 +291,9 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     }
     if (wave < 2) {  // the blocks beside the diagonal that products of 32 columns meet
       const int i = 32 * wave + c, j = 32 * wave + 16 + 4 * g;
-      store_parts4<NP>(&l.ap[0][i][j], C * PA, 0.0f, 0.0f, 0.0f, 0.0f);
-      store_parts4<NP>(&l.am[0][i][j], C * PA, 0.0f, 0.0f, 0.0f, 0.0f);
+      const float z = __int_as_float(anew(0));
+      store_parts4<NP>(&l.ap[0][i][j], C * PA, z, z, z, z);
+      store_parts4<NP>(&l.am[0][i][j], C * PA, z, z, z, z);
     }
     __syncthreads();
     {
@@ -338,11 +334,10 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
           l.dots[wave][1][i] = ends;
         }
       }
-#pragma unroll
-      for (int w = 1; w < kWave; w *= 2) both += __shfl_xor(both, w);
+      both = groups_sum(row_sum(both));
       if (mine && lane == 0) l.state[wave] = both;
     }
-    if (h + 1 < group) load_head(head + 1);
+    if (!PARK && h + 1 < group) load_head(head + 1);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
@@ -395,27 +390,25 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
       }
     }
     __syncthreads();  // the sums are whole
-    if (wave == 0) {
+    if (wave == 0) {  // (the last token in lane 0: sums over the later tokens are those up to a lane)
+      const int token = kWave - 1 - anew(tid0) % kWave;
       float sum = 0.0f, ends = 0.0f, whole = 0.0f;
 #pragma unroll
       for (int w = 0; w < DK / 16; ++w) {
-        sum += l.dots[w][0][lane];
-        ends += l.dots[w][1][lane];
+        sum += l.dots[w][0][token];
+        ends += l.dots[w][1][token];
         whole += l.state[w];
       }
 #pragma unroll
       for (int b = 0; b < KT; ++b) {
-        sum += b <= lane / 16 ? l.row[b][lane] : 0.0f;
-        sum -= b >= lane / 16 ? l.col[b][lane] : 0.0f;
+        const float row = l.row[b][token], col = l.col[b][token];  // (not all of them formed)
+        sum += b <= token / 16 ? row : 0.0f;
+        sum -= b >= token / 16 ? col : 0.0f;
       }
-#pragma unroll
-      for (int w = 1; w < kWave; w *= 2) {
-        const float other = __shfl_down(sum, w);
-        sum += lane + w < kWave ? other : 0.0f;
-        ends += __shfl_xor(ends, w);
-      }
-      if (lane < m) {
-        const int64_t num = seq_num(a.s, sp, a.H, head, t0 + lane);
+      sum = lane_sums(sum);
+      ends = of_lane(lane_sums(ends), kWave - 1);
+      if (token < m) {
+        const int64_t num = seq_num(a.s, sp, a.H, head, t0 + token);
         // (above 0 a log decay counts as 0)
         a.dlog_decay[num] = log_decay > 0.0f ? 0.0f : sum + ends + l.gates[kDeltaMisc][0] * whole;
         a.dbeta[num] = dbeta;
