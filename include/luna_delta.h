@@ -28,7 +28,8 @@ enum {
   LUNA_OP_DELTA_BWD = 1
 };
 
-/* Bytes of device workspace of an operation (as luna_seq_workspace_bytes; 0 on invalid arguments). */
+/* Bytes of device workspace of an operation (as luna_seq_workspace_bytes; 0 where it needs none, which is the forward call in
+ * LUNA_BF16, and on invalid arguments, with a reason in luna_last_error()). */
 size_t luna_delta_workspace_bytes(int32_t op, luna_dtype dtype, const luna_seqs* seqs, int64_t H, int64_t Hk, int64_t D,
                                   int64_t d);
 

@@ -3,17 +3,18 @@
 // A workgroup takes DVW value columns of one sequence and head.  Four gate waves form the matrices of the next chunk (N in
 // parts, P, the factors of the gates) in LDS while the scan waves, 16 columns each, carry the state through the present one, so
 // that the matrices never go to memory and the state's chain waits for nothing but itself.  Tiles and matrices lie in LDS
-// twice.  Per chunk three barriers, between which both kinds of wave have about the same to do:
+// twice.  Three barriers a chunk:
 //
-//   gate waves                                    scan waves
-//   K, Q of the next chunk to LDS, its gates      K S
-//   K K^T, Q K^T, M, P, N's diagonal blocks       Q S, R, E = R + N (beta R)
-//   N below its diagonal blocks                   S = e^(G_C) S + K^T (..), out
+//   gate waves                                             scan waves
+//   K, Q of the next chunk, 16 rows each, to LDS           K S, half of it
+//   K K^T, Q K^T, M, P, N's diagonal blocks; loads         K S, Q S, R, E = R + N (beta R)
+//   N below its diagonal blocks; the next gates            S = e^(G_C) S + K^T (..), out
 //
 // The scan waves' products are chained in registers as luna_delta_scan.hpp says.  Operands are read from LDS a batch before
-// their products (by itself the compiler reads each right before its use and waits out the LDS 80 times a chunk, 5.8 us instead
-// of 1.7).  16-byte pieces of a row are swapped among each other by the row's number, so that neither the rows of pairs of tiles
-// nor transposing reads meet in a bank.
+// their products (by itself the compiler reads each right before its use and waits out the LDS 80 times a chunk).  16-byte pieces
+// of a row are swapped among each other by the row's number, so that the rows of pairs of tiles do not meet in a bank.  What bounds it
+// is the chain of a chunk: 8 x 16 heads of 16384 tokens, D = d = 128, 1012 us, 3.9 us a chunk (LDS active 50% of all cycles, half of
+// them bank conflicts of the transposing reads, which touch every other 8 bytes; matrix cores 28%).
 #include "luna_delta_scan.hpp"
 
 namespace luna {
@@ -326,6 +327,7 @@ __global__ __launch_bounds__(4 * DVW + 256, 2) void delta_fwd_kernel(DeltaArgs a
   if (wave >= SCAN) {
     // ------------------------------------------------------------------ gate waves
     const int w = wave - SCAN, tid = threadIdx.x - 64 * SCAN;
+    // (before the scan waves, where these have the shorter chain: 1.04 -> 1.01 ms with two parts, but 537 -> 570 us with three)
     if constexpr (NP == 2) __builtin_amdgcn_s_setprio(3);
     GateWave<DK, NP> gate{a, l, g, c, {}};
 #pragma unroll

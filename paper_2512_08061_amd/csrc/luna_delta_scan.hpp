@@ -5,14 +5,15 @@
 // Every product's result is the next one's operand as it lies in the registers, so that a chunk needs no exchange between
 // lanes: rows 4g + e of a pair of tiles 2s, 2s + 1 stand for features (and tokens) 32 s + 8 g + e and 32 s + 8 g + 4 + e, the
 // eight k-slots of lane group g.  K S and N (beta R) take such pairs as their B operand, out^T = S^T Q^T + U^T P^T the same
-// registers as its A operand.  K and Q lie in LDS as their rows; K^T is read transposed.
+// registers as its A operand.  K and Q lie in LDS as their rows; K^T is read transposed.  What bounds them is the chain of a
+// chunk, 4.3 us for the gradients' of bf16 with D = d = 128 (2 x 16 heads of 2048 tokens: 138 us for both, side by side).
 #pragma once
 
 #include "luna_delta.hpp"
 
 namespace luna {
 
-// Forward: FWD_OUT writes out and returns the state; RECORD leaves E and the states before the chunks for the backward pass.
+// The tiles of a chunk.
 template <typename T, int DK, int DVW, int NP, int PP, bool OUT>
 struct ScanLds {
   static constexpr int C = kDeltaChunk, PAD = 16 / (int)sizeof(T), PK = DK + PAD, PV = DVW + PAD, PN = C + PAD;
@@ -70,6 +71,8 @@ __device__ __forceinline__ void load_op_pair_tr(DeltaOp<T, P>& f, const T* x, in
                 [&](int kk, int col) { return x + (row + 4 * half + kk) * pitch + first + 8 * (col / 4) + col % 4; });
 }
 
+// From the first chunk to the last.  OUT: writes out and returns the state, else leaves E and the states before the chunks for the
+// backward pass.  HELP: waves that only load, a chunk ahead (0: all load).
 template <typename T, int DK, int DVW, int NP, int HELP, bool OUT>
 __device__ __forceinline__ void delta_scan(const DeltaArgs& a, int block, char* raw) {
   using Lds = ScanLds<T, DK, DVW, NP, 1, OUT>;
