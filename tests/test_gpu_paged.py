@@ -430,3 +430,47 @@ def test_same_bits_streams_and_two_graphs():
         eager = luna.paged_attn(*args[2])
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for a, b in zip(outs + [eager], want) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("m", [1, 130])
+def test_a_captured_call_follows_the_lengths(m):
+    """The shares of the keys are worked out on the device: a captured call over caches that grow and shrink between its replays."""
+    room = [4000, 300, 2100]
+    Q, K, V, kp, vp, table, _ = make(m, room, 4, 2, 64, torch.bfloat16, 32, seed=41)
+    lens = i32(room)
+    luna.paged_attn(Q, kp, vp, table, lens)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = luna.paged_attn(Q, kp, vp, table, lens)
+    for klens in ([1, 300, 700], [4000, 0, 2100], [513, 299, 1024], [0, 0, 0], room):
+        lens.copy_(i32(klens))
+        want = luna.paged_attn(Q, kp, vp, table, lens)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        check_forward(Q, K, V, out, lse, "batch", [m] * 3, klens)
+
+
+def test_tiles_on_a_stream_and_in_two_graphs():
+    """The tile kernels with keys in shares: the same bits on another stream and from graphs replayed in turn with eager calls."""
+    klens = ([3000, 50, 700], [900, 2000])
+    args = [(x[0], x[3], x[4], x[5], i32(k)) for x, k in ((make(200, k, 8, 2, 128, torch.bfloat16, 64, seed=42 + len(k)), k) for k in klens)]
+    want = [[t.clone() for t in luna.paged_attn(*a)] for a in args]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = [luna.paged_attn(*a) for a in args]
+    side.synchronize()
+    assert all(torch.equal(x, y) for a, b in zip(got, want) for x, y in zip(a, b))
+    graphs, outs = [], []
+    for a in args:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(luna.paged_attn(*a))
+    for _ in range(3):
+        for graph in graphs:
+            graph.replay()
+        eager = luna.paged_attn(*args[0])
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for a, b in zip(outs + [eager], want + want[:1]) for x, y in zip(a, b))
