@@ -45,8 +45,9 @@ luna_status check_pages(const luna_rows* r, const char* what, luna_dtype dt, con
 
 // bytes of the parts of rows whose keys lie in several shares, or 0 where the tile kernels take the call
 size_t part_bytes(luna_dtype dt, const luna_seqs& s, const luna_pages& p, int64_t H, int64_t Hk, int64_t d) {
-  const int64_t shares = luna::paged_splits(set_of(&s), H, Hk) ? luna::paged_shares(type_of(dt), s.count, p.width * p.rows, Hk)
-                                                               : luna::paged_tile_shares(type_of(dt), set_of(&s), H, Hk, d);
+  const int64_t shares = luna::paged_splits(type_of(dt), set_of(&s), H, Hk, p.width * p.rows)
+                             ? luna::paged_shares(type_of(dt), s.count, p.width * p.rows, Hk, s.rows * (H / Hk))
+                             : luna::paged_tile_shares(type_of(dt), set_of(&s), H, Hk, d);
   if (!shares) return 0;
   return align256((size_t)(shares + s.count) * H * (s.rows < 1 ? 1 : s.rows) * (d + 2) * 4);
 }
@@ -55,10 +56,13 @@ luna_status check_attn(luna_dtype dt, const luna_seqs* seqs, const luna_pages* p
   const luna_status st = check_paged(dt, seqs, pages, H, Hk, d);
   if (st != LUNA_OK) return st;
   const luna::SeqSet qs = set_of(seqs);
+  const int64_t rows = qs.rows * (H / Hk);
   bool fits;
-  if (luna::paged_splits(qs, H, Hk)) {  // (a join takes two rows of a key head or more)
+  if (luna::paged_splits(type_of(dt), qs, H, Hk, pages->width * pages->rows)) {  // (a join takes two rows of a key head or more)
     fits = launchable(qs.count * H * qs.rows, 256) &&
-           launchable((luna::paged_shares(type_of(dt), qs.count, pages->width * pages->rows, Hk) + qs.count) * Hk, 256);
+           launchable((luna::paged_shares(type_of(dt), qs.count, pages->width * pages->rows, Hk, rows) + qs.count) * Hk *
+                          luna::paged_row_groups(type_of(dt), rows),
+                      256);
   } else {
     fits = launchable(luna::seq_slots(qs, luna::softmax_tile(type_of(dt), d)) * H, 256);
   }
@@ -144,8 +148,8 @@ luna_status luna_paged_fwd(const luna_rows* Q, const luna_rows* k_pages, const l
   a.lse = lse;
   a.parts = static_cast<float*>(ws);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  return hip_status(luna::paged_splits(a.qs, H, Hk) ? luna::launch_paged_split(type_of(dtype), a, s)
-                                                          : luna::launch_paged_tiles(type_of(dtype), a, s),
+  return hip_status(luna::paged_splits(type_of(dtype), a.qs, H, Hk, a.ks.rows) ? luna::launch_paged_split(type_of(dtype), a, s)
+                                                                                   : luna::launch_paged_tiles(type_of(dtype), a, s),
                     "paged attention launch");
 }
 

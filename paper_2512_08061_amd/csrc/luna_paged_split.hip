@@ -3,7 +3,7 @@
 // 69.5 us, 3.7 TB/s, and 7 to join), and for few tokens the chain of dependent loads (one cache of 3001: 10.3 and 5.6 us).
 //
 // The rows of a key head, m tokens of its H / Hk heads each, are one operand of up to RT tiles of 16, so that the cache is
-// read once for the whole group.  The keys of all sequences, in units of paged_unit(), are one line that is cut in equal shares,
+// read once for the whole group (in fp32 once for 32 rows, a workgroup each).  The keys of all sequences, in units of paged_unit(), are one line that is cut in equal shares,
 // a workgroup each (lengths are on the device: every workgroup adds them up by itself), so that long and short sequences
 // load the device alike.  A share may hold the end of one sequence, several, and the beginning of another; within each
 // its four waves take the units in turn, each with a running maximum, sum and unnormalised output of its own, which are joined
@@ -29,18 +29,18 @@ struct PagedLds {
 };
 
 template <typename T, int DH, int RT>
-__global__ __launch_bounds__(256) void paged_split_kernel(SoftmaxArgs a, int shares) {
+__global__ __launch_bounds__(256) void paged_split_kernel(SoftmaxArgs a, int shares, int row_groups) {
   using Lds = PagedLds<T, DH>;
   constexpr int KB = Lds::KB, P = Lds::P, KT = KB / 16, CT = DH / 16, DT = DH / 32, esz = (int)sizeof(T), E = 16 / esz;
   constexpr int PER = DH / E, VL = KB * PER / kWave;  // 16-byte pieces of a row, and of a unit's values per lane
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int lane = threadIdx.x % kWave, wave = wave_id(), g = lane / 16, c = lane % 16;
-  const int hk = blockIdx.x % a.Hk, number = blockIdx.x / a.Hk;
+  const int hk = blockIdx.x % a.Hk, row0 = blockIdx.x / a.Hk % row_groups * (16 * RT), number = blockIdx.x / a.Hk / row_groups;
   const int64_t all = units_before(a.ks, (int)a.ks.count, KB, l.scan), per = paged_per(all, shares, kPagedLeast);
   int64_t first;  // units before sequence b
   int b, share, stop = (int)a.ks.count;
-  if (per > kPagedLeast || gridDim.x == (unsigned)(shares * a.Hk)) {  // a share
+  if (per > kPagedLeast || gridDim.x == (unsigned)(shares * a.Hk * row_groups)) {  // a share
     share = number;
     if (share >= shares || share * per >= all) return;
     b = sequence_at(a.ks, share * per, KB, &first);
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256) void paged_split_kernel(SoftmaxArgs a, int sha
     int last[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const int r = 16 * rt + c, t = r / group;
+      const int r = row0 + 16 * rt + c, t = r / group;
       const bool in = r < rows && t < sq.len;
       last[rt] = in ? t + shift : -1;
       const T* q = reinterpret_cast<const T*>(a.q.data) + (in ? b * a.q.seq + (hk * group + r % group) * a.q.head + t * a.q.row : 0);
@@ -84,7 +84,8 @@ __global__ __launch_bounds__(256) void paged_split_kernel(SoftmaxArgs a, int sha
 #pragma unroll
       for (int i = 0; i < CT; ++i) o[rt][i] = zero4();
     }
-    for (int u = u0 + wave; u < u1; u += 4) {
+    const int seen = min(u1, ((min(row0 + 16 * RT, rows) - 1) / group + shift) / KB + 1);  // (the units that the last of the rows sees)
+    for (int u = u0 + wave; u < seen; u += 4) {
       const int k0 = u * KB;
       const KeyPages<KT> pages = key_pages<KT>(a, b, k0, sk.len);
       Frag<T> kf[KT][DT];
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(256) void paged_split_kernel(SoftmaxArgs a, int sha
       __syncthreads();
       constexpr int LANES = DH < kWave ? DH : kWave;  // a row's threads
       for (int r0 = 0; r0 < 16; r0 += 256 / LANES) {
-        const int r = r0 + (int)threadIdx.x / LANES, x = threadIdx.x % LANES, row = 16 * rt + r;
+        const int r = r0 + (int)threadIdx.x / LANES, x = threadIdx.x % LANES, row = row0 + 16 * rt + r;
         const float most = fmaxf(fmaxf(l.top[0][r], l.top[1][r]), fmaxf(l.top[2][r], l.top[3][r]));
         const float base = most == -__builtin_inff() ? 0.0f : most;
         float f[4], y[DH / LANES], total = 0.0f;
@@ -285,8 +286,9 @@ hipError_t launch_rows(const SoftmaxArgs& a, int shares, hipStream_t s) {
   if (e != hipSuccess) return e;
   // Of a short line a sequence of a share each, as long as these run side by side: caches of 11, 10, 510 and 19 tokens, d = 128, 15.5
   // instead of 27.3 us; eight of up to 3371, 12 heads, fp32, 21 and 42; but 200 of 30 tokens, four key heads, 44 and 35.
-  const int64_t groups = (shares + (a.ks.count * a.Hk <= 512 ? a.ks.count : 0)) * a.Hk;
-  hipLaunchKernelGGL((paged_split_kernel<T, DH, RT>), dim3((unsigned)groups), dim3(256), bytes, s, a, shares);
+  const int row_groups = (int)paged_row_groups(sizeof(T) == 2 ? Dt::BF16 : Dt::F32, a.qs.rows * (a.H / a.Hk));
+  const int64_t groups = (shares + (a.ks.count * a.Hk * row_groups <= 512 ? a.ks.count : 0)) * a.Hk * row_groups;
+  hipLaunchKernelGGL((paged_split_kernel<T, DH, RT>), dim3((unsigned)groups), dim3(256), bytes, s, a, shares, row_groups);
   return hipGetLastError();
 }
 
@@ -301,10 +303,11 @@ hipError_t launch_join(const SoftmaxArgs& a, int rows, int shares, int unit, int
 template <typename T, int DH>
 hipError_t launch_width(const SoftmaxArgs& a, hipStream_t s) {
   const int rows = (int)a.qs.rows * (a.H / a.Hk);
-  const int shares = (int)paged_shares(sizeof(T) == 2 ? Dt::BF16 : Dt::F32, a.ks.count, a.ks.rows, a.Hk);
-  const hipError_t e = rows <= 16   ? launch_rows<T, DH, 1>(a, shares, s)
-                       : rows <= 32 ? launch_rows<T, DH, 2>(a, shares, s)
-                                    : launch_rows<T, DH, 4>(a, shares, s);
+  const int shares = (int)paged_shares(sizeof(T) == 2 ? Dt::BF16 : Dt::F32, a.ks.count, a.ks.rows, a.Hk, rows);
+  hipError_t e;
+  if (rows <= 16) e = launch_rows<T, DH, 1>(a, shares, s);
+  else if (rows <= 32 || sizeof(T) == 4) e = launch_rows<T, DH, 2>(a, shares, s);
+  else if constexpr (sizeof(T) == 2) e = launch_rows<T, DH, 4>(a, shares, s);
   return e != hipSuccess ? e : launch_join<T, DH>(a, rows, shares, PagedLds<T, DH>::KB, kPagedLeast, 1, s);
 }
 
@@ -315,9 +318,9 @@ hipError_t launch_split(const SoftmaxArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int64_t paged_shares(Dt dt, int64_t count, int64_t room, int64_t Hk) {
+int64_t paged_shares(Dt dt, int64_t count, int64_t room, int64_t Hk, int64_t rows) {
   const int64_t unit = paged_unit(dt), units = count * ((room + unit - 1) / unit);
-  const int64_t most = (512 + Hk - 1) / Hk, full = (units + 3) / 4;
+  const int64_t sets = Hk * paged_row_groups(dt, rows), most = (512 + sets - 1) / sets, full = (units + 3) / 4;
   return full < 1 ? 1 : full < most ? full : most;
 }
 

@@ -300,14 +300,29 @@ inline bool softmax_splits(const SeqSet& qs, const SeqSet& ks, int64_t H, int64_
 }
 hipError_t launch_softmax_split(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 hipError_t launch_softmax_bwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
-// Over pages: the tile kernels, and the kernel for few rows (luna_paged_split.hip) of a key head.
+// Over pages: the tile kernels, and the kernel for few rows of a key head (luna_paged_split.hip).
 hipError_t launch_paged_tiles(Dt dt, const SoftmaxArgs& a, hipStream_t s);
-inline bool paged_splits(const SeqSet& qs, int64_t H, int64_t Hk) { return !qs.offsets && qs.rows * (H / Hk) <= kSplitRows; }
+// Workgroups of that kernel that share a key head's rows: in fp32 32 rows each (64 spilled, and one wave's products were the whole time
+// of a short call: 2 tokens of 32 heads on one, 3 keys, d = 128, 44.0 and 23.9 us).
+inline int64_t paged_row_groups(Dt dt, int64_t rows) { return dt == Dt::BF16 || rows < 1 ? 1 : (rows + 31) / 32; }
+// In fp32 it takes more rows as well, where the room for keys is long beside the new tokens (else shares and their join cost more than
+// the causal tiles: 90 tokens of 100 and 200 keys, 30.9 and 18.3 us) and the tiles of 64 rows of a head are too few for the device or
+// at least half empty.  d = 128, us, tiles first: 70 tokens of caches of 4096 and 1999, 8 heads, 465 and 85; 64 tokens of 16 caches of
+// 1500, 16 heads (256 tiles), 490 and 241; d = 64, 17 tokens of 12 caches of up to 6175, 32 heads on 2, 427 and 94.  With 512 full
+// tiles of long keys the tiles lead: 1000 tokens of a cache of 8000, 32 heads on 8, 1308 and 1760.
+inline bool paged_splits(Dt dt, const SeqSet& qs, int64_t H, int64_t Hk, int64_t room) {
+  if (qs.offsets) return false;
+  const int64_t rows = qs.rows * (H / Hk);
+  if (rows <= kSplitRows) return true;
+  if (dt == Dt::BF16 || room / 4 < qs.rows) return false;
+  const int64_t tiles = qs.count * H * ((qs.rows + 63) / 64);
+  return tiles < 512 || qs.count * Hk * paged_row_groups(dt, rows) <= tiles;  // (32 rows and 64)
+}
 // Tiles (bf16 with d = 64 and 128) whose keys are cut in shares as well: calls of so few tiles that the longest sequence alone would keep
 // some of the device busy to the end.  Shares of the keys, in units of kPagedTileUnit; 0: no cut.
 constexpr int kPagedTileUnit = 512;
 inline int paged_tile_shares(Dt dt, const SeqSet& qs, int64_t H, int64_t Hk, int64_t d) {
-  if (dt != Dt::BF16 || d < 64 || qs.offsets || paged_splits(qs, H, Hk)) return 0;
+  if (dt != Dt::BF16 || d < 64 || qs.offsets || paged_splits(dt, qs, H, Hk, 0)) return 0;
   const int64_t tiles = (qs.rows + 127) / 128;
   return qs.count * tiles * H > 512 ? 0 : (int)(512 / (tiles * H));
 }
@@ -315,7 +330,7 @@ hipError_t launch_paged_tile_join(const SoftmaxArgs& a, int shares, hipStream_t 
 // Keys of a unit of work of that kernel, which a wave takes at a time, and the workgroups that share the units of a key
 // head (room: of the sequences' rows of the table).
 constexpr int paged_unit(Dt dt) { return dt == Dt::BF16 ? 64 : 32; }
-int64_t paged_shares(Dt dt, int64_t count, int64_t room, int64_t Hk);
+int64_t paged_shares(Dt dt, int64_t count, int64_t room, int64_t Hk, int64_t rows);
 hipError_t launch_paged_split(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 
 // The line of all sequences' units in equal shares: units of a share; the units u0 .. u1 - 1 of a sequence with `before` units

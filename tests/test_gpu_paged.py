@@ -111,6 +111,37 @@ def test_tiles_of_long_and_short_caches(m, klens, H, Hk, d):
     check_forward(Q, K, V, out, lse, "batch", [m] * len(klens), klens)
 
 
+@pytest.mark.parametrize("m,klens,H,Hk,d", [
+    (2, [3], 32, 1, 128), (17, [700, 0, 5, 3001, 16], 32, 2, 64), (70, [2000, 69, 1], 8, 8, 128), (33, [1000, 33, 34], 6, 2, 32),
+    (130, [1500], 4, 1, 128), (17, [300] * 30, 32, 2, 64), (3, [100, 40], 33, 1, 32), (65, [300] * 70, 8, 8, 32)])
+def test_many_rows_in_fp32(m, klens, H, Hk, d):
+    """Rows of a key head in groups of 32, the last of them not full, and (the last case) more tiles than that pays for."""
+    say(f"paged rows m={m} {klens[:5]} H={H} Hk={Hk} d={d}")
+    Q, K, V, kp, vp, table, _ = make(m, klens, H, Hk, d, torch.float32, 32, seed=51)
+    out, lse = luna.paged_attn(Q, kp, vp, table, i32(klens))
+    check_forward(Q, K, V, out, lse, "batch", [m] * len(klens), klens)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_values_behind_some_rows_in_fp32(bad):
+    """A value that is not finite at a token which only the last rows see (m = 40: in another group of rows than the first)."""
+    m, n, H, d = 40, 700, 4, 64
+    Q, K, V, kp, vp, table, _ = make(m, [n], H, 1, d, torch.float32, 32, seed=52)
+    want, want_lse = luna.paged_attn(Q, kp, vp, table, i32([n]))
+    at = n - 7  # rows m - 7 and on
+    vp[int(table[0, at // 32]), 0, at % 32, 3] = bad
+    out, lse = luna.paged_attn(Q, kp, vp, table, i32([n]))
+    keep = torch.arange(d, device=device()) != 3
+    assert torch.equal(lse, want_lse)
+    # both ways of forming a row: scores off by d + 4 steps of their terms' sum, weights by twice that, an exponential's 4 steps and
+    # the 2 n of sums; a row by this share of the largest value, and two rows by twice as much
+    terms = (Q[0].double().abs() @ K[0, 0, :n].double().abs().T).max().item() / math.sqrt(d)
+    bound = 2 * (2 * (d + 4) * terms + 4 + 2 * n) * 2.0 ** -24 * V[0, 0, :n].abs().max().item()
+    assert_within(out[:, :, :m - 7], want[:, :, :m - 7], bound, "rows before")
+    assert not torch.isfinite(out[:, :, m - 7:, 3]).any()
+    assert torch.isfinite(out[..., keep]).all()
+
+
 def test_tiles_of_many_sequences():
     gen = torch.Generator(device=device()).manual_seed(32)
     klens = torch.randint(0, 1500, (200,), generator=gen, device=device()).tolist()
