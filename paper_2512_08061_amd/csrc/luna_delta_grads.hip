@@ -10,10 +10,10 @@
 //   dG_C = sum_i k_i.(e^(G_C - G) U dS'^T)_i + e^(G_C) <dS', S>,
 //   dlog_decay_t = sum_{i >= t} dG_i + dG_C.
 //
-// A workgroup takes a chunk of one key head and adds up over the value heads of its group, in their order; a wave has 16
-// features of dQ and dK, formed transposed, so that a lane holds four neighbouring features of a token.  What bounds it is one
-// workgroup a compute unit (U and dR in parts fill the LDS) in phases that wait for memory, for the LDS and for one another: bf16,
-// 2 x 16 heads of 2048 tokens, D = d = 128, 116 us for 0.33 GB.
+// A workgroup takes a chunk of one key head and adds up over the value heads of its group, in their order (with few chunks each value
+// head has a workgroup, and a launch behind adds up); a wave has 16 features of dQ and dK, formed transposed, so that a lane holds
+// four neighbouring features of a token.  What bounds it is one workgroup a compute unit (U and dR in parts fill the LDS) in phases
+// that wait for memory, for the LDS and for one another: bf16, 2 x 16 heads of 2048 tokens, D = d = 128, 116 us for 0.33 GB.
 #include "luna_delta.hpp"
 
 namespace luna {
@@ -21,9 +21,15 @@ namespace luna {
 namespace {
 
 constexpr int C = kDeltaChunk, KT = C / 16, KS = C / 32;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 
 template <int DK>
 constexpr int kGradWaves = DK == 128 ? 8 : 4;
+// Whether each value head gets a workgroup of its own, where its states have room for its dQ and dK: where that saves a quarter of the
+// turns that the compute units take.  176 tokens, 32 heads on 4, D = d = 128: 345 -> 124 us in fp32 and 214 -> 96 in bf16 for the whole
+// backward pass; 2000 tokens, 32 on 1: 1528 -> 620 and 945 -> 430; two of 1000, 16 on 4: 312 -> 266 and 185 -> 163.
+constexpr int64_t kGradUnits = 256;
+inline bool grads_apart(int64_t chunks, int group) { return 4 * ((chunks * group + kGradUnits - 1) / kGradUnits) <= 3 * group; }
 
 template <typename T, int DK, int DV, int NP>
 struct GradLds {
@@ -73,13 +79,14 @@ struct GradTile {
 };
 
 template <typename T, int DK, int DV, int NP>
-__global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(DeltaArgs a, int shares) {
   using Lds = GradLds<T, DK, DV, NP>;
   constexpr int W = Lds::W, THREADS = 64 * W, PK = Lds::PK, PA = Lds::PA, PT = Lds::PT, esz = (int)sizeof(T), FS = DK / 32, VS = DV / 32;
   extern __shared__ __attribute__((aligned(16))) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   const int tid0 = threadIdx.x, wave = wave_id();
-  const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk, group = a.H / a.Hk;
+  const int hk = blockIdx.x / shares % a.Hk, slot = blockIdx.x / shares / a.Hk, group = a.H / a.Hk;
+  const int h0 = blockIdx.x % shares * (group / shares), h1 = h0 + group / shares;  // the value heads
   const SeqPiece sp = seq_uniform(seq_piece(a.s, slot, C));
   if (sp.seq < 0) return;
   const bool packed = a.s.offsets != nullptr, mine = wave < DK / 16;
@@ -109,7 +116,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
     DecayRows<T, C, DK, PK, THREADS> x, y;
     x.load(seq_row(a.k, sp, packed, hk, t0, esz), a.k.row, m, DK, false);
     y.load(seq_row(a.q, sp, packed, hk, t0, esz), a.q.row, m, DK, false);
-    load_head(hk * group);
+    load_head(hk * group + h0);
     x.store(&l.k[0][0]);
     y.store(&l.q[0][0]);
   }
@@ -121,7 +128,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
 #pragma unroll
   for (int i = 0; i < KT; ++i) dq[i] = zero4(), dk[i] = zero4();
 
-  for (int h = 0; h < group; ++h) {
+  for (int h = h0; h < h1; ++h) {
     const int tid = anew(tid0), lane = tid % kWave, g = lane / 16, c = lane % 16, i4 = 4 * (tid % 16);
     const int head = hk * group + h;
     const int64_t at = (int64_t)slot * a.H + head;
@@ -142,7 +149,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
         sy[e] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(after, state, (32 * s + e) * DK * 4, 0));
       }
     };
-    if (PARK && h > 0) load_head(head);
+    if (PARK && h > h0) load_head(head);
     __syncthreads();  // the head before is no longer read
 #pragma unroll
     for (int n = 0; n < NG; ++n)
@@ -303,7 +310,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
       if constexpr (PARK) {
 #pragma unroll
         for (int i = 0; i < KT; ++i) dq[i] = zero4(), dk[i] = zero4();
-        if (h > 0) {
+        if (h > h0) {
           const int off = anew(tid0) * 16;
 #pragma unroll
           for (int i = 0; i < KT; ++i) {
@@ -339,7 +346,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
       both = groups_sum(row_sum(both));
       if (mine && lane == 0) l.state[wave] = both;
     }
-    if (!PARK && h + 1 < group) load_head(head + 1);
+    if (!PARK && h + 1 < h1) load_head(head + 1);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
@@ -371,8 +378,7 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
         }
       }
     }
-    if (PARK && h + 1 < group) {
-      typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+    if (PARK && h + 1 < h1) {
       const int off = anew(tid0) * 16;
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
@@ -380,7 +386,15 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, dk[i]), parked, off, (KT + i) * THREADS * 16, 0);
       }
     }
-    if (mine && h + 1 == group) {
+    if (mine && shares > 1) {  // (one head: its sums, in the place of its states, which have been read by then)
+      const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
+#pragma unroll
+      for (int it = 0; it < KT; ++it) {
+        const int off = ((16 * it + c) * DK + feat + 4 * g) * 4;
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, dq[it]), before, off, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, dk[it]), after, off, 0, 0);
+      }
+    } else if (mine && h + 1 == h1) {
       const int lane = anew(tid0) % kWave, g = lane / 16, c = lane % 16;
       const Buf bq = buffer(seq_row(a.dq, sp, packed, hk, t0, esz), (int)(((m - 1) * a.dq.row + DK) * esz));
       const Buf bk = buffer(seq_row(a.dk, sp, packed, hk, t0, esz), (int)(((m - 1) * a.dk.row + DK) * esz));
@@ -419,14 +433,35 @@ __global__ __launch_bounds__(64 * kGradWaves<DK>, 1) void delta_grads_kernel(Del
   }
 }
 
+// dQ and dK of chunks whose value heads had a workgroup each, added up in the heads' order.
+template <typename T, int DK>
+__global__ __launch_bounds__(256) void delta_grads_join_kernel(DeltaArgs a) {
+  const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk, group = a.H / a.Hk;
+  const SeqPiece sp = seq_piece(a.s, slot, C);
+  if (sp.seq < 0) return;
+  const bool packed = a.s.offsets != nullptr;
+  const int t0 = sp.index * C, m = min(C, sp.len - t0);
+  const float* from = blockIdx.y ? a.after : a.before;
+  const SeqRows& rows = blockIdx.y ? a.dk : a.dq;
+  const int64_t head0 = (int64_t)slot * a.H + hk * group;
+  for (int at = 4 * threadIdx.x; at < m * DK; at += 4 * 256) {
+    f32x4 sum = zero4();
+#pragma unroll 4
+    for (int h = 0; h < group; ++h) sum += *reinterpret_cast<const f32x4*>(from + (head0 + h) * a.d * DK + at);
+    store4(reinterpret_cast<T*>(seq_row(rows, sp, packed, hk, t0 + at / DK, (int)sizeof(T))) + at % DK, sum[0], sum[1], sum[2], sum[3]);
+  }
+}
+
 template <typename T, int DK, int DV, int NP>
 hipError_t launch_one(const DeltaArgs& a, hipStream_t s) {
   constexpr int bytes = (int)sizeof(GradLds<T, DK, DV, NP>);
   static_assert(bytes <= 160 * 1024, "one workgroup's LDS");
   const hipError_t e = allow_lds<delta_grads_kernel<T, DK, DV, NP>>(bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((delta_grads_kernel<T, DK, DV, NP>), dim3((unsigned)((int64_t)a.slots * a.Hk)), dim3(64 * kGradWaves<DK>),
-                     bytes, s, a);
+  const int64_t groups = (int64_t)a.slots * a.Hk;
+  const int group = a.H / a.Hk, shares = DV >= C && grads_apart(groups, group) ? group : 1;
+  hipLaunchKernelGGL((delta_grads_kernel<T, DK, DV, NP>), dim3((unsigned)(groups * shares)), dim3(64 * kGradWaves<DK>), bytes, s, a, shares);
+  if (shares > 1) hipLaunchKernelGGL((delta_grads_join_kernel<T, DK>), dim3((unsigned)groups, 2), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <typename T, int DK, int NP>

@@ -100,6 +100,19 @@ def test_many_heads(Hk, D, d, dtype, state):
     check_backward(Q, K, V, dO, g, beta, grads, "packed", lens, D ** -0.5)
 
 
+@pytest.mark.parametrize("H,Hk,D,d,dtype,lens", [
+    (6, 2, 128, 128, "bf16", [70] * 60), (6, 2, 128, 128, "f32", [70] * 60), (4, 2, 64, 64, "bf16", [3] * 66), (8, 1, 32, 128, "f32", [1] * 250),
+    (6, 2, 128, 128, "bf16", [70, 1]), (6, 2, 128, 128, "f32", [70, 0, 1]), (8, 1, 32, 64, "bf16", [65]), (5, 1, 64, 128, "f32", [129, 64])])
+def test_gradients_of_shared_heads(H, Hk, D, d, dtype, lens):
+    """Value heads one after another in a workgroup, and with few chunks in workgroups of their own, whose sums are joined."""
+    say(f"delta backward, shared heads: H={H} Hk={Hk} D={D} d={d} {dtype} {len(lens)} sequences")
+    Q, K, V, dO, g, beta, _ = make("packed", lens, H, Hk, D, d, of(dtype), seed=61)
+    run = lambda: luna.delta_attn_bwd(Q, K, V, dO, g, beta, scale=D ** -0.5, **kw("packed", lens))  # noqa: E731
+    grads = run()
+    check_backward(Q, K, V, dO, g, beta, grads, "packed", lens, D ** -0.5)
+    assert all(torch.equal(x, y) for x, y in zip(grads, run()))
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
 def test_what_is_not_finite_with_many_heads(bad):
     """The forward call's rules for 64 columns a workgroup: a value's column, a key's and a gate's heads, each from its token on."""
