@@ -29,7 +29,10 @@ constexpr int kGradWaves = DK == 128 ? 8 : 4;
 // turns that the compute units take.  176 tokens, 32 heads on 4, D = d = 128: 345 -> 124 us in fp32 and 214 -> 96 in bf16 for the whole
 // backward pass; 2000 tokens, 32 on 1: 1528 -> 620 and 945 -> 430; two of 1000, 16 on 4: 312 -> 266 and 185 -> 163.
 constexpr int64_t kGradUnits = 256;
-inline bool grads_apart(int64_t chunks, int group) { return 4 * ((chunks * group + kGradUnits - 1) / kGradUnits) <= 3 * group; }
+inline bool grads_apart(int64_t chunks, int group) {
+  const int64_t all = chunks * group;
+  return 4 * ((all + kGradUnits - 1) / kGradUnits) <= 3 * group && all < ((int64_t)1 << 22);  // (within a launch)
+}
 
 template <typename T, int DK, int DV, int NP>
 struct GradLds {

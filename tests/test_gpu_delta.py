@@ -113,6 +113,33 @@ def test_gradients_of_shared_heads(H, Hk, D, d, dtype, lens):
     assert all(torch.equal(x, y) for x, y in zip(grads, run()))
 
 
+def test_captured_gradients_of_shared_heads():
+    """Sums of value heads that are joined by a second launch: from a graph replayed between eager calls, and over a padded batch."""
+    lens, n, H, Hk, D, d = [70, 0, 33], 70, 6, 2, 64, 64
+    gen = torch.Generator(device=device()).manual_seed(62)
+    Q, K, V, dO, g, beta, _ = make("batch", [n] * 3, H, Hk, D, d, torch.bfloat16, seed=62)
+    used = torch.tensor(lens, dtype=torch.int32, device=device())
+    call = lambda: luna.delta_attn_bwd(Q, K, V, dO, g, beta, scale=D ** -0.5, lens=used)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = call()
+    for _ in range(3):
+        V.copy_(rand(V.shape, torch.bfloat16, gen))
+        for t in outs:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outs]
+        eager = call()
+        assert all(torch.equal(x[i, :, :k], y[i, :, :k]) for x, y in zip(got, eager) for i, k in enumerate(lens))
+    single = lambda i, k: [t[i:i + 1, :, :k].contiguous() for t in (Q, K, V, dO, g, beta)]  # noqa: E731
+    for i, k in enumerate(lens):
+        if k:
+            check_backward(*single(i, k), [t[i:i + 1, :, :k] for t in eager], "batch", [k], D ** -0.5)
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
 def test_what_is_not_finite_with_many_heads(bad):
     """The forward call's rules for 64 columns a workgroup: a value's column, a key's and a gate's heads, each from its token on."""

@@ -122,6 +122,32 @@ def test_many_rows_in_fp32(m, klens, H, Hk, d):
     check_forward(Q, K, V, out, lse, "batch", [m] * len(klens), klens)
 
 
+def test_captured_calls_of_many_rows_in_fp32():
+    """Padded queries, some more than their cache holds, and lengths that change between the replays; rows behind q_lens stay."""
+    m, room, H, d = 70, [2000, 300, 900], 4, 64
+    Q, K, V, kp, vp, table, _ = make(m, room, H, 2, d, torch.float32, 32, seed=53)
+    lens, q_lens = i32(room), i32([m] * 3)
+    out, lse = torch.empty_like(Q), torch.empty(Q.shape[:3], device=device())
+    call = lambda: luna.paged_attn(Q, kp, vp, table, lens, q_lens=q_lens, out=out, lse=lse)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for klens, qlens in ((room, [m, m - 1, 33]), ([1999, 40, 0], [1, 70, 70]), ([65, 1, 33], [64, 0, 40]), (room, [m] * 3)):
+        lens.copy_(i32(klens))
+        q_lens.copy_(i32(qlens))
+        out.fill_(7.0)
+        lse.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_forward(Q, K, V, out, lse, "batch", qlens, klens)
+        assert all((t[i, :, n:] == 7).all() for t in (out, lse) for i, n in enumerate(qlens))
+        replayed = [out.clone(), lse.clone()]
+        call()
+        assert torch.equal(out, replayed[0]) and torch.equal(lse, replayed[1])
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 def test_values_behind_some_rows_in_fp32(bad):
     """A value that is not finite at a token which only the last rows see (m = 40: in another group of rows than the first)."""
