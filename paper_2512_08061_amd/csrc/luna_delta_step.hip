@@ -8,6 +8,9 @@
 // accesses, which is what bounds it (64 x 32 heads, D = d = 128, 270 MB: 54.2 us, the rate of a copy).  S^T k, S^T q and k.q are summed side by side, before the update, of which
 // S'^T q = S^T q + (k.q) u follows; the shares of the groups are added within a wave by lane exchanges and over the
 // waves through LDS, in a fixed order.
+//
+// Infinities among keys, values and beta count as NaN, which every sum hands on: from its token on the head's or column's state and
+// rows are NaN (infinities by themselves would stay, beside the NaN of 0 times them).
 #include "luna_seq.hpp"
 #include "luna_delta.hpp"
 
@@ -18,6 +21,8 @@ namespace {
 constexpr int kStepGroups = 32;  // feature groups
 constexpr int kStepStage = 4;    // tokens staged in LDS at a time
 constexpr int kStepCols = 32;
+
+__device__ __forceinline__ float finite_or_nan(float x) { return fmaf(0.0f, x, x); }  // (0 times an infinity is NaN)
 
 template <typename T, int FEAT>
 __global__ __launch_bounds__(8 * kStepCols) void delta_step_kernel(DeltaStepArgs a) {
@@ -47,12 +52,12 @@ __global__ __launch_bounds__(8 * kStepCols) void delta_step_kernel(DeltaStepArgs
     __syncthreads();  // the stage before is no longer read
     for (int i = tid; i < tn * D; i += THREADS) {
       sq[i / D][i % D] = (float)Q[(int64_t)(t0 + i / D) * a.q.row + i % D];
-      sk[i / D][i % D] = (float)K[(int64_t)(t0 + i / D) * a.k.row + i % D];
+      sk[i / D][i % D] = finite_or_nan((float)K[(int64_t)(t0 + i / D) * a.k.row + i % D]);
     }
-    for (int i = tid; i < tn * COLS; i += THREADS) sv[i / COLS][i % COLS] = (float)V[(int64_t)(t0 + i / COLS) * a.v.row + i % COLS];
+    for (int i = tid; i < tn * COLS; i += THREADS) sv[i / COLS][i % COLS] = finite_or_nan((float)V[(int64_t)(t0 + i / COLS) * a.v.row + i % COLS]);
     if (tid < tn) {
       gates[0][tid] = exp2f(decay_log2(a.log_decay[at * a.m + t0 + tid]));
-      gates[1][tid] = a.beta[at * a.m + t0 + tid];
+      gates[1][tid] = finite_or_nan(a.beta[at * a.m + t0 + tid]);
     }
     __syncthreads();
     for (int t = 0; t < tn; ++t) {

@@ -265,6 +265,48 @@ def test_step(B, H, Hk, m, D, d, dtype):
     check_forward(Q, K, V, g, beta, out, "batch", [m] * B, D ** -0.5, S0, S)
 
 
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("B,H,Hk,m,D,d,dtype", [(2, 2, 2, 9, 128, 128, "bf16"), (1, 4, 2, 5, 64, 32, "bf16"), (2, 3, 1, 6, 32, 64, "f32")])
+def test_step_with_what_is_not_finite(B, H, Hk, m, D, d, dtype, bad):
+    """As in the call over sequences: a value makes its column NaN from its token on, a key or a gate its heads, in out and in S;
+    the tokens before, the other columns and heads keep their bits.  A query reaches its own row alone."""
+    say(f"delta step, not finite: B={B} H={H} Hk={Hk} m={m} D={D} d={d} {dtype} {bad}")
+    Q, K, V, _, g, beta, gen = make("batch", [m] * B, H, Hk, D, d, of(dtype), seed=21)
+    S0 = torch.randn((B, H, D, d), generator=gen, device=device())
+
+    def call(q, k, v, gg, b):
+        S = S0.clone()
+        return luna.delta_attn_step(q, k, v, gg, b, S, scale=D ** -0.5), S
+
+    want, wS = call(Q, K, V, g, beta)
+    for at in (0, 4, m - 1):  # (tokens pass through in groups of four)
+        v2 = V.clone()
+        v2[0, 0, at, 5] = bad
+        out, S = call(Q, K, v2, g, beta)
+        assert torch.isnan(out[0, 0, at:, 5].float()).all() and torch.isnan(S[0, 0, :, 5]).all()
+        out[0, 0, at:, 5], S[0, 0, :, 5] = want[0, 0, at:, 5], wS[0, 0, :, 5]
+        assert torch.equal(out, want) and torch.equal(S, wS)
+        for which in ("key", "log_decay", "beta"):
+            k2, g2, b2 = K.clone(), g.clone(), beta.clone()
+            heads = H // Hk if which == "key" else 1  # the value heads that it reaches, the first ones
+            if which == "key":
+                k2[0, 0, at, D - 3] = bad
+            elif which == "log_decay":
+                g2[0, 0, at] = math.nan
+            else:
+                b2[0, 0, at] = bad
+            out, S = call(Q, k2, V, g2, b2)
+            assert torch.isnan(out[0, :heads, at:].float()).all() and torch.isnan(S[0, :heads]).all(), which
+            out[0, :heads, at:], S[0, :heads] = want[0, :heads, at:], wS[0, :heads]
+            assert torch.equal(out, want) and torch.equal(S, wS), which
+        q2 = Q.clone()
+        q2[0, 0, at, 3] = bad
+        out, S = call(q2, K, V, g, beta)
+        assert not torch.isfinite(out[0, :H // Hk, at].float()).any()
+        out[0, :H // Hk, at] = want[0, :H // Hk, at]
+        assert torch.equal(out, want) and torch.equal(S, wS)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prompt_then_steps_is_the_whole_sequence(dtype):
     n, cut, H, Hk, D, d = 140, 101, 4, 2, 64, 64
