@@ -42,6 +42,19 @@ constexpr int kDeltaGateRows = 6, kDeltaGates = kDeltaGateRows * kDeltaChunk;
 // of `out` alone in the forward pass and is rounded once there.
 constexpr int kDeltaParts = 2, kDeltaExactParts = 3, kDeltaBackParts = 3;
 
+// Workgroups of the gradients' kernel that run at once, one a compute unit.
+constexpr int64_t kDeltaUnits = 256;
+// Whether each value head of a key head's chunks has a workgroup of its own there (luna_delta_grads.hip), where its states have room for
+// its dQ and dK: where the compute units then take at most three quarters of the turns that they take when a workgroup adds up its
+// heads one after the other.  The whole backward pass, D = d = 128, us, one after the other first: 176 tokens, 32 heads on 4, 345 and
+// 124 in fp32, 214 and 96 in bf16; 2000 tokens, 32 on 1, 1528 and 620, 945 and 430; 4800 tokens, 16 on 4 (300 chunks and key heads:
+// 8 turns and 5), 961 and 893, 514 and 480; but two of 3600 (452: 8 and 8) 826 and 873, 474 and 514, two of 4800 (600: 12 and 10) 1130
+// and 1125, 648 and 665.
+inline bool delta_grads_apart(int64_t chunks, int64_t group) {
+  const auto turns = [](int64_t groups) { return (groups + kDeltaUnits - 1) / kDeltaUnits; };
+  return 4 * turns(chunks * group) <= 3 * turns(chunks) * group && chunks * group < ((int64_t)1 << 22);  // (within a launch)
+}
+
 struct DeltaArgs {
   SeqRows q, k, v, o;  // widths D, D, d, d; o: out, or dO in the backward pass
   SeqSet s;

@@ -25,15 +25,6 @@ typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 
 template <int DK>
 constexpr int kGradWaves = DK == 128 ? 8 : 4;
-// Whether each value head gets a workgroup of its own, where its states have room for its dQ and dK: where that saves a quarter of the
-// turns that the compute units take.  176 tokens, 32 heads on 4, D = d = 128: 345 -> 124 us in fp32 and 214 -> 96 in bf16 for the whole
-// backward pass; 2000 tokens, 32 on 1: 1528 -> 620 and 945 -> 430; two of 1000, 16 on 4: 312 -> 266 and 185 -> 163.
-constexpr int64_t kGradUnits = 256;
-inline bool grads_apart(int64_t chunks, int group) {
-  const int64_t all = chunks * group;
-  return 4 * ((all + kGradUnits - 1) / kGradUnits) <= 3 * group && all < ((int64_t)1 << 22);  // (within a launch)
-}
-
 template <typename T, int DK, int DV, int NP>
 struct GradLds {
   static constexpr int PAD = 16 / (int)sizeof(T), PK = DK + PAD, PA = C + PAD, PT = sizeof(T) == 2 ? C : PA, W = kGradWaves<DK>;
@@ -462,7 +453,7 @@ hipError_t launch_one(const DeltaArgs& a, hipStream_t s) {
   const hipError_t e = allow_lds<delta_grads_kernel<T, DK, DV, NP>>(bytes);
   if (e != hipSuccess) return e;
   const int64_t groups = (int64_t)a.slots * a.Hk;
-  const int group = a.H / a.Hk, shares = DV >= C && grads_apart(groups, group) ? group : 1;
+  const int group = a.H / a.Hk, shares = DV >= C && delta_grads_apart(groups, group) ? group : 1;
   hipLaunchKernelGGL((delta_grads_kernel<T, DK, DV, NP>), dim3((unsigned)(groups * shares)), dim3(64 * kGradWaves<DK>), bytes, s, a, shares);
   if (shares > 1) hipLaunchKernelGGL((delta_grads_join_kernel<T, DK>), dim3((unsigned)groups, 2), dim3(256), 0, s, a);
   return hipGetLastError();

@@ -2,6 +2,8 @@
 status codes before anything is enqueued, workspace sizes, wait states of the compiled kernels."""
 import concurrent.futures as cf
 import ctypes
+import os
+import subprocess
 
 import pytest
 
@@ -110,6 +112,38 @@ def test_workspace_sizes(lib):
     # 2^31 chunks, and launches of 2^32 threads
     assert nb(0, i64(1, 1 << 30, 0, 0), H=1, Hk=1) == 0 and b"too many" in lib.luna_last_error()
     assert nb(0, i64(65535, 16384, 0, 0), H=64, Hk=64) == 0 and b"too many" in lib.luna_last_error()
+
+
+RULES = r"""
+#include <cstdio>
+#include "luna_delta.hpp"
+int main() {
+  for (int64_t chunks = 1; chunks <= 3000; ++chunks)
+    for (int64_t group = 1; group <= 40; ++group) {
+      int64_t together = 0, apart = 0;  // turns of 256 workgroups
+      for (int64_t left = chunks; left > 0; left -= 256) together += group;
+      for (int64_t left = chunks * group; left > 0; left -= 256) ++apart;
+      if (luna::delta_grads_apart(chunks, group) != (apart <= together - (together + 3) / 4))
+        return printf("%ld chunks, groups of %ld\n", (long)chunks, (long)group), 1;
+    }
+  return luna::delta_grads_apart((int64_t)1 << 20, 4) || luna::delta_grads_apart((int64_t)1 << 31, 65535);
+}
+"""
+
+
+def host_program(tmp_path, text):
+    src, exe = tmp_path / "rules.cpp", tmp_path / "rules"
+    src.write_text(text)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run(["/opt/rocm/bin/hipcc", "-x", "hip", "--offload-arch=gfx950", "-O1", "-std=c++17", "-Xclang", "-target-feature", "-Xclang",
+                    "-packed-fp32-ops", "-I", os.path.join(root, "include"), "-I", os.path.join(root, "paper_2512_08061_amd", "csrc"),
+                    str(src), "-o", str(exe)], check=True, capture_output=True)
+    p = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert p.returncode == 0, p.stdout
+
+
+def test_value_heads_apart_where_a_quarter_of_the_turns_is_saved(tmp_path):
+    host_program(tmp_path, RULES)
 
 
 def test_binding_refuses():

@@ -113,6 +113,17 @@ def test_gradients_of_shared_heads(H, Hk, D, d, dtype, lens):
     assert all(torch.equal(x, y) for x, y in zip(grads, run()))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_of_shared_heads_with_chunks_for_every_unit(dtype):
+    """More chunks and key heads than compute units, and value heads in workgroups of their own all the same (260 of a group of 4: 8
+    turns one after another, 5 apart)."""
+    lens, H, Hk, D, d = [20] * 130, 8, 2, 64, 64
+    say(f"delta backward, shared heads, 260 chunks {dtype}")
+    Q, K, V, dO, g, beta, _ = make("batch", lens, H, Hk, D, d, of(dtype), seed=63)
+    grads = luna.delta_attn_bwd(Q, K, V, dO, g, beta, scale=D ** -0.5)
+    check_backward(Q, K, V, dO, g, beta, grads, "batch", lens, D ** -0.5)
+
+
 def test_captured_gradients_of_shared_heads():
     """Sums of value heads that are joined by a second launch: from a graph replayed between eager calls, and over a padded batch."""
     lens, n, H, Hk, D, d = [70, 0, 33], 70, 6, 2, 64, 64
