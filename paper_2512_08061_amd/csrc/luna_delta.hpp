@@ -190,7 +190,6 @@ __device__ __forceinline__ void mma(f32x4& c, const DeltaOp<__bf16, P>& a, const
 }
 
 // LDS by byte addresses: what differs between lanes is worked out once, the rest lies in the instructions' offsets.
-typedef __attribute__((address_space(3))) char* LdsPtr;
 __device__ __forceinline__ unsigned lds_address(const void* p) {
   return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
 }

@@ -367,8 +367,8 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxA
 // and head: whole sequences are finished here, the parts of others are joined by a launch behind it.  (512 new tokens of caches of 4096,
 // 1999, 700 and 16384, 16 heads on 4, d = 128: 157 and 27 us; without shares the longest cache kept 64 of 256 compute units busy
 // for 348.)
-template <int DH, int GROUPS>
-__global__ __launch_bounds__(256 * GROUPS, 2) void softmax_part32_kernel(SoftmaxArgs a, int shares) {
+template <int DH>
+__global__ __launch_bounds__(256, 2) void softmax_part32_kernel(SoftmaxArgs a, int shares) {
   extern __shared__ __attribute__((aligned(16))) char raw[];
   const int tiles = (int)((a.qs.rows + 127) / 128), tile = blockIdx.x / a.H % tiles, rank = blockIdx.x / (tiles * a.H);
   const int head = head_of(blockIdx.x % a.H, a.H), heads = a.H / a.Hk;
@@ -382,7 +382,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void softmax_part32_kernel(Softmax
   sq.index = tile;
   const bool whole = held.u0 == 0 && held.u1 * kPagedTileUnit >= sk.len;
   float* rows = a.parts + (paged_part(share, b) * a.Hk + head / heads) * (a.qs.rows * heads) * (DH + 2);
-  softmax_tile32<DH, GROUPS, true>(a, raw, head, sq, sk, kPagedTileUnit * held.u0, min(sk.len, kPagedTileUnit * held.u1), whole ? nullptr : rows);
+  softmax_tile32<DH, 1, true>(a, raw, head, sq, sk, kPagedTileUnit * held.u0, min(sk.len, kPagedTileUnit * held.u1), whole ? nullptr : rows);
 }
 
 template <int DH, int GROUPS, bool PAGED>
@@ -405,11 +405,11 @@ hipError_t launch_fwd32(const SoftmaxArgs& a, hipStream_t s) {
 
 template <int DH>
 hipError_t launch_shares(const SoftmaxArgs& a, int shares, hipStream_t s) {
-  constexpr int GROUPS = 1, bytes = (int)sizeof(SoftmaxLds32<DH, GROUPS>);
-  hipError_t e = allow_lds<softmax_part32_kernel<DH, GROUPS>>(bytes);
+  constexpr int bytes = (int)sizeof(SoftmaxLds32<DH, 1>);
+  hipError_t e = allow_lds<softmax_part32_kernel<DH>>(bytes);
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)((shares + a.qs.count) * ((a.qs.rows + 127) / 128) * a.H));
-  hipLaunchKernelGGL((softmax_part32_kernel<DH, GROUPS>), grid, dim3(256 * GROUPS), bytes, s, a, shares);
+  hipLaunchKernelGGL((softmax_part32_kernel<DH>), grid, dim3(256), bytes, s, a, shares);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   return launch_paged_tile_join(a, shares, s);
 }
