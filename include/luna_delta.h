@@ -28,8 +28,14 @@ enum {
   LUNA_OP_DELTA_BWD = 1
 };
 
-/* Bytes of device workspace of an operation (as luna_seq_workspace_bytes; 0 where it needs none, which is the forward call in
- * LUNA_BF16, and on invalid arguments, with a reason in luna_last_error()). */
+/*
+ * Bytes of device workspace of an operation (as luna_seq_workspace_bytes; 0 where it needs none, which is the forward call in
+ * LUNA_BF16, and on invalid arguments, with a reason in luna_last_error()).  It grows with the chunks of 64 tokens, of which packed
+ * sequences count rows / 64 + count (each has one at least, however short) and others count * ceil(rows / 64).  Per chunk and value
+ * head the gradients take 8 D d + 512 d + 50688 bytes in LUNA_BF16 and 8 D d + 512 d + 34304 in LUNA_F32, the forward call in
+ * LUNA_F32 takes 34304: 247 KB with D = d = 128, 8.1 GB for 8 x 16 heads of 16384 tokens, 44.5 GB for 16 heads of 10000 packed
+ * sequences of 8.  A batch that this is too much for is handed over in parts: sequences do not depend on one another.
+ */
 size_t luna_delta_workspace_bytes(int32_t op, luna_dtype dtype, const luna_seqs* seqs, int64_t H, int64_t Hk, int64_t D,
                                   int64_t d);
 

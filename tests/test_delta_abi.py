@@ -169,6 +169,16 @@ def test_value_heads_apart_where_a_quarter_of_the_turns_is_saved(tmp_path):
     host_program(tmp_path, RULES)
 
 
+def test_workspace_sizes_are_those_of_the_header(lib):
+    """Per chunk and value head, as luna_delta.h says."""
+    for B, rows, off, chunks in ((8, 16384, 0, 8 * 256), (3, 65, 0, 6), (10000, 80000, FAKE, 11250), (1, 1, FAKE, 1)):
+        for D, d in ((128, 128), (32, 64), (64, 32)):
+            for op, dt, each in ((luna.OP_DELTA_BWD, luna.LUNA_BF16, 8 * D * d + 512 * d + 50688),
+                                 (luna.OP_DELTA_BWD, luna.LUNA_F32, 8 * D * d + 512 * d + 34304), (luna.OP_DELTA_FWD, luna.LUNA_F32, 34304),
+                                 (luna.OP_DELTA_FWD, luna.LUNA_BF16, 0)):
+                assert lib.luna_delta_workspace_bytes(op, dt, ref(i64(B, rows, off, 0)), 16, 4, D, d) == chunks * 16 * each, (B, D, d, op)
+
+
 def test_binding_refuses():
     """Shapes, types, devices and forms that do not go together, before the C call (CPU tensors are refused too)."""
     import torch
