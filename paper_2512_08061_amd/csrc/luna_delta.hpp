@@ -42,7 +42,7 @@ constexpr int kDeltaGateRows = 6, kDeltaGates = kDeltaGateRows * kDeltaChunk;
 // of `out` alone in the forward pass and is rounded once there.
 constexpr int kDeltaParts = 2, kDeltaExactParts = 3, kDeltaBackParts = 3;
 
-// Workgroups of the gradients' kernel, and of the serial ones in fp32 and of the backward pass, that run at once: one a compute unit.
+// Workgroups of the gradients' kernel that run at once, one a compute unit.
 constexpr int64_t kDeltaUnits = 256;
 // Whether each value head of a key head's chunks has a workgroup of its own there (luna_delta_grads.hip), where its states have room for
 // its dQ and dK: where the compute units then take at most three quarters of the turns that they take when a workgroup adds up its
@@ -54,14 +54,6 @@ inline bool delta_grads_apart(int64_t chunks, int64_t group) {
   const auto turns = [](int64_t groups) { return (groups + kDeltaUnits - 1) / kDeltaUnits; };
   return 4 * turns(chunks * group) <= 3 * turns(chunks) * group && chunks * group < ((int64_t)1 << 22);  // (within a launch)
 }
-
-// Whether these serial kernels take 32 value columns a workgroup, with two waves that load, or 64, of which all waves load (`groups`:
-// workgroups of 32): the first where they run at once.  (All but those of fp32 with D = 32 have more than 256 registers a lane, which
-// leaves a second workgroup no room, whatever their LDS.)  us, 32 columns first, 16 heads, d = 128, sequences of 2048: backward in bf16
-// with D = 128 two 282 and 338, three 428 and 426, eight 1028 and 931; in fp32 488 and 562, 756 and 682; forward in fp32 three
-// 332 and 394, eight 693 and 510.  D = 64, d = 64, 320 workgroups: backward 170 and 170 (bf16), 236 and 233 (fp32); 384:
-// 201 and 193, 282 and 253, forward 267 and 204.  D = 32: 154 and 157, 189 and 185; 182 and 174, 205 and 204; 181 and 156.
-inline bool delta_narrow(int64_t d, int64_t groups) { return d == 32 || groups <= kDeltaUnits; }
 
 struct DeltaArgs {
   SeqRows q, k, v, o;  // widths D, D, d, d; o: out, or dO in the backward pass

@@ -3,7 +3,6 @@ status codes before anything is enqueued, workspace sizes, wait states of the co
 import concurrent.futures as cf
 import ctypes
 import os
-import re
 import subprocess
 
 import pytest
@@ -141,28 +140,6 @@ def host_program(tmp_path, text):
                     str(src), "-o", str(exe)], check=True, capture_output=True)
     p = subprocess.run([str(exe)], capture_output=True, text=True)
     assert p.returncode == 0, p.stdout
-
-
-WIDTH = r"""
-#include "luna_delta.hpp"
-int main() {
-  for (int64_t groups = 1; groups <= 2000; ++groups)
-    if (!luna::delta_narrow(32, groups) || luna::delta_narrow(64, groups) != (groups <= 256) || luna::delta_narrow(128, groups) != (groups <= 256))
-      return 1;
-  return 0;
-}
-"""
-
-
-def test_serial_passes_are_narrow_where_they_run_at_once(tmp_path):
-    """32 columns a workgroup up to one workgroup for each of 256 compute units, and the compiled kernels leave room for no more (of
-    fp32 with D = 32 they do, and 64 columns are as fast)."""
-    host_program(tmp_path, WIDTH)
-    for source, dtypes in (("luna_delta_bf16.hip", "DF16b"), ("luna_delta_f32.hip", "f")):
-        text = assembly(source, str(tmp_path / (source + ".s")))
-        counts = {m.group(1): int(m.group(2)) for m in re.finditer(r"\.name: +(_Z\S+)\n(?:    +\.\S.*\n)*?    +\.vgpr_count: +(\d+)", text)}
-        narrow = {n: c for n, c in counts.items() if re.search(rf"kernelI{dtypes}Li\d+ELi32E", n)}
-        assert len(narrow) >= 3 and all(c > 256 for n, c in narrow.items() if not re.search(r"IfLi32E", n)), counts
 
 
 def test_value_heads_apart_where_a_quarter_of_the_turns_is_saved(tmp_path):
