@@ -54,9 +54,11 @@ size_t luna_paged_workspace_bytes(luna_dtype dtype, const luna_seqs* seqs, const
  * Of equal or padded query sequences with at most 64 query rows per key head (rows * H / Hk: the next tokens) the cached
  * keys of all sequences are shared out equally among the workgroups, whatever their lengths, each read once for all query
  * heads of a key head (LUNA_F32: for 32 of its rows).  So are those of LUNA_F32 calls of more rows whose tables have room for
- * four keys a new token and which make less than 512 tiles of 64 rows, or tiles that are at most half full.  All others take the keys one block after the other for tiles of 128 query rows of a head (64: LUNA_F32
- * and d = 32); of LUNA_BF16 calls with d >= 64 and at most 512 tiles the keys are shared out as well.  Sums are taken in a fixed
- * order.  What is not finite is treated as luna_softmax_fwd does.
+ * four keys a new token and which make less than 512 tiles of 64 rows, or tiles that are at most half full.  All others take
+ * the keys one block after the other for tiles of 128 query rows of a head (64: LUNA_F32 and d = 32); of equal or padded
+ * LUNA_BF16 calls with d >= 64 and at most 512 tiles the keys are shared out as well.  Packed queries, whose lengths the host
+ * does not see, always take such tiles, each with all keys of its sequence: next tokens are faster as [count][H][1][d].  Sums
+ * are taken in a fixed order.  What is not finite is treated as luna_softmax_fwd does.
  */
 luna_status luna_paged_fwd(const luna_rows* Q, const luna_rows* k_pages, const luna_rows* v_pages, luna_dtype dtype,
                            const luna_seqs* seqs, const luna_pages* pages, int64_t H, int64_t Hk, int64_t d, float scale,

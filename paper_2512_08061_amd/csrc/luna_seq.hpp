@@ -303,7 +303,8 @@ hipError_t launch_softmax_bwd(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 // Over pages: the tile kernels, and the kernel for few rows of a key head (luna_paged_split.hip).
 hipError_t launch_paged_tiles(Dt dt, const SoftmaxArgs& a, hipStream_t s);
 // Workgroups of that kernel that share a key head's rows: in fp32 32 rows each (64 spilled, and one wave's products were the whole time
-// of a short call: 2 tokens of 32 heads on one, 3 keys, d = 128, 44.0 and 23.9 us).
+// of a short call: 2 tokens of 32 heads on one, 3 keys, d = 128, 44.0 and 23.9 us).  In bf16 one takes up to 64, though 33 and more of
+// d = 128 spill 19 registers too: the cache is read once.
 inline int64_t paged_row_groups(Dt dt, int64_t rows) { return dt == Dt::BF16 || rows < 1 ? 1 : (rows + 31) / 32; }
 // In fp32 it takes more rows as well, where the room for keys is long beside the new tokens (else shares and their join cost more than
 // the causal tiles: 90 tokens of 100 and 200 keys, 30.9 and 18.3 us) and the tiles of 64 rows of a head are too few for the device or
