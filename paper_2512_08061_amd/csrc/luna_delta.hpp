@@ -42,7 +42,7 @@ constexpr int kDeltaGateRows = 6, kDeltaGates = kDeltaGateRows * kDeltaChunk;
 // of `out` alone in the forward pass and is rounded once there.
 constexpr int kDeltaParts = 2, kDeltaExactParts = 3, kDeltaBackParts = 3;
 
-// Workgroups of the gradients' kernel that run at once, one a compute unit.
+// Workgroups of the gradients' kernel, and of the serial ones in fp32 and of the backward pass, that run at once: one a compute unit.
 constexpr int64_t kDeltaUnits = 256;
 // Whether each value head of a key head's chunks has a workgroup of its own there (luna_delta_grads.hip), where its states have room for
 // its dQ and dK: where the compute units then take at most three quarters of the turns that they take when a workgroup adds up its
@@ -53,6 +53,19 @@ constexpr int64_t kDeltaUnits = 256;
 inline bool delta_grads_apart(int64_t chunks, int64_t group) {
   const auto turns = [](int64_t groups) { return (groups + kDeltaUnits - 1) / kDeltaUnits; };
   return 4 * turns(chunks * group) <= 3 * turns(chunks) * group && chunks * group < ((int64_t)1 << 22);  // (within a launch)
+}
+
+// Whether these serial kernels take 32 value columns a workgroup, with two waves that load, or 64, of which all waves load (groups:
+// workgroups of 32): the first where they run at once, since a chunk passes in less time; with D < 128 and lengths that may differ up to
+// twice as many, since the longest sequence's chain counts then and short ones leave room.  us, 32 columns first, backward unless said:
+//   equal lengths, 16 heads of 2048 tokens, D = d = 128: two in bf16 282 and 338, three 428 and 426, eight 1028 and 931; in fp32 488
+//     and 562, 756 and 682, 1692 and 1456;
+//   8 x 1000, 12 heads, d = 64 (384): D = 64 in fp32 286 and 258, in bf16 202 and 193; D = 32 207 and 206, 188 and 181; forward in fp32,
+//     384 of 1024 tokens, D = 64 267 and 204, D = 32 181 and 156;
+//   packed 33 to 1500, 12 heads, d = 64 (384): D = 64 in fp32 227 and 259, in bf16 156 and 185; D = 32 185 and 206, 142 and 173; forward
+//     in fp32, 20 to 1500, 16 heads (384), D = 64 181 and 211, D = 32 141 and 159; but packed 800 to 1100 (384) 288 and 272 in fp32.
+inline bool delta_narrow(int64_t D, int64_t d, int64_t groups, bool equal) {
+  return d == 32 || groups <= kDeltaUnits * (D < 128 && !equal ? 2 : 1);
 }
 
 struct DeltaArgs {

@@ -518,9 +518,7 @@ hipError_t launch_both_one(const DeltaArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// 32 columns and two waves that load, or 64 columns of which all waves load: the first where its workgroups run side by side
-// (backward in bf16, 16 heads, D = d = 128: 2 x 2048 tokens 301 and 366 us, but 8 x 2048 1138 and 1057).
-constexpr int kScanHelp = 2;
+constexpr int kScanHelp = 2;  // waves that load, beside those of 32 columns (see delta_narrow)
 template <typename T, int DK, int DVW, int NP, bool BOTH>
 hipError_t launch_scan_width(const DeltaArgs& a, hipStream_t s) {
   constexpr int help = DVW == 32 ? kScanHelp : 0;
@@ -529,9 +527,9 @@ hipError_t launch_scan_width(const DeltaArgs& a, hipStream_t s) {
 }
 template <typename T, int DK, int NP, bool BOTH>
 hipError_t launch_scan_feature(const DeltaArgs& a, hipStream_t s) {
-  constexpr int at_once = 256 * (160 * 1024 / (int)sizeof(ScanLds<T, DK, 32, NP, NP, true>));
-  return a.d == 32 || (BOTH ? 2 : 1) * a.s.count * a.H * (a.d / 32) <= at_once ? launch_scan_width<T, DK, 32, NP, BOTH>(a, s)
-                                                                              : launch_scan_width<T, DK, 64, NP, BOTH>(a, s);
+  const bool equal = !a.s.offsets && !a.s.lens;
+  return delta_narrow(DK, a.d, (BOTH ? 2 : 1) * a.s.count * a.H * (a.d / 32), equal) ? launch_scan_width<T, DK, 32, NP, BOTH>(a, s)
+                                                                                     : launch_scan_width<T, DK, 64, NP, BOTH>(a, s);
 }
 template <typename T, int NP, bool BOTH>
 hipError_t launch_scan_all(const DeltaArgs& a, hipStream_t s) {

@@ -142,6 +142,24 @@ def host_program(tmp_path, text):
     assert p.returncode == 0, p.stdout
 
 
+WIDTH = r"""
+#include "luna_delta.hpp"
+int main() {
+  for (int64_t groups = 1; groups <= 2000; ++groups)
+    for (int64_t D = 32; D <= 128; D *= 2)
+      for (int equal = 0; equal < 2; ++equal)
+        if (!luna::delta_narrow(D, 32, groups, equal) || luna::delta_narrow(D, 128, groups, equal) != (groups <= (D < 128 && !equal ? 512 : 256)))
+          return 1;
+  return 0;
+}
+"""
+
+
+def test_serial_passes_are_narrow_where_they_run_at_once(tmp_path):
+    """32 columns a workgroup up to one for each of 256 compute units, or two where the lengths may differ."""
+    host_program(tmp_path, WIDTH)
+
+
 def test_value_heads_apart_where_a_quarter_of_the_turns_is_saved(tmp_path):
     host_program(tmp_path, RULES)
 

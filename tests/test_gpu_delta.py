@@ -124,6 +124,24 @@ def test_gradients_of_shared_heads_with_chunks_for_every_unit(dtype):
     check_backward(Q, K, V, dO, g, beta, grads, "batch", lens, D ** -0.5)
 
 
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (32, "bf16"), (64, "f32"), (32, "f32")])
+def test_equal_lengths_of_more_columns_than_units(D, dtype):
+    """320 workgroups of 32 columns of equal sequences (64 columns each then), and the same sequences packed (32)."""
+    n, H, d = 70, 8, 64
+    for B in (10, 20):  # (both serial passes; the forward one)
+        Q, K, V, dO, g, beta, _ = make("batch", [n] * B, H, H, D, d, of(dtype), seed=64)
+        say(f"delta, {B} equal sequences D={D} {dtype}")
+        out = luna.delta_attn(Q, K, V, g, beta, scale=D ** -0.5)
+        grads = luna.delta_attn_bwd(Q, K, V, dO, g, beta, scale=D ** -0.5)
+        check_forward(Q, K, V, g, beta, out, "batch", [n] * B, D ** -0.5)
+        check_backward(Q, K, V, dO, g, beta, grads, "batch", [n] * B, D ** -0.5)
+        flat = lambda t: t.transpose(1, 2).flatten(0, 1).contiguous() if t.dim() == 4 else t.transpose(0, 1).flatten(1).contiguous()  # noqa: E731
+        Q, K, V, dO, g, beta = (flat(t) for t in (Q, K, V, dO, g, beta))
+        opt = kw("packed", [n] * B)
+        check_forward(Q, K, V, g, beta, luna.delta_attn(Q, K, V, g, beta, scale=D ** -0.5, **opt), "packed", [n] * B, D ** -0.5)
+        check_backward(Q, K, V, dO, g, beta, luna.delta_attn_bwd(Q, K, V, dO, g, beta, scale=D ** -0.5, **opt), "packed", [n] * B, D ** -0.5)
+
+
 def test_captured_gradients_of_shared_heads():
     """Sums of value heads that are joined by a second launch: from a graph replayed between eager calls, and over a padded batch."""
     lens, n, H, Hk, D, d = [70, 0, 33], 70, 6, 2, 64, 64
