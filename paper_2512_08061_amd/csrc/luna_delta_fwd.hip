@@ -13,9 +13,9 @@
 // The scan waves' products are chained in registers as luna_delta_scan.hpp says.  Operands are read from LDS a batch before
 // their products (by itself the compiler reads each right before its use and waits out the LDS 80 times a chunk).  16-byte pieces
 // of a row are swapped among each other by the row's number, so that the rows of pairs of tiles do not meet in a bank.  What bounds it
-// is the chain of a chunk: 8 x 16 heads of 16384 tokens, D = d = 128, 1012 us, 3.9 us a chunk (LDS active 50% of all cycles, half of
+// is the chain of a chunk: 8 x 16 heads of 16384 tokens, D = d = 128, 1012 to 1031 us, 4 us a chunk (LDS active 50% of all cycles, half of
 // them bank conflicts of the transposing reads, which touch every other 8 bytes; matrix cores 28%).  Tiles of 16 consecutive rows and
-// features have no such conflicts, but need two 8-byte reads for each 16-byte one of an operand's row: 1078 us.
+// features have no such conflicts, but need two 8-byte reads for each 16-byte one of an operand's row: 1078 us (of 1012).
 #include "luna_delta_scan.hpp"
 
 namespace luna {

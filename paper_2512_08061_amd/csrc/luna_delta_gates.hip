@@ -7,7 +7,7 @@
 //   N_rc = -M_rc - sum_{p < r} M_rp beta_p N_pc,
 // and wave j the blocks below the diagonal of block column j, on the fp32 matrix cores,
 //   Z = M_ij + sum_{j <= p < i} M_ip beta_p N_pj,   N_ij = -(Z + N_ii beta_i Z).
-// What bounds it is these chains: 1024 chunks in bf16, D = 128, 27 us.
+// What bounds it is these chains: 1024 chunks in bf16, D = 128, 26 us.
 #include "luna_delta.hpp"
 
 namespace luna {

@@ -13,7 +13,8 @@
 // A workgroup takes a chunk of one key head and adds up over the value heads of its group, in their order (with few chunks each value
 // head has a workgroup, and a launch behind adds up); a wave has 16 features of dQ and dK, formed transposed, so that a lane holds
 // four neighbouring features of a token.  What bounds it is one workgroup a compute unit (eight waves of 256 registers fill the
-// register files, U and dR in parts the LDS) in phases that wait for memory, for the LDS and for one another: bf16, 2 x 16 heads of 2048 tokens, D = d = 128, 116 us for 0.33 GB.
+// register files, U and dR in parts the LDS) in phases that wait for memory, for the LDS and for one another: bf16, 2 x 16 heads of
+// 2048 tokens, D = d = 128, 114 us for 0.33 GB.
 #include "luna_delta.hpp"
 
 namespace luna {

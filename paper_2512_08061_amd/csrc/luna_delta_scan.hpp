@@ -6,7 +6,7 @@
 // lanes: rows 4g + e of a pair of tiles 2s, 2s + 1 stand for features (and tokens) 32 s + 8 g + e and 32 s + 8 g + 4 + e, the
 // eight k-slots of lane group g.  K S and N (beta R) take such pairs as their B operand, out^T = S^T Q^T + U^T P^T the same
 // registers as its A operand.  K and Q lie in LDS as their rows; K^T is read transposed.  What bounds them is the chain of a
-// chunk, 4.3 us for the gradients' of bf16 with D = d = 128 (2 x 16 heads of 2048 tokens: 138 us for both, side by side).
+// chunk, 4.1 us for the gradients' of bf16 with D = d = 128 (2 x 16 heads of 2048 tokens: 132 us for both, side by side).
 #pragma once
 
 #include "luna_delta.hpp"

@@ -1,6 +1,6 @@
 // luna_paged_split.hip -- softmax attention of few rows per key head over the pages of a cache (the next tokens of
 // sequences): what bounds it is reading the keys and values once (32 caches of up to 8192 tokens, 16 heads on 4, d = 128, 258 MB:
-// 69.5 us, 3.7 TB/s, and 7 to join), and for few tokens the chain of dependent loads (one cache of 3001: 10.3 and 5.6 us).
+// 69.9 us, 3.7 TB/s, and 7.4 to join), and for few tokens the chain of dependent loads (one cache of 3001: 11.0 and 6.2 us).
 //
 // The rows of a key head, m tokens of its H / Hk heads each, are one operand of up to RT tiles of 16, so that the cache is
 // read once for the whole group (in fp32 once for 32 rows, a workgroup each).  The keys of all sequences, in units of paged_unit(), are one line that is cut in equal shares,

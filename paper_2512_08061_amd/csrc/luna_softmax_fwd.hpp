@@ -365,7 +365,7 @@ __global__ __launch_bounds__(256 * GROUPS, 2) void softmax_fwd32_kernel(SoftmaxA
 
 // Over pages, what a share of the line of all sequences' keys holds of one sequence (see PagedUnits), for the tiles of one number
 // and head: whole sequences are finished here, the parts of others are joined by a launch behind it.  (512 new tokens of caches of 4096,
-// 1999, 700 and 16384, 16 heads on 4, d = 128: 157 and 27 us; without shares the longest cache kept 64 of 256 compute units busy
+// 1999, 700 and 16384, 16 heads on 4, d = 128: 138 and 27 us; without shares the longest cache kept 64 of 256 compute units busy
 // for 348.)
 template <int DH>
 __global__ __launch_bounds__(256, 2) void softmax_part32_kernel(SoftmaxArgs a, int shares) {
