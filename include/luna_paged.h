@@ -36,7 +36,7 @@ typedef struct luna_pages {
  * components j and j + rot / 2 (interleaved 0) or 2 j and 2 j + 1 (interleaved 1).  rot is a multiple of 16 up to d; 0
  * rotates nothing (inv_freq NULL).  Q (may be NULL): the same tokens' queries, H heads, rotated alike into q_out, which may be Q
  * itself.  Positions below 0 (more new tokens than lens says) and from width * rows on are not appended.  Of two new
- * tokens at one place of a page each 16 bytes there come from either of them.  It needs no workspace.
+ * tokens at one place of a page each element there comes from one of them, not all from the same.  It needs no workspace.
  */
 luna_status luna_paged_append(const luna_rows* K, const luna_rows* V, const luna_rows* Q, luna_dtype dtype,
                               const luna_seqs* seqs, const luna_pages* pages, int64_t H, int64_t Hk, int64_t d, int64_t rot,
